@@ -53,3 +53,15 @@ from .binding import (  # noqa: F401
     moe_plan_units,
     moe_workspace_bytes,
 )
+
+# The attention calls (include/qattn.h) work on torch tensors; their module, and torch with it, is imported at first use.
+_ATTENTION = ("ATTN_BF16", "ATTN_FP8", "AttnCache", "AttnRope", "attn_append", "attn_decode", "attn_decode_workspace", "attn_prompt", "attn_read",
+              "attn_rope_frequencies")
+
+
+def __getattr__(name):
+    if name not in _ATTENTION:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    from . import attention
+    value = globals()[name] = getattr(attention, name)
+    return value

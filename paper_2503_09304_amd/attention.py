@@ -1,0 +1,191 @@
+"""The attention calls of libqmoe.so (include/qattn.h) on torch tensors: argument marshalling only.
+
+Queries, keys, values and outputs are bfloat16 tensors [tokens, heads, dim] with any token and head stride (multiples of 8
+elements) and dense heads.  Outputs are the caller's tensors.  Every call enqueues on PyTorch's current stream; a tensor that
+belongs to another stream's work is the caller's to order, as with any kernel."""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional
+
+import torch
+
+from .binding import MOE_E_ARG, MoeError, _check, _stream, lib
+
+ATTN_BF16, ATTN_FP8 = 0, 1
+ATTN_ROPE = {"half": 0, "interleaved": 1}
+ATTN_SCALE = {"none": 0, "linear": 1, "base": 2, "ramp": 3, "waves": 4}
+
+
+class _Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class _Cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n_pages", C.c_int32),
+                ("heads_kv", C.c_int32), ("page_tokens", C.c_int32), ("dim", C.c_int32), ("format", C.c_int32)]
+
+
+class _Place(C.Structure):
+    _fields_ = [("seq", C.c_void_p), ("pos", C.c_void_p), ("pages", C.c_void_p), ("n_seqs", C.c_int32), ("seq_pages", C.c_int32)]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("dims", C.c_int32), ("layout", C.c_int32), ("mscale", C.c_float)]
+
+
+_ready = None
+
+
+def _lib():
+    global _ready
+    if _ready is None:
+        L = lib()
+        P, I, F, R = C.c_void_p, C.c_int32, C.c_float, C.POINTER(_Rows)
+        L.attn_rope_frequencies.argtypes = [I, C.c_double, I, C.c_double, C.c_double, C.c_double, C.c_double, P, C.POINTER(F)]
+        L.attn_append.argtypes = [C.POINTER(_Cache), R, R, R, R, R, I, I, C.POINTER(_Place), C.POINTER(_Rope), P, P]
+        L.attn_read.argtypes = [C.POINTER(_Cache), C.POINTER(_Place), I, R, R, P, P]
+        L.attn_prompt.argtypes = [R, R, R, R, P, P, P, I, I, I, I, I, I, F, I, P]
+        L.attn_decode.argtypes = [C.POINTER(_Cache), R, R, P, I, I, P, I, P, F, P, C.c_size_t, P, P]
+        for f in ("attn_rope_frequencies", "attn_append", "attn_read", "attn_prompt", "attn_decode"):
+            getattr(L, f).restype = I
+        for f, n in (("attn_decode_workspace_bytes", 4), ("attn_decode_counter_bytes", 3)):
+            getattr(L, f).argtypes = [I] * n
+            getattr(L, f).restype = C.c_size_t
+        _ready = L
+    return _ready
+
+
+def _bad(text: str):
+    raise MoeError(MOE_E_ARG, text)
+
+
+def _heads(t, name: str, shape=None) -> _Rows:
+    """A tensor [tokens, heads, dim] as rows."""
+    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.device.type != "cuda":
+        _bad(f"{name} must be a bfloat16 tensor [tokens, heads, dim] on the GPU")
+    if shape is not None and tuple(t.shape) != shape:
+        _bad(f"{name} has shape {tuple(t.shape)}, not {shape}")
+    ts, hs, ds = t.stride()
+    if ds != 1:
+        _bad(f"the elements of a head of {name} must be dense")
+    return _Rows(t.data_ptr(), ts if t.shape[0] > 1 else 0, hs if t.shape[1] > 1 else 0)
+
+
+def _whole(t, name: str, dtype, shape) -> int:
+    """The address of a dense tensor of this type and shape."""
+    if t.dtype != dtype or t.device.type != "cuda" or not t.is_contiguous() or tuple(t.shape) != shape:
+        _bad(f"{name} must be a dense {dtype} tensor {list(shape)} on the GPU")
+    return t.data_ptr()
+
+
+def _optional(t, name: str, dtype, shape):
+    return None if t is None else _whole(t, name, dtype, shape)
+
+
+class AttnCache:
+    """Pages of keys and values: k and v [n_pages, heads_kv, page_tokens, dim], bfloat16, or float8_e4m3fn (or its bytes as uint8)
+    with the scale bytes k_scale and v_scale [n_pages, heads_kv, page_tokens]."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        if k.dim() != 4:
+            _bad("k must be [n_pages, heads_kv, page_tokens, dim]")
+        if k.dtype not in (torch.bfloat16, torch.float8_e4m3fn, torch.uint8):
+            _bad("a cache is bfloat16 or float8_e4m3fn")
+        shape = tuple(k.shape)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_pages, self.heads_kv, self.page_tokens, self.dim = shape
+        self.fp8 = k.dtype != torch.bfloat16
+        if self.fp8 != (k_scale is not None) or self.fp8 != (v_scale is not None):
+            _bad("a float8 cache needs k_scale and v_scale, a bfloat16 cache has none")
+        self._c = _Cache(_whole(k, "k", k.dtype, shape), _whole(v, "v", k.dtype, shape), _optional(k_scale, "k_scale", torch.uint8, shape[:3]),
+                         _optional(v_scale, "v_scale", torch.uint8, shape[:3]), *shape, ATTN_FP8 if self.fp8 else ATTN_BF16)
+
+    @classmethod
+    def empty(cls, n_pages: int, heads_kv: int, page_tokens: int, dim: int, fp8: bool = False, device="cuda:0") -> "AttnCache":
+        """A cache in memory of its own; its slots hold nothing until tokens are appended."""
+        shape = (n_pages, heads_kv, page_tokens, dim)
+        k, v = (torch.empty(shape, dtype=torch.uint8 if fp8 else torch.bfloat16, device=device) for _ in range(2))
+        return cls(k, v, *((torch.empty(shape[:3], dtype=torch.uint8, device=device) for _ in range(2)) if fp8 else ()))
+
+
+class AttnRope:
+    """Rotary positions: inv_freq [dims/2] float64 on the GPU (see attn_rope_frequencies), pairs "half" a rotation apart or
+    "interleaved", mscale on cos and sin."""
+
+    def __init__(self, inv_freq, layout: str = "half", mscale: float = 1.0):
+        if layout not in ATTN_ROPE:
+            _bad("layout must be half or interleaved")
+        self.inv_freq = inv_freq
+        self._c = _Rope(_whole(inv_freq, "inv_freq", torch.float64, (inv_freq.numel(),)), 2 * inv_freq.numel(), ATTN_ROPE[layout], mscale)
+
+
+def attn_rope_frequencies(dims: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, trained: float = 4096.0,
+                          fast: float = 32.0, slow: float = 1.0):
+    """(frequencies as a list, factor on cos and sin); the scalings are those of include/qattn.h.  Host only."""
+    if scaling not in ATTN_SCALE:
+        _bad(f"scaling must be one of {', '.join(ATTN_SCALE)}")
+    f, m = (C.c_double * max(1, dims // 2))(), C.c_float()
+    _check(_lib().attn_rope_frequencies(dims, base, ATTN_SCALE[scaling], factor, trained, fast, slow, f, C.byref(m)))
+    return list(f), float(m.value)
+
+
+def _place(seq, pos, pages, T: int) -> _Place:
+    if pages.dim() != 2:
+        _bad("pages must be [n_seqs, seq_pages]")
+    shape = tuple(pages.shape)
+    return _Place(_optional(seq, "seq", torch.int32, (T,)), _whole(pos, "pos", torch.int32, (T,)), _whole(pages, "pages", torch.int32, shape), *shape)
+
+
+def attn_append(cache: AttnCache, q, k, v, seq, pos, pages, rope: Optional[AttnRope], q_out, k_out=None, bad=None) -> int:
+    """Rotates q into q_out and k into k_out (may be None) and writes k and v to the cache.  seq (None: token t is sequence t's),
+    pos int32 [tokens], pages int32 [n_seqs, seq_pages]; bad int32 [1] counts tokens that are out of range.  q and q_out may be None."""
+    T, Hk, D = k.shape[0], cache.heads_kv, cache.dim
+    if (q is None) != (q_out is None):
+        _bad("q and q_out go together")
+    heads = 0 if q is None else q.shape[1]
+    qs, qo = (None, None) if q is None else (_heads(q, "q", (T, heads, D)), _heads(q_out, "q_out", (T, heads, D)))
+    ks, vs, ko = _heads(k, "k", (T, Hk, D)), _heads(v, "v", (T, Hk, D)), None if k_out is None else _heads(k_out, "k_out", (T, Hk, D))
+    place = _place(seq, pos, pages, T)
+    return _check(_lib().attn_append(cache._c, qs, ks, vs, qo, ko, heads, T, place, None if rope is None else rope._c,
+                                     _optional(bad, "bad", torch.int32, (1,)), _stream()))
+
+
+def attn_read(cache: AttnCache, seq, pos, pages, k_out, v_out, bad=None) -> int:
+    """Keys and values of the tokens at (seq, pos) out of the cache, as bfloat16."""
+    T = pos.shape[0]
+    shape = (T, cache.heads_kv, cache.dim)
+    return _check(_lib().attn_read(cache._c, _place(seq, pos, pages, T), T, _heads(k_out, "k_out", shape), _heads(v_out, "v_out", shape),
+                                   _optional(bad, "bad", torch.int32, (1,)), _stream()))
+
+
+def attn_prompt(q, k, v, cu_q, cu_k, out, scale: Optional[float] = None, causal: bool = True, lse=None) -> int:
+    """Attention over packed prompts; cu_q, cu_k int32 [n_seqs + 1] on the GPU; scale None: dim ** -0.5; lse float32 [n_q, heads_q]."""
+    (n_q, Hq, D), (n_k, Hk, _) = q.shape, k.shape
+    n = cu_q.shape[0] - 1
+    if n < 0:
+        _bad("cu_q has no entry")
+    return _check(_lib().attn_prompt(_heads(q, "q"), _heads(k, "k", (n_k, Hk, D)), _heads(v, "v", (n_k, Hk, D)), _heads(out, "out", (n_q, Hq, D)),
+                                     _optional(lse, "lse", torch.float32, (n_q, Hq)), _whole(cu_q, "cu_q", torch.int32, (n + 1,)),
+                                     _whole(cu_k, "cu_k", torch.int32, (n + 1,)), n, n_q, n_k, Hq, Hk, D, D ** -0.5 if scale is None else scale,
+                                     1 if causal else 0, _stream()))
+
+
+def attn_decode_workspace(cache: AttnCache, n_seqs: int, heads_q: int):
+    """Workspace for attn_decode calls of up to n_seqs sequences, its counters zeroed; for one stream at a time."""
+    n = int(_lib().attn_decode_workspace_bytes(n_seqs, heads_q, cache.heads_kv, cache.dim))
+    if n == 0:
+        raise MoeError(MOE_E_ARG, _lib().moe_last_error().decode())
+    return torch.zeros(n, dtype=torch.uint8, device=cache.k.device)
+
+
+def attn_decode(cache: AttnCache, q, pages, lens, out, workspace, scale: Optional[float] = None, lse=None, bad=None) -> int:
+    """One query a sequence (q [n_seqs, heads_q, dim]) over the first lens[b] tokens of its pages."""
+    n, Hq, D = q.shape
+    if pages.dim() != 2 or D != cache.dim:
+        _bad("pages must be [n_seqs, seq_pages], q [n_seqs, heads_q, dim of the cache]")
+    return _check(_lib().attn_decode(cache._c, _heads(q, "q"), _heads(out, "out", (n, Hq, D)), _optional(lse, "lse", torch.float32, (n, Hq)), n, Hq,
+                                     _whole(pages, "pages", torch.int32, (n, pages.shape[1])), pages.shape[1],
+                                     _whole(lens, "lens", torch.int32, (n,)), D ** -0.5 if scale is None else scale,
+                                     _whole(workspace, "workspace", torch.uint8, (workspace.numel(),)), workspace.numel(),
+                                     _optional(bad, "bad", torch.int32, (1,)), _stream()))

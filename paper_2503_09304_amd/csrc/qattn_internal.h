@@ -1,0 +1,74 @@
+// Internal declarations shared by the host side of the attention calls and their kernels (the public ABI is include/qattn.h).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "qattn.h"
+
+namespace qattn {
+
+constexpr int kMaxDim = 128;
+
+// Rows of heads as the kernels take them (bf16 elements).
+struct Rows {
+    uint16_t *p;
+    long ts, hs;
+};
+
+// A cache as the kernels take it.
+struct Cache {
+    uint8_t *k, *v;               // bf16 or e4m3
+    uint8_t *ks, *vs;             // scale bytes (e4m3)
+    int n_pages, Hk, page_shift, D;
+};
+
+struct AppendArgs {
+    Cache c;
+    Rows q, k, v, qo, ko;         // q.p, qo.p, ko.p may be nullptr
+    const int32_t *seq, *pos, *pages;
+    const double *inv_freq;
+    int32_t *bad;
+    int n_tokens, Hq, n_seqs, seq_pages, rot, interleaved, fp8;
+    float mscale;
+};
+hipError_t launch_append(const AppendArgs &a, hipStream_t s);
+
+struct ReadArgs {
+    Cache c;
+    Rows ko, vo;
+    const int32_t *seq, *pos, *pages;
+    int32_t *bad;
+    int n_tokens, n_seqs, seq_pages, fp8;
+};
+hipError_t launch_read(const ReadArgs &a, hipStream_t s);
+
+struct PromptArgs {
+    Rows q, k, v, o;
+    float *lse;
+    const int32_t *cu_q, *cu_k;
+    int n_seqs, n_q, n_k, Hq, Hk, D, causal;
+    float scale_log2;             // scale * log2(e)
+};
+hipError_t launch_prompt(const PromptArgs &a, hipStream_t s);
+
+struct DecodeArgs {
+    Cache c;
+    Rows q, o;
+    float *lse;
+    const int32_t *pages, *lens;
+    int32_t *bad;
+    int32_t *arrived;             // [n_seqs][Hk * group tiles], zero between calls
+    float *part;                  // pieces: [piece][16][D + 2] fp32
+    int n_seqs, Hq, seq_pages, fp8;
+    int pieces;                   // most pieces of a launch per (key/value head, group tile): the grid, and the slots of `part`
+    float scale_log2;
+};
+// A group tile is up to 16 query heads that share a key/value head.
+__host__ __device__ inline int group_tiles(int Hq, int Hk) { return (Hq / Hk + 15) / 16; }
+// Workgroups that a decode launch aims at when the sequences are long enough, over all heads; see attn_decode.hip.
+constexpr int kDecodeWgs = 1024;
+inline int decode_pieces(int n_seqs, int Hq, int Hk) { return n_seqs + (kDecodeWgs + Hk * group_tiles(Hq, Hk) - 1) / (Hk * group_tiles(Hq, Hk)); }
+hipError_t launch_decode(const DecodeArgs &a, hipStream_t s);
+
+}  // namespace qattn
