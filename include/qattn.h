@@ -120,7 +120,7 @@ int32_t attn_prompt(const attn_rows *q, const attn_rows *k, const attn_rows *v, 
 /* Attention of one query a sequence over the cache: query b sees the first lens[b] tokens of sequence b (lens [device] int32
  * [n_seqs]), whose pages are pages[b * seq_pages ..].  The formula, lse ([device] float [n_seqs, heads_q], may be NULL) and the answer
  * without keys are those of attn_prompt.  lens out of 0 .. seq_pages * page_tokens are clamped, pages out of 0 .. n_pages - 1 hold no
- * keys; both are counted in *bad (a page once for each group of 16 tokens and key/value head that met it).
+ * keys; *bad counts each of both once.
  * Long sequences are cut into pieces that run side by side; the last piece of a sequence to finish joins them, in the order of the
  * pieces, so results do not depend on timing.  workspace [device], 256-byte aligned, attn_decode_workspace_bytes(...) long: its first
  * attn_decode_counter_bytes(...) bytes have to be zero at the first call; every call leaves them zero.  Calls that share a workspace

@@ -78,12 +78,13 @@ __global__ __launch_bounds__(kWaves * 64) void prompt_tile(const PromptArgs a, i
     // each XCD's L2 holds the keys of one.  Late tiles of a sequence see the most keys: they start first.
     const int G = a.Hq / a.Hk, num = blockIdx.x + item0;
     const int hk = num % a.Hk, rest = num / a.Hk, head = hk * G + rest % G, item = tiles - 1 - rest / G;
-    const int2 at = find_piece(a.n_seqs, item, [&](int b) { const int2 s = span(a.cu_q, b, a.n_q); return (s.y - s.x + QT - 1) / QT; });
-    const int b = __builtin_amdgcn_readfirstlane(at.x);
+    const Piece at = find_piece(a.n_seqs, (uint32_t)item, [&](int b) { const int2 s = span(a.cu_q, b, a.n_q); return s.y - s.x; },
+                                [](int n) { return (uint32_t)(n + QT - 1) / QT; });
+    const int b = at.seq;
     if (b < 0) return;
     const int2 sq = span(a.cu_q, b, a.n_q), sk = span(a.cu_k, b, a.n_k);
     const int nq = __builtin_amdgcn_readfirstlane(sq.y - sq.x), nk = __builtin_amdgcn_readfirstlane(sk.y - sk.x);
-    const int r0 = __builtin_amdgcn_readfirstlane(at.y) * QT;                 // first query of the tile, within the sequence
+    const int r0 = at.piece * QT;                 // first query of the tile, within the sequence
     const long q_row = __builtin_amdgcn_readfirstlane(sq.x), k_row = __builtin_amdgcn_readfirstlane(sk.x);
     const int w0 = r0 + wave * 32 * QB;                                        // first query of the wave
     // keys that the tile's last query sees, and those that all queries of the wave see / any of them sees

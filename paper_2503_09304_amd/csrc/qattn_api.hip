@@ -1,6 +1,7 @@
 // Host side of the attention calls (include/qattn.h): argument checks, the rotary frequencies, launches.  No device code here.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -193,9 +194,11 @@ int32_t attn_decode(const attn_cache *cache, const attn_rows *q, const attn_rows
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < need)
         return set_error(MOE_E_WORKSPACE, "%s: workspace too small or not 256-byte aligned (%zu bytes needed)", call, need);
     uint8_t *w = (uint8_t *)workspace;
+    const int64_t most = (int64_t)n_seqs * std::max<int64_t>(1, ((int64_t)seq_pages * cache->page_tokens + 255) / 256);      // a piece has 256 keys at least
+    const int pieces = (int)std::min<int64_t>(most, qattn::decode_pieces(n_seqs, heads_q, cache->heads_kv));
     qattn::DecodeArgs a{cache_of(cache), rows(q), rows(out), lse, pages, lens, bad, (int32_t *)w,
                         (float *)(w + attn_decode_counter_bytes(n_seqs, heads_q, cache->heads_kv)), n_seqs, heads_q, seq_pages,
-                        cache->format == ATTN_FP8, qattn::decode_pieces(n_seqs, heads_q, cache->heads_kv), scale * 1.44269504088896340736f};
+                        cache->format == ATTN_FP8, pieces, scale * 1.44269504088896340736f};
     return hip_result(qattn::launch_decode(a, (hipStream_t)stream), call);
 }
 

@@ -61,14 +61,18 @@ struct DecodeArgs {
     int32_t *arrived;             // [n_seqs][Hk * group tiles], zero between calls
     float *part;                  // pieces: [piece][16][D + 2] fp32
     int n_seqs, Hq, seq_pages, fp8;
-    int pieces;                   // most pieces of a launch per (key/value head, group tile): the grid, and the slots of `part`
+    int pieces;                   // most pieces of all sequences per (key/value head, group tile): the grid
     float scale_log2;
 };
 // A group tile is up to 16 query heads that share a key/value head.
 __host__ __device__ inline int group_tiles(int Hq, int Hk) { return (Hq / Hk + 15) / 16; }
-// Workgroups that a decode launch aims at when the sequences are long enough, over all heads; see attn_decode.hip.
-constexpr int kDecodeWgs = 1024;
-inline int decode_pieces(int n_seqs, int Hq, int Hk) { return n_seqs + (kDecodeWgs + Hk * group_tiles(Hq, Hk) - 1) / (Hk * group_tiles(Hq, Hk)); }
+// Workgroups that a decode launch cuts the keys into, before the pieces of each sequence are rounded up: see attn_decode.hip.
+constexpr int kFewestWgs = 256, kMostWgs = 1536;
+// Most pieces of all sequences, per (key/value head, group tile).
+inline int decode_pieces(int n_seqs, int Hq, int Hk) {
+    const int heads = Hk * group_tiles(Hq, Hk);
+    return n_seqs + (kMostWgs + heads - 1) / heads;
+}
 hipError_t launch_decode(const DecodeArgs &a, hipStream_t s);
 
 }  // namespace qattn
