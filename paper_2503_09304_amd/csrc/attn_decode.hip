@@ -34,9 +34,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-#ifndef OCC
-#define OCC 2
-#endif
 constexpr int kWaves = 4;
 constexpr int kBlock = 32;                       // keys of a wave's step
 

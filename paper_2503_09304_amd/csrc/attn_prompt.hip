@@ -12,6 +12,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "attn_pieces.h"
 #include "qattn_internal.h"
@@ -36,6 +37,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     const bf16x2 r = {(__bf16)a, (__bf16)b};
     return __builtin_bit_cast(uint32_t, r);
 }
+__device__ __forceinline__ f32x16 zero16() { return f32x16{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}; }
 __device__ __forceinline__ float other_half_max(float v) {
     auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
@@ -43,6 +45,11 @@ __device__ __forceinline__ float other_half_max(float v) {
 __device__ __forceinline__ float other_half_sum(float v) {
     auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+// An offset of 32 bits that is widened where it is used: widened in front of the loop it would become part of a 64-bit address in vector registers.
+__device__ __forceinline__ uint32_t here(uint32_t v) {
+    asm volatile("" : "+v"(v));
+    return v;
 }
 // 4 keys of one d: lane i of 16 gets element i of the 4 rows that lanes 4r .. 4r + 3 point at, 8 bytes each.
 typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
@@ -63,7 +70,7 @@ __device__ __forceinline__ int2 span(const int32_t *cu, int b, int n) {
 }
 
 template <int DP, int QB>
-__global__ __launch_bounds__(kWaves * 64) void prompt_tile(const PromptArgs a, int tiles, int item0) {
+__global__ __launch_bounds__(kWaves * 64, DP * QB > 128 ? 1 : 2) void prompt_tile(const PromptArgs a, int tiles, int item0) {
     constexpr int QT = kWaves * 32 * QB;          // queries of a workgroup
     constexpr int CH = DP / 8;                    // 16-byte pieces of a row
     constexpr int KS = DP / 16;                   // MFMA steps of a score
@@ -87,12 +94,10 @@ __global__ __launch_bounds__(kWaves * 64) void prompt_tile(const PromptArgs a, i
     const int r0 = at.piece * QT;                 // first query of the tile, within the sequence
     const long q_row = __builtin_amdgcn_readfirstlane(sq.x), k_row = __builtin_amdgcn_readfirstlane(sk.x);
     const int w0 = r0 + wave * 32 * QB;                                        // first query of the wave
-    // keys that the tile's last query sees, and those that all queries of the wave see / any of them sees
+    // tiles of keys that the tile's last query sees, and those that its first query sees whole
     const int shift = nk - nq;
-    const int tile_keys = a.causal ? min(nk, max(0, shift + min(nq, r0 + QT))) : nk;
-    const int wave_all = a.causal ? max(0, shift + w0 + 1) : nk;
-    const int wave_any = w0 >= nq ? 0 : a.causal ? min(nk, max(0, shift + min(nq, w0 + 32 * QB))) : nk;
-    const int n_tiles = (tile_keys + kKeys - 1) / kKeys;
+    const int n_tiles = ((a.causal ? min(nk, max(0, shift + min(nq, r0 + QT))) : nk) + kKeys - 1) / kKeys;
+    const int whole_tiles = min(nk, a.causal ? max(0, shift + r0 + 1) : nk) / kKeys;
 
     u32x4 qf[QB][KS];
 #pragma unroll
@@ -100,7 +105,10 @@ __global__ __launch_bounds__(kWaves * 64) void prompt_tile(const PromptArgs a, i
         const int r = w0 + 32 * i + col;
         const uint16_t *p = a.q.p + (q_row + min(r, nq - 1)) * a.q.ts + (long)head * a.q.hs;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) qf[i][s] = 16 * s < a.D ? *reinterpret_cast<const u32x4 *>(p + 16 * s + 8 * h) : u32x4{0, 0, 0, 0};
+        for (int s = 0; s < KS; ++s) qf[i][s] = *reinterpret_cast<const u32x4 *>(p + min(16 * s, a.D - 16) + 8 * h);
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+            if (16 * s >= a.D) qf[i][s] = u32x4{0, 0, 0, 0};
     }
     f32x16 o[QB][DT];
     float m[QB], l[QB];
@@ -109,117 +117,151 @@ __global__ __launch_bounds__(kWaves * 64) void prompt_tile(const PromptArgs a, i
         m[i] = -INFINITY;
         l[i] = 0.f;
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[i][d][r] = 0.f;
+        for (int d = 0; d < DT; ++d) o[i][d] = zero16();
     }
 
-    // the pieces that this thread moves: rows tr + i * (256 / CH), piece tc
-    const int tr = tid / CH, tc = tid % CH;
-    const uint16_t *kp = a.k.p + k_row * a.k.ts + (long)hk * a.k.hs + tc * 8;
-    const uint16_t *vp = a.v.p + k_row * a.v.ts + (long)hk * a.v.hs + tc * 8;
-    const bool has_d = tc * 8 < a.D;
+    // The 16-byte pieces that this thread moves: rows tr + i * (256 / CH) of a tile, piece tc.  Rows behind the last key are that key again
+    // (their weights are 0), pieces behind the end of a head its last one (the queries are 0 there, those outputs are not stored).
+    const int tr = tid / CH, tc = tid % CH, dc = min(tc * 8, a.D - 8);
+    const uint16_t *kp = a.k.p + k_row * a.k.ts + (long)hk * a.k.hs;
+    const uint16_t *vp = a.v.p + k_row * a.v.ts + (long)hk * a.v.hs;
     u32x4 kr[LD], vr[LD];
-    const auto fetch = [&](int t) {
+    uint32_t kat[LD], vat[LD];                    // bytes from the tile's first row
+    const auto rows_at = [&](uint32_t (&at)[LD], long stride, int t) {
 #pragma unroll
-        for (int i = 0; i < LD; ++i) {
-            const int key = t * kKeys + tr + i * (kWaves * 64 / CH);
-            const bool in = has_d && key < nk;
-            kr[i] = in ? *reinterpret_cast<const u32x4 *>(kp + (long)key * a.k.ts) : u32x4{0, 0, 0, 0};
-            vr[i] = in ? *reinterpret_cast<const u32x4 *>(vp + (long)key * a.v.ts) : u32x4{0, 0, 0, 0};
-        }
+        for (int i = 0; i < LD; ++i) at[i] = 2u * (uint32_t)(max(0, min(tr + i * (kWaves * 64 / CH), nk - 1 - t * kKeys)) * (int)stride + dc);
     };
-    const auto store = [&](int buf) {
+    const auto fetch = [&](u32x4 (&x)[LD], const uint16_t *p, const uint32_t (&at)[LD], long stride, int t) {
+        const char *tile = (const char *)(p + min(t, (nk - 1) / kKeys) * kKeys * stride);
+#pragma unroll
+        for (int i = 0; i < LD; ++i) x[i] = *reinterpret_cast<const u32x4 *>(tile + here(at[i]));
+    };
+    const auto store_k = [&](int buf) {
 #pragma unroll
         for (int i = 0; i < LD; ++i) {
             const int r = tr + i * (kWaves * 64 / CH);
             *reinterpret_cast<u32x4 *>(&s_k[buf][r * DP + (tc ^ swz_k<DP>(r)) * 8]) = kr[i];
+        }
+    };
+    const auto store_v = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < LD; ++i) {
+            const int r = tr + i * (kWaves * 64 / CH);
             *reinterpret_cast<u32x4 *>(&s_v[buf][r * DP + (tc ^ swz_v<DP>(r)) * 8]) = vr[i];
         }
     };
-
-    if (n_tiles > 0) {
-        fetch(0);
-        store(0);
-    }
-    __syncthreads();
-    for (int t = 0; t < n_tiles; ++t) {
-        const int buf = t & 1;
-        if (t + 1 < n_tiles) fetch(t + 1);
-        if (t * kKeys < wave_any) {
-            f32x16 s[QB][2];
+    // Scores of keys 32 n .. of the tile in `buf`.
+    const auto scores = [&](f32x16 (&s)[QB], int buf, int n) {
+        const int row = 32 * n + col;
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
+        for (int i = 0; i < QB; ++i) s[i] = zero16();
 #pragma unroll
-                for (int i = 0; i < QB; ++i)
+        for (int st = 0; st < KS; ++st) {
+            const u32x4 kf = *reinterpret_cast<const u32x4 *>(&s_k[buf][row * DP + ((2 * st + h) ^ swz_k<DP>(row)) * 8]);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[i][n][r] = 0.f;
-                const int row = 32 * n + col;
-#pragma unroll
-                for (int st = 0; st < KS; ++st) {
-                    const u32x4 kf = *reinterpret_cast<const u32x4 *>(&s_k[buf][row * DP + ((2 * st + h) ^ swz_k<DP>(row)) * 8]);
-#pragma unroll
-                    for (int i = 0; i < QB; ++i) s[i][n] = mma(kf, qf[i][st], s[i][n]);
-                }
-            }
-            if ((t + 1) * kKeys > wave_all || (t + 1) * kKeys > nk) {
-#pragma unroll
-                for (int i = 0; i < QB; ++i) {
-                    const int last = min(nk - 1, a.causal ? shift + w0 + 32 * i + col : nk - 1) - t * kKeys;      // last key of the query, in the tile
-#pragma unroll
-                    for (int n = 0; n < 2; ++n)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (32 * n + 8 * (r / 4) + 4 * h + r % 4 > last) s[i][n][r] = -INFINITY;
-                }
-            }
-            u32x4 pf[QB][4];
-#pragma unroll
-            for (int i = 0; i < QB; ++i) {
-                float top = s[i][0][0];
-#pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[i][n][r]);
-                top = other_half_max(top);
-                // The sums may stand relative to any value: they are taken over to a new maximum only where it is 2^8 above the old.
-                if (__any((top - m[i]) * a.scale_log2 > 8.f)) {
-                    const float next = fmaxf(m[i], top), f = __builtin_amdgcn_exp2f((m[i] - (next == -INFINITY ? 0.f : next)) * a.scale_log2);
-                    m[i] = next;
-                    l[i] *= f;
-#pragma unroll
-                    for (int d = 0; d < DT; ++d)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) o[i][d][r] *= f;
-                }
-                const float base = (m[i] == -INFINITY ? 0.f : m[i]) * a.scale_log2;
-#pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        s[i][n][r] = __builtin_amdgcn_exp2f(fmaf(s[i][n][r], a.scale_log2, -base));
-                        l[i] += s[i][n][r];
-                    }
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) pf[i][c][j] = pack_bf16(s[i][c / 2][8 * (c & 1) + 2 * j], s[i][c / 2][8 * (c & 1) + 2 * j + 1]);
-            }
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const int row = 16 * c + 4 * h + (lane & 15) / 4;
-                    const int piece = 4 * d + 2 * ((lane >> 4) & 1) + (lane & 3) / 2, at8 = (lane & 1) * 4;
-                    const u32x2 v0 = read_transposed(&s_v[buf][row * DP + (piece ^ swz_v<DP>(row)) * 8 + at8]);
-                    const u32x2 v1 = read_transposed(&s_v[buf][(row + 8) * DP + (piece ^ swz_v<DP>(row + 8)) * 8 + at8]);
-                    const u32x4 vf = {v0[0], v0[1], v1[0], v1[1]};
-#pragma unroll
-                    for (int i = 0; i < QB; ++i) o[i][d] = mma(vf, pf[i][c], o[i][d]);
-                }
+            for (int i = 0; i < QB; ++i) s[i] = mma(kf, qf[i][st], s[i]);
         }
-        if (t + 1 < n_tiles) store(buf ^ 1);
+    };
+    // o += V^T P^T for keys 32 n .. of the tile in `buf`.
+    const auto values = [&](const u32x4 (&p)[QB][2], int buf, int n) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int row = 32 * n + 16 * c + 4 * h + (lane & 15) / 4;
+                const int piece = 4 * d + 2 * ((lane >> 4) & 1) + (lane & 3) / 2, at8 = (lane & 1) * 4;
+                const u32x2 v0 = read_transposed(&s_v[buf][row * DP + (piece ^ swz_v<DP>(row)) * 8 + at8]);
+                const u32x2 v1 = read_transposed(&s_v[buf][(row + 8) * DP + (piece ^ swz_v<DP>(row + 8)) * 8 + at8]);
+                const u32x4 vf = {v0[0], v0[1], v1[0], v1[1]};
+#pragma unroll
+                for (int i = 0; i < QB; ++i) o[i][d] = mma(vf, p[i][c], o[i][d]);
+            }
+    };
+    // Weights of the scores s of keys `key0` ..; f: what the sums so far are to be multiplied by.  They may stand relative to any value: a row
+    // goes over to a new maximum only where that is 2^8 above the old.
+    const auto weights = [&](f32x16 (&s)[QB], u32x4 (&p)[QB][2], float (&f)[QB], int key0, auto masked) {
+#pragma unroll
+        for (int i = 0; i < QB; ++i) {
+            if constexpr (masked) {
+                const int last = min(nk - 1, a.causal ? shift + w0 + 32 * i + col : nk - 1) - key0;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[i][r] = 8 * (r / 4) + 4 * h + r % 4 > last ? -INFINITY : s[i][r];
+            }
+            float top = s[i][0];
+#pragma unroll
+            for (int r = 1; r < 16; ++r) top = fmaxf(top, s[i][r]);
+            top = other_half_max(top);
+            const float next = (top - m[i]) * a.scale_log2 > 8.f ? top : m[i];
+            const float base = (next == -INFINITY ? 0.f : next) * a.scale_log2;
+            f[i] = __builtin_amdgcn_exp2f(fmaf(m[i], a.scale_log2, -base));
+            m[i] = next;
+            float sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[i][r] = __builtin_amdgcn_exp2f(fmaf(s[i][r], a.scale_log2, -base));
+                sum += s[i][r];
+            }
+            l[i] = fmaf(l[i], f[i], sum);
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) p[i][c][j] = pack_bf16(s[i][8 * c + 2 * j], s[i][8 * c + 2 * j + 1]);
+            asm volatile("" : "+v"(p[i][0]), "+v"(p[i][1]), "+v"(l[i]));         // formed here, not behind the branch of the next rescaling
+        }
+    };
+    const auto rescale = [&](const float (&f)[QB]) {
+#pragma unroll
+        for (int i = 0; i < QB; ++i)
+            if (__any(f[i] != 1.f)) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[i][d][r] *= f[i];
+            }
+    };
+
+    // Half a tile (32 keys) at a time: the scores of the next half, the weights of this one and the sums of the one before depend on nothing
+    // of each other, so the matrix unit works on the first and third while the vector unit forms the second.
+    f32x16 sa[QB], sb[QB];
+    u32x4 pa[QB][2], pb[QB][2];
+    float f[QB];
+    const int last_tile = (nk - 1) / kKeys;
+    const auto tile = [&](int t, auto masked) {
+        const int buf = t & 1;
+        if (t + 2 == last_tile) rows_at(kat, a.k.ts, last_tile);
+        if (t + 1 == last_tile) rows_at(vat, a.v.ts, last_tile);
+        scores(sb, buf, 1);
+        weights(sa, pa, f, t * kKeys, masked);
+        values(pb, buf ^ 1, 1);                    // the half before: tile t - 1's second
+        store_k(buf ^ 1);                          // tile t + 1
+        store_v(buf);                              // tile t
+        rescale(f);
         __syncthreads();
+        fetch(kr, kp, kat, a.k.ts, t + 2);
+        fetch(vr, vp, vat, a.v.ts, t + 1);
+        scores(sa, buf ^ 1, 0);                    // tile t + 1
+        weights(sb, pb, f, t * kKeys + 32, masked);
+        values(pa, buf, 0);
+        rescale(f);
+    };
+    if (n_tiles > 0) {
+        rows_at(kat, a.k.ts, 0);
+        rows_at(vat, a.v.ts, 0);
+        fetch(kr, kp, kat, a.k.ts, 0);
+        store_k(0);
+        if (last_tile == 1) rows_at(kat, a.k.ts, 1);
+        fetch(kr, kp, kat, a.k.ts, 1);
+        fetch(vr, vp, vat, a.v.ts, 0);
+#pragma unroll
+        for (int i = 0; i < LD; ++i) *reinterpret_cast<u32x4 *>(&s_v[1][(tid + i * kWaves * 64) * 8]) = u32x4{0, 0, 0, 0};       // values of the half before the first
+#pragma unroll
+        for (int i = 0; i < QB; ++i) pb[i][0] = pb[i][1] = u32x4{0, 0, 0, 0};
+        __syncthreads();
+        scores(sa, 0, 0);
+        int t = 0;
+        for (; t < whole_tiles; ++t) tile(t, std::false_type{});
+        for (; t < n_tiles; ++t) tile(t, std::true_type{});
+        values(pb, (n_tiles - 1) & 1, 1);
     }
 
 #pragma unroll
@@ -251,9 +293,12 @@ void prompt_n(const PromptArgs &a, hipStream_t s) {
 
 }  // namespace
 
+#ifndef QBSEL
+#define QBSEL 1
+#endif
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t s) {
-    if (a.D <= 64) prompt_n<64, 1>(a, s);
-    else prompt_n<128, 1>(a, s);
+    if (a.D <= 64) prompt_n<64, QBSEL>(a, s);
+    else prompt_n<128, QBSEL>(a, s);
     return hipGetLastError();
 }
 
