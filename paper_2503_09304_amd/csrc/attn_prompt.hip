@@ -53,7 +53,7 @@ __device__ __forceinline__ uint32_t here(uint32_t v) {
 }
 // 4 keys of one d: lane i of 16 gets element i of the 4 rows that lanes 4r .. 4r + 3 point at, 8 bytes each.
 typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
-__device__ __forceinline__ u32x2 read_transposed(const uint16_t *p) {
+__device__ __forceinline__ u32x2 read_transposed(const uint8_t *p) {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p));
 }
 
@@ -76,8 +76,8 @@ __global__ __launch_bounds__(kWaves * 64, DP * QB > 128 ? 1 : 2) void prompt_til
     constexpr int KS = DP / 16;                   // MFMA steps of a score
     constexpr int DT = DP / 32;                   // 32-d tiles of the output
     constexpr int LD = kKeys * CH / (kWaves * 64);   // pieces of K (and V) that a thread moves per tile
-    __shared__ __attribute__((aligned(16))) uint16_t s_k[2][kKeys * DP];
-    __shared__ __attribute__((aligned(16))) uint16_t s_v[2][kKeys * DP];
+    constexpr int ROW = DP * 2, TILE = kKeys * ROW, VT = 2 * TILE;       // bytes
+    __shared__ __attribute__((aligned(16))) uint8_t s_kv[4 * TILE];      // two tiles of K, two of V
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int h = lane >> 5, col = lane & 31;
@@ -125,57 +125,64 @@ __global__ __launch_bounds__(kWaves * 64, DP * QB > 128 ? 1 : 2) void prompt_til
     const int tr = tid / CH, tc = tid % CH, dc = min(tc * 8, a.D - 8);
     const uint16_t *kp = a.k.p + k_row * a.k.ts + (long)hk * a.k.hs;
     const uint16_t *vp = a.v.p + k_row * a.v.ts + (long)hk * a.v.hs;
-    u32x4 kr[LD], vr[LD];
+    u32x4 moved[LD];
     uint32_t kat[LD], vat[LD];                    // bytes from the tile's first row
     const auto rows_at = [&](uint32_t (&at)[LD], long stride, int t) {
 #pragma unroll
         for (int i = 0; i < LD; ++i) at[i] = 2u * (uint32_t)(max(0, min(tr + i * (kWaves * 64 / CH), nk - 1 - t * kKeys)) * (int)stride + dc);
     };
-    const auto fetch = [&](u32x4 (&x)[LD], const uint16_t *p, const uint32_t (&at)[LD], long stride, int t) {
+    const auto fetch = [&](const uint16_t *p, const uint32_t (&at)[LD], long stride, int t) {
         const char *tile = (const char *)(p + min(t, (nk - 1) / kKeys) * kKeys * stride);
 #pragma unroll
-        for (int i = 0; i < LD; ++i) x[i] = *reinterpret_cast<const u32x4 *>(tile + here(at[i]));
+        for (int i = 0; i < LD; ++i) moved[i] = *reinterpret_cast<const u32x4 *>(tile + here(at[i]));
     };
-    const auto store_k = [&](int buf) {
+    // Places in LDS (bytes; 16-byte pieces are XOR-swizzled by row, in the same way for rows that are 16 apart (K), 8 apart (V)), so that what is
+    // read and written differs from these by constants.
+    int k_to, v_to, k_from[KS], v_from[DT];
+    k_to = tr * ROW + (tc ^ swz_k<DP>(tr)) * 16;
+    v_to = VT + tr * ROW + (tc ^ swz_v<DP>(tr)) * 16;
 #pragma unroll
-        for (int i = 0; i < LD; ++i) {
-            const int r = tr + i * (kWaves * 64 / CH);
-            *reinterpret_cast<u32x4 *>(&s_k[buf][r * DP + (tc ^ swz_k<DP>(r)) * 8]) = kr[i];
-        }
-    };
-    const auto store_v = [&](int buf) {
+    for (int st = 0; st < KS; ++st) k_from[st] = col * ROW + ((2 * st + h) ^ swz_k<DP>(col)) * 16;
+    const int v_row = 4 * h + (lane & 15) / 4;
 #pragma unroll
-        for (int i = 0; i < LD; ++i) {
-            const int r = tr + i * (kWaves * 64 / CH);
-            *reinterpret_cast<u32x4 *>(&s_v[buf][r * DP + (tc ^ swz_v<DP>(r)) * 8]) = vr[i];
-        }
+    for (int d = 0; d < DT; ++d) v_from[d] = VT + v_row * ROW + ((4 * d + 2 * ((lane >> 4) & 1) + (lane & 3) / 2) ^ swz_v<DP>(v_row)) * 16 + (lane & 1) * 8;
+    const auto store = [&](int to) {
+#pragma unroll
+        for (int i = 0; i < LD; ++i) *reinterpret_cast<u32x4 *>(&s_kv[to + i * (kWaves * 64 / CH) * ROW]) = moved[i];
     };
-    // Scores of keys 32 n .. of the tile in `buf`.
-    const auto scores = [&](f32x16 (&s)[QB], int buf, int n) {
-        const int row = 32 * n + col;
+    // Scores of keys 32 n .. of a tile.
+    const auto scores = [&](f32x16 (&s)[QB], auto n) {
 #pragma unroll
         for (int i = 0; i < QB; ++i) s[i] = zero16();
 #pragma unroll
         for (int st = 0; st < KS; ++st) {
-            const u32x4 kf = *reinterpret_cast<const u32x4 *>(&s_k[buf][row * DP + ((2 * st + h) ^ swz_k<DP>(row)) * 8]);
+            const u32x4 kf = *reinterpret_cast<const u32x4 *>(&s_kv[k_from[st] + 32 * n * ROW]);
 #pragma unroll
             for (int i = 0; i < QB; ++i) s[i] = mma(kf, qf[i][st], s[i]);
         }
     };
-    // o += V^T P^T for keys 32 n .. of the tile in `buf`.
-    const auto values = [&](const u32x4 (&p)[QB][2], int buf, int n) {
+    // o += V^T P^T for keys 32 n .. of a tile.
+    const auto values = [&](const u32x4 (&p)[QB][2], auto n) {
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const int row = 32 * n + 16 * c + 4 * h + (lane & 15) / 4;
-                const int piece = 4 * d + 2 * ((lane >> 4) & 1) + (lane & 3) / 2, at8 = (lane & 1) * 4;
-                const u32x2 v0 = read_transposed(&s_v[buf][row * DP + (piece ^ swz_v<DP>(row)) * 8 + at8]);
-                const u32x2 v1 = read_transposed(&s_v[buf][(row + 8) * DP + (piece ^ swz_v<DP>(row + 8)) * 8 + at8]);
+                const u32x2 v0 = read_transposed(&s_kv[v_from[d] + (32 * n + 16 * c) * ROW]);
+                const u32x2 v1 = read_transposed(&s_kv[v_from[d] + (32 * n + 16 * c + 8) * ROW]);
                 const u32x4 vf = {v0[0], v0[1], v1[0], v1[1]};
 #pragma unroll
                 for (int i = 0; i < QB; ++i) o[i][d] = mma(vf, p[i][c], o[i][d]);
             }
+    };
+    const auto other_k = [&]() {
+        k_to ^= TILE;
+#pragma unroll
+        for (int st = 0; st < KS; ++st) k_from[st] ^= TILE;
+    };
+    const auto other_v = [&]() {
+        v_to ^= TILE;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) v_from[d] ^= TILE;
     };
     // Weights of the scores s of keys `key0` ..; f: what the sums so far are to be multiplied by.  They may stand relative to any value: a row
     // goes over to a new maximum only where that is 2^8 above the old.
@@ -193,7 +200,7 @@ __global__ __launch_bounds__(kWaves * 64, DP * QB > 128 ? 1 : 2) void prompt_til
             top = other_half_max(top);
             const float next = (top - m[i]) * a.scale_log2 > 8.f ? top : m[i];
             const float base = (next == -INFINITY ? 0.f : next) * a.scale_log2;
-            f[i] = __builtin_amdgcn_exp2f(fmaf(m[i], a.scale_log2, -base));
+            f[i] = next == m[i] ? 1.f : __builtin_amdgcn_exp2f((m[i] - next) * a.scale_log2);
             m[i] = next;
             float sum = 0.f;
 #pragma unroll
@@ -226,42 +233,49 @@ __global__ __launch_bounds__(kWaves * 64, DP * QB > 128 ? 1 : 2) void prompt_til
     u32x4 pa[QB][2], pb[QB][2];
     float f[QB];
     const int last_tile = (nk - 1) / kKeys;
+    typedef std::integral_constant<int, 0> Zero;
+    typedef std::integral_constant<int, 1> One;
+    // Tile t + 1 of K and tile t of V go to LDS meanwhile, each into the place of the one two before it, whose last reader is behind a barrier.
     const auto tile = [&](int t, auto masked) {
-        const int buf = t & 1;
-        if (t + 2 == last_tile) rows_at(kat, a.k.ts, last_tile);
-        if (t + 1 == last_tile) rows_at(vat, a.v.ts, last_tile);
-        scores(sb, buf, 1);
+        if (t + 1 == last_tile) {
+            rows_at(kat, a.k.ts, last_tile);
+            rows_at(vat, a.v.ts, last_tile);
+        }
+        fetch(kp, kat, a.k.ts, t + 1);
+        scores(sb, One{});
+        other_k();
         weights(sa, pa, f, t * kKeys, masked);
-        values(pb, buf ^ 1, 1);                    // the half before: tile t - 1's second
-        store_k(buf ^ 1);                          // tile t + 1
-        store_v(buf);                              // tile t
+        values(pb, One{});                         // the half before: tile t - 1's second
+        other_v();
+        store(k_to);
         rescale(f);
         __syncthreads();
-        fetch(kr, kp, kat, a.k.ts, t + 2);
-        fetch(vr, vp, vat, a.v.ts, t + 1);
-        scores(sa, buf ^ 1, 0);                    // tile t + 1
+        fetch(vp, vat, a.v.ts, t + 1);
+        scores(sa, Zero{});                        // tile t + 1
         weights(sb, pb, f, t * kKeys + 32, masked);
-        values(pa, buf, 0);
+        values(pa, Zero{});
+        store(v_to);
         rescale(f);
     };
     if (n_tiles > 0) {
         rows_at(kat, a.k.ts, 0);
         rows_at(vat, a.v.ts, 0);
-        fetch(kr, kp, kat, a.k.ts, 0);
-        store_k(0);
-        if (last_tile == 1) rows_at(kat, a.k.ts, 1);
-        fetch(kr, kp, kat, a.k.ts, 1);
-        fetch(vr, vp, vat, a.v.ts, 0);
+        fetch(kp, kat, a.k.ts, 0);
+        store(k_to);
+        fetch(vp, vat, a.v.ts, 0);
+        store(v_to);
 #pragma unroll
-        for (int i = 0; i < LD; ++i) *reinterpret_cast<u32x4 *>(&s_v[1][(tid + i * kWaves * 64) * 8]) = u32x4{0, 0, 0, 0};       // values of the half before the first
+        for (int i = 0; i < LD; ++i) *reinterpret_cast<u32x4 *>(&s_kv[VT + TILE + (tid + i * kWaves * 64) * 16]) = u32x4{0, 0, 0, 0};       // values of the half before the first
 #pragma unroll
         for (int i = 0; i < QB; ++i) pb[i][0] = pb[i][1] = u32x4{0, 0, 0, 0};
         __syncthreads();
-        scores(sa, 0, 0);
+        scores(sa, Zero{});
+#pragma unroll
+        for (int d = 0; d < DT; ++d) v_from[d] ^= TILE;
         int t = 0;
         for (; t < whole_tiles; ++t) tile(t, std::false_type{});
         for (; t < n_tiles; ++t) tile(t, std::true_type{});
-        values(pb, (n_tiles - 1) & 1, 1);
+        values(pb, One{});
     }
 
 #pragma unroll
