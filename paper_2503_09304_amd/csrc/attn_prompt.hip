@@ -13,6 +13,7 @@
 
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "attn_pieces.h"
 #include "qattn_internal.h"
@@ -46,6 +47,23 @@ __device__ __forceinline__ float other_half_sum(float v) {
     auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
+template <class F, int... I>
+__device__ __forceinline__ void static_for_impl(F &&f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void static_for(F &&f) {
+    static_for_impl(f, std::make_integer_sequence<int, N>{});
+}
+#ifndef NPRE
+#define NPRE 4
+#endif
+#ifndef NVAL
+#define NVAL 80
+#endif
+#ifndef SCHED
+#define SCHED 1
+#endif
 // An offset of 32 bits that is widened where it is used: widened in front of the loop it would become part of a 64-bit address in vector registers.
 __device__ __forceinline__ uint32_t here(uint32_t v) {
     asm volatile("" : "+v"(v));
@@ -184,9 +202,8 @@ __global__ __launch_bounds__(kWaves * 64, DP * QB > 128 ? 1 : 2) void prompt_til
 #pragma unroll
         for (int d = 0; d < DT; ++d) v_from[d] ^= TILE;
     };
-    // Weights of the scores s of keys `key0` ..; f: what the sums so far are to be multiplied by.  They may stand relative to any value: a row
-    // goes over to a new maximum only where that is 2^8 above the old.
-    const auto weights = [&](f32x16 (&s)[QB], u32x4 (&p)[QB][2], float (&f)[QB], int key0, auto masked) {
+    // Largest score of each row among the scores s of keys `key0` ..; masked: those that a row does not see are taken out first.
+    const auto maxima = [&](f32x16 (&s)[QB], float (&top)[QB], int key0, auto masked) {
 #pragma unroll
         for (int i = 0; i < QB; ++i) {
             if constexpr (masked) {
@@ -194,68 +211,97 @@ __global__ __launch_bounds__(kWaves * 64, DP * QB > 128 ? 1 : 2) void prompt_til
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[i][r] = 8 * (r / 4) + 4 * h + r % 4 > last ? -INFINITY : s[i][r];
             }
-            float top = s[i][0];
+            top[i] = s[i][0];
 #pragma unroll
-            for (int r = 1; r < 16; ++r) top = fmaxf(top, s[i][r]);
-            top = other_half_max(top);
-            const float next = (top - m[i]) * a.scale_log2 > 8.f ? top : m[i];
-            const float base = (next == -INFINITY ? 0.f : next) * a.scale_log2;
-            f[i] = next == m[i] ? 1.f : __builtin_amdgcn_exp2f((m[i] - next) * a.scale_log2);
-            m[i] = next;
+            for (int r = 1; r < 16; ++r) top[i] = fmaxf(top[i], s[i][r]);
+            top[i] = other_half_max(top[i]);
+        }
+    };
+    // Weights of scores, relative to m.
+    const auto weights = [&](f32x16 (&s)[QB], u32x4 (&p)[QB][2]) {
+#pragma unroll
+        for (int i = 0; i < QB; ++i) {
+            const float base = (m[i] == -INFINITY ? 0.f : m[i]) * a.scale_log2;
             float sum = 0.f;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 s[i][r] = __builtin_amdgcn_exp2f(fmaf(s[i][r], a.scale_log2, -base));
                 sum += s[i][r];
             }
-            l[i] = fmaf(l[i], f[i], sum);
+            l[i] += sum;
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) p[i][c][j] = pack_bf16(s[i][8 * c + 2 * j], s[i][8 * c + 2 * j + 1]);
-            asm volatile("" : "+v"(p[i][0]), "+v"(p[i][1]), "+v"(l[i]));         // formed here, not behind the branch of the next rescaling
         }
-    };
-    const auto rescale = [&](const float (&f)[QB]) {
-#pragma unroll
-        for (int i = 0; i < QB; ++i)
-            if (__any(f[i] != 1.f)) {
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[i][d][r] *= f[i];
-            }
     };
 
     // Half a tile (32 keys) at a time: the scores of the next half, the weights of this one and the sums of the one before depend on nothing
     // of each other, so the matrix unit works on the first and third while the vector unit forms the second.
     f32x16 sa[QB], sb[QB];
     u32x4 pa[QB][2], pb[QB][2];
-    float f[QB];
+    float top[QB];
+    // The sums may stand relative to any value: they go over to a new maximum only where that is 2^8 above the old.  The weights p of the half
+    // before are still relative to the old one, so their sums (half n of the tile at v_from) are taken first.
+    const auto grow = [&](u32x4 (&p)[QB][2], auto n) {
+        bool over = false;
+#pragma unroll
+        for (int i = 0; i < QB; ++i) over |= (top[i] - m[i]) * a.scale_log2 > 8.f;
+        if (__any(over)) {
+            values(p, n);
+#pragma unroll
+            for (int i = 0; i < QB; ++i) {
+                p[i][0] = p[i][1] = u32x4{0, 0, 0, 0};
+                const float next = (top[i] - m[i]) * a.scale_log2 > 8.f ? top[i] : m[i];
+                const float f = next == m[i] ? 1.f : __builtin_amdgcn_exp2f((m[i] - next) * a.scale_log2);
+                m[i] = next;
+                l[i] *= f;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[i][d][r] *= f;
+            }
+        }
+    };
+    // The order of such a half: matrix instructions with LDS reads for the ones behind them and VALU instructions between them.
+    const auto interleave = [&](auto masked) {
+        constexpr int M = (KS + 2 * DT) * QB, R = KS + 4 * DT, V = (masked ? 120 : NVAL) * QB / M + 1;
+        __builtin_amdgcn_sched_group_barrier(0x100, NPRE, 0);
+        static_for<M>([&](auto i) {
+            constexpr int reads = (i + 1) * (R - NPRE) / M - i * (R - NPRE) / M;
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if constexpr (reads > 0) __builtin_amdgcn_sched_group_barrier(0x100, reads, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, V, 0);
+        });
+    };
+    // Tile t + 1 of K and tile t of V go to LDS meanwhile, each into the place of the one two before it, whose last reader is behind a barrier.
     const int last_tile = (nk - 1) / kKeys;
     typedef std::integral_constant<int, 0> Zero;
     typedef std::integral_constant<int, 1> One;
-    // Tile t + 1 of K and tile t of V go to LDS meanwhile, each into the place of the one two before it, whose last reader is behind a barrier.
     const auto tile = [&](int t, auto masked) {
         if (t + 1 == last_tile) {
             rows_at(kat, a.k.ts, last_tile);
             rows_at(vat, a.v.ts, last_tile);
         }
         fetch(kp, kat, a.k.ts, t + 1);
+        grow(pb, One{});
         scores(sb, One{});
-        other_k();
-        weights(sa, pa, f, t * kKeys, masked);
+        weights(sa, pa);
         values(pb, One{});                         // the half before: tile t - 1's second
+        maxima(sb, top, t * kKeys + 32, masked);
+        other_k();
         other_v();
         store(k_to);
-        rescale(f);
+        if constexpr (SCHED) interleave(masked);
         __syncthreads();
         fetch(vp, vat, a.v.ts, t + 1);
+        grow(pa, Zero{});
         scores(sa, Zero{});                        // tile t + 1
-        weights(sb, pb, f, t * kKeys + 32, masked);
+        weights(sb, pb);
         values(pa, Zero{});
+        maxima(sa, top, (t + 1) * kKeys, masked);
         store(v_to);
-        rescale(f);
+        if constexpr (SCHED) interleave(masked);
     };
     if (n_tiles > 0) {
         rows_at(kat, a.k.ts, 0);
@@ -270,10 +316,11 @@ __global__ __launch_bounds__(kWaves * 64, DP * QB > 128 ? 1 : 2) void prompt_til
         for (int i = 0; i < QB; ++i) pb[i][0] = pb[i][1] = u32x4{0, 0, 0, 0};
         __syncthreads();
         scores(sa, Zero{});
+        maxima(sa, top, 0, std::true_type{});
 #pragma unroll
         for (int d = 0; d < DT; ++d) v_from[d] ^= TILE;
         int t = 0;
-        for (; t < whole_tiles; ++t) tile(t, std::false_type{});
+        for (; t + 1 < whole_tiles; ++t) tile(t, std::false_type{});
         for (; t < n_tiles; ++t) tile(t, std::true_type{});
         values(pb, One{});
     }
