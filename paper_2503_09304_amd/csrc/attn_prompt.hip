@@ -129,10 +129,13 @@ __global__ __launch_bounds__(kWaves * 64, DP * QB > 128 ? 1 : 2) void prompt_til
             if (16 * s >= a.D) qf[i][s] = u32x4{0, 0, 0, 0};
     }
     f32x16 o[QB][DT];
-    float m[QB], l[QB];
+    float m[QB], l[QB];                           // what a row's sums are relative to, the sum of its weights (of the lane's half of the keys)
+    float base[QB], limit[QB];                    // m in powers of two, 0 before there is one; the largest score that needs no other m
+    const float slack = 8.f / a.scale_log2;
 #pragma unroll
     for (int i = 0; i < QB; ++i) {
-        m[i] = -INFINITY;
+        m[i] = limit[i] = -INFINITY;
+        base[i] = 0.f;
         l[i] = 0.f;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[i][d] = zero16();
@@ -202,7 +205,8 @@ __global__ __launch_bounds__(kWaves * 64, DP * QB > 128 ? 1 : 2) void prompt_til
 #pragma unroll
         for (int d = 0; d < DT; ++d) v_from[d] ^= TILE;
     };
-    // Largest score of each row among the scores s of keys `key0` ..; masked: those that a row does not see are taken out first.
+    // Largest of the lane's scores of each row (its other half is in lane ^ 32), keys `key0` ..; masked: those that a row does not see are
+    // taken out first.
     const auto maxima = [&](f32x16 (&s)[QB], float (&top)[QB], int key0, auto masked) {
 #pragma unroll
         for (int i = 0; i < QB; ++i) {
@@ -214,21 +218,17 @@ __global__ __launch_bounds__(kWaves * 64, DP * QB > 128 ? 1 : 2) void prompt_til
             top[i] = s[i][0];
 #pragma unroll
             for (int r = 1; r < 16; ++r) top[i] = fmaxf(top[i], s[i][r]);
-            top[i] = other_half_max(top[i]);
         }
     };
-    // Weights of scores, relative to m.
+    // Weights of scores, relative to m, and their sum (before they are rounded: lse is as exact as fp32).
     const auto weights = [&](f32x16 (&s)[QB], u32x4 (&p)[QB][2]) {
 #pragma unroll
         for (int i = 0; i < QB; ++i) {
-            const float base = (m[i] == -INFINITY ? 0.f : m[i]) * a.scale_log2;
-            float sum = 0.f;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[i][r] = __builtin_amdgcn_exp2f(fmaf(s[i][r], a.scale_log2, -base));
-                sum += s[i][r];
+                s[i][r] = __builtin_amdgcn_exp2f(fmaf(s[i][r], a.scale_log2, -base[i]));
+                l[i] += s[i][r];
             }
-            l[i] += sum;
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -246,15 +246,17 @@ __global__ __launch_bounds__(kWaves * 64, DP * QB > 128 ? 1 : 2) void prompt_til
     const auto grow = [&](u32x4 (&p)[QB][2], auto n) {
         bool over = false;
 #pragma unroll
-        for (int i = 0; i < QB; ++i) over |= (top[i] - m[i]) * a.scale_log2 > 8.f;
+        for (int i = 0; i < QB; ++i) over |= top[i] > limit[i];
         if (__any(over)) {
             values(p, n);
 #pragma unroll
             for (int i = 0; i < QB; ++i) {
                 p[i][0] = p[i][1] = u32x4{0, 0, 0, 0};
-                const float next = (top[i] - m[i]) * a.scale_log2 > 8.f ? top[i] : m[i];
+                const float most = other_half_max(top[i]), next = most > limit[i] ? most : m[i];
                 const float f = next == m[i] ? 1.f : __builtin_amdgcn_exp2f((m[i] - next) * a.scale_log2);
                 m[i] = next;
+                base[i] = next == -INFINITY ? 0.f : next * a.scale_log2;
+                limit[i] = next + slack;
                 l[i] *= f;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
