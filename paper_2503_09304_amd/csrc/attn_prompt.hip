@@ -1,6 +1,6 @@
 // attn_prompt: attention over packed prompts, causal or not, heads grouped over shared keys.
 //
-// One pass over the keys with the running maximum and sum of the softmax.  A workgroup has 4 waves; a wave owns 32 * QB queries of one
+// One pass over the keys with the running maximum and sum of the softmax.  A workgroup has 4 waves; a wave owns 32 queries of one
 // head and goes through the keys 64 at a time:
 //     S^T[key, q] = K Q^T     v_mfma_f32_32x32x16_bf16, A = 32 keys x 16 d, B = 16 d x 32 queries
 //     O^T[d, q]   = V^T P^T   A = 32 d x 16 keys,  B = 16 keys x 32 queries
@@ -23,7 +23,7 @@ namespace {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -31,21 +31,20 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 constexpr int kWaves = 4;
 constexpr int kKeys = 64;                         // keys of a tile
 
-__device__ __forceinline__ f32x16 mma(const u32x4 &a, const u32x4 &b, const f32x16 &c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+__device__ __forceinline__ f32x4 mma(const u32x4 &a, const u32x4 &b, const f32x4 &c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     const bf16x2 r = {(__bf16)a, (__bf16)b};
     return __builtin_bit_cast(uint32_t, r);
 }
-__device__ __forceinline__ f32x16 zero16() { return f32x16{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}; }
-__device__ __forceinline__ float other_half_max(float v) {
-    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-}
-__device__ __forceinline__ float other_half_sum(float v) {
-    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+// Over the 4 lanes that hold one row, in each of them.
+template <class F>
+__device__ __forceinline__ float row_all(float v, F &&f) {
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 template <class F, int... I>
 __device__ __forceinline__ void static_for_impl(F &&f, std::integer_sequence<int, I...>) {
@@ -55,14 +54,8 @@ template <int N, class F>
 __device__ __forceinline__ void static_for(F &&f) {
     static_for_impl(f, std::make_integer_sequence<int, N>{});
 }
-#ifndef NPRE
-#define NPRE 4
-#endif
-#ifndef NVAL
-#define NVAL 80
-#endif
-#ifndef SCHED
-#define SCHED 1
+#ifndef LA
+#define LA 4
 #endif
 // An offset of 32 bits that is widened where it is used: widened in front of the loop it would become part of a 64-bit address in vector registers.
 __device__ __forceinline__ uint32_t here(uint32_t v) {
@@ -75,11 +68,12 @@ __device__ __forceinline__ u32x2 read_transposed(const uint8_t *p) {
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p));
 }
 
-// Slots of 16 bytes: piece c of row r of a tile stands at c ^ swz(r).
+// Slots of 16 bytes: piece c of row r of a tile stands at c ^ swz(r), so that what a read takes in at once, 256 bytes, comes from all banks: one piece
+// of 16 rows (K), two of 8 rows (V).
 template <int DP>
-__device__ __forceinline__ int swz_k(int r) { return DP == 128 ? (r & 15) : (r & 7); }
+__device__ __forceinline__ int swz_k(int r) { return DP == 128 ? r & 15 : (r >> 1) & 7; }
 template <int DP>
-__device__ __forceinline__ int swz_v(int r) { return DP == 128 ? 2 * (r & 7) : 2 * (r & 3); }
+__device__ __forceinline__ int swz_v(int r) { return DP == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); }
 
 // An entry of cu, held to 0..n and to what the entry before it allows.
 __device__ __forceinline__ int2 span(const int32_t *cu, int b, int n) {
@@ -87,18 +81,18 @@ __device__ __forceinline__ int2 span(const int32_t *cu, int b, int n) {
     return {lo, min(max(cu[b + 1], lo), n)};
 }
 
-template <int DP, int QB>
-__global__ __launch_bounds__(kWaves * 64, DP * QB > 128 ? 1 : 2) void prompt_tile(const PromptArgs a, int tiles, int item0) {
-    constexpr int QT = kWaves * 32 * QB;          // queries of a workgroup
+template <int DP>
+__global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a, int tiles, int item0) {
+    constexpr int QT = kWaves * 32;               // queries of a workgroup
     constexpr int CH = DP / 8;                    // 16-byte pieces of a row
-    constexpr int KS = DP / 16;                   // MFMA steps of a score
-    constexpr int DT = DP / 32;                   // 32-d tiles of the output
+    constexpr int KS = DP / 32;                   // MFMA steps of a score
+    constexpr int DT = DP / 16;                   // 16-d tiles of the output
     constexpr int LD = kKeys * CH / (kWaves * 64);   // pieces of K (and V) that a thread moves per tile
     constexpr int ROW = DP * 2, TILE = kKeys * ROW, VT = 2 * TILE;       // bytes
     __shared__ __attribute__((aligned(16))) uint8_t s_kv[4 * TILE];      // two tiles of K, two of V
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int h = lane >> 5, col = lane & 31;
+    const int g = lane >> 4, col = lane & 15;
     // Neighbouring workgroups run on different XCDs: those of one key/value head are Hk apart, so with 8 such heads
     // each XCD's L2 holds the keys of one.  Late tiles of a sequence see the most keys: they start first.
     const int G = a.Hq / a.Hk, num = blockIdx.x + item0;
@@ -111,35 +105,29 @@ __global__ __launch_bounds__(kWaves * 64, DP * QB > 128 ? 1 : 2) void prompt_til
     const int nq = __builtin_amdgcn_readfirstlane(sq.y - sq.x), nk = __builtin_amdgcn_readfirstlane(sk.y - sk.x);
     const int r0 = at.piece * QT;                 // first query of the tile, within the sequence
     const long q_row = __builtin_amdgcn_readfirstlane(sq.x), k_row = __builtin_amdgcn_readfirstlane(sk.x);
-    const int w0 = r0 + wave * 32 * QB;                                        // first query of the wave
+    const int w0 = r0 + wave * 32;                                        // first query of the wave
     // tiles of keys that the tile's last query sees, and those that its first query sees whole
     const int shift = nk - nq;
     const int n_tiles = ((a.causal ? min(nk, max(0, shift + min(nq, r0 + QT))) : nk) + kKeys - 1) / kKeys;
     const int whole_tiles = min(nk, a.causal ? max(0, shift + r0 + 1) : nk) / kKeys;
 
-    u32x4 qf[QB][KS];
+    u32x4 qf[2][KS];                              // queries w0 + col, w0 + 16 + col
 #pragma unroll
-    for (int i = 0; i < QB; ++i) {
-        const int r = w0 + 32 * i + col;
-        const uint16_t *p = a.q.p + (q_row + min(r, nq - 1)) * a.q.ts + (long)head * a.q.hs;
+    for (int q = 0; q < 2; ++q) {
+        const uint16_t *p = a.q.p + (q_row + min(w0 + 16 * q + col, nq - 1)) * a.q.ts + (long)head * a.q.hs;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) qf[i][s] = *reinterpret_cast<const u32x4 *>(p + min(16 * s, a.D - 16) + 8 * h);
+        for (int s = 0; s < KS; ++s) qf[q][s] = *reinterpret_cast<const u32x4 *>(p + min(32 * s + 8 * g, a.D - 8));
 #pragma unroll
         for (int s = 0; s < KS; ++s)
-            if (16 * s >= a.D) qf[i][s] = u32x4{0, 0, 0, 0};
+            if (32 * s + 8 * g >= a.D) qf[q][s] = u32x4{0, 0, 0, 0};
     }
-    f32x16 o[QB][DT];
-    float m[QB], l[QB];                           // what a row's sums are relative to, the sum of its weights (of the lane's half of the keys)
-    float base[QB], limit[QB];                    // m in powers of two, 0 before there is one; the largest score that needs no other m
+    f32x4 o[DT][2];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[d][0] = o[d][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // What a row's sums are relative to, in powers of two too (0 before there is one), and the largest score that needs no other; the sum of
+    // its weights, and the largest score of the half tile that is next (both of the lane's keys: the others are 16, 32 and 48 lanes away).
     const float slack = 8.f / a.scale_log2;
-#pragma unroll
-    for (int i = 0; i < QB; ++i) {
-        m[i] = limit[i] = -INFINITY;
-        base[i] = 0.f;
-        l[i] = 0.f;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) o[i][d] = zero16();
-    }
+    float m[2] = {-INFINITY, -INFINITY}, base[2] = {0.f, 0.f}, limit[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, top[2];
 
     // The 16-byte pieces that this thread moves: rows tr + i * (256 / CH) of a tile, piece tc.  Rows behind the last key are that key again
     // (their weights are 0), pieces behind the end of a head its last one (the queries are 0 there, those outputs are not stored).
@@ -163,37 +151,19 @@ __global__ __launch_bounds__(kWaves * 64, DP * QB > 128 ? 1 : 2) void prompt_til
     k_to = tr * ROW + (tc ^ swz_k<DP>(tr)) * 16;
     v_to = VT + tr * ROW + (tc ^ swz_v<DP>(tr)) * 16;
 #pragma unroll
-    for (int st = 0; st < KS; ++st) k_from[st] = col * ROW + ((2 * st + h) ^ swz_k<DP>(col)) * 16;
-    const int v_row = 4 * h + (lane & 15) / 4;
+    for (int st = 0; st < KS; ++st) k_from[st] = col * ROW + ((4 * st + g) ^ swz_k<DP>(col)) * 16;
+    const int v_row = 4 * g + col / 4;
 #pragma unroll
-    for (int d = 0; d < DT; ++d) v_from[d] = VT + v_row * ROW + ((4 * d + 2 * ((lane >> 4) & 1) + (lane & 3) / 2) ^ swz_v<DP>(v_row)) * 16 + (lane & 1) * 8;
+    for (int d = 0; d < DT; ++d) v_from[d] = VT + v_row * ROW + ((2 * d + (lane & 3) / 2) ^ swz_v<DP>(v_row)) * 16 + (lane & 1) * 8;
     const auto store = [&](int to) {
 #pragma unroll
         for (int i = 0; i < LD; ++i) *reinterpret_cast<u32x4 *>(&s_kv[to + i * (kWaves * 64 / CH) * ROW]) = moved[i];
     };
-    // Scores of keys 32 n .. of a tile.
-    const auto scores = [&](f32x16 (&s)[QB], auto n) {
-#pragma unroll
-        for (int i = 0; i < QB; ++i) s[i] = zero16();
-#pragma unroll
-        for (int st = 0; st < KS; ++st) {
-            const u32x4 kf = *reinterpret_cast<const u32x4 *>(&s_kv[k_from[st] + 32 * n * ROW]);
-#pragma unroll
-            for (int i = 0; i < QB; ++i) s[i] = mma(kf, qf[i][st], s[i]);
-        }
-    };
-    // o += V^T P^T for keys 32 n .. of a tile.
-    const auto values = [&](const u32x4 (&p)[QB][2], auto n) {
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const u32x2 v0 = read_transposed(&s_kv[v_from[d] + (32 * n + 16 * c) * ROW]);
-                const u32x2 v1 = read_transposed(&s_kv[v_from[d] + (32 * n + 16 * c + 8) * ROW]);
-                const u32x4 vf = {v0[0], v0[1], v1[0], v1[1]};
-#pragma unroll
-                for (int i = 0; i < QB; ++i) o[i][d] = mma(vf, p[i][c], o[i][d]);
-            }
+    // A operands: keys 32 n + 16 t .. of the tile at k_from, elements 32 st ..; values of keys 32 n .., elements 16 d ...
+    const auto k_frag = [&](int n, int t, int st) { return *reinterpret_cast<const u32x4 *>(&s_kv[k_from[st] + (32 * n + 16 * t) * ROW]); };
+    const auto v_frag = [&](int n, int d) {
+        const u32x2 v0 = read_transposed(&s_kv[v_from[d] + 32 * n * ROW]), v1 = read_transposed(&s_kv[v_from[d] + (32 * n + 16) * ROW]);
+        return u32x4{v0[0], v0[1], v1[0], v1[1]};
     };
     const auto other_k = [&]() {
         k_to ^= TILE;
@@ -205,77 +175,86 @@ __global__ __launch_bounds__(kWaves * 64, DP * QB > 128 ? 1 : 2) void prompt_til
 #pragma unroll
         for (int d = 0; d < DT; ++d) v_from[d] ^= TILE;
     };
-    // Largest of the lane's scores of each row (its other half is in lane ^ 32), keys `key0` ..; masked: those that a row does not see are
-    // taken out first.
-    const auto maxima = [&](f32x16 (&s)[QB], float (&top)[QB], int key0, auto masked) {
+    // o += V^T P^T for keys 32 n .. of the tile at v_from.
+    const auto add_values = [&](const u32x4 &v, const u32x4 (&p)[2], int d) {
 #pragma unroll
-        for (int i = 0; i < QB; ++i) {
+        for (int q = 0; q < 2; ++q) o[d][q] = mma(v, p[q], o[d][q]);
+    };
+    // Scores: [query tile][key tile], a lane's element r is key 16 t + 4 g + r of query 16 q + col.
+    typedef f32x4 Scores[2][2];
+    const auto add_scores = [&](const u32x4 &k, Scores &s, int t, int st) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) s[q][t] = mma(k, qf[q][st], st == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[q][t]);
+    };
+    // The largest of the lane's scores s of keys `key0` ..; masked: those that the row does not see are taken out first.
+    const auto maximum = [&](Scores &s, int key0, auto masked) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
             if constexpr (masked) {
-                const int last = min(nk - 1, a.causal ? shift + w0 + 32 * i + col : nk - 1) - key0;
+                const int last = min(nk - 1, a.causal ? shift + w0 + 16 * q + col : nk - 1) - key0 - 4 * g;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[i][r] = 8 * (r / 4) + 4 * h + r % 4 > last ? -INFINITY : s[i][r];
+                for (int r = 0; r < 8; ++r) s[q][r / 4][r % 4] = 16 * (r / 4) + r % 4 > last ? -INFINITY : s[q][r / 4][r % 4];
             }
-            top[i] = s[i][0];
+            top[q] = s[q][0][0];
 #pragma unroll
-            for (int r = 1; r < 16; ++r) top[i] = fmaxf(top[i], s[i][r]);
+            for (int r = 1; r < 8; ++r) top[q] = fmaxf(top[q], s[q][r / 4][r % 4]);
         }
     };
-    // Weights of scores, relative to m, and their sum (before they are rounded: lse is as exact as fp32).
-    const auto weights = [&](f32x16 (&s)[QB], u32x4 (&p)[QB][2]) {
-#pragma unroll
-        for (int i = 0; i < QB; ++i) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[i][r] = __builtin_amdgcn_exp2f(fmaf(s[i][r], a.scale_log2, -base[i]));
-                l[i] += s[i][r];
-            }
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) p[i][c][j] = pack_bf16(s[i][8 * c + 2 * j], s[i][8 * c + 2 * j + 1]);
-        }
-    };
-
-    // Half a tile (32 keys) at a time: the scores of the next half, the weights of this one and the sums of the one before depend on nothing
-    // of each other, so the matrix unit works on the first and third while the vector unit forms the second.
-    f32x16 sa[QB], sb[QB];
-    u32x4 pa[QB][2], pb[QB][2];
-    float top[QB];
     // The sums may stand relative to any value: they go over to a new maximum only where that is 2^8 above the old.  The weights p of the half
     // before are still relative to the old one, so their sums (half n of the tile at v_from) are taken first.
-    const auto grow = [&](u32x4 (&p)[QB][2], auto n) {
-        bool over = false;
+    const auto grow = [&](u32x4 (&p)[2], auto n) {
+        if (__any(top[0] > limit[0] || top[1] > limit[1])) {
+            static_for<DT>([&](auto d) { add_values(v_frag(n, d), p, d); });
 #pragma unroll
-        for (int i = 0; i < QB; ++i) over |= top[i] > limit[i];
-        if (__any(over)) {
-            values(p, n);
+            for (int q = 0; q < 2; ++q) {
+                p[q] = u32x4{0, 0, 0, 0};
+                const float most = row_all(top[q], [](float x, float y) { return fmaxf(x, y); }), next = most > limit[q] ? most : m[q];
+                const float f = next == m[q] ? 1.f : __builtin_amdgcn_exp2f((m[q] - next) * a.scale_log2);
+                m[q] = next;
+                base[q] = next == -INFINITY ? 0.f : next * a.scale_log2;
+                limit[q] = next + slack;
+                l[q] *= f;
 #pragma unroll
-            for (int i = 0; i < QB; ++i) {
-                p[i][0] = p[i][1] = u32x4{0, 0, 0, 0};
-                const float most = other_half_max(top[i]), next = most > limit[i] ? most : m[i];
-                const float f = next == m[i] ? 1.f : __builtin_amdgcn_exp2f((m[i] - next) * a.scale_log2);
-                m[i] = next;
-                base[i] = next == -INFINITY ? 0.f : next * a.scale_log2;
-                limit[i] = next + slack;
-                l[i] *= f;
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[i][d][r] *= f;
+                for (int d = 0; d < DT; ++d) o[d][q] *= f;
             }
         }
     };
-    // The order of such a half: matrix instructions with LDS reads for the ones behind them and VALU instructions between them.
-    const auto interleave = [&](auto masked) {
-        constexpr int M = (KS + 2 * DT) * QB, R = KS + 4 * DT, V = (masked ? 120 : NVAL) * QB / M + 1;
-        __builtin_amdgcn_sched_group_barrier(0x100, NPRE, 0);
+    // Half a tile (32 keys) at a time: the scores of the next half, the weights of this one and the sums of the one before depend on nothing
+    // of each other, so the matrix unit works on the first and third while the vector unit forms the second.
+    // Step by step: a matrix instruction, the LDS read of the one LA steps behind it, and a share of the vector work.  Left to the
+    // compiler the reads stand right in front of their use, and each waits out LDS.
+    // Scores of half n_k of the tile at k_from -> next (and their maxima -> top), weights of cur -> p_cur, sums of half n_v with p_old.
+    const auto half = [&](Scores &next, auto n_k, Scores &cur, u32x4 (&p_cur)[2], const u32x4 (&p_old)[2], auto n_v, int key0, auto masked) {
+        constexpr int N = 2 * KS, M = 2 * N;          // score steps (and as many steps for the sums), steps in all
+        // Scores and sums in turn, so that no step waits for the one before; the last scores a little earlier, their maxima are last.
+        constexpr auto is_score = [](int i) { return i < M - 4 ? i % 2 == 0 : i < M - 2; };
+        constexpr auto index = [](int i) { return i < M - 4 ? i / 2 : N - 2 + i % 2; };
+        u32x4 frag[M];
+        const auto read = [&](auto i) {
+            constexpr int j = index(i);
+            if constexpr (is_score(i)) frag[i] = k_frag(n_k, j / KS, j % KS);
+            else frag[i] = v_frag(n_v, j);
+        };
+        const auto weight = [&](int i) {
+            const int q = i / 8, t = i % 8 / 4, r = i % 4;
+            cur[q][t][r] = __builtin_amdgcn_exp2f(fmaf(cur[q][t][r], a.scale_log2, -base[q]));
+            l[q] += cur[q][t][r];
+            if (r & 1) p_cur[q][2 * t + r / 2] = pack_bf16(cur[q][t][r - 1], cur[q][t][r]);
+        };
+        static_for<LA>(read);
+        __builtin_amdgcn_sched_barrier(0);
         static_for<M>([&](auto i) {
-            constexpr int reads = (i + 1) * (R - NPRE) / M - i * (R - NPRE) / M;
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            if constexpr (reads > 0) __builtin_amdgcn_sched_group_barrier(0x100, reads, 0);
-            __builtin_amdgcn_sched_group_barrier(0x002, V, 0);
+            constexpr int j = index(i);
+            if constexpr (is_score(i)) add_scores(frag[i], next, j / KS, j % KS);
+            else add_values(frag[i], p_old, j);
+            if constexpr (i + LA < M) read(std::integral_constant<int, i + LA>{});
+            static_for<16 / M>([&](auto r) { weight(i * (16 / M) + r); });
+            __builtin_amdgcn_sched_barrier(0);
         });
+        maximum(next, key0, masked);
     };
+    Scores sa, sb;
+    u32x4 pa[2], pb[2];
     // Tile t + 1 of K and tile t of V go to LDS meanwhile, each into the place of the one two before it, whose last reader is behind a barrier.
     const int last_tile = (nk - 1) / kKeys;
     typedef std::integral_constant<int, 0> Zero;
@@ -287,23 +266,15 @@ __global__ __launch_bounds__(kWaves * 64, DP * QB > 128 ? 1 : 2) void prompt_til
         }
         fetch(kp, kat, a.k.ts, t + 1);
         grow(pb, One{});
-        scores(sb, One{});
-        weights(sa, pa);
-        values(pb, One{});                         // the half before: tile t - 1's second
-        maxima(sb, top, t * kKeys + 32, masked);
+        half(sb, One{}, sa, pa, pb, One{}, t * kKeys + 32, masked);      // the half before: tile t - 1's second
         other_k();
         other_v();
         store(k_to);
-        if constexpr (SCHED) interleave(masked);
         __syncthreads();
         fetch(vp, vat, a.v.ts, t + 1);
         grow(pa, Zero{});
-        scores(sa, Zero{});                        // tile t + 1
-        weights(sb, pb);
-        values(pa, Zero{});
-        maxima(sa, top, (t + 1) * kKeys, masked);
+        half(sa, Zero{}, sb, pb, pa, Zero{}, (t + 1) * kKeys, masked);   // the next: tile t + 1's first
         store(v_to);
-        if constexpr (SCHED) interleave(masked);
     };
     if (n_tiles > 0) {
         rows_at(kat, a.k.ts, 0);
@@ -315,53 +286,46 @@ __global__ __launch_bounds__(kWaves * 64, DP * QB > 128 ? 1 : 2) void prompt_til
 #pragma unroll
         for (int i = 0; i < LD; ++i) *reinterpret_cast<u32x4 *>(&s_kv[VT + TILE + (tid + i * kWaves * 64) * 16]) = u32x4{0, 0, 0, 0};       // values of the half before the first
 #pragma unroll
-        for (int i = 0; i < QB; ++i) pb[i][0] = pb[i][1] = u32x4{0, 0, 0, 0};
+        for (int i = 0; i < 2; ++i) pb[i] = u32x4{0, 0, 0, 0};
         __syncthreads();
-        scores(sa, Zero{});
-        maxima(sa, top, 0, std::true_type{});
+        static_for<2 * KS>([&](auto i) { add_scores(k_frag(0, i / KS, i % KS), sa, i / KS, i % KS); });
+        maximum(sa, 0, std::true_type{});
 #pragma unroll
         for (int d = 0; d < DT; ++d) v_from[d] ^= TILE;
         int t = 0;
         for (; t + 1 < whole_tiles; ++t) tile(t, std::false_type{});
         for (; t < n_tiles; ++t) tile(t, std::true_type{});
-        values(pb, One{});
+        static_for<DT>([&](auto d) { add_values(v_frag(1, d), pb, d); });
     }
 
 #pragma unroll
-    for (int i = 0; i < QB; ++i) {
-        const float sum = other_half_sum(l[i]), inv = sum > 0.f ? 1.f / sum : 0.f;
-        const int r = w0 + 32 * i + col;
+    for (int q = 0; q < 2; ++q) {
+        const float sum = row_all(l[q], [](float x, float y) { return x + y; }), inv = sum > 0.f ? 1.f / sum : 0.f;
+        const int r = w0 + 16 * q + col;
         if (r >= nq) continue;
         uint16_t *to = a.o.p + (q_row + r) * a.o.ts + (long)head * a.o.hs;
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int e = 32 * d + 8 * j + 4 * h;
-                const u32x2 x = {pack_bf16(o[i][d][4 * j] * inv, o[i][d][4 * j + 1] * inv), pack_bf16(o[i][d][4 * j + 2] * inv, o[i][d][4 * j + 3] * inv)};
-                if (e < a.D) *reinterpret_cast<u32x2 *>(to + e) = x;
-            }
-        if (a.lse != nullptr && h == 0)
-            a.lse[(q_row + r) * a.Hq + head] = sum > 0.f ? (m[i] * a.scale_log2 + __log2f(sum)) * 0.69314718055994530942f : -INFINITY;
+        for (int d = 0; d < DT; ++d) {
+            const f32x4 x = o[d][q] * inv;
+            if (16 * d < a.D) *reinterpret_cast<u32x2 *>(to + 16 * d + 4 * g) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+        }
+        if (a.lse != nullptr && g == 0) a.lse[(q_row + r) * a.Hq + head] = sum > 0.f ? (m[q] * a.scale_log2 + __log2f(sum)) * 0.69314718055994530942f : -INFINITY;
     }
 }
 
-template <int DP, int QB>
+template <int DP>
 void prompt_n(const PromptArgs &a, hipStream_t s) {
-    const long tiles = (a.n_q + (long)kWaves * 32 * QB - 1) / (kWaves * 32 * QB) + a.n_seqs, all = tiles * a.Hq;
+    const long tiles = (a.n_q + (long)kWaves * 32 - 1) / (kWaves * 32) + a.n_seqs, all = tiles * a.Hq;
     // a launch of 2^32 threads or more would lose the excess
     for (long at = 0; at < all; at += 1 << 23)
-        prompt_tile<DP, QB><<<dim3((unsigned)std::min<long>(all - at, 1 << 23)), dim3(kWaves * 64), 0, s>>>(a, (int)tiles, (int)at);
+        prompt_tile<DP><<<dim3((unsigned)std::min<long>(all - at, 1 << 23)), dim3(kWaves * 64), 0, s>>>(a, (int)tiles, (int)at);
 }
 
 }  // namespace
 
-#ifndef QBSEL
-#define QBSEL 1
-#endif
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t s) {
-    if (a.D <= 64) prompt_n<64, QBSEL>(a, s);
-    else prompt_n<128, QBSEL>(a, s);
+    if (a.D <= 64) prompt_n<64>(a, s);
+    else prompt_n<128>(a, s);
     return hipGetLastError();
 }
 
