@@ -19,6 +19,14 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
     v = add_from<0x142, 0xA>(v);      // row_bcast:15 into rows 1 and 3
     return add_from<0x143, 0xC>(v);   // row_bcast:31 into rows 2 and 3
 }
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {       // in the last lane
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xA, 0xF, false));
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xC, 0xF, false));
+}
 __device__ __forceinline__ uint32_t last_lane(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, 63); }
 
 struct Piece {
@@ -41,6 +49,51 @@ __device__ __forceinline__ Piece find_piece(int n_seqs, uint32_t item, S &&size,
         before += last_lane(upto);
     }
     return {-1, 0, 0};
+}
+
+struct Tile {
+    int seq, piece;                   // seq -1: there is no such number
+};
+
+// The same for pieces that are dealt out heaviest first: sequence b has pieces 0 .. n(b) - 1, the work of piece p is e(b) + p (what it stands for only
+// sets the order).  Numbers go by falling work, then by sequence.  shape(b): {n, e}.
+template <class F>
+__device__ __forceinline__ Tile find_heaviest(int n_seqs, uint32_t number, F &&shape) {
+    const int lane = threadIdx.x & 63;
+    const auto at = [&](int b0) { return b0 + lane < n_seqs ? shape(b0 + lane) : int2{0, 0}; };
+    const int2 mine = at(0);                                          // all there is to load where there are 64 sequences or fewer
+    // pieces with work w or more, of this lane's sequences
+    const auto from = [](int2 s, int w) { return (uint32_t)min(max(s.x + s.y - w, 0), s.x); };
+    const auto count = [&](int w) {
+        uint32_t n = from(mine, w);
+        for (int b0 = 64; b0 < n_seqs; b0 += 64) n += from(at(b0), w);
+        return last_lane(wave_scan(n));
+    };
+    int top = mine.x + mine.y;
+    for (int b0 = 64; b0 < n_seqs; b0 += 64) {
+        const int2 s = at(b0);
+        top = max(top, s.x + s.y);
+    }
+    uint32_t hi = last_lane(wave_max((uint32_t)top)), lo = 0;         // count(hi) = 0 <= number
+    if (count(0) <= number) return {-1, 0};
+    while (hi - lo > 1) {                                             // count(lo) > number >= count(hi)
+        const uint32_t mid = lo + (hi - lo) / 2;
+        (count((int)mid) > number ? lo : hi) = mid;
+    }
+    // the number-th piece with work lo, in the order of the sequences
+    uint32_t left = number - count((int)hi);
+    for (int b0 = 0; b0 < n_seqs; b0 += 64) {
+        const int2 s = b0 == 0 ? mine : at(b0);
+        unsigned long long has = __ballot(from(s, (int)lo) > from(s, (int)hi));
+        const uint32_t n = __popcll(has);
+        if (left >= n) {
+            left -= n;
+            continue;
+        }
+        const int l = __builtin_ctzll(__ballot(((has >> lane) & 1) != 0 && __popcll(has & ((1ull << lane) - 1)) == left));
+        return {b0 + l, (int)lo - __builtin_amdgcn_readlane(s.y, l)};
+    }
+    return {-1, 0};
 }
 
 }  // namespace qattn

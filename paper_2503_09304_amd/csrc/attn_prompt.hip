@@ -94,11 +94,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = lane >> 4, col = lane & 15;
     // Neighbouring workgroups run on different XCDs: those of one key/value head are Hk apart, so with 8 such heads
-    // each XCD's L2 holds the keys of one.  Late tiles of a sequence see the most keys: they start first.
+    // each XCD's L2 holds the keys of one.  Tiles that see the most keys start first.
     const int G = a.Hq / a.Hk, num = blockIdx.x + item0;
-    const int hk = num % a.Hk, rest = num / a.Hk, head = hk * G + rest % G, item = tiles - 1 - rest / G;
-    const Piece at = find_piece(a.n_seqs, (uint32_t)item, [&](int b) { const int2 s = span(a.cu_q, b, a.n_q); return s.y - s.x; },
-                                [](int n) { return (uint32_t)(n + QT - 1) / QT; });
+    const int hk = num % a.Hk, rest = num / a.Hk, head = hk * G + rest % G;
+    const Tile at = find_heaviest(a.n_seqs, (uint32_t)(rest / G), [&](int b) {
+        const int2 q = span(a.cu_q, b, a.n_q), k = span(a.cu_k, b, a.n_k);
+        const int nq = q.y - q.x, nk = k.y - k.x;
+        return int2{(nq + QT - 1) / QT, max(0, a.causal ? nk - nq : nk) / QT};
+    });
     const int b = at.seq;
     if (b < 0) return;
     const int2 sq = span(a.cu_q, b, a.n_q), sk = span(a.cu_k, b, a.n_k);
@@ -134,13 +137,13 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
     const int tr = tid / CH, tc = tid % CH, dc = min(tc * 8, a.D - 8);
     const uint16_t *kp = a.k.p + k_row * a.k.ts + (long)hk * a.k.hs;
     const uint16_t *vp = a.v.p + k_row * a.v.ts + (long)hk * a.v.hs;
-    u32x4 moved[LD];
+    u32x4 k_moved[LD], v_moved[LD];               // on their way
     uint32_t kat[LD], vat[LD];                    // bytes from the tile's first row
     const auto rows_at = [&](uint32_t (&at)[LD], long stride, int t) {
 #pragma unroll
         for (int i = 0; i < LD; ++i) at[i] = 2u * (uint32_t)(max(0, min(tr + i * (kWaves * 64 / CH), nk - 1 - t * kKeys)) * (int)stride + dc);
     };
-    const auto fetch = [&](const uint16_t *p, const uint32_t (&at)[LD], long stride, int t) {
+    const auto fetch = [&](u32x4 (&moved)[LD], const uint16_t *p, const uint32_t (&at)[LD], long stride, int t) {
         const char *tile = (const char *)(p + min(t, (nk - 1) / kKeys) * kKeys * stride);
 #pragma unroll
         for (int i = 0; i < LD; ++i) moved[i] = *reinterpret_cast<const u32x4 *>(tile + here(at[i]));
@@ -155,7 +158,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
     const int v_row = 4 * g + col / 4;
 #pragma unroll
     for (int d = 0; d < DT; ++d) v_from[d] = VT + v_row * ROW + ((2 * d + (lane & 3) / 2) ^ swz_v<DP>(v_row)) * 16 + (lane & 1) * 8;
-    const auto store = [&](int to) {
+    const auto store = [&](const u32x4 (&moved)[LD], int to) {
 #pragma unroll
         for (int i = 0; i < LD; ++i) *reinterpret_cast<u32x4 *>(&s_kv[to + i * (kWaves * 64 / CH) * ROW]) = moved[i];
     };
@@ -255,38 +258,39 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
     };
     Scores sa, sb;
     u32x4 pa[2], pb[2];
-    // Tile t + 1 of K and tile t of V go to LDS meanwhile, each into the place of the one two before it, whose last reader is behind a barrier.
+    // Tile t + 1 of K goes to LDS at the end of the first half, of V at the end of the second, each into the place of the one two before it, whose
+    // last reader is behind a barrier; each was requested a whole tile earlier.
     const int last_tile = (nk - 1) / kKeys;
     typedef std::integral_constant<int, 0> Zero;
     typedef std::integral_constant<int, 1> One;
     const auto tile = [&](int t, auto masked) {
-        if (t + 1 == last_tile) {
-            rows_at(kat, a.k.ts, last_tile);
-            rows_at(vat, a.v.ts, last_tile);
-        }
-        fetch(kp, kat, a.k.ts, t + 1);
+        if (t + 1 == last_tile) rows_at(vat, a.v.ts, last_tile);
+        if (t + 2 == last_tile) rows_at(kat, a.k.ts, last_tile);
+        fetch(v_moved, vp, vat, a.v.ts, t + 1);
         grow(pb, One{});
         half(sb, One{}, sa, pa, pb, One{}, t * kKeys + 32, masked);      // the half before: tile t - 1's second
         other_k();
         other_v();
-        store(k_to);
+        store(k_moved, k_to);
         __syncthreads();
-        fetch(vp, vat, a.v.ts, t + 1);
+        fetch(k_moved, kp, kat, a.k.ts, t + 2);
         grow(pa, Zero{});
         half(sa, Zero{}, sb, pb, pa, Zero{}, (t + 1) * kKeys, masked);   // the next: tile t + 1's first
-        store(v_to);
+        store(v_moved, v_to);
     };
     if (n_tiles > 0) {
         rows_at(kat, a.k.ts, 0);
         rows_at(vat, a.v.ts, 0);
-        fetch(kp, kat, a.k.ts, 0);
-        store(k_to);
-        fetch(vp, vat, a.v.ts, 0);
-        store(v_to);
+        fetch(k_moved, kp, kat, a.k.ts, 0);
+        fetch(v_moved, vp, vat, a.v.ts, 0);
 #pragma unroll
         for (int i = 0; i < LD; ++i) *reinterpret_cast<u32x4 *>(&s_kv[VT + TILE + (tid + i * kWaves * 64) * 16]) = u32x4{0, 0, 0, 0};       // values of the half before the first
 #pragma unroll
         for (int i = 0; i < 2; ++i) pb[i] = u32x4{0, 0, 0, 0};
+        store(k_moved, k_to);
+        if (last_tile == 1) rows_at(kat, a.k.ts, 1);
+        fetch(k_moved, kp, kat, a.k.ts, 1);
+        store(v_moved, v_to);
         __syncthreads();
         static_for<2 * KS>([&](auto i) { add_scores(k_frag(0, i / KS, i % KS), sa, i / KS, i % KS); });
         maximum(sa, 0, std::true_type{});

@@ -148,6 +148,14 @@ def test_prompt_many_workgroups():
     run_prompt([700, 1, 515, 260, 1300], [700, 1, 600, 260, 1300], 40, 40, 64, seed=13)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+def test_prompt_more_sequences_than_lanes(causal):
+    """150 sequences, some of several tiles, empty ones and contexts among them: every tile is somebody's."""
+    nq = [(37 * i) % 61 if i % 29 else 150 + i for i in range(150)]
+    nk = [n + (0, 0, 200, -5)[i % 4] if n > 5 else n for i, n in enumerate(nq)]
+    run_prompt(nq, nk, 2, 1, 64, causal, seed=17)
+
+
 def test_prompt_neighbours_do_not_leak():
     """Sequences of NaN and infinity beside others, and rows behind the last sequence."""
     g = gen(14)
