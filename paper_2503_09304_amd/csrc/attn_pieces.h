@@ -51,31 +51,37 @@ __device__ __forceinline__ Piece find_piece(int n_seqs, uint32_t item, S &&size,
     return {-1, 0, 0};
 }
 
+// Rows of a packed sequence: its queries and its keys.
+struct Span {
+    int q0, nq, k0, nk;
+};
 struct Tile {
-    int seq, piece;                   // seq -1: there is no such number
+    int piece;                        // -1: there is no such number
+    Span span;                        // of its sequence
 };
 
-// The same for pieces that are dealt out heaviest first: sequence b has pieces 0 .. n(b) - 1, the work of piece p is e(b) + p (what it stands for only
-// sets the order).  Numbers go by falling work, then by sequence.  shape(b): {n, e}.
-template <class F>
-__device__ __forceinline__ Tile find_heaviest(int n_seqs, uint32_t number, F &&shape) {
+// The same for pieces that are dealt out heaviest first: a sequence has pieces 0 .. n - 1, the work of piece p is e + p (what it stands for only
+// sets the order).  Numbers go by falling work, then by sequence.  span(b): sequence b; shape(span): {n, e}.
+template <class S, class F>
+__device__ __forceinline__ Tile find_heaviest(int n_seqs, uint32_t number, S &&span, F &&shape) {
     const int lane = threadIdx.x & 63;
-    const auto at = [&](int b0) { return b0 + lane < n_seqs ? shape(b0 + lane) : int2{0, 0}; };
-    const int2 mine = at(0);                                          // all there is to load where there are 64 sequences or fewer
+    const auto at = [&](int b0) { return b0 + lane < n_seqs ? span(b0 + lane) : Span{0, 0, 0, 0}; };
+    const Span first = at(0);                                         // all there is to load where there are 64 sequences or fewer
+    const int2 mine = shape(first);
     // pieces with work w or more, of this lane's sequences
     const auto from = [](int2 s, int w) { return (uint32_t)min(max(s.x + s.y - w, 0), s.x); };
     const auto count = [&](int w) {
         uint32_t n = from(mine, w);
-        for (int b0 = 64; b0 < n_seqs; b0 += 64) n += from(at(b0), w);
+        for (int b0 = 64; b0 < n_seqs; b0 += 64) n += from(shape(at(b0)), w);
         return last_lane(wave_scan(n));
     };
     int top = mine.x + mine.y;
     for (int b0 = 64; b0 < n_seqs; b0 += 64) {
-        const int2 s = at(b0);
+        const int2 s = shape(at(b0));
         top = max(top, s.x + s.y);
     }
     uint32_t hi = last_lane(wave_max((uint32_t)top)), lo = 0;         // count(hi) = 0 <= number
-    if (count(0) <= number) return {-1, 0};
+    if (count(0) <= number) return {-1, first};
     while (hi - lo > 1) {                                             // count(lo) > number >= count(hi)
         const uint32_t mid = lo + (hi - lo) / 2;
         (count((int)mid) > number ? lo : hi) = mid;
@@ -83,17 +89,19 @@ __device__ __forceinline__ Tile find_heaviest(int n_seqs, uint32_t number, F &&s
     // the number-th piece with work lo, in the order of the sequences
     uint32_t left = number - count((int)hi);
     for (int b0 = 0; b0 < n_seqs; b0 += 64) {
-        const int2 s = b0 == 0 ? mine : at(b0);
-        unsigned long long has = __ballot(from(s, (int)lo) > from(s, (int)hi));
+        const Span s = b0 == 0 ? first : at(b0);
+        const int2 f = shape(s);
+        const unsigned long long has = __ballot(from(f, (int)lo) > from(f, (int)hi));
         const uint32_t n = __popcll(has);
         if (left >= n) {
             left -= n;
             continue;
         }
         const int l = __builtin_ctzll(__ballot(((has >> lane) & 1) != 0 && __popcll(has & ((1ull << lane) - 1)) == left));
-        return {b0 + l, (int)lo - __builtin_amdgcn_readlane(s.y, l)};
+        return {(int)lo - __builtin_amdgcn_readlane(f.y, l),
+                {__builtin_amdgcn_readlane(s.q0, l), __builtin_amdgcn_readlane(s.nq, l), __builtin_amdgcn_readlane(s.k0, l), __builtin_amdgcn_readlane(s.nk, l)}};
     }
-    return {-1, 0};
+    return {-1, first};
 }
 
 }  // namespace qattn

@@ -97,33 +97,25 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
     // each XCD's L2 holds the keys of one.  Tiles that see the most keys start first.
     const int G = a.Hq / a.Hk, num = blockIdx.x + item0;
     const int hk = num % a.Hk, rest = num / a.Hk, head = hk * G + rest % G;
-    const Tile at = find_heaviest(a.n_seqs, (uint32_t)(rest / G), [&](int b) {
-        const int2 q = span(a.cu_q, b, a.n_q), k = span(a.cu_k, b, a.n_k);
-        const int nq = q.y - q.x, nk = k.y - k.x;
-        return int2{(nq + QT - 1) / QT, max(0, a.causal ? nk - nq : nk) / QT};
-    });
-    const int b = at.seq;
-    if (b < 0) return;
-    const int2 sq = span(a.cu_q, b, a.n_q), sk = span(a.cu_k, b, a.n_k);
-    const int nq = __builtin_amdgcn_readfirstlane(sq.y - sq.x), nk = __builtin_amdgcn_readfirstlane(sk.y - sk.x);
-    const int r0 = at.piece * QT;                 // first query of the tile, within the sequence
-    const long q_row = __builtin_amdgcn_readfirstlane(sq.x), k_row = __builtin_amdgcn_readfirstlane(sk.x);
-    const int w0 = r0 + wave * 32;                                        // first query of the wave
-    // tiles of keys that the tile's last query sees, and those that its first query sees whole
+    const Tile at = find_heaviest(a.n_seqs, (uint32_t)(rest / G),
+        [&](int b) {
+            const int2 q = span(a.cu_q, b, a.n_q), k = span(a.cu_k, b, a.n_k);
+            return Span{q.x, q.y - q.x, k.x, k.y - k.x};
+        },
+        [&](Span s) { return int2{(s.nq + QT - 1) / QT, max(0, a.causal ? s.nk - s.nq : s.nk) / QT}; });
+    const auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };          // the same in all lanes, and to be known as such
+    const int piece = scalar(at.piece);
+    if (piece < 0) return;
+    const int nq = scalar(at.span.nq), nk = scalar(at.span.nk);
+    const int r0 = piece * QT;                    // first query of the tile, within the sequence
+    const long q_row = scalar(at.span.q0), k_row = scalar(at.span.k0);
+    const int w0 = r0 + wave * 32;                // first query of the wave
+    // tiles of keys that the tile's last query sees; that the wave's last query sees, and its first query sees whole
     const int shift = nk - nq;
-    const int n_tiles = ((a.causal ? min(nk, max(0, shift + min(nq, r0 + QT))) : nk) + kKeys - 1) / kKeys;
-    const int whole_tiles = min(nk, a.causal ? max(0, shift + r0 + 1) : nk) / kKeys;
+    const auto tiles_to = [&](int r) { return ((a.causal ? min(nk, max(0, shift + min(nq, r))) : nk) + kKeys - 1) / kKeys; };
+    const int n_tiles = tiles_to(r0 + QT), wave_tiles = w0 < nq ? tiles_to(w0 + 32) : 0;
+    const int whole_tiles = min(wave_tiles, min(nk, a.causal ? max(0, shift + w0 + 1) : nk) / kKeys);
 
-    u32x4 qf[2][KS];                              // queries w0 + col, w0 + 16 + col
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-        const uint16_t *p = a.q.p + (q_row + min(w0 + 16 * q + col, nq - 1)) * a.q.ts + (long)head * a.q.hs;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) qf[q][s] = *reinterpret_cast<const u32x4 *>(p + min(32 * s + 8 * g, a.D - 8));
-#pragma unroll
-        for (int s = 0; s < KS; ++s)
-            if (32 * s + 8 * g >= a.D) qf[q][s] = u32x4{0, 0, 0, 0};
-    }
     f32x4 o[DT][2];
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d][0] = o[d][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -148,6 +140,23 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
 #pragma unroll
         for (int i = 0; i < LD; ++i) moved[i] = *reinterpret_cast<const u32x4 *>(tile + here(at[i]));
     };
+    const int last_tile = (nk - 1) / kKeys;
+    if (n_tiles > 0) {
+        rows_at(kat, a.k.ts, 0);
+        rows_at(vat, a.v.ts, 0);
+        fetch(k_moved, kp, kat, a.k.ts, 0);
+        fetch(v_moved, vp, vat, a.v.ts, 0);
+    }
+    u32x4 qf[2][KS];                              // queries w0 + col, w0 + 16 + col
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const uint16_t *p = a.q.p + (q_row + min(w0 + 16 * q + col, nq - 1)) * a.q.ts + (long)head * a.q.hs;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[q][s] = *reinterpret_cast<const u32x4 *>(p + min(32 * s + 8 * g, a.D - 8));
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+            if (32 * s + 8 * g >= a.D) qf[q][s] = u32x4{0, 0, 0, 0};
+    }
     // Places in LDS (bytes; 16-byte pieces are XOR-swizzled by row, in the same way for rows that are 16 apart (K), 8 apart (V)), so that what is
     // read and written differs from these by constants.
     int k_to, v_to, k_from[KS], v_from[DT];
@@ -260,7 +269,6 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
     u32x4 pa[2], pb[2];
     // Tile t + 1 of K goes to LDS at the end of the first half, of V at the end of the second, each into the place of the one two before it, whose
     // last reader is behind a barrier; each was requested a whole tile earlier.
-    const int last_tile = (nk - 1) / kKeys;
     typedef std::integral_constant<int, 0> Zero;
     typedef std::integral_constant<int, 1> One;
     const auto tile = [&](int t, auto masked) {
@@ -279,10 +287,6 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
         store(v_moved, v_to);
     };
     if (n_tiles > 0) {
-        rows_at(kat, a.k.ts, 0);
-        rows_at(vat, a.v.ts, 0);
-        fetch(k_moved, kp, kat, a.k.ts, 0);
-        fetch(v_moved, vp, vat, a.v.ts, 0);
 #pragma unroll
         for (int i = 0; i < LD; ++i) *reinterpret_cast<u32x4 *>(&s_kv[VT + TILE + (tid + i * kWaves * 64) * 16]) = u32x4{0, 0, 0, 0};       // values of the half before the first
 #pragma unroll
@@ -298,22 +302,43 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
         for (int d = 0; d < DT; ++d) v_from[d] ^= TILE;
         int t = 0;
         for (; t + 1 < whole_tiles; ++t) tile(t, std::false_type{});
-        for (; t < n_tiles; ++t) tile(t, std::true_type{});
+        for (; t < wave_tiles; ++t) tile(t, std::true_type{});
         static_for<DT>([&](auto d) { add_values(v_frag(1, d), pb, d); });
+        for (; t < n_tiles; ++t) {                 // for the other waves: what tile() moves, and its barrier
+            if (t + 1 == last_tile) rows_at(vat, a.v.ts, last_tile);
+            if (t + 2 == last_tile) rows_at(kat, a.k.ts, last_tile);
+            fetch(v_moved, vp, vat, a.v.ts, t + 1);
+            k_to ^= TILE;
+            v_to ^= TILE;
+            store(k_moved, k_to);
+            __syncthreads();
+            fetch(k_moved, kp, kat, a.k.ts, t + 2);
+            store(v_moved, v_to);
+        }
     }
 
+    // Out through LDS, for stores of whole rows: a lane's elements are 8 bytes of each 32 (128 sequences of 128 tokens: 3900 of a workgroup's 24000 clocks).
+    constexpr int O_ROW = DP * 2 + 16;
+    __syncthreads();                              // the other waves' last reads of K and V
+    uint8_t *s_o = &s_kv[wave * 32 * O_ROW];
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
         const float sum = row_all(l[q], [](float x, float y) { return x + y; }), inv = sum > 0.f ? 1.f / sum : 0.f;
         const int r = w0 + 16 * q + col;
-        if (r >= nq) continue;
-        uint16_t *to = a.o.p + (q_row + r) * a.o.ts + (long)head * a.o.hs;
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             const f32x4 x = o[d][q] * inv;
-            if (16 * d < a.D) *reinterpret_cast<u32x2 *>(to + 16 * d + 4 * g) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+            *reinterpret_cast<u32x2 *>(s_o + (16 * q + col) * O_ROW + 32 * d + 8 * g) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
         }
-        if (a.lse != nullptr && g == 0) a.lse[(q_row + r) * a.Hq + head] = sum > 0.f ? (m[q] * a.scale_log2 + __log2f(sum)) * 0.69314718055994530942f : -INFINITY;
+        if (a.lse != nullptr && g == 0 && r < nq)
+            a.lse[(q_row + r) * a.Hq + head] = sum > 0.f ? (m[q] * a.scale_log2 + __log2f(sum)) * 0.69314718055994530942f : -INFINITY;
+    }
+    uint16_t *to = a.o.p + q_row * a.o.ts + (long)head * a.o.hs;
+#pragma unroll
+    for (int i = 0; i < 32 * CH / 64; ++i) {
+        const int row = (i * 64 + lane) / CH, c = lane % CH;
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(s_o + row * O_ROW + c * 16);
+        if (w0 + row < nq && c * 8 < a.D) *reinterpret_cast<u32x4 *>(to + (w0 + row) * a.o.ts + c * 8) = x;
     }
 }
 
