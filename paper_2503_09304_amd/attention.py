@@ -10,15 +10,11 @@ from typing import Optional
 
 import torch
 
-from .binding import MOE_E_ARG, MoeError, _check, _stream, lib
+from .binding import MOE_E_ARG, MoeError, _check, lib
 
 ATTN_BF16, ATTN_FP8 = 0, 1
 ATTN_ROPE = {"half": 0, "interleaved": 1}
 ATTN_SCALE = {"none": 0, "linear": 1, "base": 2, "ramp": 3, "waves": 4}
-
-
-class _Rows(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
 
 
 class _Cache(C.Structure):
@@ -26,13 +22,14 @@ class _Cache(C.Structure):
                 ("heads_kv", C.c_int32), ("page_tokens", C.c_int32), ("dim", C.c_int32), ("format", C.c_int32)]
 
 
-class _Place(C.Structure):
-    _fields_ = [("seq", C.c_void_p), ("pos", C.c_void_p), ("pages", C.c_void_p), ("n_seqs", C.c_int32), ("seq_pages", C.c_int32)]
-
-
 class _Rope(C.Structure):
     _fields_ = [("inv_freq", C.c_void_p), ("dims", C.c_int32), ("layout", C.c_int32), ("mscale", C.c_float)]
 
+
+# attn_rows and attn_place are passed as slices of one array of 64-bit numbers per call: a structure object for each of a call's
+# tensors costs more than its kernel's launch.
+_ROWS, _PLACE = 3, 4
+_A2, _A2P, _A4, _A5P = (C.c_int64 * n for n in (2 * _ROWS, 2 * _ROWS + _PLACE, 4 * _ROWS, 5 * _ROWS + _PLACE))
 
 _ready = None
 
@@ -41,12 +38,12 @@ def _lib():
     global _ready
     if _ready is None:
         L = lib()
-        P, I, F, R = C.c_void_p, C.c_int32, C.c_float, C.POINTER(_Rows)
+        P, I, F = C.c_void_p, C.c_int32, C.c_float
         L.attn_rope_frequencies.argtypes = [I, C.c_double, I, C.c_double, C.c_double, C.c_double, C.c_double, P, C.POINTER(F)]
-        L.attn_append.argtypes = [C.POINTER(_Cache), R, R, R, R, R, I, I, C.POINTER(_Place), C.POINTER(_Rope), P, P]
-        L.attn_read.argtypes = [C.POINTER(_Cache), C.POINTER(_Place), I, R, R, P, P]
-        L.attn_prompt.argtypes = [R, R, R, R, P, P, P, I, I, I, I, I, I, F, I, P]
-        L.attn_decode.argtypes = [C.POINTER(_Cache), R, R, P, I, I, P, I, P, F, P, C.c_size_t, P, P]
+        L.attn_append.argtypes = [P, P, P, P, P, P, I, I, P, P, P, P]
+        L.attn_read.argtypes = [P, P, I, P, P, P, P]
+        L.attn_prompt.argtypes = [P, P, P, P, P, P, P, I, I, I, I, I, I, F, I, P]
+        L.attn_decode.argtypes = [P, P, P, P, I, I, P, I, P, F, P, C.c_size_t, P, P]
         for f in ("attn_rope_frequencies", "attn_append", "attn_read", "attn_prompt", "attn_decode"):
             getattr(L, f).restype = I
         for f, n in (("attn_decode_workspace_bytes", 4), ("attn_decode_counter_bytes", 3)):
@@ -60,27 +57,39 @@ def _bad(text: str):
     raise MoeError(MOE_E_ARG, text)
 
 
-def _heads(t, name: str, shape=None) -> _Rows:
-    """A tensor [tokens, heads, dim] as rows."""
-    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.device.type != "cuda":
-        _bad(f"{name} must be a bfloat16 tensor [tokens, heads, dim] on the GPU")
-    if shape is not None and tuple(t.shape) != shape:
-        _bad(f"{name} has shape {tuple(t.shape)}, not {shape}")
+def _heads(t, name: str, T: int, H: int, D: int):
+    """A bfloat16 tensor [T, H, D] as rows: address, token stride, head stride."""
+    if t.dtype is not torch.bfloat16 or not t.is_cuda or t.shape != (T, H, D):
+        _bad(f"{name} must be a bfloat16 tensor {[T, H, D]} on the GPU, not {t.dtype} {list(t.shape)}")
     ts, hs, ds = t.stride()
     if ds != 1:
         _bad(f"the elements of a head of {name} must be dense")
-    return _Rows(t.data_ptr(), ts if t.shape[0] > 1 else 0, hs if t.shape[1] > 1 else 0)
+    return t.data_ptr(), ts if T > 1 else 0, hs if H > 1 else 0
 
 
 def _whole(t, name: str, dtype, shape) -> int:
     """The address of a dense tensor of this type and shape."""
-    if t.dtype != dtype or t.device.type != "cuda" or not t.is_contiguous() or tuple(t.shape) != shape:
+    if t.dtype is not dtype or not t.is_cuda or t.shape != shape or not t.is_contiguous():
         _bad(f"{name} must be a dense {dtype} tensor {list(shape)} on the GPU")
     return t.data_ptr()
 
 
 def _optional(t, name: str, dtype, shape):
     return None if t is None else _whole(t, name, dtype, shape)
+
+
+def _three(t, name: str):
+    if t.dim() != 3:
+        _bad(f"{name} must be [tokens, heads, dim]")
+    return t.shape
+
+
+# torch.cuda.current_stream() builds a stream object, 2 us of a call's 9.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+def _stream(t) -> int:
+    return _raw_stream(t.get_device())
 
 
 class AttnCache:
@@ -100,6 +109,7 @@ class AttnCache:
             _bad("a float8 cache needs k_scale and v_scale, a bfloat16 cache has none")
         self._c = _Cache(_whole(k, "k", k.dtype, shape), _whole(v, "v", k.dtype, shape), _optional(k_scale, "k_scale", torch.uint8, shape[:3]),
                          _optional(v_scale, "v_scale", torch.uint8, shape[:3]), *shape, ATTN_FP8 if self.fp8 else ATTN_BF16)
+        self._at = C.addressof(self._c)
 
     @classmethod
     def empty(cls, n_pages: int, heads_kv: int, page_tokens: int, dim: int, fp8: bool = False, device="cuda:0") -> "AttnCache":
@@ -118,6 +128,7 @@ class AttnRope:
             _bad("layout must be half or interleaved")
         self.inv_freq = inv_freq
         self._c = _Rope(_whole(inv_freq, "inv_freq", torch.float64, (inv_freq.numel(),)), 2 * inv_freq.numel(), ATTN_ROPE[layout], mscale)
+        self._at = C.addressof(self._c)
 
 
 def attn_rope_frequencies(dims: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, trained: float = 4096.0,
@@ -130,45 +141,50 @@ def attn_rope_frequencies(dims: int, base: float = 10000.0, scaling: str = "none
     return list(f), float(m.value)
 
 
-def _place(seq, pos, pages, T: int) -> _Place:
+def _place(seq, pos, pages, T: int):
+    """seq, pos and pages as attn_place."""
     if pages.dim() != 2:
         _bad("pages must be [n_seqs, seq_pages]")
-    shape = tuple(pages.shape)
-    return _Place(_optional(seq, "seq", torch.int32, (T,)), _whole(pos, "pos", torch.int32, (T,)), _whole(pages, "pages", torch.int32, shape), *shape)
+    n, m = pages.shape
+    return (_optional(seq, "seq", torch.int32, (T,)) or 0, _whole(pos, "pos", torch.int32, (T,)), _whole(pages, "pages", torch.int32, (n, m)), n | m << 32)
 
 
 def attn_append(cache: AttnCache, q, k, v, seq, pos, pages, rope: Optional[AttnRope], q_out, k_out=None, bad=None) -> int:
     """Rotates q into q_out and k into k_out (may be None) and writes k and v to the cache.  seq (None: token t is sequence t's),
     pos int32 [tokens], pages int32 [n_seqs, seq_pages]; bad int32 [1] counts tokens that are out of range.  q and q_out may be None."""
-    T, Hk, D = k.shape[0], cache.heads_kv, cache.dim
+    T, Hk, D = _three(k, "k")[0], cache.heads_kv, cache.dim
     if (q is None) != (q_out is None):
         _bad("q and q_out go together")
-    heads = 0 if q is None else q.shape[1]
-    qs, qo = (None, None) if q is None else (_heads(q, "q", (T, heads, D)), _heads(q_out, "q_out", (T, heads, D)))
-    ks, vs, ko = _heads(k, "k", (T, Hk, D)), _heads(v, "v", (T, Hk, D)), None if k_out is None else _heads(k_out, "k_out", (T, Hk, D))
-    place = _place(seq, pos, pages, T)
-    return _check(_lib().attn_append(cache._c, qs, ks, vs, qo, ko, heads, T, place, None if rope is None else rope._c,
-                                     _optional(bad, "bad", torch.int32, (1,)), _stream()))
+    Hq = 0 if q is None else _three(q, "q")[1]
+    none = (0, 0, 0)
+    a = _A5P(*_heads(k, "k", T, Hk, D), *_heads(v, "v", T, Hk, D), *_place(seq, pos, pages, T),
+             *(none if q is None else _heads(q, "q", T, Hq, D)), *(none if q is None else _heads(q_out, "q_out", T, Hq, D)),
+             *(none if k_out is None else _heads(k_out, "k_out", T, Hk, D)))
+    at = C.addressof(a)
+    return _check(_lib().attn_append(cache._at, at + 80 if q is not None else None, at, at + 24, at + 104 if q is not None else None,
+                                     at + 128 if k_out is not None else None, Hq, T, at + 48, None if rope is None else rope._at,
+                                     _optional(bad, "bad", torch.int32, (1,)), _stream(k)))
 
 
 def attn_read(cache: AttnCache, seq, pos, pages, k_out, v_out, bad=None) -> int:
     """Keys and values of the tokens at (seq, pos) out of the cache, as bfloat16."""
     T = pos.shape[0]
-    shape = (T, cache.heads_kv, cache.dim)
-    return _check(_lib().attn_read(cache._c, _place(seq, pos, pages, T), T, _heads(k_out, "k_out", shape), _heads(v_out, "v_out", shape),
-                                   _optional(bad, "bad", torch.int32, (1,)), _stream()))
+    a = _A2P(*_heads(k_out, "k_out", T, cache.heads_kv, cache.dim), *_heads(v_out, "v_out", T, cache.heads_kv, cache.dim), *_place(seq, pos, pages, T))
+    at = C.addressof(a)
+    return _check(_lib().attn_read(cache._at, at + 48, T, at, at + 24, _optional(bad, "bad", torch.int32, (1,)), _stream(k_out)))
 
 
 def attn_prompt(q, k, v, cu_q, cu_k, out, scale: Optional[float] = None, causal: bool = True, lse=None) -> int:
     """Attention over packed prompts; cu_q, cu_k int32 [n_seqs + 1] on the GPU; scale None: dim ** -0.5; lse float32 [n_q, heads_q]."""
-    (n_q, Hq, D), (n_k, Hk, _) = q.shape, k.shape
+    (n_q, Hq, D), (n_k, Hk, _) = _three(q, "q"), _three(k, "k")
     n = cu_q.shape[0] - 1
     if n < 0:
         _bad("cu_q has no entry")
-    return _check(_lib().attn_prompt(_heads(q, "q"), _heads(k, "k", (n_k, Hk, D)), _heads(v, "v", (n_k, Hk, D)), _heads(out, "out", (n_q, Hq, D)),
-                                     _optional(lse, "lse", torch.float32, (n_q, Hq)), _whole(cu_q, "cu_q", torch.int32, (n + 1,)),
-                                     _whole(cu_k, "cu_k", torch.int32, (n + 1,)), n, n_q, n_k, Hq, Hk, D, D ** -0.5 if scale is None else scale,
-                                     1 if causal else 0, _stream()))
+    a = _A4(*_heads(q, "q", n_q, Hq, D), *_heads(k, "k", n_k, Hk, D), *_heads(v, "v", n_k, Hk, D), *_heads(out, "out", n_q, Hq, D))
+    at = C.addressof(a)
+    return _check(_lib().attn_prompt(at, at + 24, at + 48, at + 72, _optional(lse, "lse", torch.float32, (n_q, Hq)),
+                                     _whole(cu_q, "cu_q", torch.int32, (n + 1,)), _whole(cu_k, "cu_k", torch.int32, (n + 1,)), n, n_q, n_k, Hq, Hk, D,
+                                     D ** -0.5 if scale is None else scale, 1 if causal else 0, _stream(q)))
 
 
 def attn_decode_workspace(cache: AttnCache, n_seqs: int, heads_q: int):
@@ -181,11 +197,13 @@ def attn_decode_workspace(cache: AttnCache, n_seqs: int, heads_q: int):
 
 def attn_decode(cache: AttnCache, q, pages, lens, out, workspace, scale: Optional[float] = None, lse=None, bad=None) -> int:
     """One query a sequence (q [n_seqs, heads_q, dim]) over the first lens[b] tokens of its pages."""
-    n, Hq, D = q.shape
+    n, Hq, D = _three(q, "q")
     if pages.dim() != 2 or D != cache.dim:
         _bad("pages must be [n_seqs, seq_pages], q [n_seqs, heads_q, dim of the cache]")
-    return _check(_lib().attn_decode(cache._c, _heads(q, "q"), _heads(out, "out", (n, Hq, D)), _optional(lse, "lse", torch.float32, (n, Hq)), n, Hq,
-                                     _whole(pages, "pages", torch.int32, (n, pages.shape[1])), pages.shape[1],
-                                     _whole(lens, "lens", torch.int32, (n,)), D ** -0.5 if scale is None else scale,
-                                     _whole(workspace, "workspace", torch.uint8, (workspace.numel(),)), workspace.numel(),
-                                     _optional(bad, "bad", torch.int32, (1,)), _stream()))
+    m, nb = pages.shape[1], workspace.numel()
+    a = _A2(*_heads(q, "q", n, Hq, D), *_heads(out, "out", n, Hq, D))
+    at = C.addressof(a)
+    return _check(_lib().attn_decode(cache._at, at, at + 24, _optional(lse, "lse", torch.float32, (n, Hq)), n, Hq,
+                                     _whole(pages, "pages", torch.int32, (n, m)), m, _whole(lens, "lens", torch.int32, (n,)),
+                                     D ** -0.5 if scale is None else scale, _whole(workspace, "workspace", torch.uint8, (nb,)), nb,
+                                     _optional(bad, "bad", torch.int32, (1,)), _stream(q)))

@@ -8,9 +8,13 @@
 // Angles: pos * f in units of half turns in 64 bits, taken to the nearest quarter turn there, the rest (at most a quarter of a
 // half turn, exact to 2^-27) in fp32 sincospi.  Positions of 2^20 keep 33 bits of their angle this way; in fp32 they would
 // keep 4.  One thread per (token, pair) forms them, all heads of the token read them from LDS.
+//
+// Rows go past the caches (non-temporal loads and stores where nothing is read twice: 9826 tokens 55.7 -> 52.1 us).  Measured: 9826 tokens of 32 + 8 + 8 heads
+// of 128 into a bf16 cache 52 us, 4.6 TB/s (a copy of 4 GiB by the vendor's library 4.9); one token 4.2 us; 40276 fp8 tokens read 55 us, 4.5 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "qattn_internal.h"
 
@@ -91,154 +95,218 @@ __device__ __forceinline__ u32x4 from_fp8(const u32x2 &x, float scale) {
 
 constexpr int kThreads = 256;
 
+// The rows of a workgroup's tokens, LPR lanes each, dealt out to its threads: thread `tid` has rows tid / LPR, that + 256 / LPR, ...
+template <int LPR>
+struct RowWalk {
+    int tt, r;                        // token of the workgroup, row of it
+    int rows;
+    __device__ __forceinline__ RowWalk(int tid, int rows_) : tt(0), r(tid / LPR), rows(rows_) { wrap(); }
+    __device__ __forceinline__ void next() {
+        r += kThreads / LPR;
+        wrap();
+    }
+    __device__ __forceinline__ void wrap() {
+        while (r >= rows) {
+            r -= rows;
+            ++tt;
+        }
+    }
+};
+
 // TOK tokens a workgroup.
 template <int LPR, int TOK>
 __global__ __launch_bounds__(kThreads) void append_rows(const AppendArgs a) {
     __shared__ float2 cs[TOK][kMaxDim / 2];
-    const int tid = threadIdx.x;
-    const int pairs = a.c.D / 16, rows = a.Hq + 2 * a.c.Hk, half = a.rot / 2;
+    __shared__ long slot[TOK];                    // first key/value head's row of the token in the cache; -1: it is not written there
+    __shared__ int padding[TOK];
+    const int tid = threadIdx.x, p = tid % LPR;
+    const int D = a.c.D, Hk = a.c.Hk, rows = a.Hq + 2 * Hk, half = a.rot / 2;
+    const bool turned = p < a.rot / 16, in = p < D / 16;
+    // the lane's two pieces of 8 elements
+    const int c0 = (a.interleaved || !turned ? 2 * p : p) * 8, c1 = !a.interleaved && turned ? (p + a.rot / 16) * 8 : c0 + 8;
     for (long t0 = (long)blockIdx.x * TOK; t0 < a.n_tokens; t0 += (long)gridDim.x * TOK) {
         const int nt = (int)min((long)TOK, a.n_tokens - t0);
-        __syncthreads();                                                  // cs of the tokens before
+        // Loads of the first rows do not wait for the angles.
+        constexpr int U = 2;                      // rows that are requested before the first is used (three: 9826 tokens 61.7 us instead of 55.7)
+        RowWalk<LPR> walk(tid, rows);
+        u32x4 x0[U], x1[U];
+        int tt[U], r[U];
+        const auto request = [&]() {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                tt[u] = walk.tt;
+                r[u] = walk.r;
+                walk.next();
+                const int t = min(tt[u], nt - 1), kind = (r[u] >= a.Hq) + (r[u] >= a.Hq + Hk);        // q, k, v
+                const int h = r[u] - (kind == 0 ? 0 : kind == 1 ? a.Hq : a.Hq + Hk);
+                const Rows &src = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
+                const uint16_t *from = src.p + (t0 + t) * src.ts + h * src.hs;
+                x0[u] = *reinterpret_cast<const u32x4 *>(from + (in ? c0 : 0));
+                x1[u] = *reinterpret_cast<const u32x4 *>(from + (in ? c1 : 0));
+            }
+        };
+        request();
+        __syncthreads();                                                  // cs and slot of the tokens before
+        if (tid < nt) {
+            const long t = t0 + tid;
+            const int pos = a.pos[t];
+            const int page = page_of(a.c, a.pages, a.n_seqs, a.seq_pages, a.seq ? a.seq[t] : (int)t, pos);
+            padding[tid] = pos < 0;
+            slot[tid] = page < 0 ? -1 : cache_row(a.c, page, 0, pos);
+            if (page < 0 && pos >= 0 && a.bad != nullptr) atomicAdd(a.bad, 1);
+        }
         for (int i = tid; i < nt * half; i += kThreads) {
-            const int t = i / half, p = i - t * half;
-            cs[t][p] = angle(a.pos[t0 + t], a.inv_freq[p], a.mscale);
+            const int t = i / half, q = i - t * half;
+            cs[t][q] = angle(a.pos[t0 + t], a.inv_freq[q], a.mscale);
         }
         __syncthreads();
-        const int items = nt * rows * LPR;
-        for (int it = tid; it < (items + 63) / 64 * 64; it += kThreads) {       // whole waves, for the exchange
-            const int row = min(it / LPR, nt * rows - 1), p = it % LPR;
-            const int tt = row / rows, r = row - tt * rows;
-            const long t = t0 + tt;
-            const int pos = a.pos[t];
-            const bool active = it < items && p < pairs && pos >= 0;
-            const int kind = r < a.Hq ? 0 : r < a.Hq + a.c.Hk ? 1 : 2;        // q, k, v
-            const int h = kind == 0 ? r : kind == 1 ? r - a.Hq : r - a.Hq - a.c.Hk;
-            const bool turn = kind != 2 && p < a.rot / 16;
-            // the lane's two pieces of 8 elements
-            const int c0 = a.interleaved || p >= a.rot / 16 ? 2 * p : p, c1 = !a.interleaved && p < a.rot / 16 ? p + a.rot / 16 : c0 + 1;
-            u32x4 x0{0, 0, 0, 0}, x1{0, 0, 0, 0};
-            if (active) {
-                const Rows &src = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
-                const uint16_t *from = src.p + t * src.ts + h * src.hs;
-                x0 = *reinterpret_cast<const u32x4 *>(from + c0 * 8);
-                x1 = *reinterpret_cast<const u32x4 *>(from + c1 * 8);
-                if (turn) {
-                    const float2 *w = &cs[tt][8 * p];
+        // Whole waves go round, for the exchange between the lanes of a row.
+        for (int first = 0; first < nt * rows; first += U * (kThreads / LPR)) {
+            if (first > 0) request();
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const bool active = in && tt[u] < nt && !padding[min(tt[u], nt - 1)];
+                const int t = min(tt[u], nt - 1), kind = (r[u] >= a.Hq) + (r[u] >= a.Hq + Hk);
+                const int h = r[u] - (kind == 0 ? 0 : kind == 1 ? a.Hq : a.Hq + Hk);
+                u32x4 y0 = x0[u], y1 = x1[u];
+                if (kind != 2 && turned) {
+                    const float2 *w = &cs[t][8 * p];
                     if (a.interleaved) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const float2 u = w[i], v = w[i + 4];
-                            x0[i] = pack_bf16(lo_f(x0[i]) * u.x - hi_f(x0[i]) * u.y, hi_f(x0[i]) * u.x + lo_f(x0[i]) * u.y);
-                            x1[i] = pack_bf16(lo_f(x1[i]) * v.x - hi_f(x1[i]) * v.y, hi_f(x1[i]) * v.x + lo_f(x1[i]) * v.y);
+                            const float2 e = w[i], f = w[i + 4];
+                            y0[i] = pack_bf16(lo_f(y0[i]) * e.x - hi_f(y0[i]) * e.y, hi_f(y0[i]) * e.x + lo_f(y0[i]) * e.y);
+                            y1[i] = pack_bf16(lo_f(y1[i]) * f.x - hi_f(y1[i]) * f.y, hi_f(y1[i]) * f.x + lo_f(y1[i]) * f.y);
                         }
                     } else {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const float2 u = w[2 * i], v = w[2 * i + 1];
-                            const float al = lo_f(x0[i]), ah = hi_f(x0[i]), bl = lo_f(x1[i]), bh = hi_f(x1[i]);
-                            x0[i] = pack_bf16(al * u.x - bl * u.y, ah * v.x - bh * v.y);
-                            x1[i] = pack_bf16(bl * u.x + al * u.y, bh * v.x + ah * v.y);
+                            const float2 e = w[2 * i], f = w[2 * i + 1];
+                            const float al = lo_f(y0[i]), ah = hi_f(y0[i]), bl = lo_f(y1[i]), bh = hi_f(y1[i]);
+                            y0[i] = pack_bf16(al * e.x - bl * e.y, ah * f.x - bh * f.y);
+                            y1[i] = pack_bf16(bl * e.x + al * e.y, bh * f.x + ah * f.y);
                         }
                     }
                 }
                 const Rows &dst = kind == 0 ? a.qo : a.ko;
-                if (kind != 2 && dst.p != nullptr) {
-                    uint16_t *to = dst.p + t * dst.ts + h * dst.hs;
-                    *reinterpret_cast<u32x4 *>(to + c0 * 8) = x0;
-                    *reinterpret_cast<u32x4 *>(to + c1 * 8) = x1;
+                if (active && kind != 2 && dst.p != nullptr) {
+                    uint16_t *to = dst.p + (t0 + t) * dst.ts + h * dst.hs;
+                    __builtin_nontemporal_store(y0, reinterpret_cast<u32x4 *>(to + c0));
+                    __builtin_nontemporal_store(y1, reinterpret_cast<u32x4 *>(to + c1));
                 }
-            }
-            int page = -1;
-            if (it < items && kind != 0 && pos >= 0) {
-                page = page_of(a.c, a.pages, a.n_seqs, a.seq_pages, a.seq ? a.seq[t] : (int)t, pos);
-                if (page < 0 && kind == 1 && h == 0 && p == 0 && a.bad != nullptr) atomicAdd(a.bad, 1);
-            }
-            if (a.fp8) {
-                uint32_t m = 0;
+                const long at = slot[t];
+                const bool kept = active && kind != 0 && at >= 0;
+                const long row = at + ((long)h << a.c.page_shift);
+                if (a.fp8) {
+                    uint32_t m = 0;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    m = max(m, max(x0[i] & 0x7FFF0000u, (x0[i] << 16) & 0x7FFF0000u));
-                    m = max(m, max(x1[i] & 0x7FFF0000u, (x1[i] << 16) & 0x7FFF0000u));
+                    for (int i = 0; i < 4; ++i) {
+                        m = max(m, max(y0[i] & 0x7FFF0000u, (y0[i] << 16) & 0x7FFF0000u));
+                        m = max(m, max(y1[i] & 0x7FFF0000u, (y1[i] << 16) & 0x7FFF0000u));
+                    }
+                    const int byte = scale_byte(row_max<LPR>(in ? m : 0u));
+                    if (kept) {
+                        uint8_t *to = (kind == 1 ? a.c.k : a.c.v) + row * D;
+                        const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);
+                        const float most = byte == 247 ? 240.f : 448.f;       // 256 * 2^(247 - 127) would be over the largest bf16
+                        *reinterpret_cast<u32x2 *>(to + c0) = to_fp8(y0, inv, most);
+                        *reinterpret_cast<u32x2 *>(to + c1) = to_fp8(y1, inv, most);
+                        if (p == 0) (kind == 1 ? a.c.ks : a.c.vs)[row] = (uint8_t)byte;
+                    }
+                } else if (kept) {
+                    uint16_t *to = (uint16_t *)(kind == 1 ? a.c.k : a.c.v) + row * D;
+                    __builtin_nontemporal_store(y0, reinterpret_cast<u32x4 *>(to + c0));
+                    __builtin_nontemporal_store(y1, reinterpret_cast<u32x4 *>(to + c1));
                 }
-                const int byte = scale_byte(row_max<LPR>(m));
-                if (page >= 0 && active) {
-                    const long row_at = cache_row(a.c, page, h, pos);
-                    uint8_t *to = (kind == 1 ? a.c.k : a.c.v) + row_at * a.c.D;
-                    const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);
-                    const float most = byte == 247 ? 240.f : 448.f;       // 256 * 2^(247 - 127) would be over the largest bf16
-                    *reinterpret_cast<u32x2 *>(to + c0 * 8) = to_fp8(x0, inv, most);
-                    *reinterpret_cast<u32x2 *>(to + c1 * 8) = to_fp8(x1, inv, most);
-                    if (p == 0) (kind == 1 ? a.c.ks : a.c.vs)[row_at] = (uint8_t)byte;
-                }
-            } else if (page >= 0 && active) {
-                uint16_t *to = (uint16_t *)(kind == 1 ? a.c.k : a.c.v) + cache_row(a.c, page, h, pos) * a.c.D;
-                *reinterpret_cast<u32x4 *>(to + c0 * 8) = x0;
-                *reinterpret_cast<u32x4 *>(to + c1 * 8) = x1;
             }
         }
     }
 }
 
-template <int LPR>
-__global__ __launch_bounds__(kThreads) void read_rows(const ReadArgs a, long items) {
-    const int pairs = a.c.D / 16, rows = 2 * a.c.Hk;
-    for (long it = (long)blockIdx.x * kThreads + threadIdx.x; it < items; it += (long)gridDim.x * kThreads) {
-        const long row = it / LPR;
-        const int p = (int)(it % LPR);
-        if (p >= pairs) continue;
-        const long t = row / rows;
-        const int r = (int)(row - t * rows), kind = r >= a.c.Hk, h = kind ? r - a.c.Hk : r;
-        const int pos = a.pos[t];
+// Rows of the tokens from `first` on, n in all, LPR lanes each, U a thread, requested before the first is used.  Every lane finds its token's slot for
+// itself (through LDS, a workgroup's tokens at a time, all wait for the slots before they ask for a row: 40276 fp8 tokens 62 us instead of 55).
+template <int LPR, int U>
+__global__ __launch_bounds__(kThreads) void read_rows(const ReadArgs a, long first, uint32_t n) {
+    const int D = a.c.D, Hk = a.c.Hk, p = threadIdx.x % LPR;
+    const uint32_t row0 = blockIdx.x * (U * kThreads / LPR) + threadIdx.x / LPR;
+    if (p >= D / 16) return;
+    u32x4 x0[U], x1[U];
+    float scale[U];
+    bool none[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint32_t row = min(row0 + u * (kThreads / LPR), n - 1), tt = row / (2 * Hk), r = row - tt * (2 * Hk);
+        const long t = first + tt;
+        const int kind = r >= (uint32_t)Hk, h = kind ? r - Hk : r, pos = a.pos[t];
         const int page = page_of(a.c, a.pages, a.n_seqs, a.seq_pages, a.seq ? a.seq[t] : (int)t, pos);
-        u32x4 x0{0, 0, 0, 0}, x1{0, 0, 0, 0};
-        if (page >= 0) {
-            const long row_at = cache_row(a.c, page, h, pos);
-            const uint8_t *pool = kind ? a.c.v : a.c.k;
-            if (a.fp8) {
-                const u32x4 w = *reinterpret_cast<const u32x4 *>(pool + row_at * a.c.D + p * 16);
-                const float scale = __uint_as_float((uint32_t)(kind ? a.c.vs : a.c.ks)[row_at] << 23);
-                x0 = from_fp8(u32x2{w[0], w[1]}, scale);
-                x1 = from_fp8(u32x2{w[2], w[3]}, scale);
-            } else {
-                const u32x4 *from = reinterpret_cast<const u32x4 *>((const uint16_t *)pool + row_at * a.c.D + p * 16);
-                x0 = from[0];
-                x1 = from[1];
-            }
-        } else if (pos >= 0 && r == 0 && p == 0 && a.bad != nullptr) {
-            atomicAdd(a.bad, 1);
+        none[u] = page < 0;
+        if (page < 0 && pos >= 0 && r == 0 && p == 0 && a.bad != nullptr && row0 + u * (kThreads / LPR) < n) atomicAdd(a.bad, 1);
+        const long at = page < 0 ? 0 : cache_row(a.c, page, h, pos);
+        const uint8_t *pool = kind ? a.c.v : a.c.k;
+        if (a.fp8) {
+            x0[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(pool + at * D + p * 16));
+            scale[u] = __uint_as_float((uint32_t)(kind ? a.c.vs : a.c.ks)[at] << 23);
+        } else {
+            const u32x4 *from = reinterpret_cast<const u32x4 *>((const uint16_t *)pool + at * D + p * 16);
+            x0[u] = __builtin_nontemporal_load(from);
+            x1[u] = __builtin_nontemporal_load(from + 1);
         }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint32_t row = row0 + u * (kThreads / LPR);
+        if (row >= n) return;
+        const uint32_t tt = row / (2 * Hk), r = row - tt * (2 * Hk);
+        const int kind = r >= (uint32_t)Hk, h = kind ? r - Hk : r;
+        u32x4 y0 = x0[u], y1 = x1[u];
+        if (a.fp8) {
+            y1 = from_fp8(u32x2{y0[2], y0[3]}, scale[u]);
+            y0 = from_fp8(u32x2{y0[0], y0[1]}, scale[u]);
+        }
+        if (none[u]) y0 = y1 = u32x4{0, 0, 0, 0};
         const Rows &dst = kind ? a.vo : a.ko;
-        u32x4 *to = reinterpret_cast<u32x4 *>(dst.p + t * dst.ts + h * dst.hs + p * 16);
-        to[0] = x0;
-        to[1] = x1;
+        u32x4 *to = reinterpret_cast<u32x4 *>(dst.p + (first + tt) * dst.ts + h * dst.hs + p * 16);
+        __builtin_nontemporal_store(y0, to);
+        __builtin_nontemporal_store(y1, to + 1);
     }
 }
 
-template <int LPR>
-void append_n(const AppendArgs &a, hipStream_t s) {
-    const long most = 1 << 20;                    // workgroups; beyond that they take several turns
-    if (a.n_tokens <= 1024) {
-        append_rows<LPR, 1><<<dim3((unsigned)a.n_tokens), dim3(kThreads), 0, s>>>(a);
-    } else {
-        append_rows<LPR, 4><<<dim3((unsigned)std::min<long>(((long)a.n_tokens + 3) / 4, most)), dim3(kThreads), 0, s>>>(a);
-    }
+// Tokens a workgroup: one where that is what spreads them over the chip, else four (9826 tokens of 48 heads of 128: two 60 us, four 55.7, eight 56.7; 2000
+// tokens 12.9, 13.2, 18.2).
+constexpr long kFewTokens = 1024, kMostWgs = 1 << 20;
+template <class F>
+void by_tokens(int n_tokens, F &&launch) {
+    if (n_tokens <= kFewTokens) launch(std::integral_constant<int, 1>{}, dim3((unsigned)n_tokens));
+    else launch(std::integral_constant<int, 4>{}, dim3((unsigned)std::min<long>(((long)n_tokens + 3) / 4, kMostWgs)));
 }
 
 }  // namespace
 
 hipError_t launch_append(const AppendArgs &a, hipStream_t s) {
-    if (a.c.D <= 64) append_n<4>(a, s);
-    else append_n<8>(a, s);
+    by_tokens(a.n_tokens, [&](auto tok, dim3 grid) {
+        if (a.c.D <= 64) append_rows<4, tok><<<grid, dim3(kThreads), 0, s>>>(a);
+        else append_rows<8, tok><<<grid, dim3(kThreads), 0, s>>>(a);
+    });
     return hipGetLastError();
 }
 
 hipError_t launch_read(const ReadArgs &a, hipStream_t s) {
-    const int lpr = a.c.D <= 64 ? 4 : 8;
-    const long items = (long)a.n_tokens * 2 * a.c.Hk * lpr;
-    const unsigned grid = (unsigned)std::min<long>((items + kThreads - 1) / kThreads, 1 << 20);
-    if (lpr == 4) read_rows<4><<<dim3(grid), dim3(kThreads), 0, s>>>(a, items);
-    else read_rows<8><<<dim3(grid), dim3(kThreads), 0, s>>>(a, items);
+    const int lpr = a.c.D <= 64 ? 4 : 8, per = kThreads / lpr, rows = 2 * a.c.Hk;
+    const long most = (1l << 23) / rows;          // tokens of a launch, so that its rows and threads stay within 32 bits
+    for (long t = 0; t < a.n_tokens; t += most) {
+        const uint32_t n = (uint32_t)(std::min(most, a.n_tokens - t) * rows), wgs = (n + per - 1) / per;
+        // Two rows a thread where one would take more than 8 workgroups a CU (40276 fp8 tokens 55 us, one row 58, three 57; 509 bf16 tokens of 16 heads of 64,
+        // 254 workgroups, 3.6 and with one row 3.2).
+        const auto run = [&](auto l, auto u) { read_rows<l, u><<<dim3((wgs + u - 1) / u), dim3(kThreads), 0, s>>>(a, t, n); };
+        typedef std::integral_constant<int, 1> One;
+        typedef std::integral_constant<int, 2> Two;
+        typedef std::integral_constant<int, 4> Four;
+        typedef std::integral_constant<int, 8> Eight;
+        if (lpr == 4 && wgs <= 2048) run(Four{}, One{});
+        else if (lpr == 4) run(Four{}, Two{});
+        else if (wgs <= 2048) run(Eight{}, One{});
+        else run(Eight{}, Two{});
+    }
     return hipGetLastError();
 }
 

@@ -23,20 +23,40 @@ def test_library_exports_every_declared_symbol():
         assert hasattr(q.lib(), n), n
 
 
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class Place(C.Structure):
+    _fields_ = [("seq", C.c_void_p), ("pos", C.c_void_p), ("pages", C.c_void_p), ("n_seqs", C.c_int32), ("seq_pages", C.c_int32)]
+
+
+KEEP = []
+
+
+def pointer(s):
+    KEEP.append(s)
+    return C.addressof(s)
+
+
 def rows(ts=512, hs=128, data=FAKE):
-    return at._Rows(data, ts, hs)
+    return pointer(Rows(data, ts, hs))
+
+
+def rope(*args):
+    return pointer(at._Rope(*args))
 
 
 def cache(**kw):
     d = dict(k=FAKE, v=FAKE, k_scale=0, v_scale=0, n_pages=8, heads_kv=4, page_tokens=64, dim=128, format=q.ATTN_BF16)
     d.update(kw)
-    return at._Cache(**d)
+    return pointer(at._Cache(**d))
 
 
 def place(**kw):
     d = dict(seq=FAKE, pos=FAKE, pages=FAKE, n_seqs=2, seq_pages=4)
     d.update(kw)
-    return at._Place(**d)
+    return pointer(Place(**d))
 
 
 def refused(rc, word, code=q.MOE_E_ARG):
@@ -81,8 +101,8 @@ def test_rows_refused(r, word):
 def test_append_and_read_refusals():
     L, c, ok = at._lib(), cache(), rows()
 
-    def append(heads=4, n=4, p=place(), rope=None, qq=ok, qo=ok):
-        return L.attn_append(c, qq, ok, ok, qo, None, heads, n, p, rope, None, None)
+    def append(heads=4, n=4, p=place(), turn=None, qq=ok, qo=ok):
+        return L.attn_append(c, qq, ok, ok, qo, None, heads, n, p, turn, None, None)
 
     refused(append(n=-1), "n_tokens")
     refused(append(heads=6), "heads_q")
@@ -92,12 +112,12 @@ def test_append_and_read_refusals():
     refused(append(p=place(pages=0)), "pages")
     refused(append(p=place(n_seqs=0)), "n_seqs")
     refused(append(p=place(seq_pages=0)), "seq_pages")
-    refused(append(rope=at._Rope(0, 64, 0, 1.0)), "inv_freq")
-    refused(append(rope=at._Rope(FAKE, 24, 0, 1.0)), "dims")
-    refused(append(rope=at._Rope(FAKE, 144, 0, 1.0)), "dims")
-    refused(append(rope=at._Rope(FAKE, -16, 0, 1.0)), "dims")
-    refused(append(rope=at._Rope(FAKE, 64, 2, 1.0)), "layout")
-    refused(append(rope=at._Rope(FAKE, 64, 0, math.inf)), "mscale")
+    refused(append(turn=rope(0, 64, 0, 1.0)), "inv_freq")
+    refused(append(turn=rope(FAKE, 24, 0, 1.0)), "dims")
+    refused(append(turn=rope(FAKE, 144, 0, 1.0)), "dims")
+    refused(append(turn=rope(FAKE, -16, 0, 1.0)), "dims")
+    refused(append(turn=rope(FAKE, 64, 2, 1.0)), "layout")
+    refused(append(turn=rope(FAKE, 64, 0, math.inf)), "mscale")
     refused(L.attn_read(c, None, 4, ok, ok, None, None), "place")
     assert append(n=0) == q.MOE_OK and L.attn_read(c, place(), 0, None, None, None, None) == q.MOE_OK       # nothing to do
 
@@ -181,10 +201,10 @@ def test_frequencies_refused(kw):
 def test_tensors_refused_by_the_binding():
     import torch
     bf = torch.zeros((4, 2, 64), dtype=torch.bfloat16)
-    for call in (lambda: at._heads(bf, "q"),                                                       # not on the GPU
+    for call in (lambda: at._heads(bf, "q", 4, 2, 64),                                                       # not on the GPU
                  lambda: at.AttnCache(torch.zeros((2, 2, 16, 64)), torch.zeros((2, 2, 16, 64))),    # no bf16 or float8
                  lambda: at.AttnCache(torch.zeros((2, 2, 16, 64), dtype=torch.uint8), torch.zeros((2, 2, 16, 64), dtype=torch.uint8)),
                  lambda: at.AttnCache(bf, bf), lambda: at.AttnRope(torch.zeros(32, dtype=torch.float64), "other")):
         with pytest.raises(q.MoeError):
             call()
-    assert C.sizeof(at._Rows) == 24 and C.sizeof(at._Cache) == 56 and C.sizeof(at._Place) == 32 and C.sizeof(at._Rope) == 24
+    assert C.sizeof(Rows) == 8 * at._ROWS == 24 and C.sizeof(at._Cache) == 56 and C.sizeof(Place) == 8 * at._PLACE == 32 and C.sizeof(at._Rope) == 24
