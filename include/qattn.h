@@ -112,10 +112,14 @@ int32_t attn_read(const attn_cache *cache, const attn_place *place, int32_t n_to
  *     out_i = sum_j p_ij v_j,   p_ij = exp(scale q_i.k_j) / sum_j' exp(scale q_i.k_j')
  * A query that sees no key gives zeros.  lse ([device] float [n_q, heads_q], may be NULL): ln of the sum of the exponentials,
  * -inf for a query without keys.  Rows of out that belong to no sequence are left untouched.  Entries of cu out of 0..n_q (n_k) or
- * descending are clamped to the range and to the entry before them.  scale > 0 and finite.  out overlaps no input. */
+ * descending are clamped to the range and to the entry before them.  scale > 0 and finite.  out overlaps no input.
+ * workspace ([device], 16-byte aligned, may be NULL; its contents before and after the call are of no account): where queries are so few that
+ * they leave CUs idle, the keys of a query are cut into parts that run side by side, and a second launch joins them.
+ * attn_prompt_workspace_bytes(...) is what that takes, 0 where nothing is cut; with less than that nothing is cut either. */
+size_t attn_prompt_workspace_bytes(int32_t n_seqs, int32_t n_q, int32_t n_k, int32_t heads_q, int32_t heads_kv, int32_t dim);
 int32_t attn_prompt(const attn_rows *q, const attn_rows *k, const attn_rows *v, const attn_rows *out, float *lse, const int32_t *cu_q,
                     const int32_t *cu_k, int32_t n_seqs, int32_t n_q, int32_t n_k, int32_t heads_q, int32_t heads_kv, int32_t dim,
-                    float scale, int32_t causal, void *stream);
+                    float scale, int32_t causal, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Attention of one query a sequence over the cache: query b sees the first lens[b] tokens of sequence b (lens [device] int32
  * [n_seqs]), whose pages are pages[b * seq_pages ..].  The formula, lse ([device] float [n_seqs, heads_q], may be NULL) and the answer

@@ -42,11 +42,11 @@ def _lib():
         L.attn_rope_frequencies.argtypes = [I, C.c_double, I, C.c_double, C.c_double, C.c_double, C.c_double, P, C.POINTER(F)]
         L.attn_append.argtypes = [P, P, P, P, P, P, I, I, P, P, P, P]
         L.attn_read.argtypes = [P, P, I, P, P, P, P]
-        L.attn_prompt.argtypes = [P, P, P, P, P, P, P, I, I, I, I, I, I, F, I, P]
+        L.attn_prompt.argtypes = [P, P, P, P, P, P, P, I, I, I, I, I, I, F, I, P, C.c_size_t, P]
         L.attn_decode.argtypes = [P, P, P, P, I, I, P, I, P, F, P, C.c_size_t, P, P]
         for f in ("attn_rope_frequencies", "attn_append", "attn_read", "attn_prompt", "attn_decode"):
             getattr(L, f).restype = I
-        for f, n in (("attn_decode_workspace_bytes", 4), ("attn_decode_counter_bytes", 3)):
+        for f, n in (("attn_prompt_workspace_bytes", 6), ("attn_decode_workspace_bytes", 4), ("attn_decode_counter_bytes", 3)):
             getattr(L, f).argtypes = [I] * n
             getattr(L, f).restype = C.c_size_t
         _ready = L
@@ -175,16 +175,20 @@ def attn_read(cache: AttnCache, seq, pos, pages, k_out, v_out, bad=None) -> int:
 
 
 def attn_prompt(q, k, v, cu_q, cu_k, out, scale: Optional[float] = None, causal: bool = True, lse=None) -> int:
-    """Attention over packed prompts; cu_q, cu_k int32 [n_seqs + 1] on the GPU; scale None: dim ** -0.5; lse float32 [n_q, heads_q]."""
+    """Attention over packed prompts; cu_q, cu_k int32 [n_seqs + 1] on the GPU; scale None: dim ** -0.5; lse float32 [n_q, heads_q].
+    Where queries are few and keys many the call takes scratch memory from PyTorch's allocator, for the time of its kernels."""
     (n_q, Hq, D), (n_k, Hk, _) = _three(q, "q"), _three(k, "k")
     n = cu_q.shape[0] - 1
     if n < 0:
         _bad("cu_q has no entry")
+    L = _lib()
+    nb = L.attn_prompt_workspace_bytes(n, n_q, n_k, Hq, Hk, D)
+    ws = None if nb == 0 else torch.empty(nb, dtype=torch.uint8, device=q.device)
     a = _A4(*_heads(q, "q", n_q, Hq, D), *_heads(k, "k", n_k, Hk, D), *_heads(v, "v", n_k, Hk, D), *_heads(out, "out", n_q, Hq, D))
     at = C.addressof(a)
-    return _check(_lib().attn_prompt(at, at + 24, at + 48, at + 72, _optional(lse, "lse", torch.float32, (n_q, Hq)),
+    return _check(L.attn_prompt(at, at + 24, at + 48, at + 72, _optional(lse, "lse", torch.float32, (n_q, Hq)),
                                      _whole(cu_q, "cu_q", torch.int32, (n + 1,)), _whole(cu_k, "cu_k", torch.int32, (n + 1,)), n, n_q, n_k, Hq, Hk, D,
-                                     D ** -0.5 if scale is None else scale, 1 if causal else 0, _stream(q)))
+                                     D ** -0.5 if scale is None else scale, 1 if causal else 0, None if ws is None else ws.data_ptr(), nb, _stream(q)))
 
 
 def attn_decode_workspace(cache: AttnCache, n_seqs: int, heads_q: int):

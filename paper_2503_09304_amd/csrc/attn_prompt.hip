@@ -54,9 +54,6 @@ template <int N, class F>
 __device__ __forceinline__ void static_for(F &&f) {
     static_for_impl(f, std::make_integer_sequence<int, N>{});
 }
-#ifndef LA
-#define LA 4
-#endif
 // An offset of 32 bits that is widened where it is used: widened in front of the loop it would become part of a 64-bit address in vector registers.
 __device__ __forceinline__ uint32_t here(uint32_t v) {
     asm volatile("" : "+v"(v));
@@ -81,9 +78,45 @@ __device__ __forceinline__ int2 span(const int32_t *cu, int b, int n) {
     return {lo, min(max(cu[b + 1], lo), n)};
 }
 
+constexpr int kTileQ = kWaves * 32;                // queries of a workgroup
+
+// The tile of queries with this number, and the tiles of keys that its last query sees.
+__device__ __forceinline__ Tile tile_of(const PromptArgs &a, uint32_t number) {
+    const Tile at = find_heaviest(a.n_seqs, number,
+        [&](int b) {
+            const int2 q = span(a.cu_q, b, a.n_q), k = span(a.cu_k, b, a.n_k);
+            return Span{q.x, q.y - q.x, k.x, k.y - k.x};
+        },
+        [&](Span s) { return int2{(s.nq + kTileQ - 1) / kTileQ, max(0, a.causal ? s.nk - s.nq : s.nk) / kTileQ}; });
+    const auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };          // the same in all lanes, and to be known as such
+    return {scalar(at.piece), {scalar(at.span.q0), scalar(at.span.nq), scalar(at.span.k0), scalar(at.span.nk)}};
+}
+__device__ __forceinline__ int key_tiles(const PromptArgs &a, const Span &s, int q_end) {
+    return ((a.causal ? min(s.nk, max(0, s.nk - s.nq + min(s.nq, q_end))) : s.nk) + kKeys - 1) / kKeys;
+}
+// Parts that the keys of a tile of queries are cut into: so many that each has about as many tiles of keys as a workgroup has if the chip is full and
+// all have the same, kPartTiles at least, and none below twice that: joining costs 5 us and 8 bytes an element.  Us with parts of 16, 24 and 32 tiles at least, and
+// uncut: 64 queries on 8064 keys, 32 heads 35, 46, 50, 79; 1024 queries of four sequences on 18 124 keys 119, 113, 109, 178; five of 1 to 500 on 30 226
+// keys, 16 heads 73, 70, 73, 115; 2434 of six on 16 649 keys, 16 heads of 64 76, 75, 81, 103.
+constexpr int kPartTiles = 24;
+__device__ __forceinline__ int parts_of(const PromptArgs &a, int n_tiles) {
+    if (a.parts == 1 || n_tiles < 2 * kPartTiles - kPartTiles / 2) return 1;
+    const int lane = threadIdx.x & 63;
+    uint32_t work = 0;                            // tiles of keys of all tiles of queries
+    for (int b = lane; b < a.n_seqs; b += 64) {
+        const int2 q = span(a.cu_q, b, a.n_q), k = span(a.cu_k, b, a.n_k);
+        const unsigned long long n = (q.y - q.x + kTileQ - 1) / kTileQ, front = max(0, a.causal ? k.y - k.x - (q.y - q.x) : k.y - k.x) / kKeys;
+        work = __builtin_elementwise_add_sat(work, (uint32_t)min(n * (front + (a.causal ? n + 1 : 0ull)), 0xFFFFFFFFull));
+    }
+    work = last_lane(wave_scan(work));
+    const uint32_t even = (uint32_t)min((unsigned long long)work * a.Hq / a.slots, 1ull << 24), share = max((uint32_t)kPartTiles, even);
+    if ((uint32_t)n_tiles < 2 * even) return 1;
+    return max(1, (int)min((uint32_t)a.parts, (n_tiles + share / 2) / share));
+}
+
 template <int DP>
-__global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a, int tiles, int item0) {
-    constexpr int QT = kWaves * 32;               // queries of a workgroup
+__global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a, int item0) {
+    constexpr int QT = kTileQ;
     constexpr int CH = DP / 8;                    // 16-byte pieces of a row
     constexpr int KS = DP / 32;                   // MFMA steps of a score
     constexpr int DT = DP / 16;                   // 16-d tiles of the output
@@ -96,22 +129,19 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
     // Neighbouring workgroups run on different XCDs: those of one key/value head are Hk apart, so with 8 such heads
     // each XCD's L2 holds the keys of one.  Tiles that see the most keys start first.
     const int G = a.Hq / a.Hk, num = blockIdx.x + item0;
-    const int hk = num % a.Hk, rest = num / a.Hk, head = hk * G + rest % G;
-    const Tile at = find_heaviest(a.n_seqs, (uint32_t)(rest / G),
-        [&](int b) {
-            const int2 q = span(a.cu_q, b, a.n_q), k = span(a.cu_k, b, a.n_k);
-            return Span{q.x, q.y - q.x, k.x, k.y - k.x};
-        },
-        [&](Span s) { return int2{(s.nq + QT - 1) / QT, max(0, a.causal ? s.nk - s.nq : s.nk) / QT}; });
-    const auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };          // the same in all lanes, and to be known as such
-    const int piece = scalar(at.piece);
-    if (piece < 0) return;
-    const int nq = scalar(at.span.nq), nk = scalar(at.span.nk);
-    const int r0 = piece * QT;                    // first query of the tile, within the sequence
-    const long q_row = scalar(at.span.q0), k_row = scalar(at.span.k0);
+    const int hk = num % a.Hk, rest = num / a.Hk, head = hk * G + rest % G, part = rest / G % a.parts;
+    const Tile at = tile_of(a, (uint32_t)(rest / G / a.parts));
+    if (at.piece < 0) return;
+    const int nq = at.span.nq, r0 = at.piece * QT;                       // first query of the tile, within the sequence
+    const long q_row = at.span.q0;
     const int w0 = r0 + wave * 32;                // first query of the wave
+    // Keys of the part: a query r sees those before shift + r + 1.
+    const int all_tiles = key_tiles(a, at.span, r0 + QT), parts = parts_of(a, all_tiles);
+    if (part >= parts) return;
+    const int first_key = (int)((long)all_tiles * part / parts) * kKeys, end_key = (int)((long)all_tiles * (part + 1) / parts) * kKeys;
+    const long k_row = at.span.k0 + first_key;
+    const int nk = min(at.span.nk, end_key) - first_key, shift = at.span.nk - nq - first_key;
     // tiles of keys that the tile's last query sees; that the wave's last query sees, and its first query sees whole
-    const int shift = nk - nq;
     const auto tiles_to = [&](int r) { return ((a.causal ? min(nk, max(0, shift + min(nq, r))) : nk) + kKeys - 1) / kKeys; };
     const int n_tiles = tiles_to(r0 + QT), wave_tiles = w0 < nq ? tiles_to(w0 + 32) : 0;
     const int whole_tiles = min(wave_tiles, min(nk, a.causal ? max(0, shift + w0 + 1) : nk) / kKeys);
@@ -236,6 +266,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
     // Step by step: a matrix instruction, the LDS read of the one LA steps behind it, and a share of the vector work.  Left to the
     // compiler the reads stand right in front of their use, and each waits out LDS.
     // Scores of half n_k of the tile at k_from -> next (and their maxima -> top), weights of cur -> p_cur, sums of half n_v with p_old.
+    constexpr int LA = 4;                         // steps that LDS is read ahead (3, 6 and 8: the same within 1 %)
     const auto half = [&](Scores &next, auto n_k, Scores &cur, u32x4 (&p_cur)[2], const u32x4 (&p_old)[2], auto n_v, int key0, auto masked) {
         constexpr int N = 2 * KS, M = 2 * N;          // score steps (and as many steps for the sums), steps in all
         // Scores and sums in turn, so that no step waits for the one before; the last scores a little earlier, their maxima are last.
@@ -317,6 +348,20 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
         }
     }
 
+    if (parts > 1) {                              // join_parts' to finish
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const float sum = row_all(l[q], [](float x, float y) { return x + y; });
+            const int r = w0 + 16 * q + col;
+            if (r >= nq) continue;
+            const long at_row = ((long)part * a.n_q + q_row + r) * a.Hq + head;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+                if (16 * d < a.D) *reinterpret_cast<f32x4 *>(a.part_o + at_row * a.D + 16 * d + 4 * g) = o[d][q];
+            if (g == 0) *reinterpret_cast<float2 *>(a.part_ml + at_row * 2) = float2{m[q] * a.scale_log2, sum};
+        }
+        return;
+    }
     // Out through LDS, for stores of whole rows: a lane's elements are 8 bytes of each 32 (128 sequences of 128 tokens: 3900 of a workgroup's 24000 clocks).
     constexpr int O_ROW = DP * 2 + 16;
     __syncthreads();                              // the other waves' last reads of K and V
@@ -342,15 +387,73 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
     }
 }
 
+// The parts of 32 queries of one head joined, in their order.
+constexpr int kJoinQ = 32;
+__global__ __launch_bounds__(256) void join_parts(const PromptArgs a, int item0) {
+    const int num = blockIdx.x + item0, head = num % a.Hq, rest = num / a.Hq;
+    const Tile at = tile_of(a, (uint32_t)(rest / (kTileQ / kJoinQ)));
+    if (at.piece < 0) return;
+    const int tile0 = at.piece * kTileQ, r0 = tile0 + rest % (kTileQ / kJoinQ) * kJoinQ;
+    const int parts = parts_of(a, key_tiles(a, at.span, tile0 + kTileQ));
+    if (parts == 1) return;
+    const int rows = min(kJoinQ, at.span.nq - r0), c = a.D / 4;
+    const long stride = (long)a.n_q * a.Hq;
+    for (int i = threadIdx.x; i < rows * c; i += 256) {
+        const int r = i / c, d = (i - r * c) * 4;
+        const long row = at.span.q0 + r0 + r, at_row = row * a.Hq + head;
+        float top = -INFINITY, sum = 0.f;
+        f32x4 acc{0.f, 0.f, 0.f, 0.f};
+        constexpr int U = 4;                      // parts requested before the first is used
+        for (int p0 = 0; p0 < parts; p0 += U) {
+            float2 ml[U];
+            f32x4 v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const long x = min(p0 + u, parts - 1) * stride + at_row;
+                ml[u] = *reinterpret_cast<const float2 *>(a.part_ml + x * 2);
+                v[u] = *reinterpret_cast<const f32x4 *>(a.part_o + x * a.D + d);
+            }
+            float next = top;
+#pragma unroll
+            for (int u = 0; u < U; ++u) next = fmaxf(next, ml[u].x);
+            const float base = next == -INFINITY ? 0.f : next, keep = __builtin_amdgcn_exp2f(top - base);
+            top = next;
+            sum *= keep;
+            acc *= keep;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const float f = p0 + u < parts ? __builtin_amdgcn_exp2f(ml[u].x - base) : 0.f;
+                sum += f * ml[u].y;
+                acc += v[u] * f;
+            }
+        }
+        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        *reinterpret_cast<u32x2 *>(a.o.p + row * a.o.ts + (long)head * a.o.hs + d) = u32x2{pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)};
+        if (a.lse != nullptr && d == 0) a.lse[at_row] = sum > 0.f ? (top + __log2f(sum)) * 0.69314718055994530942f : -INFINITY;
+    }
+}
+
 template <int DP>
 void prompt_n(const PromptArgs &a, hipStream_t s) {
-    const long tiles = (a.n_q + (long)kWaves * 32 - 1) / (kWaves * 32) + a.n_seqs, all = tiles * a.Hq;
+    const long tiles = (a.n_q + (long)kTileQ - 1) / kTileQ + a.n_seqs, all = tiles * a.Hq * a.parts, most = 1 << 23;
     // a launch of 2^32 threads or more would lose the excess
-    for (long at = 0; at < all; at += 1 << 23)
-        prompt_tile<DP><<<dim3((unsigned)std::min<long>(all - at, 1 << 23)), dim3(kWaves * 64), 0, s>>>(a, (int)tiles, (int)at);
+    for (long at = 0; at < all; at += most) prompt_tile<DP><<<dim3((unsigned)std::min(all - at, most)), dim3(kWaves * 64), 0, s>>>(a, (int)at);
+    const long joins = a.parts > 1 ? tiles * a.Hq * (kTileQ / kJoinQ) : 0;
+    for (long at = 0; at < joins; at += most) join_parts<<<dim3((unsigned)std::min(joins - at, most)), dim3(256), 0, s>>>(a, (int)at);
 }
 
 }  // namespace
+
+int prompt_slots(int D) { return D <= 64 ? 768 : 512; }
+
+// Most parts for a call.  The host knows the totals only: it rules out what cannot gain, whole prompts that fill half the chip (4096 tokens of 16 heads of 64 67 us, cut
+// 77; 2048 of 32 heads of 128 53, cut 63) and short ones; the rest is parts_of's to decide.
+int prompt_parts(int n_seqs, int n_q, int n_k, int Hq, int D) {
+    const long slots = prompt_slots(D), wgs = ((n_q + (long)kTileQ - 1) / kTileQ + (n_seqs - 1) / 2) * Hq;
+    const long tiles = (long)n_k * 3 / 2 / n_seqs / kKeys;                // of a sequence's keys, half above the average
+    if (wgs >= 2 * slots || (wgs >= slots / 2 && n_k < 2l * n_q)) return 1;
+    return (int)std::max(1l, std::min(tiles / kPartTiles, 8l));
+}
 
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t s) {
     if (a.D <= 64) prompt_n<64>(a, s);

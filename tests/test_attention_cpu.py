@@ -90,10 +90,10 @@ def test_rows_refused(r, word):
     refused(L.attn_read(c, place(), 4, ok, r, None, None), word)
     refused(L.attn_append(c, ok, r, ok, ok, None, 4, 4, place(), None, None, None), word)
     refused(L.attn_append(c, ok, ok, r, ok, None, 4, 4, place(), None, None, None), word)
-    refused(L.attn_prompt(r, ok, ok, ok, None, FAKE, FAKE, 1, 4, 4, 4, 4, 128, 1.0, 1, None), word)
-    refused(L.attn_prompt(ok, r, ok, ok, None, FAKE, FAKE, 1, 4, 4, 4, 4, 128, 1.0, 1, None), word)
-    refused(L.attn_prompt(ok, ok, r, ok, None, FAKE, FAKE, 1, 4, 4, 4, 4, 128, 1.0, 1, None), word)
-    refused(L.attn_prompt(ok, ok, ok, r, None, FAKE, FAKE, 1, 4, 4, 4, 4, 128, 1.0, 1, None), word)
+    refused(L.attn_prompt(r, ok, ok, ok, None, FAKE, FAKE, 1, 4, 4, 4, 4, 128, 1.0, 1, None, 0, None), word)
+    refused(L.attn_prompt(ok, r, ok, ok, None, FAKE, FAKE, 1, 4, 4, 4, 4, 128, 1.0, 1, None, 0, None), word)
+    refused(L.attn_prompt(ok, ok, r, ok, None, FAKE, FAKE, 1, 4, 4, 4, 4, 128, 1.0, 1, None, 0, None), word)
+    refused(L.attn_prompt(ok, ok, ok, r, None, FAKE, FAKE, 1, 4, 4, 4, 4, 128, 1.0, 1, None, 0, None), word)
     refused(L.attn_decode(c, r, ok, None, 2, 4, FAKE, 4, FAKE, 1.0, FAKE, 1 << 30, None, None), word)
     refused(L.attn_decode(c, ok, r, None, 2, 4, FAKE, 4, FAKE, 1.0, FAKE, 1 << 30, None, None), word)
 
@@ -125,8 +125,8 @@ def test_append_and_read_refusals():
 def test_prompt_and_decode_refusals():
     L, c, ok = at._lib(), cache(), rows()
 
-    def prompt(n_seqs=1, n_q=4, n_k=4, Hq=8, Hk=4, D=128, scale=1.0, cu=FAKE):
-        return L.attn_prompt(ok, ok, ok, ok, None, cu, cu, n_seqs, n_q, n_k, Hq, Hk, D, scale, 1, None)
+    def prompt(n_seqs=1, n_q=4, n_k=4, Hq=8, Hk=4, D=128, scale=1.0, cu=FAKE, ws=0):
+        return L.attn_prompt(ok, ok, ok, ok, None, cu, cu, n_seqs, n_q, n_k, Hq, Hk, D, scale, 1, ws, 1 << 40, None)
 
     def decode(n=2, Hq=8, pages=FAKE, sp=4, lens=FAKE, scale=1.0, ws=FAKE, nb=1 << 40):
         return L.attn_decode(c, ok, ok, None, n, Hq, pages, sp, lens, scale, ws, nb, None, None)
@@ -135,6 +135,7 @@ def test_prompt_and_decode_refusals():
                      (dict(n_q=-1), "negative"), (dict(n_k=-1), "negative"), (dict(scale=0.0), "scale"), (dict(scale=-1.0), "scale"),
                      (dict(scale=math.nan), "scale"), (dict(scale=math.inf), "scale"), (dict(cu=0), "cu_q")]:
         refused(prompt(**kw), word)
+    refused(prompt(ws=FAKE + 8), "workspace", q.MOE_E_WORKSPACE)
     assert prompt(n_seqs=0) == q.MOE_OK and prompt(n_q=0) == q.MOE_OK
     for kw, word in [(dict(n=-1), "n_seqs"), (dict(n=65536), "n_seqs"), (dict(Hq=6), "heads"), (dict(pages=0), "pages"), (dict(lens=0), "lens"),
                      (dict(sp=0), "seq_pages"), (dict(sp=1 << 24), "seq_pages"), (dict(scale=math.nan), "scale")]:
@@ -156,6 +157,16 @@ def test_decode_workspace_sizes():
     for bad in [(-1, 8, 8, 64), (65536, 8, 8, 64), (4, 8, 3, 64), (4, 0, 0, 64), (4, 8, 8, 60)]:
         assert L.attn_decode_workspace_bytes(*bad) == 0
     assert L.attn_decode_workspace_bytes(4, 8, 8, 64) > 0
+
+
+def test_prompt_workspace_sizes():
+    """Only where queries leave CUs idle and keys are many: a part of the sums and two floats a row and head."""
+    size = at._lib().attn_prompt_workspace_bytes
+    assert size(1, 16384, 16384, 32, 8, 128) == 0 and size(1, 17, 17, 32, 8, 128) == 0 and size(64, 64, 64 * 4096, 32, 8, 128) == 0
+    for n, n_q, n_k, Hq, Hk, D in [(1, 128, 16384, 8, 8, 128), (6, 2434, 16801, 16, 16, 64), (1, 1, 1 << 20, 1, 1, 16)]:
+        one = n_q * Hq * (D + 2) * 4
+        assert size(n, n_q, n_k, Hq, Hk, D) % one == 0 and 2 <= size(n, n_q, n_k, Hq, Hk, D) // one <= 16
+    assert size(1, 128, 16384, 8, 3, 128) == 0 and size(0, 128, 16384, 8, 8, 128) == 0 and size(1, 128, 0, 8, 8, 128) == 0
 
 
 def test_frequencies():

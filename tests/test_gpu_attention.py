@@ -149,6 +149,16 @@ def test_prompt_many_workgroups():
 
 
 @pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("D", [64, 128, 80])
+def test_prompt_few_queries_many_keys(causal, D):
+    """Keys of a query cut into parts: parts that a query does not reach, short sequences that are not cut, and rows without keys among them."""
+    assert q.attention._lib().attn_prompt_workspace_bytes(5, 399, 12290, 2, 1, D) > 0
+    run_prompt([130, 1, 7, 200, 61], [6000, 2050, 7, 4213, 20], 2, 1, D, causal, seed=18)
+    run_prompt([1], [9001], 1, 1, D, causal, seed=19)
+    run_prompt([700], [700], 1, 1, D, causal, seed=20)
+
+
+@pytest.mark.parametrize("causal", [True, False])
 def test_prompt_more_sequences_than_lanes(causal):
     """150 sequences, some of several tiles, empty ones and contexts among them: every tile is somebody's."""
     nq = [(37 * i) % 61 if i % 29 else 150 + i for i in range(150)]
