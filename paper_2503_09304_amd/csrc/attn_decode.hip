@@ -14,7 +14,7 @@
 // sum, and are joined in LDS; pieces of a sequence leave fp32 sums in the workspace and the last of them to arrive joins all in the order of
 // the pieces.  More pieces even out better and cost more to join (us, cut for 256 / 512 / 1024 / 1536 workgroups, 8 key/value heads of
 // 128, bf16 unless it says fp8): one sequence of 131071 keys 89 / 94 / 101 / -, fp8 50 / 54 / 61 / -, of 16384 19.8 / 23.5 / 23.4 / -; 64 of 33 to
-// 16384 keys, fp8, 110 / 108 / 87 / 88, bf16 - / 189 / 162 / 153; 16 of 33 to 30000 91 / 79 / 66 / 68; 128 of 3000 all 248, cut for 1536 325.
+// 16384 keys, fp8, 110 / 108 / 87 / 88 (86 with pieces of a sequence of a size), bf16 - / 189 / 162 / 153; 16 of 33 to 30000 91 / 79 / 66 / 68; 128 of 3000 all 248, cut for 1536 325.
 //
 // Measured (us, TB/s): 131071 keys 90, 6.0; the same in fp8 50, 5.4; 128 sequences of 3000 keys 249, 6.3; of one key 4.7.
 #include <hip/hip_runtime.h>
@@ -135,8 +135,8 @@ __global__ __launch_bounds__(kWaves * 64, FP8 ? 4 : 3) void decode_piece(const D
     if (at.seq < 0) return;
     const auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };      // the same in all lanes, and to be known as such
     const int b = scalar(at.seq), piece = scalar(at.piece), len = scalar(at.size), n_pieces = scalar((int)pieces_of(len));
-    const int piece_keys = scalar((int)min(piece_steps, 1u << 23) * step);
-    const int k0 = piece * piece_keys, k1 = min(len, k0 + piece_keys);
+    const int piece_keys = scalar((int)((steps_of(len) + n_pieces - 1) / n_pieces) * step);        // pieces of a sequence are of a size
+    const int k0 = min(len, piece * piece_keys), k1 = min(len, k0 + piece_keys);
     const int32_t *pages = a.pages + (long)b * a.seq_pages;
     if (a.bad != nullptr && hk == 0 && gt == 0 && piece == 0) {
         int bad = tid == 0 && a.lens[b] != len;
