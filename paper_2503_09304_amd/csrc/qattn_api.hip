@@ -162,7 +162,7 @@ int32_t attn_prompt(const attn_rows *q, const attn_rows *k, const attn_rows *v, 
     if (!cu_q || !cu_k) return set_error(MOE_E_ARG, "%s: cu_q or cu_k is null", call);
     if ((rc = check_rows(q, call, "q")) || (rc = check_rows(out, call, "out"))) return rc;
     if (n_k > 0 && ((rc = check_rows(k, call, "k")) || (rc = check_rows(v, call, "v")))) return rc;
-    if (lse && !aligned(lse, 4)) return set_error(MOE_E_ARG, "%s: lse is not 4-byte aligned", call);
+    if (n_k > 0 && (k->token_stride > 1 << 24 || v->token_stride > 1 << 24)) return set_error(MOE_E_ARG, "%s: token strides of k and v must be at most 2^24", call);
     if (workspace && !aligned(workspace, 16)) return set_error(MOE_E_WORKSPACE, "%s: workspace is not 16-byte aligned", call);
     const size_t need = workspace ? attn_prompt_workspace_bytes(n_seqs, n_q, n_k, heads_q, heads_kv, dim) : 0;
     const int parts = need && workspace_bytes >= need ? qattn::prompt_parts(n_seqs, n_q, n_k, heads_q, dim) : 1;

@@ -4,12 +4,14 @@ import ctypes as C
 import math
 import os
 import re
+import subprocess
 
 import numpy as np
 import pytest
 
 import paper_2503_09304_amd as q
 from paper_2503_09304_amd import attention as at
+from paper_2503_09304_amd import build
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 FAKE = 1 << 20                    # addresses that these calls never look at
@@ -135,6 +137,7 @@ def test_prompt_and_decode_refusals():
                      (dict(n_q=-1), "negative"), (dict(n_k=-1), "negative"), (dict(scale=0.0), "scale"), (dict(scale=-1.0), "scale"),
                      (dict(scale=math.nan), "scale"), (dict(scale=math.inf), "scale"), (dict(cu=0), "cu_q")]:
         refused(prompt(**kw), word)
+    refused(L.attn_prompt(ok, rows(ts=(1 << 24) + 8), ok, ok, None, FAKE, FAKE, 1, 4, 4, 4, 4, 128, 1.0, 1, None, 0, None), "2^24")
     refused(prompt(ws=FAKE + 8), "workspace", q.MOE_E_WORKSPACE)
     assert prompt(n_seqs=0) == q.MOE_OK and prompt(n_q=0) == q.MOE_OK
     for kw, word in [(dict(n=-1), "n_seqs"), (dict(n=65536), "n_seqs"), (dict(Hq=6), "heads"), (dict(pages=0), "pages"), (dict(lens=0), "lens"),
@@ -207,6 +210,24 @@ def test_frequencies_refused(kw):
     with pytest.raises(q.MoeError) as e:
         q.attn_rope_frequencies(**dict(dict(dims=64), **kw))
     assert e.value.code == q.MOE_E_ARG
+
+
+def test_registers_and_lds_of_the_attention_kernels(tmp_path):
+    """Workgroups of 256 threads are a wave on each SIMD of 512 registers: what shares a CU by them and by 160 KB of LDS, and nothing in scratch."""
+    seen = {}
+    for src in ("attn_prompt", "attn_decode"):
+        cmd = [build.HIPCC, *build.FLAGS, "--cuda-device-only", "-Rpass-analysis=kernel-resource-usage", "-c", os.path.join(build.CSRC, src + ".hip"),
+               "-o", str(tmp_path / "kernels.o")]
+        r = subprocess.run(cmd, capture_output=True, text=True, timeout=300)
+        assert r.returncode == 0, r.stderr[-4000:]
+        for part in r.stderr.split("Function Name: ")[1:]:
+            get = lambda what: int(re.search(what + r": (\d+)", part).group(1))  # noqa: E731
+            regs, lds = get(r"\bVGPRs") + get(r"\bAGPRs"), get(r"LDS Size \[bytes/block\]")
+            assert get(r"ScratchSize \[bytes/lane\]") == 0, part.split()[0]
+            seen[part.split()[0]] = min(512 // (-(-regs // 8) * 8), 160 * 1024 // max(lds, 1))
+    for name, least in (("prompt_tileILi128E", 2), ("prompt_tileILi64E", 3), ("decode_pieceILi128ELb0E", 3), ("decode_pieceILi128ELb1E", 4), ("decode_pieceILi64E", 4)):
+        found = [n for k, n in seen.items() if name in k]
+        assert found and min(found) >= least, (name, seen)
 
 
 def test_tensors_refused_by_the_binding():
