@@ -2,13 +2,24 @@
 //
 // One pass over the keys with the running maximum and sum of the softmax.  A workgroup has 4 waves; a wave owns 32 queries of one
 // head and goes through the keys 64 at a time:
-//     S^T[key, q] = K Q^T     v_mfma_f32_32x32x16_bf16, A = 32 keys x 16 d, B = 16 d x 32 queries
-//     O^T[d, q]   = V^T P^T   A = 32 d x 16 keys,  B = 16 keys x 32 queries
-// Transposed like this a lane holds 16 keys of one query per tile, so the maximum and the sum of a row are formed inside the lane (one
-// exchange with lane ^ 32 at the end), and the weights are the second product's B operand as they stand: slot 8h + j of it
-// (h = lane / 32) is key 8 (j / 4) + 4h + j % 4 of the 16, and V^T is read in that order.
-// K and V tiles are staged in LDS, double-buffered, through registers (the loads of the next tile are in flight while one is worked on),
-// their 16-byte pieces XOR-swizzled by row.  K rows are read as they are, V^T by ds_read_b64_tr_b16.
+//     S^T[key, q] = K Q^T     v_mfma_f32_16x16x32_bf16, A = 16 keys x 32 d, B = 32 d x 16 queries
+//     O^T[d, q]   = V^T P^T   A = 16 d x 32 keys, B = 32 keys x 16 queries
+// Transposed like this a lane holds 8 of 32 keys of each of its two queries, so maxima and sums are formed inside the lane (an exchange between
+// the 4 lanes of a query is needed only where a maximum grows, and at the end), and the weights are the second product's B operand as they
+// stand: slot 8g + 4t + r of it (g = lane / 16) is key 16t + 4g + r, and V^T is read in that order.
+// K and V tiles are staged in LDS, double-buffered, through registers, each requested a whole tile before it is stored there, in 16-byte pieces
+// XOR-swizzled by row.  K rows are read as they are, V^T by ds_read_b64_tr_b16.
+//
+// What bounds it.  Per 32 keys and 32 queries of 128 elements a wave has 32 matrix instructions (512 clocks of its SIMD), 24 LDS reads and
+// 84 vector instructions, 16 of them exponentials (400 clocks).  Two workgroups share a CU: 2 waves on a SIMD.  On zeros the kernel runs at 1.27
+// PFLOP/s, on random values at 1.1, at 2.0 GHz instead of 2.4: the power limit, as for this library's other large products (a large product of the vendor's
+// library 1.19).  So what counts is clocks and energy: scores, weights and sums of three successive half tiles side by side (below), a maximum
+// that stays needs no rescaling (2^8 of room), 16x16x32 instructions (2.5 % over 32x32x16).  Steps from the first kernel, 16384 tokens, 32 heads on 8, us: 3864;
+// side by side 2494; no rescaling 2141; maxima behind the scores 2077; 16x16x32 2039; loads a tile ahead 2005; ends by wave 1979.
+// Kept out: two blocks of 32 queries a wave (LDS read half as often, but one wave a SIMD: 2300 at the time), rows padded instead of swizzled (2083, bank
+// conflicts), the sums' instructions in assembly into their own registers (2083), rescaling the sums half a tile later (2088).
+//
+// Measured (us, TFLOP/s): 16384 tokens, 32 heads of 128 on 8, 1983, 1109; 4096 144, 952; 3584 in 8 prompts 57; 16 heads of 64 608, 904; 17 tokens 6.9.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -285,6 +296,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
             if (r & 1) p_cur[q][2 * t + r / 2] = pack_bf16(cur[q][t][r - 1], cur[q][t][r]);
         };
         static_for<LA>(read);
+        __builtin_amdgcn_s_setprio(1);                // before the CU's other waves, while those are between halves: 16384 tokens 1 %, 4096 5 %
         __builtin_amdgcn_sched_barrier(0);
         static_for<M>([&](auto i) {
             constexpr int j = index(i);
@@ -294,6 +306,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
             static_for<16 / M>([&](auto r) { weight(i * (16 / M) + r); });
             __builtin_amdgcn_sched_barrier(0);
         });
+        __builtin_amdgcn_s_setprio(0);
         maximum(next, key0, masked);
     };
     Scores sa, sb;
