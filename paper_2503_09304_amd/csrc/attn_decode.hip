@@ -349,7 +349,7 @@ __global__ __launch_bounds__(kWaves * 64, FP8 ? 4 : 3) void decode_piece(const D
         for (int i = 0; i < EX; ++i) acc[i] += f * s_o[w][q][EX * x + i];
     }
     const auto finish = [&](int q, int x, float top, float sum, const float (&acc)[EX]) {
-        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        const float inv = sum != 0.f ? 1.f / sum : 0.f;
         const int head_q = hk * G + gt * 16 + q;
         uint16_t *to = a.o.p + (long)b * a.o.ts + (long)head_q * a.o.hs + EX * x;
         if (EX * x < D) {
@@ -357,7 +357,7 @@ __global__ __launch_bounds__(kWaves * 64, FP8 ? 4 : 3) void decode_piece(const D
             for (int i = 0; i < EX; i += 4)
                 *reinterpret_cast<u32x2 *>(to + i) = u32x2{pack_bf16(acc[i] * inv, acc[i + 1] * inv), pack_bf16(acc[i + 2] * inv, acc[i + 3] * inv)};
         }
-        if (a.lse != nullptr && x == 0) a.lse[(long)b * a.Hq + head_q] = sum > 0.f ? (top + __log2f(sum)) * 0.69314718055994530942f : -INFINITY;
+        if (a.lse != nullptr && x == 0) a.lse[(long)b * a.Hq + head_q] = sum != 0.f ? (top + __log2f(sum)) * 0.69314718055994530942f : -INFINITY;
     };
     if (n_pieces == 1) {
         if (q < n_q) finish(q, x, top, sum, acc);

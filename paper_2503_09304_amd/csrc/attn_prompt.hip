@@ -375,13 +375,13 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
         }
         return;
     }
-    // Out through LDS, for stores of whole rows: a lane's elements are 8 bytes of each 32 (128 sequences of 128 tokens: 3900 of a workgroup's 24000 clocks).
+    // Out through LDS, for stores of whole rows: a lane's elements are 8 bytes of each 32 (32 sequences of 128 tokens, 32 heads: 3900 of a workgroup's 25000 clocks).
     constexpr int O_ROW = DP * 2 + 16;
     __syncthreads();                              // the other waves' last reads of K and V
     uint8_t *s_o = &s_kv[wave * 32 * O_ROW];
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-        const float sum = row_all(l[q], [](float x, float y) { return x + y; }), inv = sum > 0.f ? 1.f / sum : 0.f;
+        const float sum = row_all(l[q], [](float x, float y) { return x + y; }), inv = sum != 0.f ? 1.f / sum : 0.f;
         const int r = w0 + 16 * q + col;
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
@@ -389,7 +389,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
             *reinterpret_cast<u32x2 *>(s_o + (16 * q + col) * O_ROW + 32 * d + 8 * g) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
         }
         if (a.lse != nullptr && g == 0 && r < nq)
-            a.lse[(q_row + r) * a.Hq + head] = sum > 0.f ? (m[q] * a.scale_log2 + __log2f(sum)) * 0.69314718055994530942f : -INFINITY;
+            a.lse[(q_row + r) * a.Hq + head] = sum != 0.f ? (m[q] * a.scale_log2 + __log2f(sum)) * 0.69314718055994530942f : -INFINITY;
     }
     uint16_t *to = a.o.p + q_row * a.o.ts + (long)head * a.o.hs;
 #pragma unroll
@@ -440,9 +440,9 @@ __global__ __launch_bounds__(256) void join_parts(const PromptArgs a, int item0)
                 acc += v[u] * f;
             }
         }
-        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        const float inv = sum != 0.f ? 1.f / sum : 0.f;
         *reinterpret_cast<u32x2 *>(a.o.p + row * a.o.ts + (long)head * a.o.hs + d) = u32x2{pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)};
-        if (a.lse != nullptr && d == 0) a.lse[at_row] = sum > 0.f ? (top + __log2f(sum)) * 0.69314718055994530942f : -INFINITY;
+        if (a.lse != nullptr && d == 0) a.lse[at_row] = sum != 0.f ? (top + __log2f(sum)) * 0.69314718055994530942f : -INFINITY;
     }
 }
 

@@ -493,6 +493,29 @@ def test_decode_lens_and_pages_out_of_range():
     assert torch.equal(got.view(torch.int16), want.view(torch.int16))
 
 
+def test_a_query_of_nan_shows_and_stays_alone():
+    """Its output and lse are NaN, not those of a query without keys; the others' bits are what they were."""
+    c, qq, pages, ln, out, ws = run_decode([700, 3, 9000], 8, 2, 128, 16, seed=8)
+    lse = torch.zeros(3, 8, dtype=torch.float32, device=DEV)
+    got, sick = torch.zeros_like(out), qq.contiguous()
+    sick[0, 3] = sick[2, 5] = NAN
+    q.attn_decode(c, sick, pages, ln, got, ws, lse=lse)
+    hit = torch.zeros(3, 8, dtype=torch.bool, device=DEV)
+    hit[0, 3] = hit[2, 5] = True
+    assert torch.equal(lse.isnan(), hit) and got[hit].isnan().all() and torch.equal(got[~hit], out[~hit])
+    g = gen(9)                                                                  # many keys: cut into parts
+    x, k, v = rows(g, 40, 8, 64), rows(g, 9000, 2, 64), rows(g, 9000, 2, 64)
+    cq, ck = torch.tensor([0, 40], dtype=torch.int32, device=DEV), torch.tensor([0, 9000], dtype=torch.int32, device=DEV)
+    hit = torch.zeros(40, 8, dtype=torch.bool, device=DEV)
+    hit[7, 1] = hit[39, 6] = True
+    for m in (9000, 300):
+        ck[1] = m
+        a, b, lse = torch.zeros_like(x), torch.zeros_like(x), torch.zeros(40, 8, dtype=torch.float32, device=DEV)
+        q.attn_prompt(x, k, v, cq, ck, a)
+        q.attn_prompt(torch.where(hit[:, :, None], torch.full_like(x, NAN), x), k, v, cq, ck, b, lse=lse)
+        assert torch.equal(lse.isnan(), hit) and b[hit].isnan().all() and torch.equal(b[~hit], a[~hit])
+
+
 def test_workspace_refused():
     c, qq, pages, ln, out, ws = run_decode([10], 2, 1, 64, 16, seed=6)
     with pytest.raises(q.MoeError) as e:
