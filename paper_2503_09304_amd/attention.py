@@ -6,6 +6,8 @@ belongs to another stream's work is the caller's to order, as with any kernel.""
 from __future__ import annotations
 
 import ctypes as C
+import struct
+import threading
 from typing import Optional
 
 import torch
@@ -26,10 +28,20 @@ class _Rope(C.Structure):
     _fields_ = [("inv_freq", C.c_void_p), ("dims", C.c_int32), ("layout", C.c_int32), ("mscale", C.c_float)]
 
 
-# attn_rows and attn_place are passed as slices of one array of 64-bit numbers per call: a structure object for each of a call's
-# tensors costs more than its kernel's launch.
+# attn_rows and attn_place are passed as slices of one array of 64-bit numbers, a thread's own, written anew by every call: a structure
+# object for each of a call's tensors costs more than its kernel's launch, an array object a call a tenth of the call.
 _ROWS, _PLACE = 3, 4
-_A2, _A2P, _A4, _A5P = (C.c_int64 * n for n in (2 * _ROWS, 2 * _ROWS + _PLACE, 4 * _ROWS, 5 * _ROWS + _PLACE))
+_MOST = 5 * _ROWS + _PLACE
+_pack2, _pack2p, _pack4, _pack5p = (struct.Struct(f"{n}q").pack_into for n in (2 * _ROWS, 2 * _ROWS + _PLACE, 4 * _ROWS, _MOST))
+
+
+class _Numbers(threading.local):
+    def __init__(self):
+        self.to = (C.c_int64 * _MOST)()
+        self.at = C.addressof(self.to)
+
+
+_numbers = _Numbers()
 
 _ready = None
 
@@ -157,10 +169,11 @@ def attn_append(cache: AttnCache, q, k, v, seq, pos, pages, rope: Optional[AttnR
         _bad("q and q_out go together")
     Hq = 0 if q is None else _three(q, "q")[1]
     none = (0, 0, 0)
-    a = _A5P(*_heads(k, "k", T, Hk, D), *_heads(v, "v", T, Hk, D), *_place(seq, pos, pages, T),
-             *(none if q is None else _heads(q, "q", T, Hq, D)), *(none if q is None else _heads(q_out, "q_out", T, Hq, D)),
-             *(none if k_out is None else _heads(k_out, "k_out", T, Hk, D)))
-    at = C.addressof(a)
+    w = _numbers
+    _pack5p(w.to, 0, *_heads(k, "k", T, Hk, D), *_heads(v, "v", T, Hk, D), *_place(seq, pos, pages, T),
+            *(none if q is None else _heads(q, "q", T, Hq, D)), *(none if q is None else _heads(q_out, "q_out", T, Hq, D)),
+            *(none if k_out is None else _heads(k_out, "k_out", T, Hk, D)))
+    at = w.at
     return _check(_lib().attn_append(cache._at, at + 80 if q is not None else None, at, at + 24, at + 104 if q is not None else None,
                                      at + 128 if k_out is not None else None, Hq, T, at + 48, None if rope is None else rope._at,
                                      _optional(bad, "bad", torch.int32, (1,)), _stream(k)))
@@ -169,8 +182,9 @@ def attn_append(cache: AttnCache, q, k, v, seq, pos, pages, rope: Optional[AttnR
 def attn_read(cache: AttnCache, seq, pos, pages, k_out, v_out, bad=None) -> int:
     """Keys and values of the tokens at (seq, pos) out of the cache, as bfloat16."""
     T = pos.shape[0]
-    a = _A2P(*_heads(k_out, "k_out", T, cache.heads_kv, cache.dim), *_heads(v_out, "v_out", T, cache.heads_kv, cache.dim), *_place(seq, pos, pages, T))
-    at = C.addressof(a)
+    w = _numbers
+    _pack2p(w.to, 0, *_heads(k_out, "k_out", T, cache.heads_kv, cache.dim), *_heads(v_out, "v_out", T, cache.heads_kv, cache.dim), *_place(seq, pos, pages, T))
+    at = w.at
     return _check(_lib().attn_read(cache._at, at + 48, T, at, at + 24, _optional(bad, "bad", torch.int32, (1,)), _stream(k_out)))
 
 
@@ -184,8 +198,9 @@ def attn_prompt(q, k, v, cu_q, cu_k, out, scale: Optional[float] = None, causal:
     L = _lib()
     nb = L.attn_prompt_workspace_bytes(n, n_q, n_k, Hq, Hk, D)
     ws = None if nb == 0 else torch.empty(nb, dtype=torch.uint8, device=q.device)
-    a = _A4(*_heads(q, "q", n_q, Hq, D), *_heads(k, "k", n_k, Hk, D), *_heads(v, "v", n_k, Hk, D), *_heads(out, "out", n_q, Hq, D))
-    at = C.addressof(a)
+    w = _numbers
+    _pack4(w.to, 0, *_heads(q, "q", n_q, Hq, D), *_heads(k, "k", n_k, Hk, D), *_heads(v, "v", n_k, Hk, D), *_heads(out, "out", n_q, Hq, D))
+    at = w.at
     return _check(L.attn_prompt(at, at + 24, at + 48, at + 72, _optional(lse, "lse", torch.float32, (n_q, Hq)),
                                      _whole(cu_q, "cu_q", torch.int32, (n + 1,)), _whole(cu_k, "cu_k", torch.int32, (n + 1,)), n, n_q, n_k, Hq, Hk, D,
                                      D ** -0.5 if scale is None else scale, 1 if causal else 0, None if ws is None else ws.data_ptr(), nb, _stream(q)))
@@ -205,8 +220,9 @@ def attn_decode(cache: AttnCache, q, pages, lens, out, workspace, scale: Optiona
     if pages.dim() != 2 or D != cache.dim:
         _bad("pages must be [n_seqs, seq_pages], q [n_seqs, heads_q, dim of the cache]")
     m, nb = pages.shape[1], workspace.numel()
-    a = _A2(*_heads(q, "q", n, Hq, D), *_heads(out, "out", n, Hq, D))
-    at = C.addressof(a)
+    w = _numbers
+    _pack2(w.to, 0, *_heads(q, "q", n, Hq, D), *_heads(out, "out", n, Hq, D))
+    at = w.at
     return _check(_lib().attn_decode(cache._at, at, at + 24, _optional(lse, "lse", torch.float32, (n, Hq)), n, Hq,
                                      _whole(pages, "pages", torch.int32, (n, m)), m, _whole(lens, "lens", torch.int32, (n,)),
                                      D ** -0.5 if scale is None else scale, _whole(workspace, "workspace", torch.uint8, (nb,)), nb,
