@@ -36,6 +36,9 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = 4;
 constexpr int kBlock = 32;                       // keys of a wave's step
+// Steps of a sequence that is not cut: joining its pieces would take longer.  Us uncut / in pieces of two steps at least, 8 key/value heads of 128: 257 keys
+// 7.1 / 9.2, 512 9.3 / 9.3, 700 11.3 / 9.5, 1000 14.5 / 9.9; 32 sequences of 512 keys, 4 heads, 11.9 / 12.1; of 600 13.4 / 14.0; of 1 to 1000 17.1 / 11.0.
+constexpr uint32_t kWholeSteps = 4;
 
 __device__ __forceinline__ f32x4 mma(const u32x4 &a, const u32x4 &b, const f32x4 &c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -113,8 +116,8 @@ __global__ __launch_bounds__(kWaves * 64, FP8 ? 4 : 3) void decode_piece(const D
     const int P = 1 << a.c.page_shift, most = a.seq_pages << a.c.page_shift;
     const auto len_of = [&](int b) { return min(max(a.lens[b], 0), most); };
 
-    // Pieces are whole steps of the workgroup (4 x 32 keys), two at least, as many steps as make `wgs` workgroups of all keys; a
-    // sequence without keys has one too, for its zeros.  The fewest workgroups that come out about even are taken: 256 (one a CU) or 512 for one
+    // Pieces are whole steps of the workgroup (4 x 32 keys), two at least, as many steps as make `wgs` workgroups of all keys.  Sequences of up to four
+    // are not cut, those without keys have a piece too, for its zeros.  The fewest workgroups that come out about even are taken: 256 (one a CU) or 512 for one
     // sequence or several of a length, 1024 or 1536 where pieces of all lengths have to even out (figures at the head of this file).
     const int step = kWaves * kBlock, heads = a.c.Hk * GT;
     const auto steps_of = [&](int len) { return (uint32_t)(len + step - 1) / step; };
@@ -122,7 +125,7 @@ __global__ __launch_bounds__(kWaves * 64, FP8 ? 4 : 3) void decode_piece(const D
     for (int i = 0; i < a.n_seqs; i += 64) total = __builtin_elementwise_add_sat(total, i + lane < a.n_seqs ? steps_of(len_of(i + lane)) : 0u);
     total = last_lane(wave_scan(total));
     uint32_t piece_steps = 0;
-    const auto pieces_of = [&](int len) { return max(1u, (steps_of(len) + piece_steps - 1) / piece_steps); };
+    const auto pieces_of = [&](int len) { return steps_of(len) <= kWholeSteps ? 1u : (steps_of(len) + piece_steps - 1) / piece_steps; };
     for (uint32_t wgs = kFewestWgs; ; wgs = wgs < 1024 ? 2 * wgs : kMostWgs) {
         const uint32_t shares = (wgs + heads - 1) / heads;
         piece_steps = max(2u, (total + shares - 1) / shares);
