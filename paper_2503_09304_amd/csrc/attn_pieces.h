@@ -56,23 +56,29 @@ struct Span {
     int q0, nq, k0, nk;
 };
 struct Tile {
-    int piece;                        // -1: there is no such number
+    int piece, part;                  // piece -1: there is no such number
+    int work;                         // of the piece
     Span span;                        // of its sequence
 };
 
-// The same for pieces that are dealt out heaviest first: a sequence has pieces 0 .. n - 1, the work of piece p is e + p (what it stands for only
-// sets the order).  Numbers go by falling work, then by sequence.  span(b): sequence b; shape(span): {n, e}.
-template <class S, class F>
-__device__ __forceinline__ Tile find_heaviest(int n_seqs, uint32_t number, S &&span, F &&shape) {
+// The same for pieces that are dealt out heaviest first and come in parts: a sequence has pieces 0 .. n - 1, the work of piece p is e + p, and a piece
+// of work w has parts(w) parts, those of all works below w sum(w) (sum(w + 1) - sum(w) = parts(w) > 0).  Numbers go by falling work, then by sequence, then by
+// part.  span(b): sequence b; shape(span): {n, e}.
+template <class S, class F, class P, class U>
+__device__ __forceinline__ Tile find_heaviest(int n_seqs, uint32_t number, S &&span, F &&shape, P &&parts, U &&sum) {
     const int lane = threadIdx.x & 63;
     const auto at = [&](int b0) { return b0 + lane < n_seqs ? span(b0 + lane) : Span{0, 0, 0, 0}; };
     const Span first = at(0);                                         // all there is to load where there are 64 sequences or fewer
     const int2 mine = shape(first);
-    // pieces with work w or more, of this lane's sequences
-    const auto from = [](int2 s, int w) { return (uint32_t)min(max(s.x + s.y - w, 0), s.x); };
+    const uint32_t mine_all = sum((uint32_t)(mine.x + mine.y));
+    // parts of the pieces with work w or more, of this lane's sequences
+    const auto from = [&](int2 s, uint32_t all, int w) { return all - sum((uint32_t)min(max(w, s.y), s.x + s.y)); };
     const auto count = [&](int w) {
-        uint32_t n = from(mine, w);
-        for (int b0 = 64; b0 < n_seqs; b0 += 64) n += from(shape(at(b0)), w);
+        uint32_t n = from(mine, mine_all, w);
+        for (int b0 = 64; b0 < n_seqs; b0 += 64) {
+            const int2 s = shape(at(b0));
+            n += from(s, sum((uint32_t)(s.x + s.y)), w);
+        }
         return last_lane(wave_scan(n));
     };
     int top = mine.x + mine.y;
@@ -81,27 +87,29 @@ __device__ __forceinline__ Tile find_heaviest(int n_seqs, uint32_t number, S &&s
         top = max(top, s.x + s.y);
     }
     uint32_t hi = last_lane(wave_max((uint32_t)top)), lo = 0;         // count(hi) = 0 <= number
-    if (count(0) <= number) return {-1, first};
+    if (count(0) <= number) return {-1, 0, 0, first};
     while (hi - lo > 1) {                                             // count(lo) > number >= count(hi)
         const uint32_t mid = lo + (hi - lo) / 2;
         (count((int)mid) > number ? lo : hi) = mid;
     }
-    // the number-th piece with work lo, in the order of the sequences
-    uint32_t left = number - count((int)hi);
+    // the number-th part of a piece with work lo, in the order of the sequences
+    const uint32_t number_there = number - count((int)hi), each = parts(lo);
+    uint32_t left = number_there / each;
+    const int part = (int)(number_there - left * each);
     for (int b0 = 0; b0 < n_seqs; b0 += 64) {
         const Span s = b0 == 0 ? first : at(b0);
         const int2 f = shape(s);
-        const unsigned long long has = __ballot(from(f, (int)lo) > from(f, (int)hi));
+        const unsigned long long has = __ballot((int)lo >= f.y && (int)lo < f.x + f.y);
         const uint32_t n = __popcll(has);
         if (left >= n) {
             left -= n;
             continue;
         }
         const int l = __builtin_ctzll(__ballot(((has >> lane) & 1) != 0 && __popcll(has & ((1ull << lane) - 1)) == left));
-        return {(int)lo - __builtin_amdgcn_readlane(f.y, l),
+        return {(int)lo - __builtin_amdgcn_readlane(f.y, l), part, (int)lo,
                 {__builtin_amdgcn_readlane(s.q0, l), __builtin_amdgcn_readlane(s.nq, l), __builtin_amdgcn_readlane(s.k0, l), __builtin_amdgcn_readlane(s.nk, l)}};
     }
-    return {-1, first};
+    return {-1, 0, 0, first};
 }
 
 }  // namespace qattn

@@ -91,38 +91,48 @@ __device__ __forceinline__ int2 span(const int32_t *cu, int b, int n) {
 
 constexpr int kTileQ = kWaves * 32;                // queries of a workgroup
 
-// The tile of queries with this number, and the tiles of keys that its last query sees.
-__device__ __forceinline__ Tile tile_of(const PromptArgs &a, uint32_t number) {
-    const Tile at = find_heaviest(a.n_seqs, number,
-        [&](int b) {
-            const int2 q = span(a.cu_q, b, a.n_q), k = span(a.cu_k, b, a.n_k);
-            return Span{q.x, q.y - q.x, k.x, k.y - k.x};
-        },
-        [&](Span s) { return int2{(s.nq + kTileQ - 1) / kTileQ, max(0, a.causal ? s.nk - s.nq : s.nk) / kTileQ}; });
+// The keys of a tile of queries are cut into parts where they are many and the queries few: as many as have about a share each, one at least and
+// a.parts at most.  A share is what a workgroup has if the chip is full and all have the same, kPartTiles tiles of keys at least: joining costs 5 us and 8 bytes an
+// element.  Us with 24, 16, 12 and 8 tiles at least: 16 queries on 2016 keys, 32 heads, 41, 29, 24, 21 (uncut 41); 64 on 8064 47, 36, 36, 36 (79); 512 on 4096 69, 56, 56, 56 (72); 2434
+// of six sequences on 16 649 keys, 16 heads of 64, 69, 62, 63, 63 (103).
+constexpr uint32_t kPartTiles = 8;
+// Lengths here are in steps of kTileQ keys; w: the work of a tile of queries.
+struct Cut {
+    uint32_t share, most;
+    __device__ __forceinline__ uint32_t parts(uint32_t w) const { return most == 1 ? 1u : min(max((w + share / 2) / share, 1u), most); }
+    // parts(0) + ... + parts(w - 1)
+    __device__ __forceinline__ uint32_t sum(uint32_t w) const {
+        if (most == 1) return w;
+        const uint32_t x = w + share / 2, capped = min(x, (most + 1) * share), k = capped / share;
+        return min(w, share - share / 2) + share * (k * (k - 1) / 2) + (capped - k * share) * k + (x - capped) * most;
+    }
+};
+__device__ __forceinline__ int2 tiles_of(const PromptArgs &a, const Span &s) {
+    return {(s.nq + kTileQ - 1) / kTileQ, max(0, a.causal ? s.nk - s.nq : s.nk) / kTileQ};
+}
+__device__ __forceinline__ Span span_of(const PromptArgs &a, int b) {
+    const int2 q = span(a.cu_q, b, a.n_q), k = span(a.cu_k, b, a.n_k);
+    return {q.x, q.y - q.x, k.x, k.y - k.x};
+}
+__device__ __forceinline__ Cut cut_of(const PromptArgs &a) {
+    if (a.parts == 1) return {1, 1};
+    uint32_t work = 0;                            // of all tiles, a step more of each sequence's at most
+    for (int b = threadIdx.x & 63; b < a.n_seqs; b += 64) {
+        const int2 t = tiles_of(a, span_of(a, b));
+        work += t.x * (t.y + (t.x + 1) / 2);
+    }
+    work = last_lane(wave_scan(work));
+    return {max(kPartTiles * kKeys / kTileQ, (uint32_t)min((unsigned long long)work * a.Hq / a.slots + 1, 1ull << 26)), (uint32_t)a.parts};
+}
+// The tile of queries and the part of its keys with this number; the tiles of keys that the tile's last query sees.
+__device__ __forceinline__ Tile tile_of(const PromptArgs &a, const Cut &cut, uint32_t number, bool whole) {
+    const Tile at = find_heaviest(a.n_seqs, number, [&](int b) { return span_of(a, b); }, [&](const Span &s) { return tiles_of(a, s); },
+        [&](uint32_t w) { return whole ? 1u : cut.parts(w); }, [&](uint32_t w) { return whole ? w : cut.sum(w); });
     const auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };          // the same in all lanes, and to be known as such
-    return {scalar(at.piece), {scalar(at.span.q0), scalar(at.span.nq), scalar(at.span.k0), scalar(at.span.nk)}};
+    return {scalar(at.piece), scalar(at.part), scalar(at.work), {scalar(at.span.q0), scalar(at.span.nq), scalar(at.span.k0), scalar(at.span.nk)}};
 }
 __device__ __forceinline__ int key_tiles(const PromptArgs &a, const Span &s, int q_end) {
     return ((a.causal ? min(s.nk, max(0, s.nk - s.nq + min(s.nq, q_end))) : s.nk) + kKeys - 1) / kKeys;
-}
-// Parts that the keys of a tile of queries are cut into: so many that each has about as many tiles of keys as a workgroup has if the chip is full and
-// all have the same, kPartTiles at least, and none below twice that: joining costs 5 us and 8 bytes an element.  Us with parts of 16, 24 and 32 tiles at least, and
-// uncut: 64 queries on 8064 keys, 32 heads 35, 46, 50, 79; 1024 queries of four sequences on 18 124 keys 119, 113, 109, 178; five of 1 to 500 on 30 226
-// keys, 16 heads 73, 70, 73, 115; 2434 of six on 16 649 keys, 16 heads of 64 76, 75, 81, 103.
-constexpr int kPartTiles = 24;
-__device__ __forceinline__ int parts_of(const PromptArgs &a, int n_tiles) {
-    if (a.parts == 1 || n_tiles < 2 * kPartTiles - kPartTiles / 2) return 1;
-    const int lane = threadIdx.x & 63;
-    uint32_t work = 0;                            // tiles of keys of all tiles of queries
-    for (int b = lane; b < a.n_seqs; b += 64) {
-        const int2 q = span(a.cu_q, b, a.n_q), k = span(a.cu_k, b, a.n_k);
-        const unsigned long long n = (q.y - q.x + kTileQ - 1) / kTileQ, front = max(0, a.causal ? k.y - k.x - (q.y - q.x) : k.y - k.x) / kKeys;
-        work = __builtin_elementwise_add_sat(work, (uint32_t)min(n * (front + (a.causal ? n + 1 : 0ull)), 0xFFFFFFFFull));
-    }
-    work = last_lane(wave_scan(work));
-    const uint32_t even = (uint32_t)min((unsigned long long)work * a.Hq / a.slots, 1ull << 24), share = max((uint32_t)kPartTiles, even);
-    if ((uint32_t)n_tiles < 2 * even) return 1;
-    return max(1, (int)min((uint32_t)a.parts, (n_tiles + share / 2) / share));
 }
 
 template <int DP>
@@ -140,15 +150,15 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
     // Neighbouring workgroups run on different XCDs: those of one key/value head are Hk apart, so with 8 such heads
     // each XCD's L2 holds the keys of one.  Tiles that see the most keys start first.
     const int G = a.Hq / a.Hk, num = blockIdx.x + item0;
-    const int hk = num % a.Hk, rest = num / a.Hk, head = hk * G + rest % G, part = rest / G % a.parts;
-    const Tile at = tile_of(a, (uint32_t)(rest / G / a.parts));
+    const int hk = num % a.Hk, rest = num / a.Hk, head = hk * G + rest % G;
+    const Cut cut = cut_of(a);
+    const Tile at = tile_of(a, cut, (uint32_t)(rest / G), false);
     if (at.piece < 0) return;
     const int nq = at.span.nq, r0 = at.piece * QT;                       // first query of the tile, within the sequence
     const long q_row = at.span.q0;
     const int w0 = r0 + wave * 32;                // first query of the wave
     // Keys of the part: a query r sees those before shift + r + 1.
-    const int all_tiles = key_tiles(a, at.span, r0 + QT), parts = parts_of(a, all_tiles);
-    if (part >= parts) return;
+    const int all_tiles = key_tiles(a, at.span, r0 + QT), parts = (int)cut.parts(at.work), part = at.part;
     const int first_key = (int)((long)all_tiles * part / parts) * kKeys, end_key = (int)((long)all_tiles * (part + 1) / parts) * kKeys;
     const long k_row = at.span.k0 + first_key;
     const int nk = min(at.span.nk, end_key) - first_key, shift = at.span.nk - nq - first_key;
@@ -404,10 +414,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
 constexpr int kJoinQ = 32;
 __global__ __launch_bounds__(256) void join_parts(const PromptArgs a, int item0) {
     const int num = blockIdx.x + item0, head = num % a.Hq, rest = num / a.Hq;
-    const Tile at = tile_of(a, (uint32_t)(rest / (kTileQ / kJoinQ)));
+    const Cut cut = cut_of(a);
+    const Tile at = tile_of(a, cut, (uint32_t)(rest / (kTileQ / kJoinQ)), true);
     if (at.piece < 0) return;
-    const int tile0 = at.piece * kTileQ, r0 = tile0 + rest % (kTileQ / kJoinQ) * kJoinQ;
-    const int parts = parts_of(a, key_tiles(a, at.span, tile0 + kTileQ));
+    const int r0 = at.piece * kTileQ + rest % (kTileQ / kJoinQ) * kJoinQ, parts = (int)cut.parts(at.work);
     if (parts == 1) return;
     const int rows = min(kJoinQ, at.span.nq - r0), c = a.D / 4;
     const long stride = (long)a.n_q * a.Hq;
@@ -448,7 +458,9 @@ __global__ __launch_bounds__(256) void join_parts(const PromptArgs a, int item0)
 
 template <int DP>
 void prompt_n(const PromptArgs &a, hipStream_t s) {
-    const long tiles = (a.n_q + (long)kTileQ - 1) / kTileQ + a.n_seqs, all = tiles * a.Hq * a.parts, most = 1 << 23;
+    const long tiles = (a.n_q + (long)kTileQ - 1) / kTileQ + a.n_seqs, most = 1 << 23;
+    // With parts(w) <= 1 + w / share and a share of all work * Hq / slots or more, cutting adds slots / Hq parts a head at most.
+    const long all = (a.parts == 1 ? tiles : std::min(tiles * a.parts, tiles + a.slots / a.Hq + 1)) * a.Hq;
     // a launch of 2^32 threads or more would lose the excess
     for (long at = 0; at < all; at += most) prompt_tile<DP><<<dim3((unsigned)std::min(all - at, most)), dim3(kWaves * 64), 0, s>>>(a, (int)at);
     const long joins = a.parts > 1 ? tiles * a.Hq * (kTileQ / kJoinQ) : 0;
@@ -459,13 +471,18 @@ void prompt_n(const PromptArgs &a, hipStream_t s) {
 
 int prompt_slots(int D) { return D <= 64 ? 768 : 512; }
 
-// Most parts for a call.  The host knows the totals only: it rules out what cannot gain, whole prompts that fill half the chip (4096 tokens of 16 heads of 64 67 us, cut
-// 77; 2048 of 32 heads of 128 53, cut 63) and short ones; the rest is parts_of's to decide.
+// Most parts for a call; which tiles are cut into how many the kernels decide.  The host knows the totals only, and rules out where nothing can be gained for the 5 us:
+// where most CUs have work as it is.  A second workgroup on a CU adds half to what it does, so one sequence is cut where it fills a third of the chip or less (us uncut / cut: 1024
+// queries on 2048 keys, 32 heads 48 / 58, 512 on 4096 72 / 56; 2048 on as many, 8 heads 48 / 36); several may be uneven, their longest twice the average: two thirds
+// (16 times 8 queries on 1500 keys, 32 heads 43 / 48; 1024 of four on 18 124 112 / 112; 2434 of six, 16 heads of 64 72 / 63), whole prompts half.  And short sequences: 16 tiles
+// of keys (1024 on as many, 8 heads) 26 / 29, 18 (128 on 1128, 32 heads) 29 / 27.
 int prompt_parts(int n_seqs, int n_q, int n_k, int Hq, int D) {
-    const long slots = prompt_slots(D), wgs = ((n_q + (long)kTileQ - 1) / kTileQ + (n_seqs - 1) / 2) * Hq;
-    const long tiles = (long)n_k * 3 / 2 / n_seqs / kKeys;                // of a sequence's keys, half above the average
-    if (wgs >= 2 * slots || (wgs >= slots / 2 && n_k < 2l * n_q)) return 1;
-    return (int)std::max(1l, std::min(tiles / kPartTiles, 8l));
+    const long slots = prompt_slots(D), tiles = (n_q + (long)kTileQ - 1) / kTileQ, each = (long)n_k / n_seqs / kKeys;
+    const long wgs = std::max(tiles + (n_seqs - 1) / 2, (long)n_seqs) * Hq, f = n_seqs == 1 ? 1 : 2;
+    if (3 * wgs > f * slots || (n_k < 2l * n_q && 2 * wgs >= slots) || f * each <= 2 * (long)kPartTiles) return 1;
+    if ((tiles + n_seqs) * ((long)n_k / kTileQ + tiles + 2) >= 1l << 31) return 1;                // the kernels' sums of work have 32 bits
+    const long share = std::max((long)kPartTiles, each * wgs / slots);
+    return (int)std::max(1l, std::min((f * each + share / 2) / share, 8l));
 }
 
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t s) {
