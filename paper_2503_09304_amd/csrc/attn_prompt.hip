@@ -1,7 +1,7 @@
 // attn_prompt: attention over packed prompts, causal or not, heads grouped over shared keys.
 //
 // One pass over the keys with the running maximum and sum of the softmax.  A workgroup has 4 waves; a wave owns 32 queries of one
-// head and goes through the keys 64 at a time:
+// head (of as many heads of a key/value head as share a tile, see prompt_log_tile) and goes through the keys 64 at a time:
 //     S^T[key, q] = K Q^T     v_mfma_f32_16x16x32_bf16, A = 16 keys x 32 d, B = 32 d x 16 queries
 //     O^T[d, q]   = V^T P^T   A = 16 d x 32 keys, B = 32 keys x 16 queries
 // Transposed like this a lane holds 8 of 32 keys of each of its two queries, so maxima and sums are formed inside the lane (an exchange between
@@ -19,7 +19,7 @@
 // Kept out: two blocks of 32 queries a wave (LDS read half as often, but one wave a SIMD: 2300 at the time), rows padded instead of swizzled (2083, bank
 // conflicts), the sums' instructions in assembly into their own registers (2083), rescaling the sums half a tile later (2088).
 //
-// Measured (us, TFLOP/s): 16384 tokens, 32 heads of 128 on 8, 1983, 1109; 4096 144, 952; 3584 in 8 prompts 57; 16 heads of 64 608, 904; 17 tokens 6.9.
+// Measured (us, TFLOP/s): 16384 tokens, 32 heads of 128 on 8, 1983, 1109; 4096 144, 952; 3584 in 8 prompts 51; 16 heads of 64 608, 904; 17 tokens 6.7.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -89,14 +89,15 @@ __device__ __forceinline__ int2 span(const int32_t *cu, int b, int n) {
     return {lo, min(max(cu[b + 1], lo), n)};
 }
 
-constexpr int kTileQ = kWaves * 32;                // queries of a workgroup
+constexpr int kTileRows = kWaves * 32;             // rows of a workgroup: a tile of queries (1 << a.log_tile of them) for each of the heads that it has
 
 // The keys of a tile of queries are cut into parts where they are many and the queries few: as many as have about a share each, one at least and
 // a.parts at most.  A share is what a workgroup has if the chip is full and all have the same, kPartTiles tiles of keys at least: joining costs 5 us and 8 bytes an
-// element.  Us with 24, 16, 12 and 8 tiles at least: 16 queries on 2016 keys, 32 heads, 41, 29, 24, 21 (uncut 41); 64 on 8064 47, 36, 36, 36 (79); 512 on 4096 69, 56, 56, 56 (72); 2434
-// of six sequences on 16 649 keys, 16 heads of 64, 69, 62, 63, 63 (103).
-constexpr uint32_t kPartTiles = 8;
-// Lengths here are in steps of kTileQ keys; w: the work of a tile of queries.
+// element.  Us with 8, 6 and 4 tiles at least, 32 heads on 8: 16 queries on 2016 keys 22.9, 22.9, 19.8 (uncut 41); 128 on 1128 28.4, 26.2, 26.3 (29); 200 on 1200 31, 29, 32 (30); four
+// times 16 on 500 to 8000 31, 31, 32 (59); 64 on 8064 35 each (79); 512 on 4096 57 each (72); six times 50 to 300 on 100 to 3000, 16 heads of 64, 32, 35, 35 (47).
+constexpr uint32_t kPartTiles = 4;
+// Lengths here are in steps of as many keys as a tile has queries; w: the work of a tile.
+__host__ __device__ inline int head_groups(const PromptArgs &a) { return a.Hq * (1 << a.log_tile) / kTileRows; }          // workgroups of a tile
 struct Cut {
     uint32_t share, most;
     __device__ __forceinline__ uint32_t parts(uint32_t w) const { return most == 1 ? 1u : min(max((w + share / 2) / share, 1u), most); }
@@ -108,7 +109,7 @@ struct Cut {
     }
 };
 __device__ __forceinline__ int2 tiles_of(const PromptArgs &a, const Span &s) {
-    return {(s.nq + kTileQ - 1) / kTileQ, max(0, a.causal ? s.nk - s.nq : s.nk) / kTileQ};
+    return {(s.nq + (1 << a.log_tile) - 1) >> a.log_tile, max(0, a.causal ? s.nk - s.nq : s.nk) >> a.log_tile};
 }
 __device__ __forceinline__ Span span_of(const PromptArgs &a, int b) {
     const int2 q = span(a.cu_q, b, a.n_q), k = span(a.cu_k, b, a.n_k);
@@ -122,7 +123,7 @@ __device__ __forceinline__ Cut cut_of(const PromptArgs &a) {
         work += t.x * (t.y + (t.x + 1) / 2);
     }
     work = last_lane(wave_scan(work));
-    return {max(kPartTiles * kKeys / kTileQ, (uint32_t)min((unsigned long long)work * a.Hq / a.slots + 1, 1ull << 26)), (uint32_t)a.parts};
+    return {max(kPartTiles * kKeys >> a.log_tile, (uint32_t)min((unsigned long long)work * head_groups(a) / a.slots + 1, 1ull << 26)), (uint32_t)a.parts};
 }
 // The tile of queries and the part of its keys with this number; the tiles of keys that the tile's last query sees.
 __device__ __forceinline__ Tile tile_of(const PromptArgs &a, const Cut &cut, uint32_t number, bool whole) {
@@ -137,7 +138,7 @@ __device__ __forceinline__ int key_tiles(const PromptArgs &a, const Span &s, int
 
 template <int DP>
 __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a, int item0) {
-    constexpr int QT = kTileQ;
+    const int QT = 1 << a.log_tile, wg_heads = kTileRows >> a.log_tile;
     constexpr int CH = DP / 8;                    // 16-byte pieces of a row
     constexpr int KS = DP / 32;                   // MFMA steps of a score
     constexpr int DT = DP / 16;                   // 16-d tiles of the output
@@ -149,14 +150,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
     const int g = lane >> 4, col = lane & 15;
     // Neighbouring workgroups run on different XCDs: those of one key/value head are Hk apart, so with 8 such heads
     // each XCD's L2 holds the keys of one.  Tiles that see the most keys start first.
-    const int G = a.Hq / a.Hk, num = blockIdx.x + item0;
-    const int hk = num % a.Hk, rest = num / a.Hk, head = hk * G + rest % G;
+    const int G = a.Hq / a.Hk, groups = G / wg_heads, num = blockIdx.x + item0;
+    const int hk = num % a.Hk, rest = num / a.Hk, head = hk * G + rest % groups * wg_heads + wave % wg_heads;
     const Cut cut = cut_of(a);
-    const Tile at = tile_of(a, cut, (uint32_t)(rest / G), false);
+    const Tile at = tile_of(a, cut, (uint32_t)(rest / groups), false);
     if (at.piece < 0) return;
     const int nq = at.span.nq, r0 = at.piece * QT;                       // first query of the tile, within the sequence
     const long q_row = at.span.q0;
-    const int w0 = r0 + wave * 32;                // first query of the wave
+    const int w0 = r0 + wave / wg_heads * 32;                // first query of the wave
     // Keys of the part: a query r sees those before shift + r + 1.
     const int all_tiles = key_tiles(a, at.span, r0 + QT), parts = (int)cut.parts(at.work), part = at.part;
     const int first_key = (int)((long)all_tiles * part / parts) * kKeys, end_key = (int)((long)all_tiles * (part + 1) / parts) * kKeys;
@@ -413,11 +414,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
 // The parts of 32 queries of one head joined, in their order.
 constexpr int kJoinQ = 32;
 __global__ __launch_bounds__(256) void join_parts(const PromptArgs a, int item0) {
-    const int num = blockIdx.x + item0, head = num % a.Hq, rest = num / a.Hq;
+    const int num = blockIdx.x + item0, head = num % a.Hq, rest = num / a.Hq, joins = (1 << a.log_tile) / kJoinQ;
     const Cut cut = cut_of(a);
-    const Tile at = tile_of(a, cut, (uint32_t)(rest / (kTileQ / kJoinQ)), true);
+    const Tile at = tile_of(a, cut, (uint32_t)(rest / joins), true);
     if (at.piece < 0) return;
-    const int r0 = at.piece * kTileQ + rest % (kTileQ / kJoinQ) * kJoinQ, parts = (int)cut.parts(at.work);
+    const int r0 = (at.piece << a.log_tile) + rest % joins * kJoinQ, parts = (int)cut.parts(at.work);
     if (parts == 1) return;
     const int rows = min(kJoinQ, at.span.nq - r0), c = a.D / 4;
     const long stride = (long)a.n_q * a.Hq;
@@ -458,12 +459,12 @@ __global__ __launch_bounds__(256) void join_parts(const PromptArgs a, int item0)
 
 template <int DP>
 void prompt_n(const PromptArgs &a, hipStream_t s) {
-    const long tiles = (a.n_q + (long)kTileQ - 1) / kTileQ + a.n_seqs, most = 1 << 23;
-    // With parts(w) <= 1 + w / share and a share of all work * Hq / slots or more, cutting adds slots / Hq parts a head at most.
-    const long all = (a.parts == 1 ? tiles : std::min(tiles * a.parts, tiles + a.slots / a.Hq + 1)) * a.Hq;
+    const long tiles = ((a.n_q + (1l << a.log_tile) - 1) >> a.log_tile) + a.n_seqs, groups = head_groups(a), most = 1 << 23;
+    // With parts(w) <= 1 + w / share and a share of all work * groups / slots or more, cutting adds slots / groups parts at most.
+    const long all = (a.parts == 1 ? tiles : std::min(tiles * a.parts, tiles + a.slots / groups + 1)) * groups;
     // a launch of 2^32 threads or more would lose the excess
     for (long at = 0; at < all; at += most) prompt_tile<DP><<<dim3((unsigned)std::min(all - at, most)), dim3(kWaves * 64), 0, s>>>(a, (int)at);
-    const long joins = a.parts > 1 ? tiles * a.Hq * (kTileQ / kJoinQ) : 0;
+    const long joins = a.parts > 1 ? tiles * a.Hq * ((1 << a.log_tile) / kJoinQ) : 0;
     for (long at = 0; at < joins; at += most) join_parts<<<dim3((unsigned)std::min(joins - at, most)), dim3(256), 0, s>>>(a, (int)at);
 }
 
@@ -471,18 +472,29 @@ void prompt_n(const PromptArgs &a, hipStream_t s) {
 
 int prompt_slots(int D) { return D <= 64 ? 768 : 512; }
 
+// Queries of a tile where several heads share a key/value head: 32 of four heads or 64 of two, all waves with the same keys and fewer idle in a sequence's last tile. Us with 32 / 128:
+// 3584 tokens in 8 prompts 50 / 54, 16 times 8 queries on 1500 keys 35 / 43, five chunks of 1 to 500 on 30 226 keys 56 / 61; 16384 tokens 2016 / 2018.
+static int most_heads(int Hq, int Hk) { return Hq / Hk % 4 == 0 ? 4 : Hq / Hk % 2 == 0 ? 2 : 1; }
+static long tiles_about(int n_seqs, int n_q, int queries) { return std::max((n_q + (long)queries - 1) / queries + (n_seqs - 1) / 2, (long)n_seqs); }
+// Where every workgroup of 128 queries has a CU of its own, idle waves cost nothing, and fewer busy ones are faster: 17 tokens 6.6 / 7.2, 2 times 300 13.3 / 14.2.
+int prompt_log_tile(int n_seqs, int n_q, int Hq, int Hk, int parts) {
+    if (parts == 1 && tiles_about(n_seqs, n_q, kTileRows) * Hq <= 256) return 7;
+    return most_heads(Hq, Hk) == 4 ? 5 : most_heads(Hq, Hk) == 2 ? 6 : 7;
+}
+
 // Most parts for a call; which tiles are cut into how many the kernels decide.  The host knows the totals only, and rules out where nothing can be gained for the 5 us:
 // where most CUs have work as it is.  A second workgroup on a CU adds half to what it does, so one sequence is cut where it fills a third of the chip or less (us uncut / cut: 1024
 // queries on 2048 keys, 32 heads 48 / 58, 512 on 4096 72 / 56; 2048 on as many, 8 heads 48 / 36); several may be uneven, their longest twice the average: two thirds
-// (16 times 8 queries on 1500 keys, 32 heads 43 / 48; 1024 of four on 18 124 112 / 112; 2434 of six, 16 heads of 64 72 / 63), whole prompts half.  And short sequences: 16 tiles
-// of keys (1024 on as many, 8 heads) 26 / 29, 18 (128 on 1128, 32 heads) 29 / 27.
-int prompt_parts(int n_seqs, int n_q, int n_k, int Hq, int D) {
-    const long slots = prompt_slots(D), tiles = (n_q + (long)kTileQ - 1) / kTileQ, each = (long)n_k / n_seqs / kKeys;
-    const long wgs = std::max(tiles + (n_seqs - 1) / 2, (long)n_seqs) * Hq, f = n_seqs == 1 ? 1 : 2;
-    if (3 * wgs > f * slots || (n_k < 2l * n_q && 2 * wgs >= slots) || f * each <= 2 * (long)kPartTiles) return 1;
-    if ((tiles + n_seqs) * ((long)n_k / kTileQ + tiles + 2) >= 1l << 31) return 1;                // the kernels' sums of work have 32 bits
+// (700 and 900 queries on 3700 and 2900 keys, 32 heads 95 / 102; 2434 of six on 16 649, 16 heads of 64 72 / 63), whole prompts half.  And short sequences: 16 tiles
+// of keys (1024 on as many, 8 heads) 26 / 29, 18 (128 on 1128, 32 heads) 29 / 26.  16 parts at most (with 8: four times 16 on 500 to 8000 keys 36 us instead of 31; 32: the same).
+int prompt_parts(int n_seqs, int n_q, int n_k, int Hq, int Hk, int D) {
+    const int heads = most_heads(Hq, Hk), queries = kTileRows / heads;
+    const long slots = prompt_slots(D), tiles = (n_q + (long)queries - 1) / queries, each = (long)n_k / n_seqs / kKeys;
+    const long wgs = tiles_about(n_seqs, n_q, queries) * Hq / heads, f = n_seqs == 1 ? 1 : 2;
+    if (3 * wgs > f * slots || (n_k < 2l * n_q && 2 * wgs >= slots) || f * each <= 16) return 1;
+    if ((tiles + n_seqs) * ((long)n_k / queries + tiles + 2) >= 1l << 31) return 1;                // the kernels' sums of work have 32 bits
     const long share = std::max((long)kPartTiles, each * wgs / slots);
-    return (int)std::max(1l, std::min((f * each + share / 2) / share, 8l));
+    return (int)std::max(1l, std::min((f * each + share / 2) / share, 16l));
 }
 
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t s) {

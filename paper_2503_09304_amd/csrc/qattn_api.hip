@@ -146,7 +146,7 @@ int32_t attn_read(const attn_cache *cache, const attn_place *place, int32_t n_to
 size_t attn_prompt_workspace_bytes(int32_t n_seqs, int32_t n_q, int32_t n_k, int32_t heads_q, int32_t heads_kv, int32_t dim) {
     const char *call = "attn_prompt_workspace_bytes";
     if (check_heads(heads_q, heads_kv, call) || check_dim(dim, call) || n_seqs < 1 || n_q < 1 || n_k < 1) return 0;
-    const int parts = qattn::prompt_parts(n_seqs, n_q, n_k, heads_q, dim);
+    const int parts = qattn::prompt_parts(n_seqs, n_q, n_k, heads_q, heads_kv, dim);
     return parts > 1 ? (size_t)parts * n_q * heads_q * (dim + 2) * 4 : 0;
 }
 
@@ -165,10 +165,10 @@ int32_t attn_prompt(const attn_rows *q, const attn_rows *k, const attn_rows *v, 
     if (n_k > 0 && (k->token_stride > 1 << 24 || v->token_stride > 1 << 24)) return set_error(MOE_E_ARG, "%s: token strides of k and v must be at most 2^24", call);
     if (workspace && !aligned(workspace, 16)) return set_error(MOE_E_WORKSPACE, "%s: workspace is not 16-byte aligned", call);
     const size_t need = workspace ? attn_prompt_workspace_bytes(n_seqs, n_q, n_k, heads_q, heads_kv, dim) : 0;
-    const int parts = need && workspace_bytes >= need ? qattn::prompt_parts(n_seqs, n_q, n_k, heads_q, dim) : 1;
+    const int parts = need && workspace_bytes >= need ? qattn::prompt_parts(n_seqs, n_q, n_k, heads_q, heads_kv, dim) : 1;
     float *part_o = (float *)workspace, *part_ml = parts > 1 ? part_o + (size_t)parts * n_q * heads_q * dim : nullptr;
     qattn::PromptArgs a{rows(q), n_k ? rows(k) : qattn::Rows{nullptr, 0, 0}, n_k ? rows(v) : qattn::Rows{nullptr, 0, 0}, rows(out), lse,
-                        cu_q, cu_k, n_seqs, n_q, n_k, heads_q, heads_kv, dim, causal != 0, scale * 1.44269504088896340736f, parts, qattn::prompt_slots(dim), part_o, part_ml};
+                        cu_q, cu_k, n_seqs, n_q, n_k, heads_q, heads_kv, dim, causal != 0, scale * 1.44269504088896340736f, qattn::prompt_log_tile(n_seqs, n_q, heads_q, heads_kv, parts), parts, qattn::prompt_slots(dim), part_o, part_ml};
     return hip_result(qattn::launch_prompt(a, (hipStream_t)stream), call);
 }
 

@@ -49,13 +49,15 @@ struct PromptArgs {
     const int32_t *cu_q, *cu_k;
     int n_seqs, n_q, n_k, Hq, Hk, D, causal;
     float scale_log2;             // scale * log2(e)
+    int log_tile;                 // of the queries that a workgroup has of a head
     int parts, slots;             // most parts of a query's keys; workgroups that the chip holds
     float *part_o;                // [part][n_q][Hq][D] sums, with parts > 1
     float *part_ml;               // [part][n_q][Hq][2] what they are relative to, in powers of two, and the sums of the weights
 };
-// Parts for a call: see attn_prompt.hip.
+// Tiles and parts for a call: see attn_prompt.hip.
 int prompt_slots(int D);
-int prompt_parts(int n_seqs, int n_q, int n_k, int Hq, int D);
+int prompt_log_tile(int n_seqs, int n_q, int Hq, int Hk, int parts);
+int prompt_parts(int n_seqs, int n_q, int n_k, int Hq, int Hk, int D);
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t s);
 
 struct DecodeArgs {

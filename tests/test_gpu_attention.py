@@ -166,14 +166,15 @@ def test_prompt_more_sequences_than_lanes(causal):
     run_prompt(nq, nk, 2, 1, 64, causal, seed=17)
 
 
+@pytest.mark.parametrize("Hq,Hk", [(4, 2), (4, 1), (12, 3), (3, 3)])
 @pytest.mark.parametrize("causal", [True, False])
-def test_prompt_parts_among_more_sequences_than_lanes(causal):
+def test_prompt_parts_among_more_sequences_than_lanes(causal, Hq, Hk):
     """100 sequences of which a few are cut, one of them with tiles of queries that are cut into different numbers of parts."""
     nq = [(13 * i) % 19 for i in range(100)]
     nk = [n + (0, 30, -3)[i % 3] if n > 3 else n for i, n in enumerate(nq)]
     nq[3], nk[3], nq[70], nk[70], nq[71], nk[71], nq[99], nk[99] = 1, 40000, 700, 2100, 9, 30000, 130, 21000
-    assert q.attention._lib().attn_prompt_workspace_bytes(100, sum(nq), sum(nk), 4, 2, 64) > 0
-    run_prompt(nq, nk, 4, 2, 64, causal, seed=21)
+    assert q.attention._lib().attn_prompt_workspace_bytes(100, sum(nq), sum(nk), Hq, Hk, 64) > 0
+    run_prompt(nq, nk, Hq, Hk, 64, causal, seed=21)
 
 
 def test_prompt_neighbours_do_not_leak():
