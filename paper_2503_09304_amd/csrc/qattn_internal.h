@@ -76,7 +76,8 @@ struct DecodeArgs {
 __host__ __device__ inline int group_tiles(int Hq, int Hk) { return (Hq / Hk + 15) / 16; }
 // Workgroups that a decode launch cuts the keys into, before the pieces of each sequence are rounded up: see attn_decode.hip.
 constexpr int kFewestWgs = 256, kMostWgs = 1536;
-// Most pieces of all sequences, per (key/value head, group tile).
+// Most pieces of all sequences, per (key/value head, group tile): workgroups, and places in the workspace.  Ranges are 512 / heads workgroups, rounded up, with two
+// places each.
 inline int decode_pieces(int n_seqs, int Hq, int Hk) {
     const int heads = Hk * group_tiles(Hq, Hk);
     return n_seqs + (kMostWgs + heads - 1) / heads;

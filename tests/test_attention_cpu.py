@@ -225,7 +225,7 @@ def test_registers_and_lds_of_the_attention_kernels(tmp_path):
             regs, lds = get(r"\bVGPRs") + get(r"\bAGPRs"), get(r"LDS Size \[bytes/block\]")
             assert get(r"ScratchSize \[bytes/lane\]") == 0, part.split()[0]
             seen[part.split()[0]] = min(512 // (-(-regs // 8) * 8), 160 * 1024 // max(lds, 1))
-    for name, least in (("prompt_tileILi128E", 2), ("prompt_tileILi64E", 3), ("decode_pieceILi128ELb0E", 3), ("decode_pieceILi128ELb1E", 4), ("decode_pieceILi64E", 4)):
+    for name, least in (("prompt_tileILi128E", 2), ("prompt_tileILi64E", 3), ("decode_pieceILi128E", 3), ("decode_pieceILi64E", 4)):
         found = [n for k, n in seen.items() if name in k]
         assert found and min(found) >= least, (name, seen)
 

@@ -467,6 +467,22 @@ def test_decode_pieces(lens, fp8):
     run_decode(lens, 8, 2, 128, 64, fp8, seed=len(lens))
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_decode_ranges(D, fp8):
+    """Keys enough, in sequences uneven enough, that workgroups have ranges of them: short and empty sequences within a range, at its ends, and long ones over many."""
+    lens = [0, 9000, 1, 0, 4096, 12000, 130, 7000, 0, 300, 15000, 5, 0, 2500, 128, 129, 600, 0]
+    c, qq, pages, ln, out, ws = run_decode(lens, 16, 8, D, 64, fp8, seed=22)
+    again = torch.full_like(out, NAN)
+    q.attn_decode(c, qq, pages, ln, again, ws)
+    assert torch.equal(again.view(torch.int16), out.view(torch.int16))
+
+
+def test_decode_ranges_of_many_sequences():
+    run_decode([(613 * i) % 997 for i in range(150)], 8, 8, 64, 16, False, seed=23)
+    run_decode([(613 * i) % 997 if i % 7 else 0 for i in range(150)], 34, 2, 64, 16, True, seed=24)
+
+
 def test_decode_many_sequences():
     run_decode([(37 * i) % 97 for i in range(200)], 4, 2, 64, 16, False, seed=1, width=9)
 
