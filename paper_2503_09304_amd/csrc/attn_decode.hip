@@ -40,8 +40,8 @@ constexpr int kBlock = 32;                       // keys of a wave's step
 // Steps of a sequence that is not cut: joining its pieces would take longer.  Us uncut / in pieces of two steps at least, 8 key/value heads of 128: 257 keys
 // 7.1 / 9.2, 512 9.3 / 9.3, 700 11.3 / 9.5, 1000 14.5 / 9.9; 32 sequences of 512 keys, 4 heads, 11.9 / 12.1; of 600 13.4 / 14.0; of 1 to 1000 17.1 / 11.0.
 constexpr uint32_t kWholeSteps = 4;
-// Ranges: workgroups of a launch, two on a CU (384 90 us, 448 84, 512 79, 640 and 768 81 for 64 sequences of 33 to 16384 keys, fp8), and the fewest steps of one (3, 4, 6: the same).
-// A sequence counts as a step more than it has, for its start and end (two more: within 2 %).
+// Ranges: workgroups of a launch, two on a CU (384 90 us, 448 84, 512 79, 768 80 for 64 sequences of 33 to 16384 keys, fp8), and the fewest steps of one (3, 4, 6: the same).
+// A sequence counts as a step more than it has, for its start and end (as two: 0 to 12 % slower).
 constexpr uint32_t kRangeWgs = 512, kFewestRange = 6;
 
 __device__ __forceinline__ f32x4 mma(const u32x4 &a, const u32x4 &b, const f32x4 &c) {
