@@ -478,6 +478,28 @@ def test_decode_ranges(D, fp8):
     assert torch.equal(again.view(torch.int16), out.view(torch.int16))
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+def test_decode_ranges_with_lens_and_pages_out_of_range(fp8):
+    """A length below 0 and pages that are none among sequences that are cut: counted once each."""
+    lens, P = [40, 9000, 4096, 12000, 3, 7000, 15000, 2500], 64
+    c, qq, pages, ln, out, ws = run_decode(lens, 16, 8, 64, P, fp8, seed=25)
+    hole, wild, bad = pages.clone(), ln.clone(), torch.zeros(1, dtype=torch.int32, device=DEV)
+    hole[2, 3], hole[2, 40], wild[4] = -1, c.n_pages, -7
+    got, lse = torch.full_like(out, NAN), torch.zeros(8, 16, dtype=torch.float32, device=DEV)
+    q.attn_decode(c, qq, hole, wild, got, ws, lse=lse, bad=bad)
+    assert int(bad) == 3 and (got[4] == 0).all() and torch.isinf(lse[4]).all()
+    pos = torch.arange(4096, dtype=torch.int32, device=DEV)
+    k, v = (torch.empty(4096, 8, 64, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    q.attn_read(c, torch.full_like(pos, 2), pos, pages, k, v)
+    seen = [i for i in range(4096) if i // P not in (3, 40)]
+    for hk in range(8):
+        x = qq[2, 2 * hk:2 * hk + 2].double()
+        ref = reference(x, k[seen, hk].double(), v[seen, hk].double(), torch.full((2,), len(seen), device=DEV), 64 ** -0.5)
+        check(got[2, 2 * hk:2 * hk + 2], lse[2, 2 * hk:2 * hk + 2], ref, 64, hk)
+    q.attn_decode(c, qq, pages, ln, got, ws, bad=bad)
+    assert int(bad) == 3 and torch.equal(got.view(torch.int16), out.view(torch.int16))
+
+
 def test_decode_ranges_of_many_sequences():
     run_decode([(613 * i) % 997 for i in range(150)], 8, 8, 64, 16, False, seed=23)
     run_decode([(613 * i) % 997 if i % 7 else 0 for i in range(150)], 34, 2, 64, 16, True, seed=24)
@@ -587,3 +609,33 @@ def test_calls_in_a_graph():
         step(two)
         torch.cuda.synchronize()
         assert torch.equal(one[2].view(torch.int16), two[2].view(torch.int16)), i
+
+
+def test_parts_and_ranges_in_a_graph():
+    """What cuts keys up looks at the lengths of the replay, not at those of the recording."""
+    g = gen(31)
+    x, k, v = rows(g, 40, 8, 64), rows(g, 9000, 2, 64), rows(g, 9000, 2, 64)
+    cq, ck = (torch.tensor(n, dtype=torch.int32, device=DEV) for n in ([0, 30, 40], [0, 8000, 9000]))
+    assert q.attention._lib().attn_prompt_workspace_bytes(2, 40, 9000, 8, 2, 64) > 0
+    c, qq, pages, ln, first, ws = run_decode([9000, 40, 12000, 4096, 3, 7000, 15000, 2500], 16, 8, 64, 64, seed=26)
+    out, dec = torch.zeros_like(x), torch.zeros_like(first)
+
+    def step(out, dec):
+        q.attn_prompt(x, k, v, cq, ck, out)
+        q.attn_decode(c, qq, pages, ln, dec, ws)
+
+    step(out, dec)                                                                # warm
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(out, dec)
+    for q1, k1, cut in [(30, 8000, 1), (1, 20, 1), (39, 9000, 30), (20, 4500, 2), (30, 8000, 1)]:
+        cq[1], ck[1] = q1, k1
+        ln.copy_(torch.tensor([9000, 40, 12000, 4096, 3, 7000, 15000, 2500], device=DEV) // cut)
+        graph.replay()
+        again, dagain = torch.zeros_like(out), torch.zeros_like(dec)
+        step(again, dagain)
+        torch.cuda.synchronize()
+        assert torch.equal(out.view(torch.int16), again.view(torch.int16)), (q1, k1)
+        assert torch.equal(dec.view(torch.int16), dagain.view(torch.int16)), cut
+    assert torch.equal(dec.view(torch.int16), first.view(torch.int16))
