@@ -113,7 +113,7 @@ int32_t attn_read(const attn_cache *cache, const attn_place *place, int32_t n_to
  * A query that sees no key gives zeros.  lse ([device] float [n_q, heads_q], may be NULL): ln of the sum of the exponentials,
  * -inf for a query without keys.  Rows of out that belong to no sequence are left untouched.  Entries of cu out of 0..n_q (n_k) or
  * descending are clamped to the range and to the entry before them.  scale > 0 and finite.  out overlaps no input.  Token strides of k and v: at
- * most 2^24.
+ * most 2^24; n_seqs: at most 2^20.
  * workspace ([device], 16-byte aligned, may be NULL; its contents before and after the call are of no account): where queries are so few that
  * they leave CUs idle, the keys of a query are cut into parts that run side by side, and a second launch joins them.
  * attn_prompt_workspace_bytes(...) is what that takes, 0 where nothing is cut; with less than that nothing is cut either. */
@@ -125,7 +125,7 @@ int32_t attn_prompt(const attn_rows *q, const attn_rows *k, const attn_rows *v, 
 /* Attention of one query a sequence over the cache: query b sees the first lens[b] tokens of sequence b (lens [device] int32
  * [n_seqs]), whose pages are pages[b * seq_pages ..].  The formula, lse ([device] float [n_seqs, heads_q], may be NULL) and the answer
  * without keys are those of attn_prompt.  lens out of 0 .. seq_pages * page_tokens are clamped, pages out of 0 .. n_pages - 1 hold no
- * keys; *bad counts each of both once.
+ * keys; *bad counts each of both once.  n_seqs at most 65535, seq_pages * page_tokens below 2^30, n_seqs times that below 2^38.
  * Long sequences are cut into pieces that run side by side; the last piece of a sequence to finish joins them, in the order of the
  * pieces, so results do not depend on timing.  workspace [device], 256-byte aligned, attn_decode_workspace_bytes(...) long: its first
  * attn_decode_counter_bytes(...) bytes have to be zero at the first call; every call leaves them zero.  Calls that share a workspace

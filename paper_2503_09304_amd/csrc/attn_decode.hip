@@ -140,7 +140,7 @@ __global__ __launch_bounds__(kWaves * 64, 3) void decode_piece(const DecodeArgs 
         if (last_lane(wave_scan(n)) * heads <= wgs) break;
         if constexpr (RANGES) {
             const uint32_t all = total + (uint32_t)a.n_seqs, r = (uint32_t)(((unsigned long long)all * heads + kRangeWgs - 1) / kRangeWgs);
-            if (wgs == kRangeWgs && r >= kFewestRange && total < 1u << 30) {
+            if (wgs == kRangeWgs && r >= kFewestRange && total < 1u << 28) {
                 if ((uint32_t)item > (all - 1) / r) return;
                 range = r;
                 break;

@@ -145,7 +145,7 @@ int32_t attn_read(const attn_cache *cache, const attn_place *place, int32_t n_to
 
 size_t attn_prompt_workspace_bytes(int32_t n_seqs, int32_t n_q, int32_t n_k, int32_t heads_q, int32_t heads_kv, int32_t dim) {
     const char *call = "attn_prompt_workspace_bytes";
-    if (check_heads(heads_q, heads_kv, call) || check_dim(dim, call) || n_seqs < 1 || n_q < 1 || n_k < 1) return 0;
+    if (check_heads(heads_q, heads_kv, call) || check_dim(dim, call) || n_seqs < 1 || n_seqs > 1 << 20 || n_q < 1 || n_k < 1) return 0;
     const int parts = qattn::prompt_parts(n_seqs, n_q, n_k, heads_q, heads_kv, dim);
     return parts > 1 ? (size_t)parts * n_q * heads_q * (dim + 2) * 4 : 0;
 }
@@ -157,6 +157,7 @@ int32_t attn_prompt(const attn_rows *q, const attn_rows *k, const attn_rows *v, 
     int32_t rc;
     if ((rc = check_heads(heads_q, heads_kv, call)) || (rc = check_dim(dim, call))) return rc;
     if (n_seqs < 0 || n_q < 0 || n_k < 0) return set_error(MOE_E_ARG, "%s: negative size", call);
+    if (n_seqs > 1 << 20) return set_error(MOE_E_ARG, "%s: n_seqs must be at most 2^20", call);
     if (!(scale > 0.f) || !std::isfinite(scale)) return set_error(MOE_E_ARG, "%s: scale must be positive and finite", call);
     if (n_seqs == 0 || n_q == 0) return MOE_OK;
     if (!cu_q || !cu_k) return set_error(MOE_E_ARG, "%s: cu_q or cu_k is null", call);
@@ -197,6 +198,7 @@ int32_t attn_decode(const attn_cache *cache, const attn_rows *q, const attn_rows
     if ((rc = check_cache(cache, call)) || (rc = check_heads(heads_q, cache->heads_kv, call))) return rc;
     if (n_seqs < 0 || n_seqs > 65535) return set_error(MOE_E_ARG, "%s: n_seqs must be 0..65535", call);
     if (seq_pages < 1 || (int64_t)seq_pages * cache->page_tokens >= (int64_t)1 << 30) return set_error(MOE_E_ARG, "%s: seq_pages must be positive, and seq_pages * page_tokens below 2^30", call);
+    if ((int64_t)n_seqs * seq_pages * cache->page_tokens >= (int64_t)1 << 38) return set_error(MOE_E_ARG, "%s: n_seqs * seq_pages * page_tokens must be below 2^38", call);
     if (!(scale > 0.f) || !std::isfinite(scale)) return set_error(MOE_E_ARG, "%s: scale must be positive and finite", call);
     if (n_seqs == 0) return MOE_OK;
     if (!pages || !lens) return set_error(MOE_E_ARG, "%s: pages or lens is null", call);

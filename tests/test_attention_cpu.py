@@ -134,14 +134,14 @@ def test_prompt_and_decode_refusals():
         return L.attn_decode(c, ok, ok, None, n, Hq, pages, sp, lens, scale, ws, nb, None, None)
 
     for kw, word in [(dict(Hq=6), "heads"), (dict(Hk=0), "heads"), (dict(Hq=2048, Hk=1024), "heads"), (dict(D=120), "dim"), (dict(n_seqs=-1), "negative"),
-                     (dict(n_q=-1), "negative"), (dict(n_k=-1), "negative"), (dict(scale=0.0), "scale"), (dict(scale=-1.0), "scale"),
+                     (dict(n_q=-1), "negative"), (dict(n_k=-1), "negative"), (dict(n_seqs=(1 << 20) + 1), "2^20"), (dict(scale=0.0), "scale"), (dict(scale=-1.0), "scale"),
                      (dict(scale=math.nan), "scale"), (dict(scale=math.inf), "scale"), (dict(cu=0), "cu_q")]:
         refused(prompt(**kw), word)
     refused(L.attn_prompt(ok, rows(ts=(1 << 24) + 8), ok, ok, None, FAKE, FAKE, 1, 4, 4, 4, 4, 128, 1.0, 1, None, 0, None), "2^24")
     refused(prompt(ws=FAKE + 8), "workspace", q.MOE_E_WORKSPACE)
     assert prompt(n_seqs=0) == q.MOE_OK and prompt(n_q=0) == q.MOE_OK
     for kw, word in [(dict(n=-1), "n_seqs"), (dict(n=65536), "n_seqs"), (dict(Hq=6), "heads"), (dict(pages=0), "pages"), (dict(lens=0), "lens"),
-                     (dict(sp=0), "seq_pages"), (dict(sp=1 << 24), "seq_pages"), (dict(scale=math.nan), "scale")]:
+                     (dict(sp=0), "seq_pages"), (dict(sp=1 << 24), "seq_pages"), (dict(n=65535, sp=1 << 18), "2^38"), (dict(scale=math.nan), "scale")]:
         refused(decode(**kw), word)
     need = L.attn_decode_workspace_bytes(2, 8, 4, 128)
     for kw in (dict(ws=0), dict(ws=FAKE + 64), dict(nb=need - 1)):
