@@ -127,9 +127,10 @@ int32_t attn_prompt(const attn_rows *q, const attn_rows *k, const attn_rows *v, 
  * without keys are those of attn_prompt.  lens out of 0 .. seq_pages * page_tokens are clamped, pages out of 0 .. n_pages - 1 hold no
  * keys; *bad counts each of both once.  n_seqs at most 65535, seq_pages * page_tokens below 2^30, n_seqs times that below 2^38.
  * Long sequences are cut into pieces that run side by side; the last piece of a sequence to finish joins them, in the order of the
- * pieces, so results do not depend on timing.  workspace [device], 256-byte aligned, attn_decode_workspace_bytes(...) long: its first
- * attn_decode_counter_bytes(...) bytes have to be zero at the first call; every call leaves them zero.  Calls that share a workspace
- * are ordered by the caller (one stream, for instance). */
+ * pieces, so results do not depend on timing.  workspace [device], 256-byte aligned, attn_decode_workspace_bytes(...) long or longer: its first
+ * attn_decode_counter_bytes(...) bytes have to be zero at the first call; every call leaves them zero.  Calls of different numbers of
+ * sequences, heads and dim may share a workspace that is large enough for each of them, zeroed for the one with the most counter bytes, if all of them
+ * state the same workspace_bytes (the place of the sums follows from it).  They are ordered by the caller (one stream, for instance). */
 size_t attn_decode_workspace_bytes(int32_t n_seqs, int32_t heads_q, int32_t heads_kv, int32_t dim);
 size_t attn_decode_counter_bytes(int32_t n_seqs, int32_t heads_q, int32_t heads_kv);
 int32_t attn_decode(const attn_cache *cache, const attn_rows *q, const attn_rows *out, float *lse, int32_t n_seqs, int32_t heads_q,

@@ -207,7 +207,7 @@ def attn_prompt(q, k, v, cu_q, cu_k, out, scale: Optional[float] = None, causal:
 
 
 def attn_decode_workspace(cache: AttnCache, n_seqs: int, heads_q: int):
-    """Workspace for attn_decode calls of up to n_seqs sequences, its counters zeroed; for one stream at a time."""
+    """Workspace for attn_decode calls of up to n_seqs sequences, its counters zeroed; for one stream at a time, and passed whole by each call."""
     n = int(_lib().attn_decode_workspace_bytes(n_seqs, heads_q, cache.heads_kv, cache.dim))
     if n == 0:
         raise MoeError(MOE_E_ARG, _lib().moe_last_error().decode())

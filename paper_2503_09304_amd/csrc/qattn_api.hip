@@ -174,6 +174,13 @@ int32_t attn_prompt(const attn_rows *q, const attn_rows *k, const attn_rows *v, 
 }
 
 static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+// A decode workspace: the arrival counters, then the pieces' sums.  Where the sums begin follows from the workspace's size alone, a 256th of it behind its start: by a
+// call's own counters they would begin where another call, of more sequences or heads, has its own, which every call must find zero.  A 256th is more than any
+// call's counters: a head of a sequence has 4 bytes of them and 16 * 18 * 4 bytes of sums at least.
+static size_t counter_room(size_t workspace_bytes) { return up256(workspace_bytes / 256); }
+static size_t sums_bytes(int n_seqs, int Hq, int Hk, int dim) {
+    return up256((size_t)qattn::decode_pieces(n_seqs, Hq, Hk) * Hk * qattn::group_tiles(Hq, Hk) * 16 * (dim + 2) * 4);
+}
 static bool decode_shape_ok(int n_seqs, int Hq, int Hk) { return n_seqs >= 0 && n_seqs <= 65535 && Hk >= 1 && Hk <= 1024 && Hq >= Hk && Hq <= 1024 && Hq % Hk == 0; }
 
 size_t attn_decode_counter_bytes(int32_t n_seqs, int32_t heads_q, int32_t heads_kv) {
@@ -185,9 +192,9 @@ size_t attn_decode_counter_bytes(int32_t n_seqs, int32_t heads_q, int32_t heads_
 }
 
 size_t attn_decode_workspace_bytes(int32_t n_seqs, int32_t heads_q, int32_t heads_kv, int32_t dim) {
-    const size_t counters = attn_decode_counter_bytes(n_seqs, heads_q, heads_kv);
-    if (!counters || check_dim(dim, "attn_decode_workspace_bytes")) return 0;
-    return counters + up256((size_t)qattn::decode_pieces(n_seqs, heads_q, heads_kv) * heads_kv * qattn::group_tiles(heads_q, heads_kv) * 16 * (dim + 2) * 4);
+    if (!attn_decode_counter_bytes(n_seqs, heads_q, heads_kv) || check_dim(dim, "attn_decode_workspace_bytes")) return 0;
+    const size_t sums = sums_bytes(n_seqs, heads_q, heads_kv, dim);
+    return sums + up256((sums + 254) / 255);      // the least n with n - counter_room(n) >= sums
 }
 
 int32_t attn_decode(const attn_cache *cache, const attn_rows *q, const attn_rows *out, float *lse, int32_t n_seqs, int32_t heads_q,
@@ -210,7 +217,7 @@ int32_t attn_decode(const attn_cache *cache, const attn_rows *q, const attn_rows
     const int64_t most = (int64_t)n_seqs * std::max<int64_t>(1, ((int64_t)seq_pages * cache->page_tokens + 255) / 256);      // a piece has 256 keys at least
     const int pieces = (int)std::min<int64_t>(most, qattn::decode_pieces(n_seqs, heads_q, cache->heads_kv));
     qattn::DecodeArgs a{cache_of(cache), rows(q), rows(out), lse, pages, lens, bad, (int32_t *)w,
-                        (float *)(w + attn_decode_counter_bytes(n_seqs, heads_q, cache->heads_kv)), n_seqs, heads_q, seq_pages,
+                        (float *)(w + counter_room(workspace_bytes)), n_seqs, heads_q, seq_pages,
                         cache->format == ATTN_FP8, pieces, scale * 1.44269504088896340736f};
     return hip_result(qattn::launch_decode(a, (hipStream_t)stream), call);
 }
