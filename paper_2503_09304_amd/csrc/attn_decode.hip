@@ -104,7 +104,7 @@ struct Step {
 
 // WHOLE: dim is DP, so that offsets within a tile are constants.  RANGES: there may be ranges instead of pieces.
 template <int DP, bool FP8, bool WHOLE, bool RANGES>
-__global__ __launch_bounds__(kWaves * 64, 3) void decode_piece(const DecodeArgs a) {
+__global__ __launch_bounds__(kWaves * 64, 3) void decode_piece(const DecodeArgs a, int first_wg) {
     constexpr int KS = DP / 32;                       // MFMA steps of a score
     constexpr int DT = DP / 16;                       // d tiles of the output
     constexpr int ESZ = FP8 ? 1 : 2;
@@ -116,7 +116,8 @@ __global__ __launch_bounds__(kWaves * 64, 3) void decode_piece(const DecodeArgs 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = lane >> 4, col = lane & 15;
     const int GT = group_tiles(a.Hq, a.c.Hk), G = a.Hq / a.c.Hk;
-    const int hk = blockIdx.x % a.c.Hk, gt = (blockIdx.x / a.c.Hk) % GT, item = blockIdx.x / (a.c.Hk * GT);
+    const uint32_t wg = blockIdx.x + first_wg;
+    const int hk = wg % a.c.Hk, gt = (wg / a.c.Hk) % GT, item = wg / (a.c.Hk * GT);
     const int P = 1 << a.c.page_shift, most = a.seq_pages << a.c.page_shift;
     const auto len_of = [&](int b) { return min(max(a.lens[b], 0), most); };
 
@@ -492,14 +493,16 @@ __global__ __launch_bounds__(kWaves * 64, 3) void decode_piece(const DecodeArgs 
 }  // namespace
 
 hipError_t launch_decode(const DecodeArgs &a, hipStream_t s) {
-    const dim3 grid((unsigned)(a.pieces * a.c.Hk * group_tiles(a.Hq, a.c.Hk))), block(kWaves * 64);
     // Whether the lengths that the table of pages has room for are enough for ranges.
     const long steps = (((long)a.seq_pages << a.c.page_shift) + kWaves * kBlock - 1) / (kWaves * kBlock) + 1, heads = (long)a.c.Hk * group_tiles(a.Hq, a.c.Hk);
     const bool ranges = a.n_seqs > 1 && a.n_seqs * steps * heads > kRangeWgs * (kFewestRange - 1);
     const auto run = [&](auto dp, auto fp8) {
-        if (a.c.D == dp && ranges) decode_piece<dp, fp8, true, true><<<grid, block, 0, s>>>(a);
-        else if (a.c.D == dp) decode_piece<dp, fp8, true, false><<<grid, block, 0, s>>>(a);
-        else decode_piece<dp, fp8, false, false><<<grid, block, 0, s>>>(a);
+        in_launches(decode_workgroups(a), [&](int at, unsigned n) {
+            const dim3 grid(n), block(kWaves * 64);
+            if (a.c.D == dp && ranges) decode_piece<dp, fp8, true, true><<<grid, block, 0, s>>>(a, at);
+            else if (a.c.D == dp) decode_piece<dp, fp8, true, false><<<grid, block, 0, s>>>(a, at);
+            else decode_piece<dp, fp8, false, false><<<grid, block, 0, s>>>(a, at);
+        });
     };
     typedef std::integral_constant<int, 64> D64;
     typedef std::integral_constant<int, 128> D128;

@@ -459,13 +459,12 @@ __global__ __launch_bounds__(256) void join_parts(const PromptArgs a, int item0)
 
 template <int DP>
 void prompt_n(const PromptArgs &a, hipStream_t s) {
-    const long tiles = ((a.n_q + (1l << a.log_tile) - 1) >> a.log_tile) + a.n_seqs, groups = head_groups(a), most = 1 << 23;
+    const long tiles = ((a.n_q + (1l << a.log_tile) - 1) >> a.log_tile) + a.n_seqs, groups = head_groups(a);
     // With parts(w) <= 1 + w / share and a share of all work * groups / slots or more, cutting adds slots / groups parts at most.
     const long all = (a.parts == 1 ? tiles : std::min(tiles * a.parts, tiles + a.slots / groups + 1)) * groups;
-    // a launch of 2^32 threads or more would lose the excess
-    for (long at = 0; at < all; at += most) prompt_tile<DP><<<dim3((unsigned)std::min(all - at, most)), dim3(kWaves * 64), 0, s>>>(a, (int)at);
+    in_launches(all, [&](int at, unsigned n) { prompt_tile<DP><<<dim3(n), dim3(kWaves * 64), 0, s>>>(a, at); });
     const long joins = a.parts > 1 ? tiles * a.Hq * ((1 << a.log_tile) / kJoinQ) : 0;
-    for (long at = 0; at < joins; at += most) join_parts<<<dim3((unsigned)std::min(joins - at, most)), dim3(256), 0, s>>>(a, (int)at);
+    in_launches(joins, [&](int at, unsigned n) { join_parts<<<dim3(n), dim3(256), 0, s>>>(a, at); });
 }
 
 }  // namespace

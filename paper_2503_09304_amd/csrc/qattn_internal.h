@@ -10,6 +10,14 @@ namespace qattn {
 
 constexpr int kMaxDim = 128;
 
+// Workgroups that a call's kernels are launched with: launch(first, n) for runs of all of them, in order.  A launch of 2^32 threads or more would lose the
+// excess; 2^23 workgroups of 256 are half that.
+constexpr long kMostLaunched = 1 << 23;
+template <class F>
+inline void in_launches(long all, F &&launch) {
+    for (long at = 0; at < all; at += kMostLaunched) launch((int)at, (unsigned)(all - at < kMostLaunched ? all - at : kMostLaunched));
+}
+
 // Rows of heads as the kernels take them (bf16 elements).
 struct Rows {
     uint16_t *p;
@@ -82,6 +90,7 @@ inline int decode_pieces(int n_seqs, int Hq, int Hk) {
     const int heads = Hk * group_tiles(Hq, Hk);
     return n_seqs + (kMostWgs + heads - 1) / heads;
 }
+inline long decode_workgroups(const DecodeArgs &a) { return (long)a.pieces * a.c.Hk * group_tiles(a.Hq, a.c.Hk); }
 hipError_t launch_decode(const DecodeArgs &a, hipStream_t s);
 
 }  // namespace qattn

@@ -100,7 +100,32 @@ static void test_workspaces_are_long_enough() {
         }
 }
 
+// The workgroups of a call, as it launches them: all of them, in order, no launch of 2^32 threads.
+static void test_launches_of_many_workgroups() {
+    struct Call { int n, Hq, Hk; bool several; };
+    for (const Call &c : {Call{1, 32, 8, false}, Call{64, 32, 8, false}, Call{65535, 64, 64, false}, Call{65535, 256, 256, true}, Call{16400, 1024, 1024, true},
+                          Call{65535, 1024, 1024, true}, Call{65535, 1024, 1, false}}) {
+        decode(c.n, c.Hq, c.Hk, 16, attn_decode_workspace_bytes(c.n, c.Hq, c.Hk, 16));
+        const long all = qattn::decode_workgroups(g_decode.at(0));
+        CHECK(all >= (long)c.n * c.Hk * qattn::group_tiles(c.Hq, c.Hk));
+        long next = 0;
+        int launches = 0;
+        qattn::in_launches(all, [&](int at, unsigned n) {
+            CHECK(at == next && n > 0 && (unsigned long long)n * 256 < 1ull << 32);
+            next += n;
+            ++launches;
+        });
+        CHECK(next == all && (launches > 1) == c.several);
+    }
+    for (long all : {0l, 1l, (1l << 23) - 1, 1l << 23, (1l << 23) + 1, 5l << 23}) {
+        long next = 0;
+        qattn::in_launches(all, [&](int at, unsigned n) { CHECK(at == next); next += n; });
+        CHECK(next == all);
+    }
+}
+
 int main() {
+    test_launches_of_many_workgroups();
     test_workspaces_are_long_enough();
     test_calls_that_share_a_workspace();
     std::printf(g_fail ? "%d checks failed\n" : "all attention host checks passed\n", g_fail);

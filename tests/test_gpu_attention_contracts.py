@@ -1,9 +1,9 @@
-"""What the attention calls promise beside their formulas (-m gpu): workspaces that calls share."""
+"""What the attention calls promise beside their formulas (-m gpu): workspaces that calls share, calls of any size."""
 import pytest
 import torch
 
 import paper_2503_09304_amd as q
-from test_gpu_attention import DEV, NAN, fresh, gen, rows, table
+from test_gpu_attention import DEV, NAN, check, fresh, gen, rows, table
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +45,26 @@ def test_decode_batches_of_any_size_share_a_workspace(fp8, spare):
         c, qq = case[:2]
         want = decode(*case, q.attn_decode_workspace(c, n, qq.shape[1]), n)
         assert not got[0].isnan().any() and not got[1].isnan().any() and same(got, want), n
+
+
+def test_decode_of_more_workgroups_than_a_launch_takes():
+    """16400 sequences of 1024 heads, 0 to 2 tokens long, on one page: 2^24 workgroups and more."""
+    n, H, D = 16400, 1024, 16
+    g = gen(42)
+    k, v = rows(g, 2, H, D), rows(g, 2, H, D)
+    c = fresh(1, H, 16, D, False)
+    pages = torch.zeros((n, 1), dtype=torch.int32, device=DEV)
+    q.attn_append(c, None, k, v, torch.zeros(2, dtype=torch.int32, device=DEV), torch.arange(2, dtype=torch.int32, device=DEV), pages, None, None)
+    lens = (torch.arange(n, device=DEV) % 3).to(torch.int32)
+    qq = torch.randn(n, H, D, generator=g, device=DEV, dtype=torch.bfloat16)
+    out, lse = decode(c, qq, pages, lens, q.attn_decode_workspace(c, n, H), n)
+    one, two = v[0].double(), v[1].double()
+    for at in range(0, n, 1640):
+        x, size = qq[at:at + 1640].double(), lens[at:at + 1640]
+        s = torch.stack([(x * k[j].double()).sum(-1) for j in range(2)], -1) * D ** -0.5
+        big = torch.stack([(x * k[j].double()).abs().sum(-1) for j in range(2)], -1).amax(-1) * D ** -0.5
+        s = s.masked_fill(torch.arange(2, device=DEV) >= size[:, None, None], -torch.inf)
+        rl = torch.logsumexp(s, -1)
+        p = torch.exp(s - torch.where(torch.isinf(rl), torch.zeros_like(rl), rl)[..., None])
+        ref = [p[..., :1] * one + p[..., 1:] * two, rl, p[..., :1] * one.abs() + p[..., 1:] * two.abs(), big]
+        check(out[at:at + 1640].flatten(0, 1), lse[at:at + 1640].flatten(), [r.flatten(0, 1) for r in ref], D, at)
