@@ -19,13 +19,17 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
     v = add_from<0x142, 0xA>(v);      // row_bcast:15 into rows 1 and 3
     return add_from<0x143, 0xC>(v);   // row_bcast:31 into rows 2 and 3
 }
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {       // in the last lane
-    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, false));
-    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, false));
-    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, false));
-    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, false));
-    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xA, 0xF, false));
-    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xC, 0xF, false));
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t max_from(uint32_t v) {
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false));
+}
+__device__ __forceinline__ uint32_t wave_scan_max(uint32_t v) {       // the largest of the lanes up to each lane
+    v = max_from<0x111, 0xF>(v);
+    v = max_from<0x112, 0xF>(v);
+    v = max_from<0x114, 0xF>(v);
+    v = max_from<0x118, 0xF>(v);
+    v = max_from<0x142, 0xA>(v);
+    return max_from<0x143, 0xC>(v);
 }
 __device__ __forceinline__ uint32_t last_lane(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, 63); }
 
@@ -55,6 +59,60 @@ __device__ __forceinline__ Piece find_piece(int n_seqs, uint32_t item, S &&size,
 struct Span {
     int q0, nq, k0, nk;
 };
+// Largest offsets of queries and keys so far.
+struct Reached {
+    uint32_t q = 0, k = 0;
+};
+// The sequences of a call, 64 at a time, one a lane, from their offsets cu[b], cu[b + 1].  Where these descend a sequence begins at the largest before, so
+// sequences share no row whatever the offsets hold; that is looked for once, in front (in every look, 1000 sequences of 9 queries take 508 us instead of 291).
+struct Sequences {
+    const int32_t *cu_q, *cu_k;
+    int n, n_q, n_k;
+    bool ascend;
+    uint32_t top;                     // the largest n + e of a shape {n, e}
+    template <class F>
+    __device__ __forceinline__ Sequences(const int32_t *cu_q_, const int32_t *cu_k_, int n_, int n_q_, int n_k_, F &&shape)
+        : cu_q(cu_q_), cu_k(cu_k_), n(n_), n_q(n_q_), n_k(n_k_), ascend(true) {
+        int sign = 0, most = 0;
+        Reached r;
+        const auto look = [&]() {
+            for (int b0 = 0; b0 < n; b0 += 64) {
+                const Span s = at(b0, r);
+                const int2 f = shape(s);
+                sign |= s.nq | s.nk;
+                most = max(most, f.x + f.y);
+            }
+        };
+        look();
+        ascend = !__any(sign < 0);
+        if (!ascend) {
+            most = 0;
+            look();
+        }
+        top = last_lane(wave_scan_max((uint32_t)most));
+    }
+    // Sequence b0 + lane, entries held to the range only; behind the last no rows.
+    __device__ __forceinline__ Span as_they_are(int b0) const {
+        const int b = b0 + (threadIdx.x & 63);
+        if (b >= n) return {0, 0, 0, 0};
+        const int q0 = min(max(cu_q[b], 0), n_q), q1 = min(max(cu_q[b + 1], 0), n_q), k0 = min(max(cu_k[b], 0), n_k), k1 = min(max(cu_k[b + 1], 0), n_k);
+        return {q0, q1 - q0, k0, k1 - k0};
+    }
+    // The same behind those that have reached so far (for b0 = 0, 64, ... in turn).
+    __device__ __forceinline__ Span at(int b0, Reached &reached) const {
+        Span s = as_they_are(b0);
+        if (ascend) return s;
+        const auto behind = [](int &first, int &count, uint32_t &from) {
+            const uint32_t lo = max(from, wave_scan_max((uint32_t)first)), hi = max(lo, (uint32_t)(first + count));
+            from = last_lane(hi);
+            first = (int)lo;
+            count = (int)(hi - lo);
+        };
+        behind(s.q0, s.nq, reached.q);
+        behind(s.k0, s.nk, reached.k);
+        return s;
+    }
+};
 struct Tile {
     int piece, part;                  // piece -1: there is no such number
     int work;                         // of the piece
@@ -63,30 +121,29 @@ struct Tile {
 
 // The same for pieces that are dealt out heaviest first and come in parts: a sequence has pieces 0 .. n - 1, the work of piece p is e + p, and a piece
 // of work w has parts(w) parts, those of all works below w sum(w) (sum(w + 1) - sum(w) = parts(w) > 0).  Numbers go by falling work, then by sequence, then by
-// part.  span(b): sequence b; shape(span): {n, e}.
-template <class S, class F, class P, class U>
-__device__ __forceinline__ Tile find_heaviest(int n_seqs, uint32_t number, S &&span, F &&shape, P &&parts, U &&sum) {
+// part.  shape(span): {n, e}.
+template <class F, class P, class U>
+__device__ __forceinline__ Tile find_heaviest(const Sequences &seqs, uint32_t number, F &&shape, P &&parts, U &&sum) {
     const int lane = threadIdx.x & 63;
-    const auto at = [&](int b0) { return b0 + lane < n_seqs ? span(b0 + lane) : Span{0, 0, 0, 0}; };
-    const Span first = at(0);                                         // all there is to load where there are 64 sequences or fewer
+    Reached behind_first;
+    const Span first = seqs.at(0, behind_first);                      // all there is to load where there are 64 sequences or fewer
+    const auto others = [&](auto &&f) {
+        Reached r = behind_first;
+        for (int b0 = 64; b0 < seqs.n; b0 += 64) f(seqs.at(b0, r));
+    };
     const int2 mine = shape(first);
     const uint32_t mine_all = sum((uint32_t)(mine.x + mine.y));
     // parts of the pieces with work w or more, of this lane's sequences
     const auto from = [&](int2 s, uint32_t all, int w) { return all - sum((uint32_t)min(max(w, s.y), s.x + s.y)); };
     const auto count = [&](int w) {
         uint32_t n = from(mine, mine_all, w);
-        for (int b0 = 64; b0 < n_seqs; b0 += 64) {
-            const int2 s = shape(at(b0));
+        others([&](const Span &span) {
+            const int2 s = shape(span);
             n += from(s, sum((uint32_t)(s.x + s.y)), w);
-        }
+        });
         return last_lane(wave_scan(n));
     };
-    int top = mine.x + mine.y;
-    for (int b0 = 64; b0 < n_seqs; b0 += 64) {
-        const int2 s = shape(at(b0));
-        top = max(top, s.x + s.y);
-    }
-    uint32_t hi = last_lane(wave_max((uint32_t)top)), lo = 0;         // count(hi) = 0 <= number
+    uint32_t hi = seqs.top, lo = 0;                                   // count(hi) = 0 <= number
     if (count(0) <= number) return {-1, 0, 0, first};
     while (hi - lo > 1) {                                             // count(lo) > number >= count(hi)
         const uint32_t mid = lo + (hi - lo) / 2;
@@ -96,8 +153,9 @@ __device__ __forceinline__ Tile find_heaviest(int n_seqs, uint32_t number, S &&s
     const uint32_t number_there = number - count((int)hi), each = parts(lo);
     uint32_t left = number_there / each;
     const int part = (int)(number_there - left * each);
-    for (int b0 = 0; b0 < n_seqs; b0 += 64) {
-        const Span s = b0 == 0 ? first : at(b0);
+    Reached r = behind_first;
+    for (int b0 = 0; b0 < seqs.n; b0 += 64) {
+        const Span s = b0 == 0 ? first : seqs.at(b0, r);
         const int2 f = shape(s);
         const unsigned long long has = __ballot((int)lo >= f.y && (int)lo < f.x + f.y);
         const uint32_t n = __popcll(has);

@@ -83,12 +83,6 @@ __device__ __forceinline__ int swz_k(int r) { return DP == 128 ? r & 15 : (r >> 
 template <int DP>
 __device__ __forceinline__ int swz_v(int r) { return DP == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); }
 
-// An entry of cu, held to 0..n and to what the entry before it allows.
-__device__ __forceinline__ int2 span(const int32_t *cu, int b, int n) {
-    const int lo = min(max(cu[b], 0), n);
-    return {lo, min(max(cu[b + 1], lo), n)};
-}
-
 constexpr int kTileRows = kWaves * 32;             // rows of a workgroup: a tile of queries (1 << a.log_tile of them) for each of the heads that it has
 
 // The keys of a tile of queries are cut into parts where they are many and the queries few: as many as have about a share each, one at least and
@@ -111,23 +105,21 @@ struct Cut {
 __device__ __forceinline__ int2 tiles_of(const PromptArgs &a, const Span &s) {
     return {(s.nq + (1 << a.log_tile) - 1) >> a.log_tile, max(0, a.causal ? s.nk - s.nq : s.nk) >> a.log_tile};
 }
-__device__ __forceinline__ Span span_of(const PromptArgs &a, int b) {
-    const int2 q = span(a.cu_q, b, a.n_q), k = span(a.cu_k, b, a.n_k);
-    return {q.x, q.y - q.x, k.x, k.y - k.x};
-}
-__device__ __forceinline__ Cut cut_of(const PromptArgs &a) {
+__device__ __forceinline__ Sequences sequences(const PromptArgs &a) { return {a.cu_q, a.cu_k, a.n_seqs, a.n_q, a.n_k, [&](const Span &s) { return tiles_of(a, s); }}; }
+__device__ __forceinline__ Cut cut_of(const PromptArgs &a, const Sequences &seqs) {
     if (a.parts == 1) return {1, 1};
     uint32_t work = 0;                            // of all tiles, a step more of each sequence's at most
-    for (int b = threadIdx.x & 63; b < a.n_seqs; b += 64) {
-        const int2 t = tiles_of(a, span_of(a, b));
+    Reached reached;
+    for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
+        const int2 t = tiles_of(a, seqs.at(b0, reached));
         work += t.x * (t.y + (t.x + 1) / 2);
     }
     work = last_lane(wave_scan(work));
     return {max(kPartTiles * kKeys >> a.log_tile, (uint32_t)min((unsigned long long)work * head_groups(a) / a.slots + 1, 1ull << 26)), (uint32_t)a.parts};
 }
 // The tile of queries and the part of its keys with this number; the tiles of keys that the tile's last query sees.
-__device__ __forceinline__ Tile tile_of(const PromptArgs &a, const Cut &cut, uint32_t number, bool whole) {
-    const Tile at = find_heaviest(a.n_seqs, number, [&](int b) { return span_of(a, b); }, [&](const Span &s) { return tiles_of(a, s); },
+__device__ __forceinline__ Tile tile_of(const PromptArgs &a, const Sequences &seqs, const Cut &cut, uint32_t number, bool whole) {
+    const Tile at = find_heaviest(seqs, number, [&](const Span &s) { return tiles_of(a, s); },
         [&](uint32_t w) { return whole ? 1u : cut.parts(w); }, [&](uint32_t w) { return whole ? w : cut.sum(w); });
     const auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };          // the same in all lanes, and to be known as such
     return {scalar(at.piece), scalar(at.part), scalar(at.work), {scalar(at.span.q0), scalar(at.span.nq), scalar(at.span.k0), scalar(at.span.nk)}};
@@ -152,8 +144,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
     // each XCD's L2 holds the keys of one.  Tiles that see the most keys start first.
     const int G = a.Hq / a.Hk, groups = G / wg_heads, num = blockIdx.x + item0;
     const int hk = num % a.Hk, rest = num / a.Hk, head = hk * G + rest % groups * wg_heads + wave % wg_heads;
-    const Cut cut = cut_of(a);
-    const Tile at = tile_of(a, cut, (uint32_t)(rest / groups), false);
+    const Sequences seqs = sequences(a);
+    const Cut cut = cut_of(a, seqs);
+    const Tile at = tile_of(a, seqs, cut, (uint32_t)(rest / groups), false);
     if (at.piece < 0) return;
     const int nq = at.span.nq, r0 = at.piece * QT;                       // first query of the tile, within the sequence
     const long q_row = at.span.q0;
@@ -415,8 +408,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
 constexpr int kJoinQ = 32;
 __global__ __launch_bounds__(256) void join_parts(const PromptArgs a, int item0) {
     const int num = blockIdx.x + item0, head = num % a.Hq, rest = num / a.Hq, joins = (1 << a.log_tile) / kJoinQ;
-    const Cut cut = cut_of(a);
-    const Tile at = tile_of(a, cut, (uint32_t)(rest / joins), true);
+    const Sequences seqs = sequences(a);
+    const Cut cut = cut_of(a, seqs);
+    const Tile at = tile_of(a, seqs, cut, (uint32_t)(rest / joins), true);
     if (at.piece < 0) return;
     const int r0 = (at.piece << a.log_tile) + rest % joins * kJoinQ, parts = (int)cut.parts(at.work);
     if (parts == 1) return;

@@ -1,8 +1,11 @@
-"""What the attention calls promise beside their formulas (-m gpu): workspaces that calls share, calls of any size."""
+"""What the attention calls promise beside their formulas (-m gpu): workspaces that calls share, calls of any size, offsets that
+descend."""
+import numpy as np
 import pytest
 import torch
 
 import paper_2503_09304_amd as q
+from paper_2503_09304_amd import attention
 from test_gpu_attention import DEV, NAN, check, fresh, gen, rows, table
 
 pytestmark = pytest.mark.gpu
@@ -38,7 +41,7 @@ def test_decode_batches_of_any_size_share_a_workspace(fp8, spare):
     wide, narrow = batch(lens, 32, 8, 128, 64, fp8, 40), batch(lens[:20], 12, 3, 64, 16, fp8, 41)
     own = q.attn_decode_workspace(wide[0], 64, 32)
     ws = torch.zeros(own.numel() + spare, dtype=torch.uint8, device=DEV)
-    counters = q.attention._lib().attn_decode_counter_bytes(64, 32, 8)
+    counters = attention._lib().attn_decode_counter_bytes(64, 32, 8)
     for case, n in [(wide, 64), (wide, 32), (wide, 1), (wide, 64), (narrow, 20), (wide, 64), (wide, 9), (narrow, 3), (wide, 63), (wide, 64)]:
         got = decode(*case, ws, n)
         assert (ws[:counters] == 0).all(), n
@@ -68,3 +71,47 @@ def test_decode_of_more_workgroups_than_a_launch_takes():
         p = torch.exp(s - torch.where(torch.isinf(rl), torch.zeros_like(rl), rl)[..., None])
         ref = [p[..., :1] * one + p[..., 1:] * two, rl, p[..., :1] * one.abs() + p[..., 1:] * two.abs(), big]
         check(out[at:at + 1640].flatten(0, 1), lse[at:at + 1640].flatten(), [r.flatten(0, 1) for r in ref], D, at)
+
+
+def prompt(qq, k, v, cq, ck, causal):
+    cq, ck = (torch.from_numpy(np.asarray(x, dtype=np.int32)).to(DEV) for x in (cq, ck))
+    out, lse = torch.full_like(qq, 7.0), torch.full(qq.shape[:2], 7.0, dtype=torch.float32, device=DEV)
+    q.attn_prompt(qq, k, v, cq, ck, out, causal=causal, lse=lse)
+    return out, lse
+
+
+def held(cu, n):
+    """Entries clamped to the range and to the entry before them."""
+    return np.maximum.accumulate(np.clip(cu, 0, n))
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_offsets_that_descend_in_the_middle(causal):
+    """Each entry is at least the one before it: the bits of offsets that are so already, no row another sequence's, rows of none untouched."""
+    g = gen(43)
+    for Hq, Hk, D in [(2, 2, 64), (8, 2, 128)]:
+        qq, k, v = rows(g, 300, Hq, D), rows(g, 300, Hk, D), rows(g, 300, Hk, D)
+        for cq, ck in [([0, 30, 10, 40], [0, 30, 10, 40]), ([5, 250, 20, 260, 30, 270, 40], [0, 100, 200, 210, 230, 250, 300]),
+                       ([0, 100, 150, 160, 200], [0, 90, 20, 300, 10]), ([0, 1 << 30, 5, 9], [-5, -9, 300, 7])]:
+            got, want = prompt(qq, k, v, cq, ck, causal), prompt(qq, k, v, held(cq, 300), held(ck, 300), causal)
+            assert same(got, want), (cq, ck)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("n", [3, 64, 65, 150, 200])
+def test_offsets_of_any_kind(n, causal):
+    """Among up to 200 sequences: descents at any place, some of them between the 64 that are looked at together, and entries out of range; uncut, and cut into parts."""
+    r, g, Hq, Hk, D = np.random.default_rng(n), gen(44), 4, 1, 64
+    for T, M in [(1500, 1500), (150, 700 * max(n, 13))]:
+        qq, k, v = rows(g, T, Hq, D), rows(g, M, Hk, D), rows(g, M, Hk, D)
+        assert (attention._lib().attn_prompt_workspace_bytes(n, T, M, Hq, Hk, D) > 0) == (T == 150)
+        for share in (0.02, 0.3):
+            cu = []
+            for m in (T, M):
+                x = np.sort(r.integers(0, m + 1, n + 1))
+                wild = r.random(n + 1) < share
+                x[wild] = r.integers(-m, 2 * m, wild.sum())
+                x[n // 2] = x[n // 2 - 1] // 2
+                cu.append(x)
+            got, want = prompt(qq, k, v, *cu, causal), prompt(qq, k, v, held(cu[0], T), held(cu[1], M), causal)
+            assert same(got, want), share
