@@ -13,7 +13,7 @@
  * Conventions that hold for every call
  *  - Pointers marked [device] are GPU global memory owned by the caller; the library allocates nothing, creates no stream, keeps
  *    no state between calls and never waits: calls enqueue on `stream` (a hipStream_t as void*, NULL = the default stream) and
- *    return, so they can be captured into a graph.
+ *    return, so they can be captured into a graph.  The current device is that of the pointers and of the stream.
  *  - Return value: MOE_OK or a negative moe_status (qmoe.h), with the text in moe_last_error().  On an error nothing was enqueued
  *    (MOE_E_HIP excepted).
  *  - Queries, keys, values and outputs are bfloat16.  Products are summed in fp32, the softmax is in fp32, its weights are

@@ -1,8 +1,9 @@
 """The attention calls of libqmoe.so (include/qattn.h) on torch tensors: argument marshalling only.
 
 Queries, keys, values and outputs are bfloat16 tensors [tokens, heads, dim] with any token and head stride (multiples of 8
-elements) and dense heads.  Outputs are the caller's tensors.  Every call enqueues on PyTorch's current stream; a tensor that
-belongs to another stream's work is the caller's to order, as with any kernel."""
+elements) and dense heads.  Outputs are the caller's tensors.  All tensors of a call are on one device, which need not be the current
+one; the call enqueues on PyTorch's current stream of that device.  A tensor that belongs to another stream's work is the caller's to order, as
+with any kernel."""
 from __future__ import annotations
 
 import ctypes as C
@@ -69,25 +70,34 @@ def _bad(text: str):
     raise MoeError(MOE_E_ARG, text)
 
 
-def _heads(t, name: str, T: int, H: int, D: int):
-    """A bfloat16 tensor [T, H, D] as rows: address, token stride, head stride."""
-    if t.dtype is not torch.bfloat16 or not t.is_cuda or t.shape != (T, H, D):
-        _bad(f"{name} must be a bfloat16 tensor {[T, H, D]} on the GPU, not {t.dtype} {list(t.shape)}")
+def _device(t, name: str) -> int:
+    d = t.get_device()
+    if d < 0:
+        _bad(f"{name} must be on the GPU")
+    return d
+
+
+def _heads(t, name: str, T: int, H: int, D: int, dev: Optional[int] = None):
+    """A bfloat16 tensor [T, H, D] on this device (None: any) as rows: address, token stride, head stride."""
+    if dev is None:
+        dev = _device(t, name)
+    if t.dtype is not torch.bfloat16 or t.shape != (T, H, D) or t.get_device() != dev:
+        _bad(f"{name} must be a bfloat16 tensor {[T, H, D]} on GPU {dev}, not {t.dtype} {list(t.shape)} on {t.device}")
     ts, hs, ds = t.stride()
     if ds != 1:
         _bad(f"the elements of a head of {name} must be dense")
     return t.data_ptr(), ts if T > 1 else 0, hs if H > 1 else 0
 
 
-def _whole(t, name: str, dtype, shape) -> int:
-    """The address of a dense tensor of this type and shape."""
-    if t.dtype is not dtype or not t.is_cuda or t.shape != shape or not t.is_contiguous():
-        _bad(f"{name} must be a dense {dtype} tensor {list(shape)} on the GPU")
+def _whole(t, name: str, dtype, shape, dev: int) -> int:
+    """The address of a dense tensor of this type and shape on this device."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        _bad(f"{name} must be a dense {dtype} tensor {list(shape)} on GPU {dev}, not {t.dtype} {list(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _optional(t, name: str, dtype, shape):
-    return None if t is None else _whole(t, name, dtype, shape)
+def _optional(t, name: str, dtype, shape, dev: int):
+    return None if t is None else _whole(t, name, dtype, shape, dev)
 
 
 def _three(t, name: str):
@@ -98,10 +108,15 @@ def _three(t, name: str):
 
 # torch.cuda.current_stream() builds a stream object, 2 us of a call's 9.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _stream(t) -> int:
-    return _raw_stream(t.get_device())
+def _enqueue(f, dev: int, *args) -> int:
+    """f(*args, stream) on the current stream of this device, with the device current: a launch on a default stream goes to the current device's."""
+    if _current_device() == dev:
+        return _check(f(*args, _raw_stream(dev)))
+    with torch.cuda.device(dev):
+        return _check(f(*args, _raw_stream(dev)))
 
 
 class AttnCache:
@@ -119,8 +134,9 @@ class AttnCache:
         self.fp8 = k.dtype != torch.bfloat16
         if self.fp8 != (k_scale is not None) or self.fp8 != (v_scale is not None):
             _bad("a float8 cache needs k_scale and v_scale, a bfloat16 cache has none")
-        self._c = _Cache(_whole(k, "k", k.dtype, shape), _whole(v, "v", k.dtype, shape), _optional(k_scale, "k_scale", torch.uint8, shape[:3]),
-                         _optional(v_scale, "v_scale", torch.uint8, shape[:3]), *shape, ATTN_FP8 if self.fp8 else ATTN_BF16)
+        self._device = d = _device(k, "k")
+        self._c = _Cache(_whole(k, "k", k.dtype, shape, d), _whole(v, "v", k.dtype, shape, d), _optional(k_scale, "k_scale", torch.uint8, shape[:3], d),
+                         _optional(v_scale, "v_scale", torch.uint8, shape[:3], d), *shape, ATTN_FP8 if self.fp8 else ATTN_BF16)
         self._at = C.addressof(self._c)
 
     @classmethod
@@ -139,7 +155,8 @@ class AttnRope:
         if layout not in ATTN_ROPE:
             _bad("layout must be half or interleaved")
         self.inv_freq = inv_freq
-        self._c = _Rope(_whole(inv_freq, "inv_freq", torch.float64, (inv_freq.numel(),)), 2 * inv_freq.numel(), ATTN_ROPE[layout], mscale)
+        self._device = _device(inv_freq, "inv_freq")
+        self._c = _Rope(_whole(inv_freq, "inv_freq", torch.float64, (inv_freq.numel(),), self._device), 2 * inv_freq.numel(), ATTN_ROPE[layout], mscale)
         self._at = C.addressof(self._c)
 
 
@@ -153,39 +170,41 @@ def attn_rope_frequencies(dims: int, base: float = 10000.0, scaling: str = "none
     return list(f), float(m.value)
 
 
-def _place(seq, pos, pages, T: int):
+def _place(seq, pos, pages, T: int, dev: int):
     """seq, pos and pages as attn_place."""
     if pages.dim() != 2:
         _bad("pages must be [n_seqs, seq_pages]")
     n, m = pages.shape
-    return (_optional(seq, "seq", torch.int32, (T,)) or 0, _whole(pos, "pos", torch.int32, (T,)), _whole(pages, "pages", torch.int32, (n, m)), n | m << 32)
+    return (_optional(seq, "seq", torch.int32, (T,), dev) or 0, _whole(pos, "pos", torch.int32, (T,), dev), _whole(pages, "pages", torch.int32, (n, m), dev), n | m << 32)
 
 
 def attn_append(cache: AttnCache, q, k, v, seq, pos, pages, rope: Optional[AttnRope], q_out, k_out=None, bad=None) -> int:
     """Rotates q into q_out and k into k_out (may be None) and writes k and v to the cache.  seq (None: token t is sequence t's),
     pos int32 [tokens], pages int32 [n_seqs, seq_pages]; bad int32 [1] counts tokens that are out of range.  q and q_out may be None."""
-    T, Hk, D = _three(k, "k")[0], cache.heads_kv, cache.dim
+    T, Hk, D, dev = _three(k, "k")[0], cache.heads_kv, cache.dim, cache._device
     if (q is None) != (q_out is None):
         _bad("q and q_out go together")
+    if rope is not None and rope._device != dev:
+        _bad(f"inv_freq must be on GPU {dev}")
     Hq = 0 if q is None else _three(q, "q")[1]
     none = (0, 0, 0)
     w = _numbers
-    _pack5p(w.to, 0, *_heads(k, "k", T, Hk, D), *_heads(v, "v", T, Hk, D), *_place(seq, pos, pages, T),
-            *(none if q is None else _heads(q, "q", T, Hq, D)), *(none if q is None else _heads(q_out, "q_out", T, Hq, D)),
-            *(none if k_out is None else _heads(k_out, "k_out", T, Hk, D)))
+    _pack5p(w.to, 0, *_heads(k, "k", T, Hk, D, dev), *_heads(v, "v", T, Hk, D, dev), *_place(seq, pos, pages, T, dev),
+            *(none if q is None else _heads(q, "q", T, Hq, D, dev)), *(none if q is None else _heads(q_out, "q_out", T, Hq, D, dev)),
+            *(none if k_out is None else _heads(k_out, "k_out", T, Hk, D, dev)))
     at = w.at
-    return _check(_lib().attn_append(cache._at, at + 80 if q is not None else None, at, at + 24, at + 104 if q is not None else None,
-                                     at + 128 if k_out is not None else None, Hq, T, at + 48, None if rope is None else rope._at,
-                                     _optional(bad, "bad", torch.int32, (1,)), _stream(k)))
+    return _enqueue(_lib().attn_append, dev, cache._at, at + 80 if q is not None else None, at, at + 24, at + 104 if q is not None else None,
+                    at + 128 if k_out is not None else None, Hq, T, at + 48, None if rope is None else rope._at,
+                    _optional(bad, "bad", torch.int32, (1,), dev))
 
 
 def attn_read(cache: AttnCache, seq, pos, pages, k_out, v_out, bad=None) -> int:
     """Keys and values of the tokens at (seq, pos) out of the cache, as bfloat16."""
-    T = pos.shape[0]
+    T, Hk, D, dev = pos.shape[0], cache.heads_kv, cache.dim, cache._device
     w = _numbers
-    _pack2p(w.to, 0, *_heads(k_out, "k_out", T, cache.heads_kv, cache.dim), *_heads(v_out, "v_out", T, cache.heads_kv, cache.dim), *_place(seq, pos, pages, T))
+    _pack2p(w.to, 0, *_heads(k_out, "k_out", T, Hk, D, dev), *_heads(v_out, "v_out", T, Hk, D, dev), *_place(seq, pos, pages, T, dev))
     at = w.at
-    return _check(_lib().attn_read(cache._at, at + 48, T, at, at + 24, _optional(bad, "bad", torch.int32, (1,)), _stream(k_out)))
+    return _enqueue(_lib().attn_read, dev, cache._at, at + 48, T, at, at + 24, _optional(bad, "bad", torch.int32, (1,), dev))
 
 
 def attn_prompt(q, k, v, cu_q, cu_k, out, scale: Optional[float] = None, causal: bool = True, lse=None) -> int:
@@ -195,15 +214,15 @@ def attn_prompt(q, k, v, cu_q, cu_k, out, scale: Optional[float] = None, causal:
     n = cu_q.shape[0] - 1
     if n < 0:
         _bad("cu_q has no entry")
-    L = _lib()
+    L, dev = _lib(), _device(q, "q")
+    w = _numbers
+    _pack4(w.to, 0, *_heads(q, "q", n_q, Hq, D, dev), *_heads(k, "k", n_k, Hk, D, dev), *_heads(v, "v", n_k, Hk, D, dev), *_heads(out, "out", n_q, Hq, D, dev))
     nb = L.attn_prompt_workspace_bytes(n, n_q, n_k, Hq, Hk, D)
     ws = None if nb == 0 else torch.empty(nb, dtype=torch.uint8, device=q.device)
-    w = _numbers
-    _pack4(w.to, 0, *_heads(q, "q", n_q, Hq, D), *_heads(k, "k", n_k, Hk, D), *_heads(v, "v", n_k, Hk, D), *_heads(out, "out", n_q, Hq, D))
     at = w.at
-    return _check(L.attn_prompt(at, at + 24, at + 48, at + 72, _optional(lse, "lse", torch.float32, (n_q, Hq)),
-                                     _whole(cu_q, "cu_q", torch.int32, (n + 1,)), _whole(cu_k, "cu_k", torch.int32, (n + 1,)), n, n_q, n_k, Hq, Hk, D,
-                                     D ** -0.5 if scale is None else scale, 1 if causal else 0, None if ws is None else ws.data_ptr(), nb, _stream(q)))
+    return _enqueue(L.attn_prompt, dev, at, at + 24, at + 48, at + 72, _optional(lse, "lse", torch.float32, (n_q, Hq), dev),
+                    _whole(cu_q, "cu_q", torch.int32, (n + 1,), dev), _whole(cu_k, "cu_k", torch.int32, (n + 1,), dev), n, n_q, n_k, Hq, Hk, D,
+                    D ** -0.5 if scale is None else scale, 1 if causal else 0, None if ws is None else ws.data_ptr(), nb)
 
 
 def attn_decode_workspace(cache: AttnCache, n_seqs: int, heads_q: int):
@@ -219,11 +238,11 @@ def attn_decode(cache: AttnCache, q, pages, lens, out, workspace, scale: Optiona
     n, Hq, D = _three(q, "q")
     if pages.dim() != 2 or D != cache.dim:
         _bad("pages must be [n_seqs, seq_pages], q [n_seqs, heads_q, dim of the cache]")
-    m, nb = pages.shape[1], workspace.numel()
+    m, nb, dev = pages.shape[1], workspace.numel(), cache._device
     w = _numbers
-    _pack2(w.to, 0, *_heads(q, "q", n, Hq, D), *_heads(out, "out", n, Hq, D))
+    _pack2(w.to, 0, *_heads(q, "q", n, Hq, D, dev), *_heads(out, "out", n, Hq, D, dev))
     at = w.at
-    return _check(_lib().attn_decode(cache._at, at, at + 24, _optional(lse, "lse", torch.float32, (n, Hq)), n, Hq,
-                                     _whole(pages, "pages", torch.int32, (n, m)), m, _whole(lens, "lens", torch.int32, (n,)),
-                                     D ** -0.5 if scale is None else scale, _whole(workspace, "workspace", torch.uint8, (nb,)), nb,
-                                     _optional(bad, "bad", torch.int32, (1,)), _stream(q)))
+    return _enqueue(_lib().attn_decode, dev, cache._at, at, at + 24, _optional(lse, "lse", torch.float32, (n, Hq), dev), n, Hq,
+                    _whole(pages, "pages", torch.int32, (n, m), dev), m, _whole(lens, "lens", torch.int32, (n,), dev),
+                    D ** -0.5 if scale is None else scale, _whole(workspace, "workspace", torch.uint8, (nb,), dev), nb,
+                    _optional(bad, "bad", torch.int32, (1,), dev))

@@ -1,7 +1,14 @@
 """Host side of the attention calls on the CPU: qattn_api.hip compiled as plain C++ with recording stubs in place of the kernels'
 launchers (tests/host_stub/attn_test.cpp), and the binding with stand-ins for tensors."""
+import math
 import os
 import subprocess
+
+import pytest
+import torch
+
+import paper_2503_09304_amd as q
+from paper_2503_09304_amd import attention as at
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 STUB = os.path.join(ROOT, "tests", "host_stub")
@@ -17,3 +24,108 @@ def test_host_side_with_recorded_launches(tmp_path):
     assert r.returncode == 0, r.stderr[-4000:]
     r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and "all attention host checks passed" in r.stdout, r.stdout[-3000:]
+
+
+class Stand:
+    """Stands for a tensor on GPU `device`: what the binding looks at."""
+    def __init__(self, shape, dtype, device=1):
+        self.shape, self.dtype, self.on, self.device, self.is_cuda = tuple(shape), dtype, device, f"cuda:{device}", True
+
+    def get_device(self):
+        return self.on
+
+    def dim(self):
+        return len(self.shape)
+
+    def stride(self):
+        return tuple(math.prod(self.shape[i + 1:]) for i in range(len(self.shape)))
+
+    def numel(self):
+        return math.prod(self.shape)
+
+    def data_ptr(self):
+        return 1 << 20
+
+    def is_contiguous(self):
+        return True
+
+
+class Recorded:
+    """Stands for the library: which call came last, and which device was current."""
+    def __init__(self, now):
+        self.now, self.last = now, None
+
+    def __getattr__(self, name):
+        def call(*args):
+            if name.endswith("_bytes"):
+                return 0
+            self.last = (name, self.now[-1], args[-1])
+            return 0
+        return call
+
+
+def calls():
+    """Of each call: itself, and its tensors by name."""
+    bf, i32, f32 = torch.bfloat16, torch.int32, torch.float32
+    heads, T = lambda h: Stand((4, h, 64), bf), 4  # noqa: E731
+    place = dict(seq=Stand((T,), i32), pos=Stand((T,), i32), pages=Stand((2, 3), i32), bad=Stand((1,), i32))
+    cache = dict(k=Stand((9, 2, 16, 64), torch.uint8), v=Stand((9, 2, 16, 64), torch.uint8), k_scale=Stand((9, 2, 16), torch.uint8), v_scale=Stand((9, 2, 16), torch.uint8))
+    freq = Stand((32,), torch.float64)
+    of = lambda c: at.AttnCache(c["cache_k"], c["cache_v"], c["cache_k_scale"], c["cache_v_scale"])  # noqa: E731
+    cached = {"cache_" + n: t for n, t in cache.items()}
+    return {
+        "attn_append": (lambda c: at.attn_append(of(c), c["q"], c["k"], c["v"], c["seq"], c["pos"], c["pages"], at.AttnRope(c["freq"]), c["q_out"], c["k_out"], c["bad"]),
+                        dict(cached, **place, q=heads(4), k=heads(2), v=heads(2), q_out=heads(4), k_out=heads(2), freq=freq)),
+        "attn_read": (lambda c: at.attn_read(of(c), c["seq"], c["pos"], c["pages"], c["k_out"], c["v_out"], c["bad"]),
+                      dict(cached, **place, k_out=heads(2), v_out=heads(2))),
+        "attn_prompt": (lambda c: at.attn_prompt(c["q"], c["k"], c["v"], c["cu_q"], c["cu_k"], c["out"], lse=c["lse"]),
+                        dict(q=heads(4), k=heads(2), v=heads(2), out=heads(4), cu_q=Stand((3,), i32), cu_k=Stand((3,), i32), lse=Stand((4, 4), f32))),
+        "attn_decode": (lambda c: at.attn_decode(of(c), c["q"], c["pages"], c["lens"], c["out"], c["workspace"], lse=c["lse"], bad=c["bad"]),
+                        dict(cached, q=heads(4), out=heads(4), pages=Stand((4, 3), i32), lens=Stand((4,), i32), lse=Stand((4, 4), f32), bad=place["bad"],
+                             workspace=Stand((1 << 20,), torch.uint8))),
+    }
+
+
+@pytest.fixture
+def two_gpus(monkeypatch):
+    """Device 0 is current; the streams of device d are number 100 + d."""
+    now = [0]
+
+    class Guard:
+        def __init__(self, device):
+            self.device = device
+
+        def __enter__(self):
+            now.append(self.device)
+
+        def __exit__(self, *args):
+            now.pop()
+
+    library = Recorded(now)
+    monkeypatch.setattr(at, "_lib", lambda: library)
+    monkeypatch.setattr(at, "_raw_stream", lambda d: 100 + d)
+    monkeypatch.setattr(at, "_current_device", lambda: now[-1], raising=False)
+    monkeypatch.setattr(torch.cuda, "device", Guard)
+    return library
+
+
+@pytest.mark.parametrize("name", ["attn_append", "attn_read", "attn_prompt", "attn_decode"])
+def test_calls_go_to_the_device_of_their_tensors(name, two_gpus):
+    call, tensors = calls()[name]
+    for device in (0, 1):
+        for t in tensors.values():
+            t.on = device
+        assert call(tensors) == q.MOE_OK
+        assert two_gpus.last == (name, device, 100 + device) and two_gpus.now == [0]
+
+
+@pytest.mark.parametrize("name", ["attn_append", "attn_read", "attn_prompt", "attn_decode"])
+def test_tensors_of_two_devices_are_refused(name, two_gpus):
+    call, tensors = calls()[name]
+    for odd in tensors:
+        for device in (0, -1):
+            for n, t in tensors.items():
+                t.on = device if n == odd else 1
+            with pytest.raises(q.MoeError) as e:
+                call(tensors)
+            assert e.value.code == q.MOE_E_ARG and two_gpus.last is None, odd
