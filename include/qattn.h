@@ -19,6 +19,7 @@
  *  - Queries, keys, values and outputs are bfloat16.  Products are summed in fp32, the softmax is in fp32, its weights are
  *    rounded to bf16 once (they are a matrix operand), outputs are rounded to bf16 once.
  *  - Heads: query head h reads key/value head h / (heads_q / heads_kv).  A head has dim elements, a multiple of 16 from 16 to 128.
+ *  - Calls of no tokens (queries, sequences) do nothing and look at no pointer of theirs but the cache's.
  *  - Tokens that take part are assumed finite.  What lies beside them (slots of a page that no token was written to, rows between
  *    strides) may hold anything, NaN included, and reaches no output.
  *  - Numbers on the device (seq, pos, pages, lens, cu) cannot be checked by the host.  The kernels check them: what they do with

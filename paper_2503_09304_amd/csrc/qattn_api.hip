@@ -59,6 +59,7 @@ qattn::Cache cache_of(const attn_cache *c) {
 
 int32_t check_place(const attn_place *p, int n_tokens, const char *call) {
     if (n_tokens < 0) return set_error(MOE_E_ARG, "%s: n_tokens negative", call);
+    if (n_tokens == 0) return MOE_OK;             // tensors without elements have no address
     if (!p || !p->pos || !p->pages) return set_error(MOE_E_ARG, "%s: the place or its pos or pages is null", call);
     if (p->n_seqs < 1 || p->seq_pages < 1) return set_error(MOE_E_ARG, "%s: n_seqs and seq_pages must be positive", call);
     return MOE_OK;
@@ -204,10 +205,10 @@ int32_t attn_decode(const attn_cache *cache, const attn_rows *q, const attn_rows
     int32_t rc;
     if ((rc = check_cache(cache, call)) || (rc = check_heads(heads_q, cache->heads_kv, call))) return rc;
     if (n_seqs < 0 || n_seqs > 65535) return set_error(MOE_E_ARG, "%s: n_seqs must be 0..65535", call);
+    if (n_seqs == 0) return MOE_OK;
     if (seq_pages < 1 || (int64_t)seq_pages * cache->page_tokens >= (int64_t)1 << 30) return set_error(MOE_E_ARG, "%s: seq_pages must be positive, and seq_pages * page_tokens below 2^30", call);
     if ((int64_t)n_seqs * seq_pages * cache->page_tokens >= (int64_t)1 << 38) return set_error(MOE_E_ARG, "%s: n_seqs * seq_pages * page_tokens must be below 2^38", call);
     if (!(scale > 0.f) || !std::isfinite(scale)) return set_error(MOE_E_ARG, "%s: scale must be positive and finite", call);
-    if (n_seqs == 0) return MOE_OK;
     if (!pages || !lens) return set_error(MOE_E_ARG, "%s: pages or lens is null", call);
     if ((rc = check_rows(q, call, "q")) || (rc = check_rows(out, call, "out"))) return rc;
     const size_t need = attn_decode_workspace_bytes(n_seqs, heads_q, cache->heads_kv, cache->dim);

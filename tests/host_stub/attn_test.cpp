@@ -124,7 +124,23 @@ static void test_launches_of_many_workgroups() {
     }
 }
 
+// Calls of nothing: tensors without elements have no address.
+static void test_calls_of_nothing() {
+    const attn_cache c{kBase, kBase, nullptr, nullptr, 8, 4, 64, 64, ATTN_BF16};
+    const attn_rows none{nullptr, 0, 0};
+    for (const attn_place &p : {attn_place{nullptr, nullptr, nullptr, 0, 0}, attn_place{nullptr, nullptr, (int32_t *)kBase, 3, 4}, attn_place{nullptr, nullptr, nullptr, 0, 4}}) {
+        CHECK(attn_append(&c, &none, &none, &none, &none, &none, 8, 0, &p, nullptr, nullptr, nullptr) == MOE_OK);
+        CHECK(attn_append(&c, nullptr, &none, &none, nullptr, nullptr, 0, 0, &p, nullptr, nullptr, nullptr) == MOE_OK);
+        CHECK(attn_read(&c, &p, 0, &none, &none, nullptr, nullptr) == MOE_OK);
+        CHECK(attn_append(&c, &none, &none, &none, &none, &none, 8, 1, &p, nullptr, nullptr, nullptr) == MOE_E_ARG);
+    }
+    CHECK(attn_prompt(&none, &none, &none, &none, nullptr, nullptr, nullptr, 0, 0, 0, 8, 4, 64, 1.f, 1, nullptr, 0, nullptr) == MOE_OK);
+    CHECK(attn_prompt(&none, &none, &none, &none, nullptr, (int32_t *)kBase, (int32_t *)kBase, 3, 0, 0, 8, 4, 64, 1.f, 1, nullptr, 0, nullptr) == MOE_OK);
+    CHECK(attn_decode(&c, &none, &none, nullptr, 0, 8, nullptr, 0, nullptr, 1.f, nullptr, 0, nullptr, nullptr) == MOE_OK);
+}
+
 int main() {
+    test_calls_of_nothing();
     test_launches_of_many_workgroups();
     test_workspaces_are_long_enough();
     test_calls_that_share_a_workspace();

@@ -1,5 +1,5 @@
 """What the attention calls promise beside their formulas (-m gpu): workspaces that calls share, calls of any size, offsets that
-descend."""
+descend, calls of nothing."""
 import numpy as np
 import pytest
 import torch
@@ -115,3 +115,24 @@ def test_offsets_of_any_kind(n, causal):
                 cu.append(x)
             got, want = prompt(qq, k, v, *cu, causal), prompt(qq, k, v, held(cu[0], T), held(cu[1], M), causal)
             assert same(got, want), share
+
+
+@pytest.mark.parametrize("n_pages", [0, 3])
+def test_calls_of_nothing(n_pages):
+    """No tokens, no queries, no sequences, no keys."""
+    Hq, Hk, D = 8, 2, 64
+    c = fresh(4, Hk, 16, D, False)
+    bf, none = dict(dtype=torch.bfloat16, device=DEV), torch.empty(0, dtype=torch.int32, device=DEV)
+    pages = torch.empty((0, n_pages), dtype=torch.int32, device=DEV)
+    qq, k = torch.empty((0, Hq, D), **bf), torch.empty((0, Hk, D), **bf)
+    assert q.attn_append(c, qq, k, k, none, none, pages, None, qq, k) == q.MOE_OK
+    assert q.attn_append(c, None, k, k, None, none, pages, None, None) == q.MOE_OK
+    assert q.attn_read(c, none, none, pages, k, k) == q.MOE_OK
+    assert q.attn_decode(c, qq, pages, none, qq, q.attn_decode_workspace(c, 0, Hq), lse=torch.empty((0, Hq), device=DEV)) == q.MOE_OK
+    for cu in ([0], [0, 0, 0]):
+        cu = torch.tensor(cu, dtype=torch.int32, device=DEV)
+        assert q.attn_prompt(qq, k, k, cu, cu, qq) == q.MOE_OK
+    cq, ck = torch.tensor([0, 5], dtype=torch.int32, device=DEV), torch.tensor([0, 0], dtype=torch.int32, device=DEV)
+    out, lse = torch.full((5, Hq, D), 7.0, **bf), torch.zeros((5, Hq), device=DEV)
+    assert q.attn_prompt(torch.ones((5, Hq, D), **bf), k, k, cq, ck, out, lse=lse) == q.MOE_OK
+    assert (out == 0).all() and (lse == -torch.inf).all() and c.k.isnan().all() and c.v.isnan().all()
