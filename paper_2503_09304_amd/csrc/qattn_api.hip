@@ -146,7 +146,7 @@ int32_t attn_read(const attn_cache *cache, const attn_place *place, int32_t n_to
 
 size_t attn_prompt_workspace_bytes(int32_t n_seqs, int32_t n_q, int32_t n_k, int32_t heads_q, int32_t heads_kv, int32_t dim) {
     const char *call = "attn_prompt_workspace_bytes";
-    if (check_heads(heads_q, heads_kv, call) || check_dim(dim, call) || n_seqs < 1 || n_seqs > 1 << 20 || n_q < 1 || n_k < 1) return 0;
+    if (check_heads(heads_q, heads_kv, call) || check_dim(dim, call) || n_seqs < 1 || n_seqs > 1 << 20 || n_q < 1 || n_q > 1 << 30 || n_k < 1 || n_k > 1 << 30) return 0;
     const int parts = qattn::prompt_parts(n_seqs, n_q, n_k, heads_q, heads_kv, dim);
     return parts > 1 ? (size_t)parts * n_q * heads_q * (dim + 2) * 4 : 0;
 }
@@ -159,6 +159,7 @@ int32_t attn_prompt(const attn_rows *q, const attn_rows *k, const attn_rows *v, 
     if ((rc = check_heads(heads_q, heads_kv, call)) || (rc = check_dim(dim, call))) return rc;
     if (n_seqs < 0 || n_q < 0 || n_k < 0) return set_error(MOE_E_ARG, "%s: negative size", call);
     if (n_seqs > 1 << 20) return set_error(MOE_E_ARG, "%s: n_seqs must be at most 2^20", call);
+    if (n_q > 1 << 30 || n_k > 1 << 30) return set_error(MOE_E_ARG, "%s: n_q and n_k must be at most 2^30", call);      // rows up to the end of a tile have 32 bits
     if (!(scale > 0.f) || !std::isfinite(scale)) return set_error(MOE_E_ARG, "%s: scale must be positive and finite", call);
     if (n_seqs == 0 || n_q == 0) return MOE_OK;
     if (!cu_q || !cu_k) return set_error(MOE_E_ARG, "%s: cu_q or cu_k is null", call);

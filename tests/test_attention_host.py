@@ -9,6 +9,7 @@ import torch
 
 import paper_2503_09304_amd as q
 from paper_2503_09304_amd import attention as at
+from test_attention_cpu import FAKE, refused, rows
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 STUB = os.path.join(ROOT, "tests", "host_stub")
@@ -24,6 +25,15 @@ def test_host_side_with_recorded_launches(tmp_path):
     assert r.returncode == 0, r.stderr[-4000:]
     r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and "all attention host checks passed" in r.stdout, r.stdout[-3000:]
+
+
+def test_prompts_of_more_rows_than_a_tile_counts():
+    """Up to the end of its last tile of 128 a row's number has to stay below 2^31."""
+    L, ok = at._lib(), rows()
+    for n_q, n_k in [((1 << 31) - 1, 4), (4, (1 << 31) - 1), ((1 << 30) + 1, 4), (4, (1 << 30) + 1)]:
+        refused(L.attn_prompt(ok, ok, ok, ok, None, FAKE, FAKE, 1, n_q, n_k, 8, 4, 128, 1.0, 1, None, 0, None), "2^30")
+        assert L.attn_prompt_workspace_bytes(1, n_q, n_k, 8, 4, 128) == 0
+    assert L.attn_prompt_workspace_bytes(1, 16, 1 << 20, 8, 4, 128) > 0
 
 
 class Stand:
