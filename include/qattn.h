@@ -113,7 +113,7 @@ int32_t attn_read(const attn_cache *cache, const attn_place *place, int32_t n_to
  *     out_i = sum_j p_ij v_j,   p_ij = exp(scale q_i.k_j) / sum_j' exp(scale q_i.k_j')
  * A query that sees no key gives zeros.  lse ([device] float [n_q, heads_q], may be NULL): ln of the sum of the exponentials,
  * -inf for a query without keys.  Rows of out that belong to no sequence are left untouched.  Entries of cu out of 0..n_q (n_k) or
- * descending are clamped to the range and to the entry before them.  scale > 0 and finite.  out overlaps no input.  Token strides of k and v: at
+ * descending are clamped to the range and to the entry before them.  scale > 0, at most 2^127.  out overlaps no input.  Token strides of k and v: at
  * most 2^24; n_seqs: at most 2^20; n_q and n_k: at most 2^30.
  * workspace ([device], 16-byte aligned, may be NULL; its contents before and after the call are of no account): where queries are so few that
  * they leave CUs idle, the keys of a query are cut into parts that run side by side, and a second launch joins them.

@@ -16,6 +16,8 @@ int32_t hip_result(hipError_t e, const char *what) {
     return e == hipSuccess ? MOE_OK : set_error(MOE_E_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
+constexpr float kLog2E = 1.44269504088896340736f;          // exponentials are powers of two in the kernels
+
 bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
 int32_t check_rows(const attn_rows *r, const char *call, const char *name) {
@@ -160,7 +162,7 @@ int32_t attn_prompt(const attn_rows *q, const attn_rows *k, const attn_rows *v, 
     if (n_seqs < 0 || n_q < 0 || n_k < 0) return set_error(MOE_E_ARG, "%s: negative size", call);
     if (n_seqs > 1 << 20) return set_error(MOE_E_ARG, "%s: n_seqs must be at most 2^20", call);
     if (n_q > 1 << 30 || n_k > 1 << 30) return set_error(MOE_E_ARG, "%s: n_q and n_k must be at most 2^30", call);      // rows up to the end of a tile have 32 bits
-    if (!(scale > 0.f) || !std::isfinite(scale)) return set_error(MOE_E_ARG, "%s: scale must be positive and finite", call);
+    if (!(scale > 0.f) || !std::isfinite(scale * kLog2E)) return set_error(MOE_E_ARG, "%s: scale must be positive, and scale * log2(e) finite", call);
     if (n_seqs == 0 || n_q == 0) return MOE_OK;
     if (!cu_q || !cu_k) return set_error(MOE_E_ARG, "%s: cu_q or cu_k is null", call);
     if ((rc = check_rows(q, call, "q")) || (rc = check_rows(out, call, "out"))) return rc;
@@ -171,7 +173,7 @@ int32_t attn_prompt(const attn_rows *q, const attn_rows *k, const attn_rows *v, 
     const int parts = need && workspace_bytes >= need ? qattn::prompt_parts(n_seqs, n_q, n_k, heads_q, heads_kv, dim) : 1;
     float *part_o = (float *)workspace, *part_ml = parts > 1 ? part_o + (size_t)parts * n_q * heads_q * dim : nullptr;
     qattn::PromptArgs a{rows(q), n_k ? rows(k) : qattn::Rows{nullptr, 0, 0}, n_k ? rows(v) : qattn::Rows{nullptr, 0, 0}, rows(out), lse,
-                        cu_q, cu_k, n_seqs, n_q, n_k, heads_q, heads_kv, dim, causal != 0, scale * 1.44269504088896340736f, qattn::prompt_log_tile(n_seqs, n_q, heads_q, heads_kv, parts), parts, qattn::prompt_slots(dim), part_o, part_ml};
+                        cu_q, cu_k, n_seqs, n_q, n_k, heads_q, heads_kv, dim, causal != 0, scale * kLog2E, qattn::prompt_log_tile(n_seqs, n_q, heads_q, heads_kv, parts), parts, qattn::prompt_slots(dim), part_o, part_ml};
     return hip_result(qattn::launch_prompt(a, (hipStream_t)stream), call);
 }
 
@@ -209,7 +211,7 @@ int32_t attn_decode(const attn_cache *cache, const attn_rows *q, const attn_rows
     if (n_seqs == 0) return MOE_OK;
     if (seq_pages < 1 || (int64_t)seq_pages * cache->page_tokens >= (int64_t)1 << 30) return set_error(MOE_E_ARG, "%s: seq_pages must be positive, and seq_pages * page_tokens below 2^30", call);
     if ((int64_t)n_seqs * seq_pages * cache->page_tokens >= (int64_t)1 << 38) return set_error(MOE_E_ARG, "%s: n_seqs * seq_pages * page_tokens must be below 2^38", call);
-    if (!(scale > 0.f) || !std::isfinite(scale)) return set_error(MOE_E_ARG, "%s: scale must be positive and finite", call);
+    if (!(scale > 0.f) || !std::isfinite(scale * kLog2E)) return set_error(MOE_E_ARG, "%s: scale must be positive, and scale * log2(e) finite", call);
     if (!pages || !lens) return set_error(MOE_E_ARG, "%s: pages or lens is null", call);
     if ((rc = check_rows(q, call, "q")) || (rc = check_rows(out, call, "out"))) return rc;
     const size_t need = attn_decode_workspace_bytes(n_seqs, heads_q, cache->heads_kv, cache->dim);
@@ -220,7 +222,7 @@ int32_t attn_decode(const attn_cache *cache, const attn_rows *q, const attn_rows
     const int pieces = (int)std::min<int64_t>(most, qattn::decode_pieces(n_seqs, heads_q, cache->heads_kv));
     qattn::DecodeArgs a{cache_of(cache), rows(q), rows(out), lse, pages, lens, bad, (int32_t *)w,
                         (float *)(w + counter_room(workspace_bytes)), n_seqs, heads_q, seq_pages,
-                        cache->format == ATTN_FP8, pieces, scale * 1.44269504088896340736f};
+                        cache->format == ATTN_FP8, pieces, scale * kLog2E};
     return hip_result(qattn::launch_decode(a, (hipStream_t)stream), call);
 }
 

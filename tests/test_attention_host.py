@@ -9,7 +9,7 @@ import torch
 
 import paper_2503_09304_amd as q
 from paper_2503_09304_amd import attention as at
-from test_attention_cpu import FAKE, refused, rows
+from test_attention_cpu import FAKE, cache, refused, rows
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 STUB = os.path.join(ROOT, "tests", "host_stub")
@@ -34,6 +34,14 @@ def test_prompts_of_more_rows_than_a_tile_counts():
         refused(L.attn_prompt(ok, ok, ok, ok, None, FAKE, FAKE, 1, n_q, n_k, 8, 4, 128, 1.0, 1, None, 0, None), "2^30")
         assert L.attn_prompt_workspace_bytes(1, n_q, n_k, 8, 4, 128) == 0
     assert L.attn_prompt_workspace_bytes(1, 16, 1 << 20, 8, 4, 128) > 0
+
+
+def test_scales_whose_power_of_two_overflows():
+    L, ok, c = at._lib(), rows(), cache()
+    for scale in (2.0 ** 127.9, 2.4e38):
+        refused(L.attn_prompt(ok, ok, ok, ok, None, FAKE, FAKE, 1, 4, 4, 8, 4, 128, scale, 1, None, 0, None), "scale")
+        refused(L.attn_decode(c, ok, ok, None, 2, 8, FAKE, 4, FAKE, scale, FAKE, 1 << 30, None, None), "scale")
+    assert L.attn_prompt(ok, ok, ok, ok, None, FAKE, FAKE, 1, 0, 4, 8, 4, 128, 2.0 ** 127, 1, None, 0, None) == q.MOE_OK
 
 
 class Stand:
