@@ -48,8 +48,8 @@ typedef struct {
  *     k_scale, v_scale  [n_pages, heads_kv, page_tokens]       ATTN_FP8 only, else NULL
  * ATTN_BF16: bfloat16.  ATTN_FP8: e4m3 (OCP: largest 448), and for each token and head one scale byte e8m0 (2^(byte-127), as in the
  * 4-bit weights of qmoe.h): value = element * scale.  The scale is the smallest power of two, 2^-126 at least, for which no
- * element is over 448, so writing rounds each bf16 element once, to 4 significant bits (one that would round to 2^128 to 1.875 * 2^127),
- * and a value read back is exactly a bf16.
+ * element is over 448, so writing rounds each bf16 element once, to 4 significant bits and no finer than 2^-9 of the scale (one that would round to
+ * 2^128 to 1.875 * 2^127), and a value read back is exactly a bf16, those below 2^-126 among them.
  * page_tokens: 16, 32, 64, 128 or 256.  k and v 16-byte aligned, scales 4-byte aligned. */
 enum { ATTN_BF16 = 0, ATTN_FP8 = 1 };
 typedef struct {

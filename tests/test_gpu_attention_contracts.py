@@ -6,7 +6,7 @@ import torch
 
 import paper_2503_09304_amd as q
 from paper_2503_09304_amd import attention
-from test_gpu_attention import DEV, NAN, check, fresh, gen, rows, table
+from test_gpu_attention import DEV, NAN, check, fresh, gen, quantised, rows, table
 
 pytestmark = pytest.mark.gpu
 
@@ -136,3 +136,21 @@ def test_calls_of_nothing(n_pages):
     out, lse = torch.full((5, Hq, D), 7.0, **bf), torch.zeros((5, Hq), device=DEV)
     assert q.attn_prompt(torch.ones((5, Hq, D), **bf), k, k, cq, ck, out, lse=lse) == q.MOE_OK
     assert (out == 0).all() and (lse == -torch.inf).all() and c.k.isnan().all() and c.v.isnan().all()
+
+
+def test_the_smallest_values_in_the_fp8_cache():
+    """Rows whose largest element is 2^-133 to 2^-110: below 2^-126 too what is read back is what the definition gives, bit for bit."""
+    D, g = 64, gen(45)
+    top = torch.exp2(-torch.arange(110, 134, device=DEV).double())[:, None, None]
+    x = torch.rand(24, 1, D, generator=g, device=DEV).double() * 2 - 1
+    x[:, :, :8] = torch.exp2(-torch.arange(8, device=DEV).double())               # the largest and 7 halvings of it
+    v = (x * top).to(torch.bfloat16)
+    pos, seq = torch.arange(24, dtype=torch.int32, device=DEV), torch.zeros(24, dtype=torch.int32, device=DEV)
+    pages, n_pages = table([24], 16, 0)
+    c = fresh(n_pages, 1, 16, D, True)
+    q.attn_append(c, None, v, -v, seq, pos, pages, None, None)
+    k2, v2 = torch.empty_like(v), torch.empty_like(v)
+    q.attn_read(c, seq, pos, pages, k2, v2)
+    want = quantised(v)
+    assert (want.abs() < 2.0 ** -126).any() and (want != 0).any(2).all()
+    assert torch.equal(k2.double(), want) and torch.equal(v2.double(), -want)
