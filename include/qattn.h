@@ -97,7 +97,8 @@ int32_t attn_rope_frequencies(int32_t dims, double base, int32_t scaling, double
  * and cache, v -> cache; q_out and k_out are rounded to bf16 once, and the cache takes the rounded keys.  q and q_out may be NULL
  * (both, with heads_q 0), k_out may be NULL; q_out may be q and k_out may be k, otherwise outputs overlap no input.
  * A row of padding writes nothing.  A token whose sequence, page index or page is out of range is counted in *bad and not written
- * to the cache; its q_out and k_out are.  Two tokens of a call in one slot: either may stand there afterwards. */
+ * to the cache; its q_out and k_out are.  Tokens of a call have slots of their own: what a slot that two of them name holds afterwards is not
+ * specified (it may be parts of both, or the elements of one under the scale of the other). */
 int32_t attn_append(const attn_cache *cache, const attn_rows *q, const attn_rows *k, const attn_rows *v, const attn_rows *q_out,
                     const attn_rows *k_out, int32_t heads_q, int32_t n_tokens, const attn_place *place, const attn_rope *rope,
                     int32_t *bad, void *stream);

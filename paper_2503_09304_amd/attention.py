@@ -180,7 +180,8 @@ def _place(seq, pos, pages, T: int, dev: int):
 
 def attn_append(cache: AttnCache, q, k, v, seq, pos, pages, rope: Optional[AttnRope], q_out, k_out=None, bad=None) -> int:
     """Rotates q into q_out and k into k_out (may be None) and writes k and v to the cache.  seq (None: token t is sequence t's),
-    pos int32 [tokens], pages int32 [n_seqs, seq_pages]; bad int32 [1] counts tokens that are out of range.  q and q_out may be None."""
+    pos int32 [tokens], pages int32 [n_seqs, seq_pages]; bad int32 [1] counts tokens that are out of range.  q and q_out may be None.
+    No two tokens of a call have the same slot: what it holds afterwards is not specified."""
     T, Hk, D, dev = _three(k, "k")[0], cache.heads_kv, cache.dim, cache._device
     if (q is None) != (q_out is None):
         _bad("q and q_out go together")
