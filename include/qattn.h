@@ -19,6 +19,9 @@
  *  - Queries, keys, values and outputs are bfloat16.  Products are summed in fp32, the softmax is in fp32, its weights are
  *    rounded to bf16 once (they are a matrix operand), outputs are rounded to bf16 once.
  *  - Heads: query head h reads key/value head h / (heads_q / heads_kv).  A head has dim elements, a multiple of 16 from 16 to 128.
+ *  - A call's results are the same bits every time.  A sequence's may differ in the last bits with the others of its call: in how many places its keys are
+ *    cut, and so the order of its sums, goes by all lengths of the call (attn_decode, and attn_prompt with a workspace).  attn_prompt without a workspace
+ *    cuts nothing: there a sequence's bits are the same whatever stands beside it.
  *  - Calls of no tokens (queries, sequences) do nothing and look at no pointer of theirs but the cache's.
  *  - Tokens that take part are assumed finite.  What lies beside them (slots of a page that no token was written to, rows between
  *    strides) may hold anything, NaN included, and reaches no output.

@@ -1,5 +1,7 @@
 """What the attention calls promise beside their formulas (-m gpu): workspaces that calls share, calls of any size, offsets that
-descend, calls of nothing."""
+descend, calls of nothing, the smallest values of the 8-bit cache, bits that do not depend on other sequences."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -154,3 +156,29 @@ def test_the_smallest_values_in_the_fp8_cache():
     want = quantised(v)
     assert (want.abs() < 2.0 ** -126).any() and (want != 0).any(2).all()
     assert torch.equal(k2.double(), want) and torch.equal(v2.double(), -want)
+
+
+def uncut(qq, k, v, cq, ck, D, causal):
+    """attn_prompt of the C library without a workspace, which the binding always gives."""
+    out, lse = torch.full_like(qq, 7.0), torch.full(qq.shape[:2], 7.0, dtype=torch.float32, device=DEV)
+    held_rows = [(C.c_int64 * 3)(t.data_ptr(), t.stride(0), t.stride(1)) for t in (qq, k, v, out)]
+    cq, ck = (torch.tensor(x, dtype=torch.int32, device=DEV) for x in (cq, ck))
+    rc = attention._lib().attn_prompt(*held_rows, lse.data_ptr(), cq.data_ptr(), ck.data_ptr(), len(cq) - 1, len(qq), len(k), qq.shape[1], k.shape[1], D, D ** -0.5,
+                                      causal, None, 0, torch.cuda.current_stream().cuda_stream)
+    assert rc == q.MOE_OK
+    torch.cuda.synchronize()
+    return out, lse
+
+
+@pytest.mark.parametrize("causal", [0, 1])
+@pytest.mark.parametrize("Hq,Hk,D", [(8, 2, 128), (6, 2, 64), (3, 3, 80)])
+def test_a_prompt_that_is_not_cut_has_the_same_bits_in_any_company(Hq, Hk, D, causal):
+    g = gen(46)
+    nq, nk = [1, 33, 200, 64, 5, 129], [1, 700, 200, 3000, 2, 129]
+    cq, ck = (np.concatenate([[0], np.cumsum(n)]).tolist() for n in (nq, nk))
+    qq, k, v = rows(g, cq[-1], Hq, D, 3.0), rows(g, ck[-1], Hk, D), rows(g, ck[-1], Hk, D)
+    whole = uncut(qq, k, v, cq, ck, D, causal)
+    for b in range(len(nq)):
+        a, z, ka, kz = cq[b], cq[b + 1], ck[b], ck[b + 1]
+        alone = uncut(qq[a:z], k[ka:kz], v[ka:kz], [0, z - a], [0, kz - ka], D, causal)
+        assert same(alone, [x[a:z] for x in whole]), b
