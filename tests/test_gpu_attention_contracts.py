@@ -1,5 +1,6 @@
 """What the attention calls promise beside their formulas (-m gpu): workspaces that calls share, calls of any size, offsets that
-descend, calls of nothing, the smallest values of the 8-bit cache, bits that do not depend on other sequences."""
+descend, calls of nothing, the smallest values of the 8-bit cache, bits that do not depend on other sequences;
+and the tiles of heads of 128 against the formula."""
 import ctypes as C
 
 import numpy as np
@@ -8,7 +9,7 @@ import torch
 
 import paper_2503_09304_amd as q
 from paper_2503_09304_amd import attention
-from test_gpu_attention import DEV, NAN, check, fresh, gen, quantised, rows, table
+from test_gpu_attention import DEV, NAN, check, fresh, gen, quantised, rows, run_prompt, table
 
 pytestmark = pytest.mark.gpu
 
@@ -182,3 +183,31 @@ def test_a_prompt_that_is_not_cut_has_the_same_bits_in_any_company(Hq, Hk, D, ca
         a, z, ka, kz = cq[b], cq[b + 1], ck[b], ck[b + 1]
         alone = uncut(qq[a:z], k[ka:kz], v[ka:kz], [0, z - a], [0, kz - ka], D, causal)
         assert same(alone, [x[a:z] for x in whole]), b
+
+
+@pytest.mark.parametrize("Hq,Hk,D,queries", [(32, 8, 128, 32), (16, 4, 128, 32), (8, 1, 128, 128), (32, 8, 112, 32), (16, 4, 96, 32), (12, 2, 128, 64), (24, 12, 128, 64), (40, 8, 128, 128)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_tiles_shared_by_heads(Hq, Hk, D, queries, causal):
+    """Workgroups of 32 queries of four heads of up to 128, 64 of two, 128 of one: prompts that fill the chip, a context among them, against the formula in 64 bits."""
+    nq, nk = [700, 1, 515, 33, 1300, 64], [700, 1, 900, 33, 1300, 20]
+    L = attention._lib()
+    assert L.attn_prompt_workspace_bytes(6, sum(nq), sum(nk), Hq, Hk, D) == 0
+    assert 1 << L._ZN5qattn15prompt_log_tileEiiiii(6, sum(nq), Hq, Hk, 1) == queries
+    run_prompt(nq, nk, Hq, Hk, D, causal, seed=Hq + D)
+
+
+@pytest.mark.parametrize("Hq,Hk,queries", [(32, 8, 32), (4, 1, 32), (6, 3, 64), (5, 1, 128)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_tiles_shared_by_heads_in_parts(Hq, Hk, queries, causal):
+    """The same with keys that are cut into parts: chunks of a few queries on long contexts, heads of 128."""
+    nq, nk = [16, 70, 1], [4000, 2500, 7001]
+    L = attention._lib()
+    size = L.attn_prompt_workspace_bytes(3, sum(nq), sum(nk), Hq, Hk, 128)
+    parts = size // (sum(nq) * Hq * 130 * 4)
+    assert parts > 1 and 1 << L._ZN5qattn15prompt_log_tileEiiiii(3, sum(nq), Hq, Hk, parts) == queries
+    run_prompt(nq, nk, Hq, Hk, 128, causal, seed=Hq)
+
+
+def test_a_long_prompt_of_the_benchmarks_heads():
+    """Heads of 128, four to a key/value head, 5000 tokens: many tiles of keys, maxima that are taken over."""
+    run_prompt([5000], [5000], 32, 8, 128, seed=47, spread=2.0)
