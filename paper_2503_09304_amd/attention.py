@@ -101,9 +101,17 @@ def _optional(t, name: str, dtype, shape, dev: int):
 
 
 def _three(t, name: str):
-    if t.dim() != 3:
+    s = t.shape
+    if len(s) != 3:
         _bad(f"{name} must be [tokens, heads, dim]")
-    return t.shape
+    if s[0] >> 31:
+        _long(name)
+    return s
+
+
+def _long(name: str):
+    """Counts are int32 in the library; ctypes would cut them off."""
+    _bad(f"{name} has 2^31 rows or more")
 
 
 # torch.cuda.current_stream() builds a stream object, 2 us of a call's 9.
@@ -175,6 +183,8 @@ def _place(seq, pos, pages, T: int, dev: int):
     if pages.dim() != 2:
         _bad("pages must be [n_seqs, seq_pages]")
     n, m = pages.shape
+    if (n | m) >> 31:
+        _long("pages")
     return (_optional(seq, "seq", torch.int32, (T,), dev) or 0, _whole(pos, "pos", torch.int32, (T,), dev), _whole(pages, "pages", torch.int32, (n, m), dev), n | m << 32)
 
 
@@ -202,6 +212,8 @@ def attn_append(cache: AttnCache, q, k, v, seq, pos, pages, rope: Optional[AttnR
 def attn_read(cache: AttnCache, seq, pos, pages, k_out, v_out, bad=None) -> int:
     """Keys and values of the tokens at (seq, pos) out of the cache, as bfloat16."""
     T, Hk, D, dev = pos.shape[0], cache.heads_kv, cache.dim, cache._device
+    if T >> 31:
+        _long("pos")
     w = _numbers
     _pack2p(w.to, 0, *_heads(k_out, "k_out", T, Hk, D, dev), *_heads(v_out, "v_out", T, Hk, D, dev), *_place(seq, pos, pages, T, dev))
     at = w.at
@@ -213,6 +225,8 @@ def attn_prompt(q, k, v, cu_q, cu_k, out, scale: Optional[float] = None, causal:
     Where queries are few and keys many the call takes scratch memory from PyTorch's allocator, for the time of its kernels."""
     (n_q, Hq, D), (n_k, Hk, _) = _three(q, "q"), _three(k, "k")
     n = cu_q.shape[0] - 1
+    if n >> 31 > 0:
+        _long("cu_q")
     if n < 0:
         _bad("cu_q has no entry")
     L, dev = _lib(), _device(q, "q")
@@ -240,6 +254,8 @@ def attn_decode(cache: AttnCache, q, pages, lens, out, workspace, scale: Optiona
     if pages.dim() != 2 or D != cache.dim:
         _bad("pages must be [n_seqs, seq_pages], q [n_seqs, heads_q, dim of the cache]")
     m, nb, dev = pages.shape[1], workspace.numel(), cache._device
+    if m >> 31:
+        _long("pages")
     w = _numbers
     _pack2(w.to, 0, *_heads(q, "q", n, Hq, D, dev), *_heads(out, "out", n, Hq, D, dev))
     at = w.at

@@ -147,3 +147,16 @@ def test_tensors_of_two_devices_are_refused(name, two_gpus):
             with pytest.raises(q.MoeError) as e:
                 call(tensors)
             assert e.value.code == q.MOE_E_ARG and two_gpus.last is None, odd
+
+
+@pytest.mark.parametrize("name,long", [("attn_append", ("k", "v", "q", "q_out", "k_out", "seq", "pos")), ("attn_append", ("q",)), ("attn_append", ("pages",)), ("attn_read", ("k_out", "v_out", "seq", "pos")),
+                                       ("attn_prompt", ("q", "out", "lse")), ("attn_prompt", ("k", "v")), ("attn_prompt", ("cu_q", "cu_k")),
+                                       ("attn_decode", ("q", "out", "lse", "pages", "lens"))])
+def test_counts_of_33_bits_are_refused(name, long, two_gpus):
+    """2^32 rows more than there are: the library's 32 bits would be the rows that there are."""
+    call, tensors = calls()[name]
+    for t in long:
+        tensors[t].shape = (tensors[t].shape[0] + (1 << 32), *tensors[t].shape[1:])
+    with pytest.raises(q.MoeError) as e:
+        call(tensors)
+    assert e.value.code == q.MOE_E_ARG and two_gpus.last is None
