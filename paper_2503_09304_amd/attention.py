@@ -114,7 +114,7 @@ def _long(name: str):
     _bad(f"{name} has 2^31 rows or more")
 
 
-# torch.cuda.current_stream() builds a stream object, 2 us of a call's 9.
+# torch.cuda.current_stream() builds a stream object, 2 us of a call's 8.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 

@@ -10,7 +10,7 @@
 // keep 4.  One thread per (token, pair) forms them, all heads of the token read them from LDS.
 //
 // Rows go past the caches (non-temporal loads and stores where nothing is read twice: 9826 tokens 55.7 -> 52.1 us).  Measured: 9826 tokens of 32 + 8 + 8 heads
-// of 128 into a bf16 cache 52 us, 4.6 TB/s (a copy of 4 GiB by the vendor's library 4.9); one token 4.2 us; 40276 fp8 tokens read 55 us, 4.5 TB/s.
+// of 128 into a bf16 cache 51 us, 4.7 TB/s (a copy of 4 GiB by the vendor's library 4.9), into an fp8 cache and read back 64, 4.4; one token 4.0 us; 40276 fp8 tokens read 54 us, 4.6 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -17,7 +17,7 @@
 // 19.8 / 23.5 / 23.4.  Pieces for 1024 or 1536 / ranges: 64 of 33 to 16384 keys, fp8, 86 / 79, bf16 154 / 142; 16 of 33 to 30000 71 / 62; 300 of 1 to 2000, 4 heads, 61 / 53; 100000 keys
 // beside three short sequences 88 / 80.
 //
-// Measured (us, TB/s): 131071 keys 90, 6.0; the same in fp8 50, 5.4; 128 sequences of 3000 keys 249, 6.3; 64 of 33 to 16384, fp8, 79, 4.8; of one key 4.5.
+// Measured (us, TB/s): 131071 keys 86, 6.2; the same in fp8 50, 5.5; 128 sequences of 3000 keys 242, 6.5; 64 of 33 to 16384, fp8, 77, 4.9; of one key 4.5.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -283,6 +283,9 @@ __global__ __launch_bounds__(kWaves * 64, 3) void decode_piece(const DecodeArgs 
 #pragma unroll
                 for (int i = 0; i < 8; ++i) p[i] *= power(st.vs[i / 4], i % 4);
             }
+            // Weights to bf16, as the values beside them in the product are: half a step, and errors against 64 bits 1.1 to 1.4 times those of fp32 weights (131071 keys:
+            // 2.3e-3 of the outputs' size to 1.7e-3, which is what rounding the outputs alone leaves).  A second product with what the rounding leaves would hide
+            // behind the loads; attn_prompt's weights have none, and a token is to see its context the same way in both.
             const u32x4 pf = {pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
             // tile (u, e): d = 64 u + VE * (lane % 16) + e
 #pragma unroll
@@ -493,7 +496,9 @@ __global__ __launch_bounds__(kWaves * 64, 3) void decode_piece(const DecodeArgs 
 }  // namespace
 
 hipError_t launch_decode(const DecodeArgs &a, hipStream_t s) {
-    // Whether the lengths that the table of pages has room for are enough for ranges.
+    // Whether the lengths that the table of pages has room for are enough for ranges.  Heads between 16 and 128 run as the next of 64 and 128, in pieces only: no
+    // configuration of this library has them, and more kernels were not built for them.  64 sequences of 33 to 16384 keys, bf16, heads of 128 134 us, 5.6 TB/s; of 112 158, 4.2;
+    // of 96 135, 4.2; of 80 132, 3.6; of 64 68, 5.6.
     const long steps = (((long)a.seq_pages << a.c.page_shift) + kWaves * kBlock - 1) / (kWaves * kBlock) + 1, heads = (long)a.c.Hk * group_tiles(a.Hq, a.c.Hk);
     const bool ranges = a.n_seqs > 1 && a.n_seqs * steps * heads > kRangeWgs * (kFewestRange - 1);
     const auto run = [&](auto dp, auto fp8) {

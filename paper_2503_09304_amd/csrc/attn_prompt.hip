@@ -14,12 +14,13 @@
 // 84 vector instructions, 16 of them exponentials (400 clocks).  Two workgroups share a CU: 2 waves on a SIMD.  On zeros the kernel runs at 1.27
 // PFLOP/s, on random values at 1.1, at 2.0 GHz instead of 2.4: the power limit, as for this library's other large products (a large product of the vendor's
 // library 1.19).  So what counts is clocks and energy: scores, weights and sums of three successive half tiles side by side (below), a maximum
-// that stays needs no rescaling (2^8 of room), 16x16x32 instructions (2.5 % over 32x32x16).  Steps from the first kernel, 16384 tokens, 32 heads on 8, us: 3864;
+// that stays needs no rescaling (2^8 of room), 16x16x32 instructions (2.5 % over 32x32x16).  Steps from the first kernel, 16384 tokens, 32 heads on 8, us, each on its day's box: 3864;
 // side by side 2494; no rescaling 2141; maxima behind the scores 2077; 16x16x32 2039; loads a tile ahead 2005; ends by wave 1979.
 // Kept out: two blocks of 32 queries a wave (LDS read half as often, but one wave a SIMD: 2300 at the time), rows padded instead of swizzled (2083, bank
 // conflicts), the sums' instructions in assembly into their own registers (2083), rescaling the sums half a tile later (2088).
 //
-// Measured (us, TFLOP/s): 16384 tokens, 32 heads of 128 on 8, 1983, 1109; 4096 144, 952; 3584 in 8 prompts 51; 16 heads of 64 608, 904; 17 tokens 6.7.
+// Measured (us, TFLOP/s; boxes differ by 3 %): 16384 tokens, 32 heads of 128 on 8, 2000 to 2050, 1100 to 1072; 4096 147, 937; 3584 in 8 prompts 46 to 48; 16 heads of 64
+// on as many 608 to 622, 904; 17 tokens 6.9.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -297,6 +298,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prompt_tile(const PromptArgs a
             const int q = i / 8, t = i % 8 / 4, r = i % 4;
             cur[q][t][r] = __builtin_amdgcn_exp2f(fmaf(cur[q][t][r], a.scale_log2, -base[q]));
             l[q] += cur[q][t][r];
+            // To bf16, as the values beside them in the product are: half a step, and errors against 64 bits 1.3 times those of fp32 weights (16384 tokens:
+            // 2.1e-3 of the outputs' size to 1.6e-3, which is what rounding the outputs alone leaves).  A product with what the rounding leaves would be half
+            // as many matrix instructions again where these are the bound.
             if (r & 1) p_cur[q][2 * t + r / 2] = pack_bf16(cur[q][t][r - 1], cur[q][t][r]);
         };
         static_for<LA>(read);
@@ -490,6 +494,8 @@ int prompt_parts(int n_seqs, int n_q, int n_k, int Hq, int Hk, int D) {
     return (int)std::max(1l, std::min((f * each + share / 2) / share, 16l));
 }
 
+// Heads between run as the next of 64 and 128, their missing elements as zeros that are multiplied too: 16384 tokens, 32 heads on 8, 2010 us with heads of 128, 1971 of 96,
+// 1957 of 80.  No configuration of this library has others, and kernels of their own were not built for them.
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t s) {
     if (a.D <= 64) prompt_n<64>(a, s);
     else prompt_n<128>(a, s);

@@ -8,9 +8,11 @@ prompts marked LS, time to first token, turnaround time, job completion rate).
 
 What is modelled.  A model is `layers` MoE layers.  Everything between two MoE layers (in a real
 model the attention block and the residual) and the source of the hidden states are not part of this
-library: the caller passes a `glue` object that supplies them (serve_glue.py at the repository root
+loop: the caller passes a `glue` object that supplies them (serve_glue.py at the repository root
 is the synthetic one the benchmark and the tests use: rows of a seeded bank as hidden states, x + y
-as the stand-in for the block between layers).  This module only drives the scheduler and the layer
+as the stand-in for the block between layers).  The library's attention calls (include/qattn.h) need to
+know sequences and positions, which this loop does not hand to the glue: decoder_example.py has them
+between MoE layers.  This module only drives the scheduler and the layer
 calls; PyTorch appears in it for device buffers, events and host-to-device copies of index arrays.
 A prefill iteration runs all prompt tokens of the batch's jobs through the stack and yields each
 job's first token; a decode iteration runs one token per job.
@@ -36,7 +38,7 @@ Two policies share all of that code:
     until all its jobs are done before the next prompts are taken; control returns to the scheduler
     only between iterations.
 Per-row results never depend on the policy (same contexts' configurations, deterministic kernels),
-which `digest=True` lets a test check bit for bit.
+which `digest=True` lets a test check bit for bit, with a glue whose rows do not depend on one another.
 """
 from __future__ import annotations
 
