@@ -23,7 +23,8 @@
  *    cut, and so the order of its sums, goes by all lengths of the call (attn_decode, and attn_prompt with a workspace).  attn_prompt without a workspace
  *    cuts nothing: there a sequence's bits are the same whatever stands beside it.
  *  - Calls of no tokens (queries, sequences) do nothing and look at no pointer of theirs but the cache's.
- *  - Tokens that take part are assumed finite.  What lies beside them (slots of a page that no token was written to, rows between
+ *  - Tokens that take part are assumed finite.  (A value that is not reaches, in a causal prompt, also queries of its sequence that stand
+ *    fewer than 128 tokens before it: their weight for it is 0, and 0 times it is NaN.)  What lies beside them (slots of a page that no token was written to, rows between
  *    strides) may hold anything, NaN included, and reaches no output.
  *  - Numbers on the device (seq, pos, pages, lens, cu) cannot be checked by the host.  The kernels check them: what they do with
  *    one that is out of range is said at each call; nothing is read or written out of bounds, and *bad ([device] int32, may be NULL),
