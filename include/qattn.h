@@ -24,8 +24,8 @@
  *    cuts nothing: there a sequence's bits are the same whatever stands beside it.
  *  - Calls of no tokens (queries, sequences) do nothing and look at no pointer of theirs but the cache's.
  *  - Tokens that take part are assumed finite.  (A value that is not reaches, in a causal prompt, also queries of its sequence that stand
- *    fewer than 128 tokens before it: their weight for it is 0, and 0 times it is NaN.)  What lies beside them (slots of a page that no token was written to, rows between
- *    strides) may hold anything, NaN included, and reaches no output.
+ *    fewer than 128 tokens before it: their weight for it is 0, and 0 times it is NaN.)  What lies beside them (slots of a page that
+ *    no token was written to, rows between strides) may hold anything, NaN included, and reaches no output.
  *  - Numbers on the device (seq, pos, pages, lens, cu) cannot be checked by the host.  The kernels check them: what they do with
  *    one that is out of range is said at each call; nothing is read or written out of bounds, and *bad ([device] int32, may be NULL),
  *    which the caller has set to 0, counts them.
@@ -40,7 +40,8 @@ extern "C" {
 #endif
 
 /* Rows of heads: element d of head h of token t is data[t * token_stride + h * head_stride + d].  Strides in elements, multiples
- * of 8 and not negative; data 16-byte aligned.  So q, k and v may be slices of the rows of one product. */
+ * of 8 and not negative; data 16-byte aligned.  So q, k and v may be slices of the rows of one product, or, with a stride of 0, one row
+ * for all tokens or heads; the rows of an output are apart. */
 typedef struct {
     void *data; /* [device] bf16 */
     int64_t token_stride;
