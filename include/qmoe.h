@@ -183,6 +183,31 @@ int32_t moe_pack_weights(const moe_config *cfg, const moe_weights *src, moe_weig
 int32_t moe_route(moe_ctx *ctx, const void *x, int32_t n_tokens, const moe_weights *w,
                   const float *logit_bias, void *stream);
 
+/* The router with scores, a bias for the choice alone, and groups of experts: other rules by which models with many experts
+ * choose (load is balanced through choice_bias; groups keep a token's experts on few devices).
+ *   l[e] = sum_h x[n,h]*Wg[h,e] + logit_bias[e]                                  (fp32 accumulation; MOE_GET_LOGITS)
+ *   s[e] = 1 / (1 + exp(-l[e]))  or  exp(l[e]) / sum_e' exp(l[e'])               (MOE_SCORE_SIGMOID, _SOFTMAX)
+ *   v[e] = s[e] + choice_bias[e]
+ *   a group (E / groups consecutive experts) is worth the sum of its group_best largest v; only the top_groups groups that are worth most count
+ *   slot j of token n = j-th of their experts in the order (v descending, expert index ascending)
+ *   w[n,j] = factor * s_j / sum_{i<k} s_i   or, without renormalise,   factor * s_j
+ * Scores and all that follows are computed in 64 bits from the fp32 logits, w rounded to fp32 once: what is chosen does not hang on the last bits of an
+ * exponential.  Groups worth the same go by their index.  A value that is NaN counts less than any number, one of -inf (a choice_bias of
+ * -inf bars an expert) less than any other: such experts are chosen where nothing else is left.  Where all chosen scores are 0 and
+ * renormalise is set, w[n,j] = factor / k.
+ * groups: 1..64, a divisor of E; top_groups 1..groups; group_best 1..4, at most E / groups; k at most top_groups * E / groups (each refused with MOE_E_ARG);
+ * factor finite.  logit_bias, choice_bias [device] float[E] or NULL.  Everything else as moe_route; moe_permute and what follows are the same. */
+enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 };
+typedef struct {
+    int32_t score;            /* MOE_SCORE_x */
+    const float *logit_bias;
+    const float *choice_bias;
+    int32_t groups, top_groups, group_best;
+    int32_t renormalise;
+    float factor;
+} moe_scoring;
+int32_t moe_route_scored(moe_ctx *ctx, const void *x, int32_t n_tokens, const moe_weights *w, const moe_scoring *scoring, void *stream);
+
 /* The router for callers that cannot allocate: code under HIP graph capture, tight serving loops,
  * harnesses that forbid hipMalloc.  Same results as moe_route with row-major weights, bit for bit, but
  * no context, no workspace and no allocation of any kind (device, pinned or host): the one scratch

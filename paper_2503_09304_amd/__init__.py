@@ -39,6 +39,7 @@ from .binding import (  # noqa: F401
     MoeConfig,
     MoeCursor,
     MoeError,
+    MoeScoring,
     MoeUnit,
     MoeWeights,
     SchedBatch,
@@ -54,14 +55,19 @@ from .binding import (  # noqa: F401
     moe_workspace_bytes,
 )
 
-# The attention calls (include/qattn.h) work on torch tensors; their module, and torch with it, is imported at first use.
+# The attention calls (include/qattn.h) and the dense calls (include/qdense.h) work on torch tensors; their modules, and torch with them, are imported at
+# first use.
 _ATTENTION = ("ATTN_BF16", "ATTN_FP8", "AttnCache", "AttnRope", "attn_append", "attn_decode", "attn_decode_workspace", "attn_prompt", "attn_read",
               "attn_rope_frequencies")
+_DENSE = ("DenseMatrix4", "dense_linear", "dense_norm")
 
 
 def __getattr__(name):
-    if name not in _ATTENTION:
+    if name in _ATTENTION:
+        from . import attention as module
+    elif name in _DENSE:
+        from . import dense as module
+    else:
         raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
-    from . import attention
-    value = globals()[name] = getattr(attention, name)
+    value = globals()[name] = getattr(module, name)
     return value

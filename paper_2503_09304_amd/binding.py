@@ -43,6 +43,11 @@ class MoeUnit(C.Structure):
     _fields_ = [("expert", C.c_int32), ("cls", C.c_int32), ("row0", C.c_int32), ("rows", C.c_int32)]
 
 
+class _Scoring(C.Structure):
+    _fields_ = [("score", C.c_int32), ("logit_bias", C.c_void_p), ("choice_bias", C.c_void_p), ("groups", C.c_int32),
+                ("top_groups", C.c_int32), ("group_best", C.c_int32), ("renormalise", C.c_int32), ("factor", C.c_float)]
+
+
 class MoeError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"qmoe error {code}: {msg}")
@@ -93,6 +98,7 @@ def lib():
         L.moe_route_noalloc.argtypes = [C.POINTER(MoeConfig), C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
                                         C.c_void_p, C.c_void_p, C.c_void_p]
         L.moe_route.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.POINTER(MoeWeights), C.c_void_p, C.c_void_p]
+        L.moe_route_scored.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.POINTER(MoeWeights), C.POINTER(_Scoring), C.c_void_p]
         L.moe_permute.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(MoeCursor), C.c_void_p]
         L.moe_expert_run.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(MoeWeights), C.c_uint32,
                                      C.POINTER(MoeCursor), C.c_void_p]
@@ -110,7 +116,7 @@ def lib():
         L.moe_pack_weights.argtypes = [C.POINTER(MoeConfig), C.POINTER(MoeWeights), C.POINTER(MoeWeights), C.c_void_p]
         L.moe_profile.argtypes = [C.c_void_p, C.c_int32]
         L.moe_profile_read.argtypes = [C.c_void_p, C.POINTER(C.c_float), C.POINTER(C.c_uint32)]
-        for f in ("moe_expert_enqueue", "moe_expert_stop", "moe_expert_collect", "moe_expert_run_units", "moe_combine_complete", "moe_pack_weights", "moe_profile", "moe_profile_read", "moe_create", "moe_destroy", "moe_route", "moe_permute", "moe_expert_run", "moe_combine",
+        for f in ("moe_expert_enqueue", "moe_expert_stop", "moe_expert_collect", "moe_expert_run_units", "moe_combine_complete", "moe_pack_weights", "moe_profile", "moe_profile_read", "moe_create", "moe_destroy", "moe_route", "moe_route_scored", "moe_permute", "moe_expert_run", "moe_combine",
                   "moe_get", "moe_units", "moe_plan_units"):
             getattr(L, f).restype = C.c_int32
         # include/qsched.h
@@ -176,6 +182,24 @@ def _stream() -> int:
     return int(torch.cuda.current_stream().cuda_stream)
 
 
+class MoeScoring:
+    """How Context.route_scored chooses (moe_scoring of include/qmoe.h).  logit_bias, choice_bias: float32 tensors [E] on the context's
+    GPU, or None; they are looked at when the router runs."""
+
+    SCORES = {"softmax": 0, "sigmoid": 1}
+
+    def __init__(self, score: str = "softmax", logit_bias=None, choice_bias=None, groups: int = 1, top_groups: int = 1, group_best: int = 1,
+                 renormalise: bool = True, factor: float = 1.0):
+        import torch
+        if score not in self.SCORES:
+            raise MoeError(MOE_E_ARG, f"score must be one of {', '.join(self.SCORES)}")
+        for name, b in (("logit_bias", logit_bias), ("choice_bias", choice_bias)):
+            if b is not None and (b.dtype is not torch.float32 or b.dim() != 1 or not b.is_cuda or not b.is_contiguous()):
+                raise MoeError(MOE_E_ARG, f"{name} must be a dense float32 tensor [E] on the GPU")
+        self.logit_bias, self.choice_bias = logit_bias, choice_bias
+        self._c = _Scoring(self.SCORES[score], _ptr(logit_bias), _ptr(choice_bias), groups, top_groups, group_best, 1 if renormalise else 0, factor)
+
+
 class Context:
     """One in-flight layer-batch: the opaque moe_ctx plus the torch tensor that backs its workspace.
     Methods are the C calls with tensors in place of pointers.  The stream of every call is PyTorch's
@@ -223,6 +247,18 @@ class Context:
     def route(self, x, w: MoeWeights, bias=None, n_tokens=None):
         n = x.shape[0] if n_tokens is None else n_tokens
         rc = _check(lib().moe_route(self.h, _ptr(x), n, C.byref(w), _ptr(bias), self._stream()))
+        self.N, self._w = n, w
+        return rc
+
+    def route_scored(self, x, w: MoeWeights, scoring: MoeScoring, n_tokens=None):
+        """The router by scores, a bias for the choice alone, and groups of experts."""
+        E = self.cfg.E
+        for name in ("logit_bias", "choice_bias"):
+            b = getattr(scoring, name)
+            if b is not None and (b.shape[0] != E or b.device != self.ws.device):
+                raise MoeError(MOE_E_ARG, f"{name} must have {E} elements on {self.ws.device}")
+        n = x.shape[0] if n_tokens is None else n_tokens
+        rc = _check(lib().moe_route_scored(self.h, _ptr(x), n, C.byref(w), C.byref(scoring._c), self._stream()))
         self.N, self._w = n, w
         return rc
 

@@ -314,18 +314,17 @@ int32_t moe_destroy(moe_ctx *ctx) {
     return MOE_OK;
 }
 
-int32_t moe_route(moe_ctx *ctx, const void *x, int32_t n_tokens, const moe_weights *w, const float *logit_bias,
-                  void *stream) {
-    if (!ctx) return fail(MOE_E_ARG, "moe_route: null context");
-    if (ctx->pending) return fail(MOE_E_STATE, "moe_route: an enqueued launch sequence is pending; call moe_expert_collect first");
+static int32_t route(const char *call, moe_ctx *ctx, const void *x, int32_t n_tokens, const moe_weights *w, const float *logit_bias,
+                     const moe_scoring *scoring, void *stream) {
+    if (ctx->pending) return fail(MOE_E_STATE, "%s: an enqueued launch sequence is pending; call moe_expert_collect first", call);
     if (n_tokens < 0 || n_tokens > ctx->cfg.max_tokens)
-        return fail(MOE_E_ARG, "moe_route: n_tokens %d outside 0..%d", n_tokens, ctx->cfg.max_tokens);
-    if (!w || !w->Wg || !w->W1 || !w->W3 || !w->W2) return fail(MOE_E_ARG, "moe_route: null weight pointer");
+        return fail(MOE_E_ARG, "%s: n_tokens %d outside 0..%d", call, n_tokens, ctx->cfg.max_tokens);
+    if (!w || !w->Wg || !w->W1 || !w->W3 || !w->W2) return fail(MOE_E_ARG, "%s: null weight pointer", call);
     if (w->layout != MOE_W_ROWMAJOR && w->layout != MOE_W_PACKED && w->layout != MOE_W_MXFP4)
-        return fail(MOE_E_ARG, "moe_route: weight layout %d is not one the kernels read (row-major 4-bit weights go through moe_pack_weights)", w->layout);
-    if (w->layout != MOE_W_ROWMAJOR && ctx->cfg.dtype != MOE_BF16) return fail(MOE_E_ARG, "moe_route: packed weights are bf16 only");
-    if (w->layout == MOE_W_MXFP4 && (!w->S1 || !w->S3 || !w->S2)) return fail(MOE_E_ARG, "moe_route: 4-bit weights need the scale pointers S1, S3, S2");
-    if (n_tokens > 0 && !x) return fail(MOE_E_ARG, "moe_route: null x");
+        return fail(MOE_E_ARG, "%s: weight layout %d is not one the kernels read (row-major 4-bit weights go through moe_pack_weights)", call, w->layout);
+    if (w->layout != MOE_W_ROWMAJOR && ctx->cfg.dtype != MOE_BF16) return fail(MOE_E_ARG, "%s: packed weights are bf16 only", call);
+    if (w->layout == MOE_W_MXFP4 && (!w->S1 || !w->S3 || !w->S2)) return fail(MOE_E_ARG, "%s: 4-bit weights need the scale pointers S1, S3, S2", call);
+    if (n_tokens > 0 && !x) return fail(MOE_E_ARG, "%s: null x", call);
     if (!ctx->pinned) {
         const size_t words = stop_word(ctx) + (size_t)qmoe::kStopCopies * qmoe::kStopStride;
         hipError_t e = hipHostMalloc((void **)&ctx->pinned, words * sizeof(int32_t), hipHostMallocMapped | hipHostMallocCoherent);
@@ -340,6 +339,7 @@ int32_t moe_route(moe_ctx *ctx, const void *x, int32_t n_tokens, const moe_weigh
     }
     if (n_tokens > 0) {
         qmoe::RouteArgs a{};
+        a.scoring = scoring;
         a.x = x; a.Wg = w->Wg; a.bias = logit_bias;
         a.WgT = at<void>(ctx, ctx->lay.wgt);
         a.parts = at<float>(ctx, ctx->lay.parts);
@@ -363,6 +363,27 @@ int32_t moe_route(moe_ctx *ctx, const void *x, int32_t n_tokens, const moe_weigh
     ctx->done_valid = false;
     ctx->cnt.assign(2 * (size_t)ctx->cfg.E, 0);
     return MOE_OK;
+}
+
+int32_t moe_route(moe_ctx *ctx, const void *x, int32_t n_tokens, const moe_weights *w, const float *logit_bias, void *stream) {
+    if (!ctx) return fail(MOE_E_ARG, "moe_route: null context");
+    return route("moe_route", ctx, x, n_tokens, w, logit_bias, nullptr, stream);
+}
+
+int32_t moe_route_scored(moe_ctx *ctx, const void *x, int32_t n_tokens, const moe_weights *w, const moe_scoring *scoring, void *stream) {
+    const char *call = "moe_route_scored";
+    if (!ctx || !scoring) return fail(MOE_E_ARG, "%s: null context or scoring", call);
+    const moe_scoring &c = *scoring;
+    const int32_t E = ctx->cfg.E;
+    if (c.score != MOE_SCORE_SOFTMAX && c.score != MOE_SCORE_SIGMOID) return fail(MOE_E_ARG, "%s: unknown score", call);
+    if (c.groups < 1 || c.groups > qmoe::kMaxGroups || E % c.groups) return fail(MOE_E_ARG, "%s: groups must be 1..%d and divide E", call, qmoe::kMaxGroups);
+    const int32_t size = E / c.groups;
+    if (c.top_groups < 1 || c.top_groups > c.groups) return fail(MOE_E_ARG, "%s: top_groups must be 1..groups", call);
+    if (c.group_best < 1 || c.group_best > qmoe::kMaxGroupBest || c.group_best > size)
+        return fail(MOE_E_ARG, "%s: group_best must be 1..%d, at most E / groups", call, qmoe::kMaxGroupBest);
+    if (ctx->cfg.k > c.top_groups * size) return fail(MOE_E_ARG, "%s: top_groups * E / groups experts are fewer than k", call);
+    if (!std::isfinite(c.factor)) return fail(MOE_E_ARG, "%s: factor is not finite", call);
+    return route(call, ctx, x, n_tokens, w, c.logit_bias, scoring, stream);
 }
 
 int32_t moe_permute(moe_ctx *ctx, const uint8_t *prio, moe_cursor *cursor, void *stream) {

@@ -15,6 +15,8 @@ constexpr int kPermBlock = 1024;  // assignments ranked by one workgroup of the 
 constexpr int kMaxExperts = 256;  // 2*E bucket counters of a 16-wave workgroup must fit in LDS
 constexpr int kMaxTopK = 32;
 constexpr int kMaxChunkRows = 256;
+constexpr int kMaxGroups = 64;    // of experts (moe_scoring): a lane each
+constexpr int kMaxGroupBest = 4;
 
 // A launch of at most this many row segments carries them in its kernel arguments (and may merge
 // row-adjacent units of one expert into one segment); larger launches read the device unit list.
@@ -38,6 +40,7 @@ struct RouteArgs {
     float *topk_w;
     int N, H, E, k, dtype;
     bool packed;  // Wg already transposed and padded ([E16][H])
+    const moe_scoring *scoring;   // moe_route_scored, else nullptr
 };
 // The bf16 router in two launches, its GEMM dealt out in 8 K ranges to workgroups of their own: where one workgroup per
 // 16 tokens leaves CUs idle while each takes in all the weights.  One launch takes a wave's share of K (H / 256 MFMA steps)
@@ -62,6 +65,8 @@ inline size_t gate_parts_floats(int max_tokens, int E) {
     return (n + 15) / 16 * 8 * (size_t)((E + 15) / 16) * 256;
 }
 hipError_t launch_route(const RouteArgs &a, hipStream_t s);
+// The choice of moe_route_scored from logits that are there.
+hipError_t launch_score(const RouteArgs &a, hipStream_t s);
 
 // Records the text moe_last_error() returns on this thread and hands `code` back (printf-style).
 int32_t set_error(int32_t code, const char *fmt, ...);

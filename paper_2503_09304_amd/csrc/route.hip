@@ -431,7 +431,8 @@ hipError_t launch_route(const RouteArgs &a, hipStream_t s) {
         else if (a.E % 4 == 0) hipLaunchKernelGGL((gate_topk_f32<4, true>), g, b, 0, s, x, wg, a.bias, a.logits, a.topk_idx, a.topk_w, a.N, a.H, a.E, a.k);
         else hipLaunchKernelGGL((gate_topk_f32<8, false>), g, b, 0, s, x, wg, a.bias, a.logits, a.topk_idx, a.topk_w, a.N, a.H, a.E, a.k);
     }
-    return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess && a.scoring != nullptr ? launch_score(a, s) : e;
 }
 
 }  // namespace qmoe
