@@ -17,140 +17,147 @@
 namespace qdense {
 namespace {
 
-// A lane's part of 16 tokens by 128 columns: 32 columns of one token, zero behind the last one.
-template <int XT>
-struct XTile {
-    u32x4 v[XT == X_BF16 ? 4 : 2];
-    uint32_t byte;
-    // row: of this lane's token; k: first column of the tile
-    __device__ __forceinline__ void load(const char *row, const uint8_t *scale, int k, int g, int K) {
-        const u32x4 zero = {0, 0, 0, 0};
-        const int mine = k + 32 * g;
-        const bool in = mine < K;
-        if constexpr (XT == X_BF16) {
-            const u32x4 *from = reinterpret_cast<const u32x4 *>(row + 2 * (in ? mine : 0));
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const u32x4 r = from[s];
-                v[s] = in ? r : zero;
-            }
-        } else {
-            byte = scale[(in ? mine : 0) / 32];
-            byte = in ? byte : 127;
-            if constexpr (XT == X_FP8) {          // the scaled instruction's 8-bit operand: columns 16 g .. and 64 + 16 g ..
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const int at = k + 64 * s + 16 * g;
-                    const u32x4 r = *reinterpret_cast<const u32x4 *>(row + (at < K ? at : 0));
-                    v[s] = at < K ? r : zero;
-                }
-            } else {
-                const u32x4 *from = reinterpret_cast<const u32x4 *>(row + (in ? mine : 0));
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const u32x4 r = from[s];
-                    v[s] = in ? r : zero;
-                }
-            }
-        }
-    }
-    __device__ __forceinline__ bf16x8 step(int s) const {
-        if constexpr (XT == X_BF16) return __builtin_bit_cast(bf16x8, v[s]);
-        else return widened8(v[s / 2][2 * (s % 2)], v[s / 2][2 * (s % 2) + 1], power(byte));
-    }
-};
+// Few tokens: bound by the matrix.  Each wave has RB tiles of 16 rows and a slice of the columns, and streams its part of the matrix, D tiles ahead of their
+// use; KS waves of a workgroup share rows and add their sums in LDS.  The tokens' columns of the workgroup's range are in LDS from the start, 16-byte pieces
+// in the places that read() says, so that the lanes of one read use all banks.
+constexpr int kWaves = 8;
 
-// acc += w x of one tile of the matrix.
-template <int XT, int NT>
-__device__ __forceinline__ void multiply(f32x4 (&acc)[NT], const u32x4 &w, uint32_t wbyte, const XTile<XT> (&x)[NT]) {
-    if constexpr (XT == X_FP8) {
-        const i32x8 a = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const i32x8 b = {(int)x[n].v[0][0], (int)x[n].v[0][1], (int)x[n].v[0][2], (int)x[n].v[0][3],
-                             (int)x[n].v[1][0], (int)x[n].v[1][1], (int)x[n].v[1][2], (int)x[n].v[1][3]};
-            acc[n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc[n], 4, 0, 0, (int)wbyte, 0, (int)x[n].byte);
-        }
-    } else {
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const bf16x8 a = weights8(w[s], power(wbyte));
-#pragma unroll
-            for (int n = 0; n < NT; ++n) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, x[n].step(s), acc[n], 0, 0, 0);
-        }
-    }
-}
-
-// Few tokens: bound by the matrix.  A workgroup has RB * 16 rows, NT * 16 tokens and a range of columns, which its W waves share
-// out; their sums meet in LDS.
-template <int XT, int NT, int RB, int W>
-__global__ __launch_bounds__(64 * W) void linear_few(const LinearArgs a) {
-    __shared__ f32x4 red[W][RB * NT][64];
-    const int w = threadIdx.x >> 6, l = threadIdx.x & 63, g = l >> 4;
-    const int blocks = (a.K + 127) / 128, sets = (a.K + 511) / 512, row_tiles = (a.R + 15) / 16;
-    const int per_range = (blocks + a.ranges - 1) / a.ranges, from = min(blocks, (int)blockIdx.z * per_range), to = min(blocks, from + per_range);
-    const int per = (to - from + W - 1) / W, b0 = min(to, from + w * per), b1 = min(to, b0 + per);
-    const int rt = blockIdx.x * RB, t0 = blockIdx.y * (NT * 16);
-    const char *row[NT];
-    const uint8_t *scale[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const long t = min(t0 + n * 16 + (l & 15), a.n_tokens - 1);
-        row[n] = a.x.p + t * a.x.ts * (XT == X_BF16 ? 2 : 1);
-        scale[n] = a.x.scale + t * (a.K / 32);
-    }
+template <int XT, int NT, int RB, int KS, int D>
+__global__ __launch_bounds__(64 * kWaves) void linear_few(const LinearArgs a, long first_wg, int range_blocks) {
+    extern __shared__ __align__(16) char lds[];
+    constexpr int PIECES = XT == X_BF16 ? 16 : 8;        // of 16 bytes, in a token's 128 columns
+    constexpr int GROUPS = kWaves / KS;
+    const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, g = l >> 4;
+    const int blocks = (a.K + 127) / 128, sets = (a.K + 511) / 512, row_tiles = (a.R + 15) / 16, row_wgs = (row_tiles + GROUPS * RB - 1) / (GROUPS * RB);
+    long wg = first_wg + blockIdx.x;
+    const int z = (int)(wg % a.ranges);
+    wg /= a.ranges;
+    const int rt = (int)(wg % row_wgs) * (GROUPS * RB) + w / KS * RB, t0 = (int)(wg / row_wgs) * (NT * 16);
+    const int from = z * range_blocks, n_blocks = min(blocks, from + range_blocks) - from, n_tok = min(NT * 16, a.n_tokens - t0);
+    const int per = (n_blocks + KS - 1) / KS, s0 = min(n_blocks, w % KS * per), s1 = min(n_blocks, s0 + per);
     const uint8_t *codes[RB], *scales[RB];
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
         const long tile = min(rt + r, row_tiles - 1);
-        codes[r] = a.codes + tile * blocks * 1024 + l * 16;
+        codes[r] = a.codes + (tile * blocks + from) * 1024 + l * 16;
         scales[r] = a.scales + tile * sets * 256 + l * 4;
     }
-    f32x4 acc[RB][NT];
+    u32x4 c[D][RB];
+    uint32_t sc[D][RB];
+    const auto ask = [&](int u, int b) {
 #pragma unroll
-    for (int r = 0; r < RB; ++r)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc[r][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    constexpr int U = NT == 1 ? 4 : NT == 2 ? 2 : 1;
-    for (int b = b0; b < b1; b += U) {
-        u32x4 c[U][RB];
-        uint32_t sc[U][RB];
-        XTile<XT> x[U][NT];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int at = min(b + u, b1 - 1);
-#pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                c[u][r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(codes[r] + (long)at * 1024));
-                sc[u][r] = *reinterpret_cast<const uint32_t *>(scales[r] + (at >> 2) * 256) >> 8 * (at & 3) & 255;
-            }
-#pragma unroll
-            for (int n = 0; n < NT; ++n) x[u][n].load(row[n], scale[n], at * 128, g, a.K);
+        for (int r = 0; r < RB; ++r) {
+            c[u][r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(codes[r] + (long)b * 1024));
+            sc[u][r] = *reinterpret_cast<const uint32_t *>(scales[r] + ((from + b) >> 2) * 256);
         }
+    };
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (b + u < b1) {
-#pragma unroll
-                for (int r = 0; r < RB; ++r) multiply<XT, NT>(acc[r], c[u][r], sc[u][r], x[u]);
+    for (int u = 0; u < D; ++u)
+        if (s0 + u < s1) ask(u, s0 + u);
+    // Tokens to LDS.
+    const int row = n_blocks * PIECES * 16;              // bytes of a token there
+    uint8_t *xb = reinterpret_cast<uint8_t *>(lds) + (n_tok * row + 1023) / 1024 * 1024;       // the last wave's load may write up to there
+    {
+        const int pieces = n_tok * n_blocks * PIECES, k_pieces = a.K / (XT == X_BF16 ? 8 : 16);
+        for (int i0 = w * 64; i0 < pieces; i0 += 64 * kWaves) {
+            const int i = min(i0 + l, pieces - 1), t = i / (n_blocks * PIECES), p = i - t * (n_blocks * PIECES), b = p / PIECES;
+            const int q = XT == X_BF16 ? (p ^ t) & 15 : (p ^ t >> 1) & 7;
+            const int piece = (from + b) * PIECES + (XT == X_BF16 ? 4 * (q & 3) + (q >> 2) : XT == X_FP8 ? q : 2 * (q & 3) + (q >> 2));
+            to_lds(a.x.p + (t0 + t) * a.x.ts * (XT == X_BF16 ? 2 : 1) + (piece < k_pieces ? piece : 0) * 16, lds + i0 * 16);       // behind the last column weights are zero
+        }
+        if constexpr (XT != X_BF16) {
+            const int n = a.K / 32;
+            for (int i = tid; i < n_tok * n_blocks * 4; i += 64 * kWaves) {
+                const int t = i / (n_blocks * 4), k = from * 4 + i - t * (n_blocks * 4);
+                xb[i] = a.x.scale[(long)(t0 + t) * n + min(k, n - 1)];
             }
+        }
+    }
+    f32x4 acc[RB][NT];
+    int at[NT], sw[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int t = min(n * 16 + (l & 15), n_tok - 1);
+        at[n] = t * row;
+        sw[n] = XT == X_BF16 ? ((t & 15) ^ g) * 16 : ((t >> 1 & 7) ^ g) * 16;
+#pragma unroll
+        for (int r = 0; r < RB; ++r) acc[r][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // this wave's pieces are in LDS
+    __syncthreads();
+    for (int b0 = s0; b0 < s1; b0 += D) {
+#pragma unroll
+        for (int u = 0; u < D; ++u) {
+            const int b = b0 + u;
+            if (b >= s1) break;
+            const int shift = 8 * ((from + b) & 3);
+            if constexpr (XT == X_FP8) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const u32x4 lo = *reinterpret_cast<const u32x4 *>(lds + at[n] + b * 128 + sw[n]);
+                    const u32x4 hi = *reinterpret_cast<const u32x4 *>(lds + at[n] + b * 128 + (sw[n] ^ 64));
+                    const int byte = xb[at[n] / 32 + b * 4 + g];
+                    const i32x8 v = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) {
+                        const i32x8 wv = {(int)c[u][r][0], (int)c[u][r][1], (int)c[u][r][2], (int)c[u][r][3], 0, 0, 0, 0};
+                        acc[r][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, v, acc[r][n], 4, 0, 0, (int)(sc[u][r] >> shift & 255), 0, byte);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    bf16x8 wv[RB];
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) wv[r] = weights8(c[u][r][s], power(sc[u][r] >> shift & 255));
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        bf16x8 v;
+                        if constexpr (XT == X_BF16) {
+                            v = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(lds + at[n] + b * 256 + (sw[n] ^ 64 * s)));
+                        } else {
+                            const u32x2 o = *reinterpret_cast<const u32x2 *>(lds + at[n] + b * 128 + (sw[n] ^ 64 * (s >> 1)) + 8 * (s & 1));
+                            v = widened8(o[0], o[1], power(xb[at[n] / 32 + b * 4 + g]));
+                        }
+#pragma unroll
+                        for (int r = 0; r < RB; ++r) acc[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[r], v, acc[r][n], 0, 0, 0);
+                    }
+                }
+            }
+            if (b + D < s1) ask(u, b + D);
+        }
+    }
+    if constexpr (KS > 1) {
+        f32x4 *red = reinterpret_cast<f32x4 *>(lds);
+        __syncthreads();                                 // the tokens have been read
+        if (w % KS)
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) red[(w * (RB * NT) + r * NT + n) * 64 + l] = acc[r][n];
+        __syncthreads();
+        if (w % KS) return;
+#pragma unroll 1
+        for (int k = 1; k < KS; ++k)
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const f32x4 o = red[((w + k) * (RB * NT) + r * NT + n) * 64 + l];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[r][n][e] += o[e];
+                }
     }
 #pragma unroll
-    for (int r = 0; r < RB; ++r)
+    for (int n = 0; n < NT; ++n) {
+        const int t = t0 + n * 16 + (l & 15);
+        if (t >= a.n_tokens) continue;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) red[w][r * NT + n][l] = acc[r][n];
-    __syncthreads();
-    for (int i = w; i < RB * NT; i += W) {
-        f32x4 v = red[0][i][l];
-#pragma unroll
-        for (int j = 1; j < W; ++j) {
-            const f32x4 o = red[j][i][l];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += o[e];
-        }
-        const int t = t0 + (i % NT) * 16 + (l & 15), r = (rt + i / NT) * 16 + g * 4;
-        if (t < a.n_tokens && r < a.R) {
-            if (a.ranges == 1) store4(a, t, r, v);
-            else *reinterpret_cast<f32x4 *>(a.part + ((long)blockIdx.z * a.n_tokens + t) * (row_tiles * 16l) + r) = v;
+        for (int r = 0; r < RB; ++r) {
+            const int o = (rt + r) * 16 + g * 4;
+            if (o >= a.R) continue;
+            if (a.ranges == 1) store4(a, t, o, acc[r][n]);
+            else *reinterpret_cast<f32x4 *>(a.part + ((long)z * a.n_tokens + t) * (row_tiles * 16l) + o) = acc[r][n];
         }
     }
 }
@@ -190,30 +197,66 @@ __global__ __launch_bounds__(256) void pack4(const uint8_t *codes, const uint8_t
     }
 }
 
+constexpr int kFewTokens = 128;
+constexpr size_t kMostLds = 128 * 1024;
+
 }  // namespace
 
-int linear_ranges(int n_tokens, int R, int K, int x_type, int out_type) { return 1; }
+// How a call of few tokens is cut: see Few below.
+struct Few {
+    int nt, rb, ks, ranges, range_blocks;
+    size_t lds;
+};
+static Few few_of(int n_tokens, int R, int K, bool bf16) {
+    const int blocks = (K + 127) / 128, row_tiles = (R + 15) / 16;
+    Few f{};
+    f.nt = n_tokens <= 16 ? 1 : n_tokens <= 32 ? 2 : 4;
+    f.rb = f.nt == 4 ? 2 : 1;
+    const int tokens = std::min(n_tokens, f.nt * 16), token_tiles = (n_tokens + f.nt * 16 - 1) / (f.nt * 16);
+    const size_t per_block = (size_t)tokens * (bf16 ? 256 : 132);
+    const int most = (int)std::min<size_t>(blocks, kMostLds / per_block);
+    f.ranges = (blocks + most - 1) / most;
+    const long units = (long)((row_tiles + f.rb - 1) / f.rb) * token_tiles;         // waves without a cut of the columns
+    while (f.nt == 4 && f.ranges < 16 && units * f.ranges * 8 < 8 * 256 && blocks / (2 * f.ranges) >= 4) f.ranges *= 2;
+    f.range_blocks = (blocks + f.ranges - 1) / f.ranges;
+    f.ranges = (blocks + f.range_blocks - 1) / f.range_blocks;
+    f.ks = 1;
+    while (f.ks < 8 && units * f.ranges * f.ks < 2048 && f.range_blocks >= 2 * f.ks) f.ks *= 2;
+    f.lds = std::max<size_t>((size_t)f.range_blocks * per_block + 1024, (size_t)(f.ks > 1 ? kWaves * f.rb * f.nt * 1024 : 0));
+    return f;
+}
+
+int linear_ranges(int n_tokens, int R, int K, int x_type, int) {
+    return n_tokens > kFewTokens ? 1 : few_of(n_tokens, R, K, x_type == DENSE_BF16).ranges;
+}
 
 hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
-    if (a.n_tokens > 128) return launch_linear_many(a, s);
+    if (a.n_tokens > kFewTokens) return launch_linear_many(a, s);
+    const Few f = few_of(a.n_tokens, a.R, a.K, a.x_type == DENSE_BF16);
+    if (f.ranges > a.ranges) return launch_linear_many(a, s);
     const int row_tiles = (a.R + 15) / 16;
-    const auto go = [&](auto xt, auto nt, auto rb, auto w) {
-        constexpr int RB = decltype(rb)::value, NT = decltype(nt)::value, W = decltype(w)::value;
-        linear_few<decltype(xt)::value, NT, RB, W><<<dim3((row_tiles + RB - 1) / RB, (a.n_tokens + NT * 16 - 1) / (NT * 16), a.ranges), dim3(64 * W), 0, s>>>(a);
+    const auto go = [&](auto xt, auto nt, auto ks) {
+        constexpr int XT = decltype(xt)::value, NT = decltype(nt)::value, KS = decltype(ks)::value, RB = NT == 4 ? 2 : 1, D = NT == 4 ? 4 : 8, PER = kWaves / KS * RB;
+        const long all = (long)((row_tiles + PER - 1) / PER) * ((a.n_tokens + NT * 16 - 1) / (NT * 16)) * f.ranges;
+        constexpr long kMost = 1 << 22;                  // workgroups of 512 threads that a launch may have
+        for (long at = 0; at < all; at += kMost)
+            linear_few<XT, NT, RB, KS, D><<<dim3((unsigned)std::min(kMost, all - at)), dim3(64 * kWaves), f.lds, s>>>(a, at, f.range_blocks);
+    };
+    const auto by_slices = [&](auto xt, auto nt) {
+        if (f.ks == 1) go(xt, nt, std::integral_constant<int, 1>{});
+        else if (f.ks == 2) go(xt, nt, std::integral_constant<int, 2>{});
+        else if (f.ks == 4) go(xt, nt, std::integral_constant<int, 4>{});
+        else go(xt, nt, std::integral_constant<int, 8>{});
     };
     const auto by_tokens = [&](auto xt) {
-        typedef std::integral_constant<int, 1> One;
-        typedef std::integral_constant<int, 2> Two;
-        typedef std::integral_constant<int, 4> Four;
-        typedef std::integral_constant<int, 8> Eight;
-        if (a.n_tokens <= 16) go(xt, One{}, One{}, Eight{});
-        else if (a.n_tokens <= 32) go(xt, Two{}, One{}, Eight{});
-        else go(xt, Four{}, Four{}, Four{});
+        if (f.nt == 1) by_slices(xt, std::integral_constant<int, 1>{});
+        else if (f.nt == 2) by_slices(xt, std::integral_constant<int, 2>{});
+        else by_slices(xt, std::integral_constant<int, 4>{});
     };
     if (a.x_type == DENSE_BF16) by_tokens(std::integral_constant<int, X_BF16>{});
     else if (a.out_type == DENSE_BF16) by_tokens(std::integral_constant<int, X_FP8>{});
     else by_tokens(std::integral_constant<int, X_WIDE>{});
-    if (a.ranges > 1) {
+    if (f.ranges > 1) {
         const long n = (long)a.n_tokens * row_tiles * 4;
         join_ranges<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s>>>(a);
     }
