@@ -197,43 +197,83 @@ __global__ __launch_bounds__(256) void pack4(const uint8_t *codes, const uint8_t
     }
 }
 
-constexpr int kFewTokens = 128;
 constexpr size_t kMostLds = 128 * 1024;
 
 }  // namespace
 
-// How a call of few tokens is cut: see Few below.
-struct Few {
-    int nt, rb, ks, ranges, range_blocks;
-    size_t lds;
+// How a call is cut into workgroups.
+struct Plan {
+    bool many;
+    int tiles;                    // of 16 tokens, a workgroup's
+    int ks;                       // few: waves that share rows
+    int ranges, range_blocks;     // of 128 columns
+    size_t lds;                   // few
 };
-static Few few_of(int n_tokens, int R, int K, bool bf16) {
+static void cut(Plan &p, int blocks, int ranges) {
+    p.range_blocks = (blocks + ranges - 1) / ranges;
+    p.ranges = (blocks + p.range_blocks - 1) / p.range_blocks;
+}
+static Plan few_of(int n_tokens, int R, int K, bool bf16, int ranges) {
     const int blocks = (K + 127) / 128, row_tiles = (R + 15) / 16;
-    Few f{};
-    f.nt = n_tokens <= 16 ? 1 : n_tokens <= 32 ? 2 : 4;
-    f.rb = f.nt == 4 ? 2 : 1;
-    const int tokens = std::min(n_tokens, f.nt * 16), token_tiles = (n_tokens + f.nt * 16 - 1) / (f.nt * 16);
+    Plan f{};
+    f.tiles = n_tokens <= 16 ? 1 : n_tokens <= 32 ? 2 : 4;
+    const int rb = f.tiles == 4 ? 2 : 1, tokens = std::min(n_tokens, f.tiles * 16), token_tiles = (n_tokens + f.tiles * 16 - 1) / (f.tiles * 16);
     const size_t per_block = (size_t)tokens * (bf16 ? 256 : 132);
     const int most = (int)std::min<size_t>(blocks, kMostLds / per_block);
-    f.ranges = (blocks + most - 1) / most;
-    const long units = (long)((row_tiles + f.rb - 1) / f.rb) * token_tiles;         // waves without a cut of the columns
-    while (f.nt == 4 && f.ranges < 16 && units * f.ranges * 8 < 8 * 256 && blocks / (2 * f.ranges) >= 4) f.ranges *= 2;
-    f.range_blocks = (blocks + f.ranges - 1) / f.ranges;
-    f.ranges = (blocks + f.range_blocks - 1) / f.range_blocks;
+    cut(f, blocks, std::max(ranges, (blocks + most - 1) / most));
+    const long units = (long)((row_tiles + rb - 1) / rb) * token_tiles * f.ranges;
     f.ks = 1;
-    while (f.ks < 8 && units * f.ranges * f.ks < 2048 && f.range_blocks >= 2 * f.ks) f.ks *= 2;
-    f.lds = std::max<size_t>((size_t)f.range_blocks * per_block + 1024, (size_t)(f.ks > 1 ? kWaves * f.rb * f.nt * 1024 : 0));
+    while (f.ks < 8 && units * f.ks < 2048 && f.range_blocks >= 2 * f.ks) f.ks *= 2;
+    f.lds = std::max<size_t>((size_t)f.range_blocks * per_block + 1024, (size_t)(f.ks > 1 ? kWaves * rb * f.tiles * 1024 : 0));
     return f;
 }
-
-int linear_ranges(int n_tokens, int R, int K, int x_type, int) {
-    return n_tokens > kFewTokens ? 1 : few_of(n_tokens, R, K, x_type == DENSE_BF16).ranges;
+static Plan many_of(int n_tokens, int R, int K, int tiles, int ranges) {
+    Plan f{};
+    f.many = true;
+    f.tiles = tiles;
+    cut(f, (K + 127) / 128, ranges);
+    return f;
+}
+// Us that a plan takes, by what was measured (H 1024 to 14336, 1024 to 32000 rows, 1 to 2048 tokens; most within 15 %): a launch 3; what a CU has to take in, at 28 bytes
+// a ns, 20 where LDS leaves room for one workgroup; tiles of many tokens per block of 128 columns and workgroup on a CU; ranges cost a launch, and their sums are written and read.
+static float us_of(const Plan &p, int n_tokens, int R, int K, bool bf16) {
+    const int row_tiles = (R + 15) / 16, token_tiles = (n_tokens + p.tiles * 16 - 1) / (p.tiles * 16);
+    const float join = p.ranges == 1 ? 0.f : (p.many ? 4.f : 2.2f) + (float)p.ranges * n_tokens * R * 8.f / 6e6f;
+    if (p.many) {
+        const long wgs = (long)((row_tiles + 15) / 16) * token_tiles * p.ranges, on_cu = (wgs + 255) / 256;
+        const float block = p.tiles == 8 ? (bf16 ? on_cu > 1 ? 1.5f : 1.75f : 0.95f) : (bf16 ? on_cu > 1 ? 0.83f : 0.95f : 0.6f);
+        return 3.f + (float)on_cu * p.range_blocks * block + join;
+    }
+    const int per = kWaves / p.ks * (p.tiles == 4 ? 2 : 1);
+    const long wgs = (long)((row_tiles + per - 1) / per) * token_tiles * p.ranges, on_cu = (wgs + 255) / 256;
+    const float x = (float)std::min(n_tokens, p.tiles * 16) * (bf16 ? 256.f : 132.f) * p.range_blocks, w = (float)per * p.range_blocks * 1088.f;
+    return 3.f + (float)on_cu * (x + w) / (p.lds > 80 * 1024 ? 20e3f : 28e3f) + join;
+}
+static Plan plan_of(int n_tokens, int R, int K, bool bf16) {
+    const int blocks = (K + 127) / 128;
+    Plan best{};
+    float least = 0.f;
+    const auto look = [&](const Plan &p) {
+        const float us = us_of(p, n_tokens, R, K, bf16);
+        if (best.tiles == 0 || us < least) {
+            best = p;
+            least = us;
+        }
+    };
+    for (const int z : {1, 2, 3, 4, 6, 8, 12, 16}) {
+        if (z > blocks) break;
+        if (n_tokens <= 64) look(few_of(n_tokens, R, K, bf16, z));
+        if (n_tokens > 16) look(many_of(n_tokens, R, K, 4, z));
+        if (n_tokens > 64) look(many_of(n_tokens, R, K, 8, z));
+    }
+    return best;
 }
 
+int linear_ranges(int n_tokens, int R, int K, int x_type, int) { return plan_of(n_tokens, R, K, x_type == DENSE_BF16).ranges; }
+
 hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
-    if (a.n_tokens > kFewTokens) return launch_linear_many(a, s);
-    const Few f = few_of(a.n_tokens, a.R, a.K, a.x_type == DENSE_BF16);
-    if (f.ranges > a.ranges) return launch_linear_many(a, s);
+    Plan f = plan_of(a.n_tokens, a.R, a.K, a.x_type == DENSE_BF16);
+    if (f.ranges > a.ranges) f = many_of(a.n_tokens, a.R, a.K, a.n_tokens > 64 ? 8 : 4, 1);        // no workspace
     const int row_tiles = (a.R + 15) / 16;
     const auto go = [&](auto xt, auto nt, auto ks) {
         constexpr int XT = decltype(xt)::value, NT = decltype(nt)::value, KS = decltype(ks)::value, RB = NT == 4 ? 2 : 1, D = NT == 4 ? 4 : 8, PER = kWaves / KS * RB;
@@ -249,11 +289,14 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
         else go(xt, nt, std::integral_constant<int, 8>{});
     };
     const auto by_tokens = [&](auto xt) {
-        if (f.nt == 1) by_slices(xt, std::integral_constant<int, 1>{});
-        else if (f.nt == 2) by_slices(xt, std::integral_constant<int, 2>{});
+        if (f.tiles == 1) by_slices(xt, std::integral_constant<int, 1>{});
+        else if (f.tiles == 2) by_slices(xt, std::integral_constant<int, 2>{});
         else by_slices(xt, std::integral_constant<int, 4>{});
     };
-    if (a.x_type == DENSE_BF16) by_tokens(std::integral_constant<int, X_BF16>{});
+    if (f.many) {
+        const hipError_t e = launch_linear_many(a, f.tiles, f.range_blocks, s);
+        if (e != hipSuccess) return e;
+    } else if (a.x_type == DENSE_BF16) by_tokens(std::integral_constant<int, X_BF16>{});
     else if (a.out_type == DENSE_BF16) by_tokens(std::integral_constant<int, X_FP8>{});
     else by_tokens(std::integral_constant<int, X_WIDE>{});
     if (f.ranges > 1) {
