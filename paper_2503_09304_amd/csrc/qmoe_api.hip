@@ -340,6 +340,7 @@ static int32_t route(const char *call, moe_ctx *ctx, const void *x, int32_t n_to
     if (n_tokens > 0) {
         qmoe::RouteArgs a{};
         a.scoring = scoring;
+        a.scratch = at<float>(ctx, ctx->lay.out);
         a.x = x; a.Wg = w->Wg; a.bias = logit_bias;
         a.WgT = at<void>(ctx, ctx->lay.wgt);
         a.parts = at<float>(ctx, ctx->lay.parts);

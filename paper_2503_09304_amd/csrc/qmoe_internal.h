@@ -41,6 +41,7 @@ struct RouteArgs {
     int N, H, E, k, dtype;
     bool packed;  // Wg already transposed and padded ([E16][H])
     const moe_scoring *scoring;   // moe_route_scored, else nullptr
+    float *scratch;               // for it: k * H floats a token
 };
 // The bf16 router in two launches, its GEMM dealt out in 8 K ranges to workgroups of their own: where one workgroup per
 // 16 tokens leaves CUs idle while each takes in all the weights.  One launch takes a wave's share of K (H / 256 MFMA steps)
@@ -65,8 +66,9 @@ inline size_t gate_parts_floats(int max_tokens, int E) {
     return (n + 15) / 16 * 8 * (size_t)((E + 15) / 16) * 256;
 }
 hipError_t launch_route(const RouteArgs &a, hipStream_t s);
-// The choice of moe_route_scored from logits that are there.
-hipError_t launch_score(const RouteArgs &a, hipStream_t s);
+// moe_route_scored: gate GEMM and choice (bf16; row-major weights need an even E), or the choice alone: planes 0: from the logits, else from that many partial ones.
+hipError_t launch_gate_scored(const RouteArgs &a, hipStream_t s);
+hipError_t launch_score(const RouteArgs &a, const float *part, int planes, hipStream_t s);
 
 // Records the text moe_last_error() returns on this thread and hands `code` back (printf-style).
 int32_t set_error(int32_t code, const char *fmt, ...);

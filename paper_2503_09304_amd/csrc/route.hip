@@ -405,6 +405,7 @@ hipError_t launch_pack_gate(const void *Wg, void *WgT, int H, int E, hipStream_t
 
 hipError_t launch_route(const RouteArgs &a, hipStream_t s) {
     if (a.N <= 0) return hipSuccess;
+    if (a.scoring != nullptr && a.dtype == MOE_BF16 && (a.packed || a.E % 2 == 0)) return launch_gate_scored(a, s);
     if (a.dtype == MOE_BF16) {
         const int E16 = (a.E + 15) / 16 * 16, nb = E16 / 16;
         const long tot = (long)E16 * a.H;
@@ -432,7 +433,7 @@ hipError_t launch_route(const RouteArgs &a, hipStream_t s) {
         else hipLaunchKernelGGL((gate_topk_f32<8, false>), g, b, 0, s, x, wg, a.bias, a.logits, a.topk_idx, a.topk_w, a.N, a.H, a.E, a.k);
     }
     const hipError_t e = hipGetLastError();
-    return e == hipSuccess && a.scoring != nullptr ? launch_score(a, s) : e;
+    return e == hipSuccess && a.scoring != nullptr ? launch_score(a, nullptr, 0, s) : e;
 }
 
 }  // namespace qmoe

@@ -1,146 +1,331 @@
-// The choice of moe_route_scored: scores by softmax or sigmoid, a bias that counts for the choice alone, the best groups, the best
-// experts of those, their weights.
+// moe_route_scored: the gate GEMM in ranges of the hidden size, and the choice behind it: scores by softmax or sigmoid, a bias that counts for the choice
+// alone, the best groups, the best experts of those, their weights.
 //
-// Everything behind the logits is in 64 bits: two values that differ by less than the error of an fp32 exponential would change
-// places with any other way to compute it.
+// Everything behind the logits is in 64 bits: two values that differ by less than the error of an fp32 exponential would change places with any other way
+// to compute it.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <climits>
+#include <type_traits>
 
 #include "qmoe_internal.h"
 
 namespace qmoe {
 namespace {
 
-constexpr int kSlots = kMaxExperts / 64;
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// ---- gate GEMM ----
+
+// 16 bytes a lane from memory to LDS, lane l's at `to` + 16 l; the caller waits (vmcnt) before the barrier behind which they are read.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"          // that m0 is reserved: nothing else here uses it
+__device__ __forceinline__ void to_lds(const char *from, const char *to) {
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)to);
+    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(at) : "m0", "memory");
+}
+#pragma clang diagnostic pop
+
+constexpr int kMostRanges = 16;
+constexpr int kStage = 128;           // columns of the hidden size that stand in LDS at once
+
+// Products of TT * 16 tokens with all experts over a range of the hidden size: a wave has 32 experts (and, where experts are few, one of `slices` parts of the range).
+// Lane l's operands are experts 2 (l%16) and 2 (l%16) + 1 of the wave's.  Row-major weights [H][E] (E even): it takes the pairs of 8 rows and turns them over in
+// registers, so no transposed copy is written first.
+template <int TT, bool PACKED>
+__global__ __launch_bounds__(512) void gate_ranges(const uint16_t *__restrict__ x, const uint16_t *__restrict__ Wg, float *__restrict__ part, int N, int H, int E,
+                                                   int blocks, int slices, int range) {
+    extern __shared__ __align__(16) char lds[];
+    constexpr int STAGE_BYTES = TT * 16 * kStage * 2;
+    const int w = threadIdx.x >> 6, l = threadIdx.x & 63, t16 = l & 15, g = l >> 4;
+    const int pb = w % blocks, sl = w / blocks;
+    const int t0 = blockIdx.x * (TT * 16), from = blockIdx.y * range, to = min(H, from + range);
+    const int per = ((to - from + slices - 1) / slices + 31) / 32 * 32, k0 = min(to, from + sl * per), k1 = min(to, k0 + per);
+    char *const mine = lds + sl * 2 * STAGE_BYTES;
+    // The blocks' waves of a slice bring its tokens: a load has 4 tokens by 128 columns; token t's piece p (of 16 bytes) stands in place p ^ t, so that
+    // the 16 tokens of a read use all banks.
+    const auto bring = [&](int k, int buf) {
+        for (int j = pb; j < TT * 4; j += blocks) {
+            const int t = j * 4 + l / 16, at = k + ((l ^ t) & 15) * 8;
+            to_lds((const char *)(x + (long)min(t0 + t, N - 1) * H + (at < H ? at : 0)), mine + buf * STAGE_BYTES + j * 1024);
+        }
+    };
+    const int e0 = pb * 32 + 2 * t16;
+    u32x4 wv[4][2];
+    uint32_t raw[4][8];
+    const auto ask = [&](int k) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            if (k + 32 * s >= k1) break;
+            const int row = k + 32 * s + 8 * g;
+            if constexpr (PACKED) {
+                wv[s][0] = *reinterpret_cast<const u32x4 *>(Wg + (long)min(e0, E - 1) * H + row);
+                wv[s][1] = *reinterpret_cast<const u32x4 *>(Wg + (long)min(e0 + 1, E - 1) * H + row);
+            } else {
+                const uint16_t *p = Wg + (long)row * E + min(e0, E - 2);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) raw[s][i] = *reinterpret_cast<const uint32_t *>(p + (long)i * E);
+            }
+        }
+    };
+    f32x4 acc[TT][2];
+#pragma unroll
+    for (int n = 0; n < TT; ++n) acc[n][0] = acc[n][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int rounds = (per + kStage - 1) / kStage;      // of all slices alike: they share the barriers
+    bring(min(k0, H - 1) & ~31, 0);
+    ask(k0);
+    for (int i = 0; i < rounds; ++i) {
+        const int k = k0 + i * kStage;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // this wave's pieces are in LDS
+        __syncthreads();
+        u32x4 now[4][2];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            if constexpr (PACKED) {
+                now[s][0] = wv[s][0];
+                now[s][1] = wv[s][1];
+            } else {
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {            // rows 2h and 2h + 1
+                    now[s][0][h] = __builtin_amdgcn_perm(raw[s][2 * h + 1], raw[s][2 * h], 0x05040100u);
+                    now[s][1][h] = __builtin_amdgcn_perm(raw[s][2 * h + 1], raw[s][2 * h], 0x07060302u);
+                }
+            }
+        }
+        if (i + 1 < rounds && k + kStage < k1) {
+            bring(k + kStage, (i + 1) & 1);
+            ask(k + kStage);
+        }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            if (k + 32 * s >= k1) break;
+#pragma unroll
+            for (int n = 0; n < TT; ++n) {
+                const bf16x8 a = *reinterpret_cast<const bf16x8 *>(mine + (i & 1) * STAGE_BYTES + (n * 16 + t16) * 256 + ((4 * s + g) ^ t16) * 16);
+                acc[n][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, now[s][0]), acc[n][0], 0, 0, 0);
+                acc[n][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, now[s][1]), acc[n][1], 0, 0, 0);
+            }
+        }
+    }
+    if (slices > 1) {
+        f32x4 *red = reinterpret_cast<f32x4 *>(lds);
+        __syncthreads();                                 // the tokens have been read
+        if (sl > 0)
+#pragma unroll
+            for (int n = 0; n < TT; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) red[((w - blocks) * (2 * TT) + 2 * n + h) * 64 + l] = acc[n][h];
+        __syncthreads();
+        if (sl > 0) return;
+        for (int i = 1; i < slices; ++i)
+#pragma unroll
+            for (int n = 0; n < TT; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const f32x4 o = red[((w + (i - 1) * blocks) * (2 * TT) + 2 * n + h) * 64 + l];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[n][h][e] += o[e];
+                }
+    }
+#pragma unroll
+    for (int n = 0; n < TT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = t0 + n * 16 + 4 * g + i;
+            float *o = part + ((long)blockIdx.y * N + t) * E + e0;
+            if (t < N && e0 < E) o[0] = acc[n][0][i];
+            if (t < N && e0 + 1 < E) o[1] = acc[n][1][i];
+        }
+}
+
+// ---- choice ----
+
 constexpr int kTokens = 4;            // tokens a workgroup, one wave each
 
 struct Rule {
-    const float *choice_bias;
-    int sigmoid, groups, take, best, renorm;
+    const float *logit_bias, *choice_bias;
+    int sigmoid, groups, take, renorm;
     float factor;
 };
 
-// An order of doubles as integers: NaN below everything, -0 and 0 equal.
-__device__ __forceinline__ long long order_key(double v) {
-    const long long b = __builtin_bit_cast(long long, v + 0.0);
-    return v != v ? LLONG_MIN : b ^ ((b >> 63) & LLONG_MAX);
+// Largest value of the wave's 64 lanes, in every lane.
+template <class T>
+__device__ __forceinline__ T wave_max(T v) {
+    const auto step = [&](auto ctrl) {
+        const int old = __builtin_bit_cast(int, v);
+        v = max(v, __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(old, old, decltype(ctrl)::value, 0xf, 0xf, false)));
+    };
+    step(std::integral_constant<int, 0x111>{});          // row_shr 1, 2, 4, 8; row_bcast 15 and 31: lane 63 holds the wave's
+    step(std::integral_constant<int, 0x112>{});
+    step(std::integral_constant<int, 0x114>{});
+    step(std::integral_constant<int, 0x118>{});
+    step(std::integral_constant<int, 0x142>{});
+    step(std::integral_constant<int, 0x143>{});
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
-__device__ __forceinline__ long long lane_of(long long v, int lane) {
-    const int lo = __builtin_amdgcn_readlane((int)v, lane), hi = __builtin_amdgcn_readlane((int)(v >> 32), lane);
-    return (long long)hi << 32 | (unsigned)lo;
+__device__ __forceinline__ double lane_of(double v, int lane) {
+    const long long b = __builtin_bit_cast(long long, v);
+    const int lo = __builtin_amdgcn_readlane((int)b, lane), hi = __builtin_amdgcn_readlane((int)(b >> 32), lane);
+    return __builtin_bit_cast(double, (long long)hi << 32 | (unsigned)lo);
 }
-__device__ __forceinline__ double lane_of(double v, int lane) { return __builtin_bit_cast(double, lane_of(__builtin_bit_cast(long long, v), lane)); }
-__device__ __forceinline__ long long wave_max(long long v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
-    return v;
-}
+// Sum over the wave, the same order for every lane.
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
     return v;
 }
 
-// A wave has a token; lane l has experts l, l + 64, ...
-__global__ __launch_bounds__(64 * kTokens) void score_topk(const float *__restrict__ logits, const Rule rule, int32_t *__restrict__ topk_idx,
-                                                           float *__restrict__ topk_w, int N, int E, int k) {
-    __shared__ double value[kTokens][kMaxExperts];
+// An order of doubles as pairs of integers, the high words first: NaN below everything, -0 and 0 equal.  A high word of INT_MIN is left for what must not be chosen.
+struct Key {
+    int hi;
+    unsigned lo;
+};
+__device__ __forceinline__ Key key_of(double v) {
+    const long long b = __builtin_bit_cast(long long, v + 0.0), k = b ^ ((b >> 63) & LLONG_MAX);
+    return v != v ? Key{INT_MIN + 1, 0u} : Key{(int)(k >> 32), (unsigned)k};
+}
+__device__ __forceinline__ double largest_first(double &a, double b) {       // a: the larger, returns the other
+    const bool more = b > a;                             // a NaN stays out
+    const double other = more ? a : b;
+    a = more ? b : a;
+    return other;
+}
+
+// A wave has a token; lane l has experts l, l + 64, ..., NS in all.  BEST: values that a group's worth is the sum of (0: one group).
+template <int NS, int BEST>
+__global__ __launch_bounds__(64 * kTokens) void score_topk(const float *__restrict__ part, int planes, float *__restrict__ logits, const Rule rule,
+                                                           int32_t *__restrict__ topk_idx, float *__restrict__ topk_w, int N, int E, int k) {
+    __shared__ double value[BEST ? kTokens : 1][BEST ? NS * 64 : 1];
     const int wv = threadIdx.x >> 6, l = threadIdx.x & 63;
     const int t = blockIdx.x * kTokens + wv;
     if (t >= N) return;                                  // no barrier follows: a wave reads what it wrote itself
-    const float *lg = logits + (long)t * E;
-    float x[kSlots];
+    float x[NS];
+    if (planes == 0) {
 #pragma unroll
-    for (int c = 0; c < kSlots; ++c) x[c] = l + 64 * c < E ? lg[l + 64 * c] : -INFINITY;
-    double s[kSlots];
+        for (int c = 0; c < NS; ++c) x[c] = l + 64 * c < E ? logits[(long)t * E + l + 64 * c] : -INFINITY;
+    } else {
+        float q[NS][kMostRanges];                        // all asked for before the first is used (one by one: a token on 256 experts 23 us instead of 8)
+        const float *p = part + (long)t * E;
+#pragma unroll
+        for (int z = 0; z < kMostRanges; ++z)
+            if (z < planes)
+#pragma unroll
+                for (int c = 0; c < NS; ++c) q[c][z] = p[(long)z * N * E + min(l + 64 * c, E - 1)];
+#pragma unroll
+        for (int c = 0; c < NS; ++c) {
+            const int e = l + 64 * c;
+            float v = q[c][0];
+#pragma unroll
+            for (int z = 1; z < kMostRanges; ++z)
+                if (z < planes) v += q[c][z];
+            if (rule.logit_bias != nullptr) v += rule.logit_bias[min(e, E - 1)];
+            if (e < E) logits[(long)t * E + e] = v;
+            x[c] = e < E ? v : -INFINITY;
+        }
+    }
+    double s[NS];
     if (rule.sigmoid) {
 #pragma unroll
-        for (int c = 0; c < kSlots; ++c) s[c] = 1.0 / (1.0 + exp(-(double)x[c]));
+        for (int c = 0; c < NS; ++c) s[c] = 1.0 / (1.0 + exp(-(double)x[c]));
     } else {
-        float m = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+        float m = x[0];
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+        for (int c = 1; c < NS; ++c) m = fmaxf(m, x[c]);
+        m = wave_max(m);
         double sum = 0.0;
 #pragma unroll
-        for (int c = 0; c < kSlots; ++c) {
+        for (int c = 0; c < NS; ++c) {
             s[c] = l + 64 * c < E ? exp((double)x[c] - (double)m) : 0.0;
             sum += s[c];
         }
-        sum = wave_sum(sum);
+        const double inv = 1.0 / wave_sum(sum);
 #pragma unroll
-        for (int c = 0; c < kSlots; ++c) s[c] /= sum;
+        for (int c = 0; c < NS; ++c) s[c] *= inv;
     }
-    long long key[kSlots];
+    Key key[NS];
 #pragma unroll
-    for (int c = 0; c < kSlots; ++c) {
+    for (int c = 0; c < NS; ++c) {
         const int e = l + 64 * c;
         double v = s[c];
-        if (e < E) {
-            if (rule.choice_bias != nullptr) v += (double)rule.choice_bias[e];
-            value[wv][e] = v;
-        }
-        key[c] = order_key(v);
+        if (e < E && rule.choice_bias != nullptr) v += (double)rule.choice_bias[e];
+        if constexpr (BEST > 0) value[wv][e] = v;
+        key[c] = key_of(v);
+        if (e >= E) key[c].hi = INT_MIN;
     }
-    unsigned long long taken_groups = ~0ull;             // bit g: the token may choose from group g
-    const int size = E / rule.groups;
-    if (rule.take < rule.groups) {
-        long long worth = LLONG_MIN;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // lanes read what others of their wave wrote
-        if (l < rule.groups) {
-            double best[kMaxGroupBest];
+    if constexpr (BEST > 0) {
+        // 64 / groups lanes, rounded down to a power of two, look through a group and put together what they found.
+        const int size = E / rule.groups, log_lanes = 31 - __builtin_clz(64 / rule.groups), lanes = 1 << log_lanes, grp = l >> log_lanes;
+        double best[BEST];
 #pragma unroll
-            for (int i = 0; i < kMaxGroupBest; ++i) best[i] = -INFINITY;
-            for (int i = 0; i < size; ++i) {
-                double v = value[wv][l * size + i];
+        for (int i = 0; i < BEST; ++i) best[i] = -INFINITY;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");       // lanes read what others of their wave wrote
+        for (int i = l & (lanes - 1); i < size && grp < rule.groups; i += lanes) {
+            double v = value[wv][grp * size + i];
 #pragma unroll
-                for (int j = 0; j < kMaxGroupBest; ++j) {            // kept in descending order
-                    const double b = best[j];
-                    const bool more = v > b;
-                    best[j] = more ? v : b;
-                    v = more ? b : v;
-                }
+            for (int j = 0; j < BEST; ++j) v = largest_first(best[j], v);
+        }
+        for (int o = 1; o < lanes; o <<= 1) {
+            double other[BEST];
+#pragma unroll
+            for (int j = 0; j < BEST; ++j) other[j] = __shfl_xor(best[j], o, 64);
+#pragma unroll
+            for (int i = 0; i < BEST; ++i) {
+                double v = other[i];
+#pragma unroll
+                for (int j = 0; j < BEST; ++j) v = largest_first(best[j], v);
             }
-            double sum = best[0];
-#pragma unroll
-            for (int j = 1; j < kMaxGroupBest; ++j)
-                if (j < rule.best) sum += best[j];
-            worth = order_key(sum);
         }
+        double worth = best[0];
+#pragma unroll
+        for (int j = 1; j < BEST; ++j) worth += best[j];
+        const Key mine = key_of(worth);
         int rank = 0;
-        for (int g = 0; g < rule.groups; ++g) {
-            const long long o = lane_of(worth, g);
-            rank += o > worth || (o == worth && g < l) ? 1 : 0;
+        for (int n = 0; n < rule.groups; ++n) {
+            const int hi = __builtin_amdgcn_readlane(mine.hi, n << log_lanes);
+            const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)mine.lo, n << log_lanes);
+            rank += hi > mine.hi || (hi == mine.hi && (lo > mine.lo || (lo == mine.lo && n < grp))) ? 1 : 0;
         }
-        taken_groups = __ballot(l < rule.groups && rank < rule.take);
-    }
-    unsigned long long left[kSlots];
+        const unsigned long long kept = __ballot(rank < rule.take);
+        const unsigned inv = 65536u / size + 1;          // e / size = e * inv / 65536 for e below 256
 #pragma unroll
-    for (int c = 0; c < kSlots; ++c) {
-        const int e = l + 64 * c;
-        const bool in = e < E && (taken_groups >> (e / size) & 1);
-        left[c] = __ballot(in);
-        if (!in) key[c] = LLONG_MIN;
+        for (int c = 0; c < NS; ++c)
+            if (!(kept >> (((l + 64 * c) * inv >> 16) << log_lanes & 63) & 1)) key[c].hi = INT_MIN;
     }
     double mine = 0.0;
     int mine_e = 0;
     for (int j = 0; j < k; ++j) {
-        long long m = LLONG_MIN;
+        int top = key[0].hi;
 #pragma unroll
-        for (int c = 0; c < kSlots; ++c) m = max(m, left[c] >> l & 1 ? key[c] : LLONG_MIN);
-        m = wave_max(m);
+        for (int c = 1; c < NS; ++c) top = max(top, key[c].hi);
+        top = wave_max(top);
+        unsigned long long at[NS];
+        int n = 0;
+#pragma unroll
+        for (int c = 0; c < NS; ++c) {
+            at[c] = __ballot(key[c].hi == top);
+            n += __builtin_popcountll(at[c]);
+        }
+        if (n > 1) {                                     // values that differ in the low word alone, or not at all
+            unsigned low = 0;
+#pragma unroll
+            for (int c = 0; c < NS; ++c) low = max(low, key[c].hi == top ? key[c].lo : 0u);
+            low = wave_max(low);
+#pragma unroll
+            for (int c = 0; c < NS; ++c) at[c] = __ballot(key[c].hi == top && key[c].lo == low);
+        }
         int e = 0;
 #pragma unroll
-        for (int c = kSlots - 1; c >= 0; --c) {
-            const unsigned long long b = __ballot(key[c] == m) & left[c];
-            if (b) e = 64 * c + __builtin_ctzll(b);
-        }
-        double sv = 0.0;
+        for (int c = NS - 1; c >= 0; --c)
+            if (at[c]) e = 64 * c + __builtin_ctzll(at[c]);
+        double sv = s[0];
 #pragma unroll
-        for (int c = 0; c < kSlots; ++c)
+        for (int c = 0; c < NS; ++c)
             if (c == e >> 6) {
-                left[c] &= ~(1ull << (e & 63));
                 sv = s[c];
+                key[c].hi = l == (e & 63) ? INT_MIN : key[c].hi;
             }
         sv = lane_of(sv, e & 63);
         if (l == j) {
@@ -148,7 +333,7 @@ __global__ __launch_bounds__(64 * kTokens) void score_topk(const float *__restri
             mine_e = e;
         }
     }
-    const double sum = wave_sum(l < k ? mine : 0.0);
+    const double sum = rule.renorm ? wave_sum(l < k ? mine : 0.0) : 0.0;
     if (l < k) {
         const double w = !rule.renorm ? mine : sum == 0.0 ? 1.0 / k : mine / sum;
         topk_idx[(long)t * k + l] = mine_e;
@@ -158,11 +343,48 @@ __global__ __launch_bounds__(64 * kTokens) void score_topk(const float *__restri
 
 }  // namespace
 
-hipError_t launch_score(const RouteArgs &a, hipStream_t s) {
+hipError_t launch_score(const RouteArgs &a, const float *part, int planes, hipStream_t s) {
     const moe_scoring &c = *a.scoring;
-    const Rule rule{c.choice_bias, c.score == MOE_SCORE_SIGMOID, c.groups, c.top_groups, c.group_best, c.renormalise, c.factor};
-    score_topk<<<dim3((a.N + kTokens - 1) / kTokens), dim3(64 * kTokens), 0, s>>>(a.logits, rule, a.topk_idx, a.topk_w, a.N, a.E, a.k);
+    const Rule rule{c.logit_bias, c.choice_bias, c.score == MOE_SCORE_SIGMOID, c.groups, c.top_groups, c.renormalise, c.factor};
+    const auto go = [&](auto ns, auto best) {
+        score_topk<decltype(ns)::value, decltype(best)::value><<<dim3((a.N + kTokens - 1) / kTokens), dim3(64 * kTokens), 0, s>>>(part, planes, a.logits, rule, a.topk_idx, a.topk_w, a.N,
+                                                                                                                                 a.E, a.k);
+    };
+    const auto by_best = [&](auto ns) {
+        if (c.top_groups == c.groups) go(ns, std::integral_constant<int, 0>{});
+        else if (c.group_best == 1) go(ns, std::integral_constant<int, 1>{});
+        else if (c.group_best == 2) go(ns, std::integral_constant<int, 2>{});
+        else if (c.group_best == 3) go(ns, std::integral_constant<int, 3>{});
+        else go(ns, std::integral_constant<int, 4>{});
+    };
+    if (a.E <= 64) by_best(std::integral_constant<int, 1>{});
+    else if (a.E <= 128) by_best(std::integral_constant<int, 2>{});
+    else by_best(std::integral_constant<int, 4>{});
     return hipGetLastError();
+}
+
+hipError_t launch_gate_scored(const RouteArgs &a, hipStream_t s) {
+    const int blocks = (a.E + 31) / 32, tt = a.N <= 16 ? 1 : a.N <= 32 ? 2 : 4, tiles = (a.N + tt * 16 - 1) / (tt * 16);
+    // Parts of the range a workgroup: up to 8 waves, 4 parts.  Ranges: as many as give 256 workgroups, 16 at most, each part 32 columns at least; what the scratch holds.
+    int slices = std::max(1, std::min(4, 8 / blocks));
+    while (slices > 1 && a.H < 32 * slices) slices /= 2;
+    const long fit = (long)a.k * a.H / a.E;              // the context's room for k rows of H floats a token
+    long ranges = std::max(1l, std::min({256l / tiles, (long)kMostRanges, (long)a.H / (64 * slices), fit}));
+    const int range = (int)(((a.H + ranges - 1) / ranges + 63) / 64 * 64);
+    ranges = (a.H + range - 1) / range;
+    float *part = ranges > 1 ? a.scratch : a.logits;
+    const auto go = [&](auto t, auto packed) {
+        constexpr int TT = decltype(t)::value;
+        const size_t lds = std::max<size_t>((size_t)slices * 2 * TT * 16 * kStage * 2, (size_t)(slices - 1) * blocks * 2 * TT * 1024);
+        gate_ranges<TT, decltype(packed)::value><<<dim3(tiles, (unsigned)ranges), dim3(64 * blocks * slices), lds, s>>>((const uint16_t *)a.x, (const uint16_t *)a.Wg, part, a.N, a.H, a.E, blocks,
+                                                                                                                    slices, range);
+    };
+    const auto by_layout = [&](auto t) { a.packed ? go(t, std::true_type{}) : go(t, std::false_type{}); };
+    if (tt == 1) by_layout(std::integral_constant<int, 1>{});
+    else if (tt == 2) by_layout(std::integral_constant<int, 2>{});
+    else by_layout(std::integral_constant<int, 4>{});
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? launch_score(a, part, (int)ranges, s) : e;
 }
 
 }  // namespace qmoe
