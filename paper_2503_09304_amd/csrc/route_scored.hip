@@ -30,35 +30,34 @@ __device__ __forceinline__ void to_lds(const char *from, const char *to) {
 #pragma clang diagnostic pop
 
 constexpr int kMostRanges = 16;
-constexpr int kStage = 128;           // columns of the hidden size that stand in LDS at once
 
 // Products of TT * 16 tokens with all experts over a range of the hidden size: a wave has 32 experts (and, where experts are few, one of `slices` parts of the range).
 // Lane l's operands are experts 2 (l%16) and 2 (l%16) + 1 of the wave's.  Row-major weights [H][E] (E even): it takes the pairs of 8 rows and turns them over in
 // registers, so no transposed copy is written first.
-template <int TT, bool PACKED>
+template <int TT, int STEPS, bool PACKED>
 __global__ __launch_bounds__(512) void gate_ranges(const uint16_t *__restrict__ x, const uint16_t *__restrict__ Wg, float *__restrict__ part, int N, int H, int E,
                                                    int blocks, int slices, int range) {
     extern __shared__ __align__(16) char lds[];
-    constexpr int STAGE_BYTES = TT * 16 * kStage * 2;
+    constexpr int kStage = 32 * STEPS, PIECES = 4 * STEPS, STAGE_BYTES = TT * 16 * kStage * 2;       // columns that stand in LDS at once, in pieces of 8
     const int w = threadIdx.x >> 6, l = threadIdx.x & 63, t16 = l & 15, g = l >> 4;
     const int pb = w % blocks, sl = w / blocks;
     const int t0 = blockIdx.x * (TT * 16), from = blockIdx.y * range, to = min(H, from + range);
     const int per = ((to - from + slices - 1) / slices + 31) / 32 * 32, k0 = min(to, from + sl * per), k1 = min(to, k0 + per);
     char *const mine = lds + sl * 2 * STAGE_BYTES;
-    // The blocks' waves of a slice bring its tokens: a load has 4 tokens by 128 columns; token t's piece p (of 16 bytes) stands in place p ^ t, so that
-    // the 16 tokens of a read use all banks.
+    // The blocks' waves of a slice bring its tokens.  Token t's piece p stands in place p ^ t of its 16 (of 32, in its half), so that the 16 tokens of a
+    // read use all banks.
     const auto bring = [&](int k, int buf) {
-        for (int j = pb; j < TT * 4; j += blocks) {
-            const int t = j * 4 + l / 16, at = k + ((l ^ t) & 15) * 8;
+        for (int j = pb; j < TT * STEPS; j += blocks) {
+            const int i = j * 64 + l, t = i / PIECES, at = k + ((i % PIECES) ^ (t & 15)) * 8;
             to_lds((const char *)(x + (long)min(t0 + t, N - 1) * H + (at < H ? at : 0)), mine + buf * STAGE_BYTES + j * 1024);
         }
     };
     const int e0 = pb * 32 + 2 * t16;
-    u32x4 wv[4][2];
-    uint32_t raw[4][8];
+    u32x4 wv[STEPS][2];
+    uint32_t raw[STEPS][8];
     const auto ask = [&](int k) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
+        for (int s = 0; s < STEPS; ++s) {
             if (k + 32 * s >= k1) break;
             const int row = k + 32 * s + 8 * g;
             if constexpr (PACKED) {
@@ -81,9 +80,9 @@ __global__ __launch_bounds__(512) void gate_ranges(const uint16_t *__restrict__ 
         const int k = k0 + i * kStage;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // this wave's pieces are in LDS
         __syncthreads();
-        u32x4 now[4][2];
+        u32x4 now[STEPS][2];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
+        for (int s = 0; s < STEPS; ++s) {
             if constexpr (PACKED) {
                 now[s][0] = wv[s][0];
                 now[s][1] = wv[s][1];
@@ -100,11 +99,11 @@ __global__ __launch_bounds__(512) void gate_ranges(const uint16_t *__restrict__ 
             ask(k + kStage);
         }
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
+        for (int s = 0; s < STEPS; ++s) {
             if (k + 32 * s >= k1) break;
 #pragma unroll
             for (int n = 0; n < TT; ++n) {
-                const bf16x8 a = *reinterpret_cast<const bf16x8 *>(mine + (i & 1) * STAGE_BYTES + (n * 16 + t16) * 256 + ((4 * s + g) ^ t16) * 16);
+                const bf16x8 a = *reinterpret_cast<const bf16x8 *>(mine + (i & 1) * STAGE_BYTES + (n * 16 + t16) * (PIECES * 16) + ((4 * s + g) ^ t16) * 16);
                 acc[n][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, now[s][0]), acc[n][0], 0, 0, 0);
                 acc[n][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, now[s][1]), acc[n][1], 0, 0, 0);
             }
@@ -171,11 +170,22 @@ __device__ __forceinline__ double lane_of(double v, int lane) {
     const int lo = __builtin_amdgcn_readlane((int)b, lane), hi = __builtin_amdgcn_readlane((int)(b >> 32), lane);
     return __builtin_bit_cast(double, (long long)hi << 32 | (unsigned)lo);
 }
-// Sum over the wave, the same order for every lane.
+// Sum over the wave, in every lane.
 __device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
-    return v;
+    const auto step = [&](auto ctrl, auto rows) {        // lanes without a source, and rows that are not asked, add 0
+        const long long b = __builtin_bit_cast(long long, v);
+        const int lo = __builtin_amdgcn_update_dpp(0, (int)b, decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+        const int hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+        v += __builtin_bit_cast(double, (long long)hi << 32 | (unsigned)lo);
+    };
+    typedef std::integral_constant<int, 0xf> All;
+    step(std::integral_constant<int, 0x111>{}, All{});   // row_shr 1, 2, 4, 8: lane 15 of a row holds the row's sum
+    step(std::integral_constant<int, 0x112>{}, All{});
+    step(std::integral_constant<int, 0x114>{}, All{});
+    step(std::integral_constant<int, 0x118>{}, All{});
+    step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});      // row_bcast 15 into rows 1 and 3, 31 into rows 2 and 3: lane 63 holds the wave's
+    step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+    return lane_of(v, 63);
 }
 
 // An order of doubles as pairs of integers, the high words first: NaN below everything, -0 and 0 equal.  A high word of INT_MIN is left for what must not be chosen.
@@ -188,35 +198,38 @@ __device__ __forceinline__ Key key_of(double v) {
     return v != v ? Key{INT_MIN + 1, 0u} : Key{(int)(k >> 32), (unsigned)k};
 }
 __device__ __forceinline__ double largest_first(double &a, double b) {       // a: the larger, returns the other
-    const bool more = b > a;                             // a NaN stays out
-    const double other = more ? a : b;
-    a = more ? b : a;
+    const double other = fmin(a, b);
+    a = fmax(a, b);
     return other;
 }
 
-// A wave has a token; lane l has experts l, l + 64, ..., NS in all.  BEST: values that a group's worth is the sum of (0: one group).
-template <int NS, int BEST>
-__global__ __launch_bounds__(64 * kTokens) void score_topk(const float *__restrict__ part, int planes, float *__restrict__ logits, const Rule rule,
-                                                           int32_t *__restrict__ topk_idx, float *__restrict__ topk_w, int N, int E, int k) {
-    __shared__ double value[BEST ? kTokens : 1][BEST ? NS * 64 : 1];
-    const int wv = threadIdx.x >> 6, l = threadIdx.x & 63;
-    const int t = blockIdx.x * kTokens + wv;
-    if (t >= N) return;                                  // no barrier follows: a wave reads what it wrote itself
-    float x[NS];
+// A wave has a token, lane l experts l, l + 64, ..., NS in all.  SPLIT: NS waves have a token, 64 experts each up to the scores, and one of them chooses: fewer
+// instructions one after the other where tokens leave the chip idle (61 tokens on 256 experts us_split / us_one).  BEST: values that a group's worth is the sum
+// of (0: all groups count).
+template <int NS, int BEST, bool SPLIT>
+__global__ __launch_bounds__(64 * (SPLIT ? NS : kTokens)) void score_topk(const float *__restrict__ part, int planes, float *__restrict__ logits, const Rule rule,
+                                                                          int32_t *__restrict__ topk_idx, float *__restrict__ topk_w, int N, int E, int k) {
+    constexpr int ROWS = SPLIT ? 1 : kTokens, M = SPLIT ? 1 : NS;        // M: slots of this wave
+    __shared__ double value[BEST || SPLIT ? ROWS : 1][BEST || SPLIT ? NS * 64 : 1], score[ROWS][NS * 64];
+    __shared__ double across[SPLIT ? 2 : 1][NS];
+    const int wv = threadIdx.x >> 6, l = threadIdx.x & 63, row = SPLIT ? 0 : wv, c0 = SPLIT ? wv : 0;
+    const int t = blockIdx.x * ROWS + row;
+    if (t >= N) return;                                  // without SPLIT: no barrier follows, a wave reads what it wrote itself
+    float x[M];
     if (planes == 0) {
 #pragma unroll
-        for (int c = 0; c < NS; ++c) x[c] = l + 64 * c < E ? logits[(long)t * E + l + 64 * c] : -INFINITY;
+        for (int c = 0; c < M; ++c) x[c] = l + 64 * (c + c0) < E ? logits[(long)t * E + l + 64 * (c + c0)] : -INFINITY;
     } else {
-        float q[NS][kMostRanges];                        // all asked for before the first is used (one by one: a token on 256 experts 23 us instead of 8)
+        float q[M][kMostRanges];                         // all asked for before the first is used (one by one: a token on 256 experts 23 us instead of 14)
         const float *p = part + (long)t * E;
 #pragma unroll
         for (int z = 0; z < kMostRanges; ++z)
             if (z < planes)
 #pragma unroll
-                for (int c = 0; c < NS; ++c) q[c][z] = p[(long)z * N * E + min(l + 64 * c, E - 1)];
+                for (int c = 0; c < M; ++c) q[c][z] = p[(long)z * N * E + min(l + 64 * (c + c0), E - 1)];
 #pragma unroll
-        for (int c = 0; c < NS; ++c) {
-            const int e = l + 64 * c;
+        for (int c = 0; c < M; ++c) {
+            const int e = l + 64 * (c + c0);
             float v = q[c][0];
 #pragma unroll
             for (int z = 1; z < kMostRanges; ++z)
@@ -226,46 +239,76 @@ __global__ __launch_bounds__(64 * kTokens) void score_topk(const float *__restri
             x[c] = e < E ? v : -INFINITY;
         }
     }
-    double s[NS];
+    double s[M];
     if (rule.sigmoid) {
 #pragma unroll
-        for (int c = 0; c < NS; ++c) s[c] = 1.0 / (1.0 + exp(-(double)x[c]));
+        for (int c = 0; c < M; ++c) s[c] = 1.0 / (1.0 + exp(-(double)x[c]));
     } else {
         float m = x[0];
 #pragma unroll
-        for (int c = 1; c < NS; ++c) m = fmaxf(m, x[c]);
+        for (int c = 1; c < M; ++c) m = fmaxf(m, x[c]);
         m = wave_max(m);
+        if constexpr (SPLIT) {
+            if (l == 0) across[0][wv] = m;
+            __syncthreads();
+#pragma unroll
+            for (int c = 0; c < NS; ++c) m = fmaxf(m, (float)across[0][c]);
+        }
         double sum = 0.0;
 #pragma unroll
-        for (int c = 0; c < NS; ++c) {
-            s[c] = l + 64 * c < E ? exp((double)x[c] - (double)m) : 0.0;
+        for (int c = 0; c < M; ++c) {
+            s[c] = l + 64 * (c + c0) < E ? exp((double)x[c] - (double)m) : 0.0;
             sum += s[c];
         }
-        const double inv = 1.0 / wave_sum(sum);
+        sum = wave_sum(sum);
+        if constexpr (SPLIT) {
+            if (l == 0) across[1][wv] = sum;
+            __syncthreads();
+            sum = across[1][0];
 #pragma unroll
-        for (int c = 0; c < NS; ++c) s[c] *= inv;
+            for (int c = 1; c < NS; ++c) sum += across[1][c];
+        }
+        const double inv = 1.0 / sum;
+#pragma unroll
+        for (int c = 0; c < M; ++c) s[c] *= inv;
     }
     Key key[NS];
 #pragma unroll
-    for (int c = 0; c < NS; ++c) {
-        const int e = l + 64 * c;
+    for (int c = 0; c < M; ++c) {
+        const int e = l + 64 * (c + c0);
         double v = s[c];
-        if (e < E && rule.choice_bias != nullptr) v += (double)rule.choice_bias[e];
-        if constexpr (BEST > 0) value[wv][e] = v;
-        key[c] = key_of(v);
-        if (e >= E) key[c].hi = INT_MIN;
+        if (rule.choice_bias != nullptr) v += (double)rule.choice_bias[min(e, E - 1)];
+        if constexpr (BEST > 0 || SPLIT) value[row][e] = v;
+        score[row][e] = s[c];
+        if constexpr (!SPLIT) key[c] = key_of(v);
     }
+    if constexpr (SPLIT) {
+        __syncthreads();
+        if (wv > 0) return;
+#pragma unroll
+        for (int c = 0; c < NS; ++c) key[c] = key_of(value[0][l + 64 * c]);
+    } else {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");       // lanes read what others of their wave wrote
+    }
+#pragma unroll
+    for (int c = 0; c < NS; ++c)
+        if (l + 64 * c >= E) key[c].hi = INT_MIN;
     if constexpr (BEST > 0) {
         // 64 / groups lanes, rounded down to a power of two, look through a group and put together what they found.
         const int size = E / rule.groups, log_lanes = 31 - __builtin_clz(64 / rule.groups), lanes = 1 << log_lanes, grp = l >> log_lanes;
         double best[BEST];
 #pragma unroll
         for (int i = 0; i < BEST; ++i) best[i] = -INFINITY;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");       // lanes read what others of their wave wrote
-        for (int i = l & (lanes - 1); i < size && grp < rule.groups; i += lanes) {
-            double v = value[wv][grp * size + i];
+        for (int i0 = l & (lanes - 1); i0 < size && grp < rule.groups; i0 += 4 * lanes) {        // at most 8 values a lane
+            double v[4];
 #pragma unroll
-            for (int j = 0; j < BEST; ++j) v = largest_first(best[j], v);
+            for (int i = 0; i < 4; ++i) v[i] = value[row][grp * size + min(i0 + i * lanes, size - 1)];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                double o = i0 + i * lanes < size && v[i] == v[i] ? v[i] : -INFINITY;       // a NaN adds nothing to its group's worth
+#pragma unroll
+                for (int j = 0; j < BEST; ++j) o = largest_first(best[j], o);
+            }
         }
         for (int o = 1; o < lanes; o <<= 1) {
             double other[BEST];
@@ -294,7 +337,6 @@ __global__ __launch_bounds__(64 * kTokens) void score_topk(const float *__restri
         for (int c = 0; c < NS; ++c)
             if (!(kept >> (((l + 64 * c) * inv >> 16) << log_lanes & 63) & 1)) key[c].hi = INT_MIN;
     }
-    double mine = 0.0;
     int mine_e = 0;
     for (int j = 0; j < k; ++j) {
         int top = key[0].hi;
@@ -320,19 +362,12 @@ __global__ __launch_bounds__(64 * kTokens) void score_topk(const float *__restri
 #pragma unroll
         for (int c = NS - 1; c >= 0; --c)
             if (at[c]) e = 64 * c + __builtin_ctzll(at[c]);
-        double sv = s[0];
 #pragma unroll
         for (int c = 0; c < NS; ++c)
-            if (c == e >> 6) {
-                sv = s[c];
-                key[c].hi = l == (e & 63) ? INT_MIN : key[c].hi;
-            }
-        sv = lane_of(sv, e & 63);
-        if (l == j) {
-            mine = sv;
-            mine_e = e;
-        }
+            if (l + 64 * c == e) key[c].hi = INT_MIN;
+        if (l == j) mine_e = e;
     }
+    const double mine = score[row][mine_e];
     const double sum = rule.renorm ? wave_sum(l < k ? mine : 0.0) : 0.0;
     if (l < k) {
         const double w = !rule.renorm ? mine : sum == 0.0 ? 1.0 / k : mine / sum;
@@ -346,9 +381,11 @@ __global__ __launch_bounds__(64 * kTokens) void score_topk(const float *__restri
 hipError_t launch_score(const RouteArgs &a, const float *part, int planes, hipStream_t s) {
     const moe_scoring &c = *a.scoring;
     const Rule rule{c.logit_bias, c.choice_bias, c.score == MOE_SCORE_SIGMOID, c.groups, c.top_groups, c.renormalise, c.factor};
+    const bool split = a.N <= 512 && a.E > 64;
     const auto go = [&](auto ns, auto best) {
-        score_topk<decltype(ns)::value, decltype(best)::value><<<dim3((a.N + kTokens - 1) / kTokens), dim3(64 * kTokens), 0, s>>>(part, planes, a.logits, rule, a.topk_idx, a.topk_w, a.N,
-                                                                                                                                 a.E, a.k);
+        constexpr int NS = decltype(ns)::value, BEST = decltype(best)::value;
+        if (NS > 1 && split) score_topk<NS, BEST, (NS > 1)><<<dim3(a.N), dim3(64 * NS), 0, s>>>(part, planes, a.logits, rule, a.topk_idx, a.topk_w, a.N, a.E, a.k);
+        else score_topk<NS, BEST, false><<<dim3((a.N + kTokens - 1) / kTokens), dim3(64 * kTokens), 0, s>>>(part, planes, a.logits, rule, a.topk_idx, a.topk_w, a.N, a.E, a.k);
     };
     const auto by_best = [&](auto ns) {
         if (c.top_groups == c.groups) go(ns, std::integral_constant<int, 0>{});
@@ -359,30 +396,31 @@ hipError_t launch_score(const RouteArgs &a, const float *part, int planes, hipSt
     };
     if (a.E <= 64) by_best(std::integral_constant<int, 1>{});
     else if (a.E <= 128) by_best(std::integral_constant<int, 2>{});
+    else if (a.E <= 192) by_best(std::integral_constant<int, 3>{});
     else by_best(std::integral_constant<int, 4>{});
     return hipGetLastError();
 }
 
 hipError_t launch_gate_scored(const RouteArgs &a, hipStream_t s) {
     const int blocks = (a.E + 31) / 32, tt = a.N <= 16 ? 1 : a.N <= 32 ? 2 : 4, tiles = (a.N + tt * 16 - 1) / (tt * 16);
-    // Parts of the range a workgroup: up to 8 waves, 4 parts.  Ranges: as many as give 256 workgroups, 16 at most, each part 32 columns at least; what the scratch holds.
-    int slices = std::max(1, std::min(4, 8 / blocks));
-    while (slices > 1 && a.H < 32 * slices) slices /= 2;
+    // Parts of the range a workgroup: up to 8 waves, 4 parts.  Ranges: as many as give 256 workgroups, 16 at most, each part 64 columns at least; what the scratch holds.
+    const int slices = std::max(1, std::min({4, 8 / blocks, a.H / 64})), steps = blocks >= 3 ? 8 : 4;
     const long fit = (long)a.k * a.H / a.E;              // the context's room for k rows of H floats a token
     long ranges = std::max(1l, std::min({256l / tiles, (long)kMostRanges, (long)a.H / (64 * slices), fit}));
     const int range = (int)(((a.H + ranges - 1) / ranges + 63) / 64 * 64);
     ranges = (a.H + range - 1) / range;
     float *part = ranges > 1 ? a.scratch : a.logits;
-    const auto go = [&](auto t, auto packed) {
-        constexpr int TT = decltype(t)::value;
-        const size_t lds = std::max<size_t>((size_t)slices * 2 * TT * 16 * kStage * 2, (size_t)(slices - 1) * blocks * 2 * TT * 1024);
-        gate_ranges<TT, decltype(packed)::value><<<dim3(tiles, (unsigned)ranges), dim3(64 * blocks * slices), lds, s>>>((const uint16_t *)a.x, (const uint16_t *)a.Wg, part, a.N, a.H, a.E, blocks,
-                                                                                                                    slices, range);
+    const auto go = [&](auto t, auto st, auto packed) {
+        constexpr int TT = decltype(t)::value, STEPS = decltype(st)::value;
+        const size_t lds = std::max<size_t>((size_t)slices * 2 * TT * 16 * STEPS * 64, (size_t)(slices - 1) * blocks * 2 * TT * 1024);
+        gate_ranges<TT, STEPS, decltype(packed)::value><<<dim3(tiles, (unsigned)ranges), dim3(64 * blocks * slices), lds, s>>>((const uint16_t *)a.x, (const uint16_t *)a.Wg, part, a.N, a.H,
+                                                                                                                           a.E, blocks, slices, range);
     };
-    const auto by_layout = [&](auto t) { a.packed ? go(t, std::true_type{}) : go(t, std::false_type{}); };
-    if (tt == 1) by_layout(std::integral_constant<int, 1>{});
-    else if (tt == 2) by_layout(std::integral_constant<int, 2>{});
-    else by_layout(std::integral_constant<int, 4>{});
+    const auto by_layout = [&](auto t, auto st) { a.packed ? go(t, st, std::true_type{}) : go(t, st, std::false_type{}); };
+    const auto by_steps = [&](auto t) { steps == 8 ? by_layout(t, std::integral_constant<int, 8>{}) : by_layout(t, std::integral_constant<int, 4>{}); };
+    if (tt == 1) by_steps(std::integral_constant<int, 1>{});
+    else if (tt == 2) by_steps(std::integral_constant<int, 2>{});
+    else by_steps(std::integral_constant<int, 4>{});
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? launch_score(a, part, (int)ranges, s) : e;
 }
