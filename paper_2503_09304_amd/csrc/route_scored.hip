@@ -17,6 +17,7 @@ namespace {
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // ---- gate GEMM ----
 
@@ -29,23 +30,23 @@ __device__ __forceinline__ void to_lds(const char *from, const char *to) {
 }
 #pragma clang diagnostic pop
 
-constexpr int kMostRanges = 16;
+constexpr int kMostRanges = 16, kMostWaves = 16;
+constexpr int kStage = 128;           // columns of the hidden size that stand in LDS at once
 
 // Products of TT * 16 tokens with all experts over a range of the hidden size: a wave has 32 experts (and, where experts are few, one of `slices` parts of the range).
 // Lane l's operands are experts 2 (l%16) and 2 (l%16) + 1 of the wave's.  Row-major weights [H][E] (E even): it takes the pairs of 8 rows and turns them over in
 // registers, so no transposed copy is written first.
-template <int TT, int STEPS, bool PACKED>
-__global__ __launch_bounds__(512) void gate_ranges(const uint16_t *__restrict__ x, const uint16_t *__restrict__ Wg, float *__restrict__ part, int N, int H, int E,
+template <int TT, bool PACKED>
+__global__ __launch_bounds__(64 * kMostWaves) void gate_ranges(const uint16_t *__restrict__ x, const uint16_t *__restrict__ Wg, float *__restrict__ part, int N, int H, int E,
                                                    int blocks, int slices, int range) {
     extern __shared__ __align__(16) char lds[];
-    constexpr int kStage = 32 * STEPS, PIECES = 4 * STEPS, STAGE_BYTES = TT * 16 * kStage * 2;       // columns that stand in LDS at once, in pieces of 8
+    constexpr int STEPS = kStage / 32, PIECES = kStage / 8, STAGE_BYTES = TT * 16 * kStage * 2;
     const int w = threadIdx.x >> 6, l = threadIdx.x & 63, t16 = l & 15, g = l >> 4;
     const int pb = w % blocks, sl = w / blocks;
     const int t0 = blockIdx.x * (TT * 16), from = blockIdx.y * range, to = min(H, from + range);
     const int per = ((to - from + slices - 1) / slices + 31) / 32 * 32, k0 = min(to, from + sl * per), k1 = min(to, k0 + per);
     char *const mine = lds + sl * 2 * STAGE_BYTES;
-    // The blocks' waves of a slice bring its tokens.  Token t's piece p stands in place p ^ t of its 16 (of 32, in its half), so that the 16 tokens of a
-    // read use all banks.
+    // The blocks' waves of a slice bring its tokens.  Token t's piece p (8 columns) stands in place p ^ t of its 16, so that the 16 tokens of a read use all banks.
     const auto bring = [&](int k, int buf) {
         for (int j = pb; j < TT * STEPS; j += blocks) {
             const int i = j * 64 + l, t = i / PIECES, at = k + ((i % PIECES) ^ (t & 15)) * 8;
@@ -135,8 +136,13 @@ __global__ __launch_bounds__(512) void gate_ranges(const uint16_t *__restrict__ 
         for (int i = 0; i < 4; ++i) {
             const int t = t0 + n * 16 + 4 * g + i;
             float *o = part + ((long)blockIdx.y * N + t) * E + e0;
-            if (t < N && e0 < E) o[0] = acc[n][0][i];
-            if (t < N && e0 + 1 < E) o[1] = acc[n][1][i];
+            if (t >= N || e0 >= E) continue;
+            if (E % 2 == 0) {
+                *reinterpret_cast<f32x2 *>(o) = f32x2{acc[n][0][i], acc[n][1][i]};
+            } else {
+                o[0] = acc[n][0][i];
+                if (e0 + 1 < E) o[1] = acc[n][1][i];
+            }
         }
 }
 
@@ -381,7 +387,7 @@ __global__ __launch_bounds__(64 * (SPLIT ? NS : kTokens)) void score_topk(const 
 hipError_t launch_score(const RouteArgs &a, const float *part, int planes, hipStream_t s) {
     const moe_scoring &c = *a.scoring;
     const Rule rule{c.logit_bias, c.choice_bias, c.score == MOE_SCORE_SIGMOID, c.groups, c.top_groups, c.renormalise, c.factor};
-    const bool split = a.N <= 512 && a.E > 64;
+    const bool split = a.N <= 2048 && a.E > 64;
     const auto go = [&](auto ns, auto best) {
         constexpr int NS = decltype(ns)::value, BEST = decltype(best)::value;
         if (NS > 1 && split) score_topk<NS, BEST, (NS > 1)><<<dim3(a.N), dim3(64 * NS), 0, s>>>(part, planes, a.logits, rule, a.topk_idx, a.topk_w, a.N, a.E, a.k);
@@ -403,24 +409,23 @@ hipError_t launch_score(const RouteArgs &a, const float *part, int planes, hipSt
 
 hipError_t launch_gate_scored(const RouteArgs &a, hipStream_t s) {
     const int blocks = (a.E + 31) / 32, tt = a.N <= 16 ? 1 : a.N <= 32 ? 2 : 4, tiles = (a.N + tt * 16 - 1) / (tt * 16);
-    // Parts of the range a workgroup: up to 8 waves, 4 parts.  Ranges: as many as give 256 workgroups, 16 at most, each part 64 columns at least; what the scratch holds.
-    const int slices = std::max(1, std::min({4, 8 / blocks, a.H / 64})), steps = blocks >= 3 ? 8 : 4;
+    // Parts of the range a workgroup: up to 16 waves, 4 parts.  Ranges: as many as give 256 workgroups, 16 at most, each part 64 columns at least; what the scratch holds.
+    const int slices = std::max(1, std::min({4, kMostWaves / blocks, a.H / 64}));
     const long fit = (long)a.k * a.H / a.E;              // the context's room for k rows of H floats a token
     long ranges = std::max(1l, std::min({256l / tiles, (long)kMostRanges, (long)a.H / (64 * slices), fit}));
     const int range = (int)(((a.H + ranges - 1) / ranges + 63) / 64 * 64);
     ranges = (a.H + range - 1) / range;
     float *part = ranges > 1 ? a.scratch : a.logits;
-    const auto go = [&](auto t, auto st, auto packed) {
-        constexpr int TT = decltype(t)::value, STEPS = decltype(st)::value;
-        const size_t lds = std::max<size_t>((size_t)slices * 2 * TT * 16 * STEPS * 64, (size_t)(slices - 1) * blocks * 2 * TT * 1024);
-        gate_ranges<TT, STEPS, decltype(packed)::value><<<dim3(tiles, (unsigned)ranges), dim3(64 * blocks * slices), lds, s>>>((const uint16_t *)a.x, (const uint16_t *)a.Wg, part, a.N, a.H,
-                                                                                                                           a.E, blocks, slices, range);
+    const auto go = [&](auto t, auto packed) {
+        constexpr int TT = decltype(t)::value;
+        const size_t lds = std::max<size_t>((size_t)slices * 2 * TT * 16 * kStage * 2, (size_t)(slices - 1) * blocks * 2 * TT * 1024);
+        gate_ranges<TT, decltype(packed)::value><<<dim3(tiles, (unsigned)ranges), dim3(64 * blocks * slices), lds, s>>>((const uint16_t *)a.x, (const uint16_t *)a.Wg, part, a.N, a.H, a.E, blocks,
+                                                                                                                    slices, range);
     };
-    const auto by_layout = [&](auto t, auto st) { a.packed ? go(t, st, std::true_type{}) : go(t, st, std::false_type{}); };
-    const auto by_steps = [&](auto t) { steps == 8 ? by_layout(t, std::integral_constant<int, 8>{}) : by_layout(t, std::integral_constant<int, 4>{}); };
-    if (tt == 1) by_steps(std::integral_constant<int, 1>{});
-    else if (tt == 2) by_steps(std::integral_constant<int, 2>{});
-    else by_steps(std::integral_constant<int, 4>{});
+    const auto by_layout = [&](auto t) { a.packed ? go(t, std::true_type{}) : go(t, std::false_type{}); };
+    if (tt == 1) by_layout(std::integral_constant<int, 1>{});
+    else if (tt == 2) by_layout(std::integral_constant<int, 2>{});
+    else by_layout(std::integral_constant<int, 4>{});
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? launch_score(a, part, (int)ranges, s) : e;
 }

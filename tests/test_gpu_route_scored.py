@@ -91,6 +91,15 @@ def test_tokens(N, E, H):
     check(N, H, E, min(E, 8), groups=4, take=4 if E == 8 else 2, best=2, factor=2.5)
 
 
+@pytest.mark.parametrize("E", [1, 2, 31, 32, 33, 64, 66, 96, 128, 150, 160, 192, 224, 255, 256])
+@pytest.mark.parametrize("N", [1, 30, 2100])
+def test_experts(N, E):
+    """Waves, slices and ranges go by the experts; room for ranges by k and H."""
+    for H, k in ((64, 1), (1024, min(E, 3))):
+        check(N, H, E, k)
+        check(N, H, E, k, "softmax", packed=True)
+
+
 @pytest.mark.parametrize("H", [64, 128, 192, 576, 1024, 1600, 4096, 7168])
 @pytest.mark.parametrize("packed", [False, True])
 def test_inner_sizes(H, packed):
