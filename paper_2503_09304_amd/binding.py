@@ -177,9 +177,17 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else int(t.data_ptr())
 
 
+_current_stream = None
+
+
 def _stream() -> int:
-    import torch
-    return int(torch.cuda.current_stream().cuda_stream)
+    """PyTorch's current stream of the current device.  torch.cuda.current_stream() builds a stream object, 2 us of a call's 10."""
+    global _current_stream
+    if _current_stream is None:
+        import torch
+        raw, device = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+        _current_stream = (lambda: raw(device())) if raw and device else (lambda: int(torch.cuda.current_stream().cuda_stream))
+    return _current_stream()
 
 
 class MoeScoring:
@@ -216,7 +224,8 @@ class Context:
         self.cfg = MoeConfig(E, k, H, F, dtype, chunk_rows, max_tokens, down_ksplit)
         self.nbytes = moe_workspace_bytes(self.cfg)
         self.ws = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
-        assert self.ws.data_ptr() % 256 == 0
+        self._ws_at, self._typed = self.ws.data_ptr(), None
+        assert self._ws_at % 256 == 0
         h = C.c_void_p()
         _check(lib().moe_create(C.byref(self.cfg), self.ws.data_ptr(), self.nbytes, C.byref(h)))
         self.h = h
@@ -252,11 +261,9 @@ class Context:
 
     def route_scored(self, x, w: MoeWeights, scoring: MoeScoring, n_tokens=None):
         """The router by scores, a bias for the choice alone, and groups of experts."""
-        E = self.cfg.E
-        for name in ("logit_bias", "choice_bias"):
-            b = getattr(scoring, name)
-            if b is not None and (b.shape[0] != E or b.device != self.ws.device):
-                raise MoeError(MOE_E_ARG, f"{name} must have {E} elements on {self.ws.device}")
+        for b in (scoring.logit_bias, scoring.choice_bias):
+            if b is not None and (b.shape[0] != self.cfg.E or b.get_device() != self.ws.get_device()):
+                raise MoeError(MOE_E_ARG, f"logit_bias and choice_bias must have {self.cfg.E} elements on {self.ws.device}")
         n = x.shape[0] if n_tokens is None else n_tokens
         rc = _check(lib().moe_route_scored(self.h, _ptr(x), n, C.byref(w), C.byref(scoring._c), self._stream()))
         self.N, self._w = n, w
@@ -329,30 +336,33 @@ class Context:
 
     def get(self, what: str):
         """A tensor view (no copy) of one workspace region of the current layer-batch."""
-        import torch
         p, nb = C.c_void_p(), C.c_size_t()
         _check(lib().moe_get(self.h, GET[what], C.byref(p), C.byref(nb)))
-        off = (p.value or 0) - self.ws.data_ptr()
-        raw = self.ws[off: off + nb.value]
         N, k, E, H, F = self.N, self.cfg.k, self.cfg.E, self.cfg.H, self.cfg.F
-        act_dt = torch.bfloat16 if self.cfg.dtype == MOE_BF16 else torch.float32
+        if not self._typed:
+            import torch
+            self._typed = {t: self.ws.view(t) for t in (torch.float32, torch.int32, torch.bfloat16)}
+        f32, i32, bf16 = self._typed.values()
         if what == "logits":
-            return raw.view(torch.float32).view(N, E)
-        if what == "topk_idx":
-            return raw.view(torch.int32).view(N, k)
-        if what == "topk_w":
-            return raw.view(torch.float32).view(N, k)
-        if what == "counts":
-            return raw.view(torch.int32).view(E, 2)
-        if what in ("offsets", "perm", "inv"):
-            return raw.view(torch.int32)
-        if what == "expert_out":
-            return raw.view(torch.float32).view(N * k, H)
-        if what == "act":
-            return raw.view(act_dt).view(N * k, F)
-        if what == "units":
-            return raw.view(torch.int32).view(-1, 4)
-        raise KeyError(what)
+            of, shape = f32, (N, E)
+        elif what == "topk_idx":
+            of, shape = i32, (N, k)
+        elif what == "topk_w":
+            of, shape = f32, (N, k)
+        elif what == "counts":
+            of, shape = i32, (E, 2)
+        elif what in ("offsets", "perm", "inv"):
+            of, shape = i32, (nb.value // 4,)
+        elif what == "expert_out":
+            of, shape = f32, (N * k, H)
+        elif what == "act":
+            of, shape = bf16 if self.cfg.dtype == MOE_BF16 else f32, (N * k, F)
+        elif what == "units":
+            of, shape = i32, (nb.value // 16, 4)
+        else:
+            raise KeyError(what)
+        off = ((p.value or 0) - self._ws_at) // of.element_size()
+        return of.as_strided(shape, (shape[1], 1) if len(shape) == 2 else (1,), off)
 
 
 class SchedError(RuntimeError):
