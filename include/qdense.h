@@ -65,7 +65,7 @@ int32_t dense_norm(const dense_rows *x, const dense_rows *add, const dense_rows 
  * k - k%32 .. at ((k%128)/32 * 16 + r%16) * 4 + (k%512)/128. */
 typedef struct {
     const void *codes;     /* [device] dense_matrix4_code_bytes(rows, cols), 16-byte aligned  */
-    const uint8_t *scales; /* [device] dense_matrix4_scale_bytes(rows, cols), 4-byte aligned  */
+    const uint8_t *scales; /* [device] dense_matrix4_scale_bytes(rows, cols), 16-byte aligned */
     int32_t rows, cols;
 } dense_matrix4;
 

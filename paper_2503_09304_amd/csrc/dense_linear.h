@@ -46,11 +46,13 @@ __device__ __forceinline__ float power(uint32_t byte) { return __uint_as_float(b
 // apart.  Nothing is returned; the caller waits (vmcnt) before the barrier behind which the bytes are read.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"          // that m0 is reserved: nothing else here uses it
-__device__ __forceinline__ void to_lds(const char *from, const char *to) {
-    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)to);
+__device__ __forceinline__ void to_lds_at(const char *from, uint32_t at) {        // at: of the wave's, in LDS
     asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(at) : "m0", "memory");
 }
 #pragma clang diagnostic pop
+__device__ __forceinline__ void to_lds(const char *from, const char *to) {
+    to_lds_at(from, __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)to));
+}
 
 // Four rows r .. r+3 of one token.
 __device__ __forceinline__ void store4(const LinearArgs &a, int t, int r, const f32x4 &v) {

@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "dense_linear.h"
@@ -17,44 +18,36 @@
 namespace qdense {
 namespace {
 
-// Few tokens: bound by the matrix.  Each wave has RB tiles of 16 rows and a slice of the columns, and streams its part of the matrix, D tiles ahead of their
-// use; KS waves of a workgroup share rows and add their sums in LDS.  The tokens' columns of the workgroup's range are in LDS from the start, 16-byte pieces
-// in the places that read() says, so that the lanes of one read use all banks.
-constexpr int kWaves = 8;
+// Up to 16 tokens: bound by the matrix.  A wave has 16 rows and a slice of the columns, and streams its part of the matrix, AHEAD tiles ahead of their use; KS waves of a
+// workgroup share rows and add their sums in LDS.  The tokens' columns of the workgroup's range are in LDS from the start.
+constexpr int kWaves = 8, kFewTokens = 16;
+constexpr size_t kMostLds = 128 * 1024;
 
-template <int XT, int NT, int RB, int KS, int D>
+template <int XT, int KS>
 __global__ __launch_bounds__(64 * kWaves) void linear_few(const LinearArgs a, long first_wg, int range_blocks) {
     extern __shared__ __align__(16) char lds[];
     constexpr int PIECES = XT == X_BF16 ? 16 : 8;        // of 16 bytes, in a token's 128 columns
-    constexpr int GROUPS = kWaves / KS;
+    constexpr int GROUPS = kWaves / KS, AHEAD = 8;
     const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, g = l >> 4;
-    const int blocks = (a.K + 127) / 128, sets = (a.K + 511) / 512, row_tiles = (a.R + 15) / 16, row_wgs = (row_tiles + GROUPS * RB - 1) / (GROUPS * RB);
+    const int blocks = (a.K + 127) / 128, sets = (a.K + 511) / 512, row_tiles = (a.R + 15) / 16, row_wgs = (row_tiles + GROUPS - 1) / GROUPS;
     long wg = first_wg + blockIdx.x;
     const int z = (int)(wg % a.ranges);
     wg /= a.ranges;
-    const int rt = (int)(wg % row_wgs) * (GROUPS * RB) + w / KS * RB, t0 = (int)(wg / row_wgs) * (NT * 16);
-    const int from = z * range_blocks, n_blocks = min(blocks, from + range_blocks) - from, n_tok = min(NT * 16, a.n_tokens - t0);
+    const int rt = (int)(wg % row_wgs) * GROUPS + w / KS, t0 = (int)(wg / row_wgs) * kFewTokens;
+    const int from = z * range_blocks, n_blocks = min(blocks, from + range_blocks) - from, n_tok = min(kFewTokens, a.n_tokens - t0);
     const int per = (n_blocks + KS - 1) / KS, s0 = min(n_blocks, w % KS * per), s1 = min(n_blocks, s0 + per);
-    const uint8_t *codes[RB], *scales[RB];
-#pragma unroll
-    for (int r = 0; r < RB; ++r) {
-        const long tile = min(rt + r, row_tiles - 1);
-        codes[r] = a.codes + (tile * blocks + from) * 1024 + l * 16;
-        scales[r] = a.scales + tile * sets * 256 + l * 4;
-    }
-    u32x4 c[D][RB];
-    uint32_t sc[D][RB];
+    const long tile = min(rt, row_tiles - 1);
+    const uint8_t *codes = a.codes + (tile * blocks + from) * 1024 + l * 16, *scales = a.scales + tile * sets * 256 + l * 4;
+    u32x4 c[AHEAD];
+    uint32_t sc[AHEAD];
     const auto ask = [&](int u, int b) {
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            c[u][r] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(codes[r] + (long)b * 1024));
-            sc[u][r] = *reinterpret_cast<const uint32_t *>(scales[r] + ((from + b) >> 2) * 256);
-        }
+        c[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(codes + (long)b * 1024));
+        sc[u] = *reinterpret_cast<const uint32_t *>(scales + ((from + b) >> 2) * 256);
     };
 #pragma unroll
-    for (int u = 0; u < D; ++u)
+    for (int u = 0; u < AHEAD; ++u)
         if (s0 + u < s1) ask(u, s0 + u);
-    // Tokens to LDS.
+    // Tokens to LDS, pieces in such an order that the lanes of one read use all banks.
     const int row = n_blocks * PIECES * 16;              // bytes of a token there
     uint8_t *xb = reinterpret_cast<uint8_t *>(lds) + (n_tok * row + 1023) / 1024 * 1024;       // the last wave's load may write up to there
     {
@@ -73,93 +66,57 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few(const LinearArgs a, lo
             }
         }
     }
-    f32x4 acc[RB][NT];
-    int at[NT], sw[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int t = min(n * 16 + (l & 15), n_tok - 1);
-        at[n] = t * row;
-        sw[n] = XT == X_BF16 ? ((t & 15) ^ g) * 16 : ((t >> 1 & 7) ^ g) * 16;
-#pragma unroll
-        for (int r = 0; r < RB; ++r) acc[r][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    const int tok = min(l & 15, n_tok - 1);
+    const char *x = lds + tok * row;
+    const uint8_t *xs = xb + tok * (n_blocks * 4) + g;
+    const int sw = XT == X_BF16 ? (tok ^ g) * 16 : (tok >> 1 ^ g) * 16;
+    f32x4 acc{0.f, 0.f, 0.f, 0.f};
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // this wave's pieces are in LDS
     __syncthreads();
-    for (int b0 = s0; b0 < s1; b0 += D) {
+    for (int b0 = s0; b0 < s1; b0 += AHEAD) {
 #pragma unroll
-        for (int u = 0; u < D; ++u) {
+        for (int u = 0; u < AHEAD; ++u) {
             const int b = b0 + u;
             if (b >= s1) break;
-            const int shift = 8 * ((from + b) & 3);
+            const uint32_t wbyte = sc[u] >> 8 * ((from + b) & 3) & 255;
             if constexpr (XT == X_FP8) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const u32x4 lo = *reinterpret_cast<const u32x4 *>(lds + at[n] + b * 128 + sw[n]);
-                    const u32x4 hi = *reinterpret_cast<const u32x4 *>(lds + at[n] + b * 128 + (sw[n] ^ 64));
-                    const int byte = xb[at[n] / 32 + b * 4 + g];
-                    const i32x8 v = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-#pragma unroll
-                    for (int r = 0; r < RB; ++r) {
-                        const i32x8 wv = {(int)c[u][r][0], (int)c[u][r][1], (int)c[u][r][2], (int)c[u][r][3], 0, 0, 0, 0};
-                        acc[r][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, v, acc[r][n], 4, 0, 0, (int)(sc[u][r] >> shift & 255), 0, byte);
-                    }
-                }
+                const u32x4 lo = *reinterpret_cast<const u32x4 *>(x + b * 128 + sw), hi = *reinterpret_cast<const u32x4 *>(x + b * 128 + (sw ^ 64));
+                const i32x8 v = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+                const i32x8 wv = {(int)c[u][0], (int)c[u][1], (int)c[u][2], (int)c[u][3], 0, 0, 0, 0};
+                acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, v, acc, 4, 0, 0, (int)wbyte, 0, (int)xs[b * 4]);
             } else {
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
-                    bf16x8 wv[RB];
-#pragma unroll
-                    for (int r = 0; r < RB; ++r) wv[r] = weights8(c[u][r][s], power(sc[u][r] >> shift & 255));
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        bf16x8 v;
-                        if constexpr (XT == X_BF16) {
-                            v = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(lds + at[n] + b * 256 + (sw[n] ^ 64 * s)));
-                        } else {
-                            const u32x2 o = *reinterpret_cast<const u32x2 *>(lds + at[n] + b * 128 + (sw[n] ^ 64 * (s >> 1)) + 8 * (s & 1));
-                            v = widened8(o[0], o[1], power(xb[at[n] / 32 + b * 4 + g]));
-                        }
-#pragma unroll
-                        for (int r = 0; r < RB; ++r) acc[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[r], v, acc[r][n], 0, 0, 0);
+                    bf16x8 v;
+                    if constexpr (XT == X_BF16) {
+                        v = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(x + b * 256 + (sw ^ 64 * s)));
+                    } else {
+                        const u32x2 o = *reinterpret_cast<const u32x2 *>(x + b * 128 + (sw ^ 64 * (s >> 1)) + 8 * (s & 1));
+                        v = widened8(o[0], o[1], power(xs[b * 4]));
                     }
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(weights8(c[u][s], power(wbyte)), v, acc, 0, 0, 0);
                 }
             }
-            if (b + D < s1) ask(u, b + D);
+            if (b + AHEAD < s1) ask(u, b + AHEAD);
         }
     }
     if constexpr (KS > 1) {
         f32x4 *red = reinterpret_cast<f32x4 *>(lds);
         __syncthreads();                                 // the tokens have been read
-        if (w % KS)
-#pragma unroll
-            for (int r = 0; r < RB; ++r)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) red[(w * (RB * NT) + r * NT + n) * 64 + l] = acc[r][n];
+        if (w % KS) red[w * 64 + l] = acc;
         __syncthreads();
         if (w % KS) return;
-#pragma unroll 1
-        for (int k = 1; k < KS; ++k)
 #pragma unroll
-            for (int r = 0; r < RB; ++r)
+        for (int k = 1; k < KS; ++k) {
+            const f32x4 o = red[(w + k) * 64 + l];
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const f32x4 o = red[((w + k) * (RB * NT) + r * NT + n) * 64 + l];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[r][n][e] += o[e];
-                }
-    }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int t = t0 + n * 16 + (l & 15);
-        if (t >= a.n_tokens) continue;
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            const int o = (rt + r) * 16 + g * 4;
-            if (o >= a.R) continue;
-            if (a.ranges == 1) store4(a, t, o, acc[r][n]);
-            else *reinterpret_cast<f32x4 *>(a.part + ((long)z * a.n_tokens + t) * (row_tiles * 16l) + o) = acc[r][n];
+            for (int e = 0; e < 4; ++e) acc[e] += o[e];
         }
     }
+    const int t = t0 + (l & 15), o = rt * 16 + g * 4;
+    if (t >= a.n_tokens || o >= a.R) return;
+    if (a.ranges == 1) store4(a, t, o, acc);
+    else *reinterpret_cast<f32x4 *>(a.part + ((long)z * a.n_tokens + t) * (row_tiles * 16l) + o) = acc;
 }
 
 // The ranges' sums, added in their order.
@@ -197,74 +154,77 @@ __global__ __launch_bounds__(256) void pack4(const uint8_t *codes, const uint8_t
     }
 }
 
-constexpr size_t kMostLds = 128 * 1024;
-
 }  // namespace
 
 // How a call is cut into workgroups.
 struct Plan {
-    bool many;
-    int tiles;                    // of 16 tokens, a workgroup's
-    int ks;                       // few: waves that share rows
+    int tiles, rows;              // linear_some: of 16 tokens a workgroup, of 16 rows a wave; tiles 1: linear_few; 8: linear_many
+    int ks;                       // linear_few: waves that share rows
     int ranges, range_blocks;     // of 128 columns
-    size_t lds;                   // few
+    size_t lds;                   // linear_few
 };
 static void cut(Plan &p, int blocks, int ranges) {
     p.range_blocks = (blocks + ranges - 1) / ranges;
     p.ranges = (blocks + p.range_blocks - 1) / p.range_blocks;
 }
 static Plan few_of(int n_tokens, int R, int K, bool bf16, int ranges) {
-    const int blocks = (K + 127) / 128, row_tiles = (R + 15) / 16;
-    Plan f{};
-    f.tiles = n_tokens <= 16 ? 1 : n_tokens <= 32 ? 2 : 4;
-    const int rb = f.tiles == 4 ? 2 : 1, tokens = std::min(n_tokens, f.tiles * 16), token_tiles = (n_tokens + f.tiles * 16 - 1) / (f.tiles * 16);
-    const size_t per_block = (size_t)tokens * (bf16 ? 256 : 132);
+    const int blocks = (K + 127) / 128, row_tiles = (R + 15) / 16, token_tiles = (n_tokens + kFewTokens - 1) / kFewTokens;
+    Plan p{1, 1, 1, 1, 1, 0};
+    const size_t per_block = (size_t)std::min(n_tokens, kFewTokens) * (bf16 ? 256 : 132);
     const int most = (int)std::min<size_t>(blocks, kMostLds / per_block);
-    cut(f, blocks, std::max(ranges, (blocks + most - 1) / most));
-    const long units = (long)((row_tiles + rb - 1) / rb) * token_tiles * f.ranges;
-    f.ks = 1;
-    while (f.ks < 8 && units * f.ks < 2048 && f.range_blocks >= 2 * f.ks) f.ks *= 2;
-    f.lds = std::max<size_t>((size_t)f.range_blocks * per_block + 1024, (size_t)(f.ks > 1 ? kWaves * rb * f.tiles * 1024 : 0));
-    return f;
+    cut(p, blocks, std::max(ranges, (blocks + most - 1) / most));
+    const long units = (long)row_tiles * token_tiles * p.ranges;
+    while (p.ks < 8 && units * p.ks < 2048 && p.range_blocks >= 2 * p.ks) p.ks *= 2;
+    p.lds = std::max<size_t>((size_t)p.range_blocks * per_block + 1024, (size_t)(p.ks > 1 ? kWaves * 1024 : 0));
+    return p;
 }
-static Plan many_of(int n_tokens, int R, int K, int tiles, int ranges) {
-    Plan f{};
-    f.many = true;
-    f.tiles = tiles;
-    cut(f, (K + 127) / 128, ranges);
-    return f;
+static Plan some_of(int K, bool bf16, int tiles, int rows, int ranges) {
+    Plan p{tiles, rows, 1, 1, 1, 0};
+    const int blocks = (K + 127) / 128;
+    cut(p, blocks, bf16 ? ranges : std::max(ranges, (blocks + kSomeBlocks - 1) / kSomeBlocks));
+    return p;
 }
-// Us that a plan takes, by what was measured (H 1024 to 14336, 1024 to 32000 rows, 1 to 2048 tokens; most within 15 %): a launch 3; what a CU has to take in, at 28 bytes
-// a ns, 20 where LDS leaves room for one workgroup; tiles of many tokens per block of 128 columns and workgroup on a CU; ranges cost a launch, and their sums are written and read.
+// Us that a plan takes, by what was measured (columns 1024 to 14336, rows 1024 to 32000, 1 to 8192 tokens): a launch and the first bytes 3.6; for every block of 128 columns of the
+// workgroups that a CU has what one takes alone, or among others; linear_few what a CU takes in, at 28 bytes a ns, 20 where LDS leaves room for one workgroup; ranges a
+// launch and their sums' way to memory and back; outputs their way to memory.
 static float us_of(const Plan &p, int n_tokens, int R, int K, bool bf16) {
     const int row_tiles = (R + 15) / 16, token_tiles = (n_tokens + p.tiles * 16 - 1) / (p.tiles * 16);
-    const float join = p.ranges == 1 ? 0.f : (p.many ? 4.f : 2.2f) + (float)p.ranges * n_tokens * R * 8.f / 6e6f;
-    if (p.many) {
-        const long wgs = (long)((row_tiles + 15) / 16) * token_tiles * p.ranges, on_cu = (wgs + 255) / 256;
-        const float block = p.tiles == 8 ? (bf16 ? on_cu > 1 ? 1.5f : 1.75f : 0.95f) : (bf16 ? on_cu > 1 ? 0.83f : 0.95f : 0.6f);
-        return 3.f + (float)on_cu * p.range_blocks * block + join;
+    const float sums = (float)n_tokens * R, ends = (p.ranges == 1 ? 0.f : 2.6f + sums * p.ranges * 8.f / 6e6f) + sums * 2.f / 4.5e6f;
+    if (p.tiles == 1) {
+        const int per = kWaves / p.ks;
+        const long wgs = (long)((row_tiles + per - 1) / per) * token_tiles * p.ranges, on_cu = (wgs + 255) / 256;
+        const float x = (float)std::min(n_tokens, kFewTokens) * (bf16 ? 256.f : 132.f) * p.range_blocks, w = (float)per * p.range_blocks * 1088.f;
+        return 3.f + (float)on_cu * (x + w) / (p.lds > 80 * 1024 ? 20e3f : 28e3f) + ends;
     }
-    const int per = kWaves / p.ks * (p.tiles == 4 ? 2 : 1);
+    const int per = p.tiles == 8 ? 16 : 4 * p.rows;
     const long wgs = (long)((row_tiles + per - 1) / per) * token_tiles * p.ranges, on_cu = (wgs + 255) / 256;
-    const float x = (float)std::min(n_tokens, p.tiles * 16) * (bf16 ? 256.f : 132.f) * p.range_blocks, w = (float)per * p.range_blocks * 1088.f;
-    return 3.f + (float)on_cu * (x + w) / (p.lds > 80 * 1024 ? 20e3f : 28e3f) + join;
+    static const float alone[2][4] = {{.27f, .33f, .60f, .80f}, {.28f, .43f, .70f, 1.1f}}, among[2][4] = {{.24f, .27f, .45f, .62f}, {.225f, .31f, .48f, .88f}};
+    const int kind = p.tiles == 2 ? p.rows - 1 : p.rows == 2 ? 2 : 3;
+    const float block = p.tiles == 8 ? (bf16 ? on_cu > 1 ? 1.46f : 1.75f : on_cu > 1 ? 0.9f : 1.1f) : (on_cu > 1 ? among : alone)[bf16][kind];
+    return 3.6f + (float)on_cu * p.range_blocks * block + ends;
 }
 static Plan plan_of(int n_tokens, int R, int K, bool bf16) {
     const int blocks = (K + 127) / 128;
-    Plan best{};
-    float least = 0.f;
+    Plan best{8, 4, 1, 1, blocks, 0};
+    float least = n_tokens > 64 ? us_of(best, n_tokens, R, K, bf16) : INFINITY;
     const auto look = [&](const Plan &p) {
         const float us = us_of(p, n_tokens, R, K, bf16);
-        if (best.tiles == 0 || us < least) {
+        if (us < least) {
             best = p;
             least = us;
         }
     };
     for (const int z : {1, 2, 3, 4, 6, 8, 12, 16}) {
-        if (z > blocks) break;
-        if (n_tokens <= 64) look(few_of(n_tokens, R, K, bf16, z));
-        if (n_tokens > 16) look(many_of(n_tokens, R, K, 4, z));
-        if (n_tokens > 64) look(many_of(n_tokens, R, K, 8, z));
+        if (z > 1 && (z > blocks || (long)n_tokens * R * z > 1 << 26)) break;
+        if (n_tokens <= kFewTokens) look(few_of(n_tokens, R, K, bf16, z));
+        if (n_tokens <= 4096) {
+            look(some_of(K, bf16, 2, 1, z));
+            look(some_of(K, bf16, 2, 2, z));
+        }
+        if (n_tokens > 32) {
+            look(some_of(K, bf16, 4, 2, z));
+            look(some_of(K, bf16, 4, 4, z));
+        }
     }
     return best;
 }
@@ -272,34 +232,31 @@ static Plan plan_of(int n_tokens, int R, int K, bool bf16) {
 int linear_ranges(int n_tokens, int R, int K, int x_type, int) { return plan_of(n_tokens, R, K, x_type == DENSE_BF16).ranges; }
 
 hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
-    Plan f = plan_of(a.n_tokens, a.R, a.K, a.x_type == DENSE_BF16);
-    if (f.ranges > a.ranges) f = many_of(a.n_tokens, a.R, a.K, a.n_tokens > 64 ? 8 : 4, 1);        // no workspace
+    const Plan p = plan_of(a.n_tokens, a.R, a.K, a.x_type == DENSE_BF16);
+    if (p.tiles == 8 || p.ranges > a.ranges) return launch_linear_many(a, s);              // or no workspace
     const int row_tiles = (a.R + 15) / 16;
-    const auto go = [&](auto xt, auto nt, auto ks) {
-        constexpr int XT = decltype(xt)::value, NT = decltype(nt)::value, KS = decltype(ks)::value, RB = NT == 4 ? 2 : 1, D = NT == 4 ? 4 : 8, PER = kWaves / KS * RB;
-        const long all = (long)((row_tiles + PER - 1) / PER) * ((a.n_tokens + NT * 16 - 1) / (NT * 16)) * f.ranges;
-        constexpr long kMost = 1 << 22;                  // workgroups of 512 threads that a launch may have
-        for (long at = 0; at < all; at += kMost)
-            linear_few<XT, NT, RB, KS, D><<<dim3((unsigned)std::min(kMost, all - at)), dim3(64 * kWaves), f.lds, s>>>(a, at, f.range_blocks);
-    };
-    const auto by_slices = [&](auto xt, auto nt) {
-        if (f.ks == 1) go(xt, nt, std::integral_constant<int, 1>{});
-        else if (f.ks == 2) go(xt, nt, std::integral_constant<int, 2>{});
-        else if (f.ks == 4) go(xt, nt, std::integral_constant<int, 4>{});
-        else go(xt, nt, std::integral_constant<int, 8>{});
-    };
-    const auto by_tokens = [&](auto xt) {
-        if (f.tiles == 1) by_slices(xt, std::integral_constant<int, 1>{});
-        else if (f.tiles == 2) by_slices(xt, std::integral_constant<int, 2>{});
-        else by_slices(xt, std::integral_constant<int, 4>{});
-    };
-    if (f.many) {
-        const hipError_t e = launch_linear_many(a, f.tiles, f.range_blocks, s);
+    if (p.tiles > 1) {
+        const hipError_t e = launch_linear_some(a, p.tiles, p.rows, p.range_blocks, s);
         if (e != hipSuccess) return e;
-    } else if (a.x_type == DENSE_BF16) by_tokens(std::integral_constant<int, X_BF16>{});
-    else if (a.out_type == DENSE_BF16) by_tokens(std::integral_constant<int, X_FP8>{});
-    else by_tokens(std::integral_constant<int, X_WIDE>{});
-    if (f.ranges > 1) {
+    } else {
+        const auto go = [&](auto xt, auto ks) {
+            constexpr int XT = decltype(xt)::value, KS = decltype(ks)::value, PER = kWaves / KS;
+            const long all = (long)((row_tiles + PER - 1) / PER) * ((a.n_tokens + kFewTokens - 1) / kFewTokens) * p.ranges;
+            constexpr long kMost = 1 << 22;              // workgroups of 512 threads that a launch may have
+            for (long at = 0; at < all; at += kMost)
+                linear_few<XT, KS><<<dim3((unsigned)std::min(kMost, all - at)), dim3(64 * kWaves), p.lds, s>>>(a, at, p.range_blocks);
+        };
+        const auto by_slices = [&](auto xt) {
+            if (p.ks == 1) go(xt, std::integral_constant<int, 1>{});
+            else if (p.ks == 2) go(xt, std::integral_constant<int, 2>{});
+            else if (p.ks == 4) go(xt, std::integral_constant<int, 4>{});
+            else go(xt, std::integral_constant<int, 8>{});
+        };
+        if (a.x_type == DENSE_BF16) by_slices(std::integral_constant<int, X_BF16>{});
+        else if (a.out_type == DENSE_BF16) by_slices(std::integral_constant<int, X_FP8>{});
+        else by_slices(std::integral_constant<int, X_WIDE>{});
+    }
+    if (p.ranges > 1) {
         const long n = (long)a.n_tokens * row_tiles * 4;
         join_ranges<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s>>>(a);
     }

@@ -46,7 +46,7 @@ int32_t check_matrix(const dense_matrix4 *w, const char *call) {
     if (!w) return set_error(MOE_E_ARG, "%s: the matrix is null", call);
     if (!matrix_ok(w->rows, w->cols)) return set_error(MOE_E_ARG, "%s: rows must be 1..2^24, cols a multiple of 32 from 32 to 2^20", call);
     if (!w->codes || !w->scales) return set_error(MOE_E_ARG, "%s: codes or scales is null", call);
-    if (!aligned(w->codes, 16) || !aligned(w->scales, 4)) return set_error(MOE_E_ARG, "%s: codes must be 16-byte, scales 4-byte aligned", call);
+    if (!aligned(w->codes, 16) || !aligned(w->scales, 16)) return set_error(MOE_E_ARG, "%s: codes and scales must be 16-byte aligned", call);
     return MOE_OK;
 }
 
