@@ -128,11 +128,19 @@ __global__ __launch_bounds__(256) void join_ranges(const LinearArgs a) {
     if (r >= a.R) return;
     const long plane = (long)a.n_tokens * quads * 4;
     const float *from = a.part + (long)t * quads * 4 + r;
-    f32x4 v = *reinterpret_cast<const f32x4 *>(from);
-    for (int z = 1; z < a.ranges; ++z) {
-        const f32x4 o = *reinterpret_cast<const f32x4 *>(from + z * plane);
+    constexpr int U = 8;                                 // asked for before the first is added
+    f32x4 v{0.f, 0.f, 0.f, 0.f};
+    for (int z0 = 0; z0 < a.ranges; z0 += U) {
+        f32x4 o[U];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += o[e];
+        for (int u = 0; u < U; ++u)
+            if (z0 + u < a.ranges) o[u] = *reinterpret_cast<const f32x4 *>(from + (z0 + u) * plane);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (z0 + u < a.ranges) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += o[u][e];
+            }
     }
     store4(a, t, r, v);
 }
@@ -159,7 +167,7 @@ __global__ __launch_bounds__(256) void pack4(const uint8_t *codes, const uint8_t
 // How a call is cut into workgroups.
 struct Plan {
     int tiles, rows;              // linear_some: of 16 tokens a workgroup, of 16 rows a wave; tiles 1: linear_few; 8: linear_many
-    int ks;                       // linear_few: waves that share rows
+    int ks;                       // waves that share rows
     int ranges, range_blocks;     // of 128 columns
     size_t lds;                   // linear_few
 };
@@ -178,8 +186,8 @@ static Plan few_of(int n_tokens, int R, int K, bool bf16, int ranges) {
     p.lds = std::max<size_t>((size_t)p.range_blocks * per_block + 1024, (size_t)(p.ks > 1 ? kWaves * 1024 : 0));
     return p;
 }
-static Plan some_of(int K, bool bf16, int tiles, int rows, int ranges) {
-    Plan p{tiles, rows, 1, 1, 1, 0};
+static Plan some_of(int K, bool bf16, int tiles, int rows, int ks, int ranges) {
+    Plan p{tiles, rows, ks, 1, 1, 0};
     const int blocks = (K + 127) / 128;
     cut(p, blocks, bf16 ? ranges : std::max(ranges, (blocks + kSomeBlocks - 1) / kSomeBlocks));
     return p;
@@ -196,11 +204,12 @@ static float us_of(const Plan &p, int n_tokens, int R, int K, bool bf16) {
         const float x = (float)std::min(n_tokens, kFewTokens) * (bf16 ? 256.f : 132.f) * p.range_blocks, w = (float)per * p.range_blocks * 1088.f;
         return 3.f + (float)on_cu * (x + w) / (p.lds > 80 * 1024 ? 20e3f : 28e3f) + ends;
     }
-    const int per = p.tiles == 8 ? 16 : 4 * p.rows;
+    const int per = p.tiles == 8 ? 16 : 4 * p.rows / p.ks;
     const long wgs = (long)((row_tiles + per - 1) / per) * token_tiles * p.ranges, on_cu = (wgs + 255) / 256;
     static const float alone[2][4] = {{.27f, .33f, .60f, .80f}, {.28f, .43f, .70f, 1.1f}}, among[2][4] = {{.24f, .27f, .45f, .62f}, {.225f, .31f, .48f, .88f}};
     const int kind = p.tiles == 2 ? p.rows - 1 : p.rows == 2 ? 2 : 3;
     const float block = p.tiles == 8 ? (bf16 ? on_cu > 1 ? 1.46f : 1.75f : on_cu > 1 ? 0.9f : 1.1f) : (on_cu > 1 ? among : alone)[bf16][kind];
+    if (p.ks > 1) return 3.6f + (float)on_cu * ((p.range_blocks + p.ks - 1) / p.ks) * .45f + ends;
     return 3.6f + (float)on_cu * p.range_blocks * block + ends;
 }
 static Plan plan_of(int n_tokens, int R, int K, bool bf16) {
@@ -217,13 +226,14 @@ static Plan plan_of(int n_tokens, int R, int K, bool bf16) {
     for (const int z : {1, 2, 3, 4, 6, 8, 12, 16}) {
         if (z > 1 && (z > blocks || (long)n_tokens * R * z > 1 << 26)) break;
         if (n_tokens <= kFewTokens) look(few_of(n_tokens, R, K, bf16, z));
+        if (n_tokens <= 1024) look(some_of(K, bf16, 2, 1, 4, z));
         if (n_tokens <= 4096) {
-            look(some_of(K, bf16, 2, 1, z));
-            look(some_of(K, bf16, 2, 2, z));
+            look(some_of(K, bf16, 2, 1, 1, z));
+            look(some_of(K, bf16, 2, 2, 1, z));
         }
         if (n_tokens > 32) {
-            look(some_of(K, bf16, 4, 2, z));
-            look(some_of(K, bf16, 4, 4, z));
+            look(some_of(K, bf16, 4, 2, 1, z));
+            look(some_of(K, bf16, 4, 4, 1, z));
         }
     }
     return best;
@@ -236,7 +246,7 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
     if (p.tiles == 8 || p.ranges > a.ranges) return launch_linear_many(a, s);              // or no workspace
     const int row_tiles = (a.R + 15) / 16;
     if (p.tiles > 1) {
-        const hipError_t e = launch_linear_some(a, p.tiles, p.rows, p.range_blocks, s);
+        const hipError_t e = launch_linear_some(a, p.tiles, p.rows, p.ks, p.range_blocks, s);
         if (e != hipSuccess) return e;
     } else {
         const auto go = [&](auto xt, auto ks) {

@@ -24,19 +24,21 @@ __device__ __forceinline__ void wait_for(int later) {    // for all but the load
     else wait_for<C, R - 1>(later);
 }
 
-template <int XT, int NT, int RB, int AHEAD>
+// KS 4: the workgroup has 16 * RB rows, and each wave every fourth block of the range, with tokens of its own and no barrier between blocks; the waves' sums meet in LDS.
+template <int XT, int NT, int RB, int KS, int AHEAD>
 __global__ __launch_bounds__(64 * kWaves) void linear_some(const LinearArgs a, long first_wg, int range_blocks) {
     constexpr int PIECES = XT == X_BF16 ? 16 : 8;        // of 16 bytes, in a token's 128 columns
-    constexpr int TOK = NT * 16, X = TOK * PIECES * 16, LOADS = X / 1024 / kWaves, WAVE = RB * 1024 + 1024, SLOT = X + kWaves * WAVE, SLOTS = AHEAD + 1;
+    constexpr int TOK = NT * 16, X = TOK * PIECES * 16, SHARE = kWaves / KS, LOADS = X / 1024 / SHARE, WAVE = RB * 1024 + 1024, SLOT = KS * X + kWaves * WAVE, SLOTS = AHEAD + 1;
     constexpr int COUNT = LOADS + RB + 1;                // a wave's loads for a block
-    static_assert(LOADS >= 1 && (TOK / LOADS) % 16 == 0, "the order of pieces goes by the token's place in 16");
+    static_assert(KS == 1 || KS == kWaves, "waves share tokens or have their own");
+    static_assert(LOADS >= 1 && (KS == 1 || SLOTS * SLOT >= kWaves * RB * NT * 1024), "room for a wave's load, and for the sums");
     static_assert(COUNT * AHEAD < 64, "the counter of loads under way has six bits");
     __shared__ __align__(16) char lds[SLOTS * SLOT];
     __shared__ uint32_t xb[XT == X_BF16 ? 1 : kSomeBlocks][XT == X_BF16 ? 1 : TOK];
     const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, g = l >> 4, t16 = l & 15;
-    const int blocks = (a.K + 127) / 128, sets = (a.K + 511) / 512, row_tiles = (a.R + 15) / 16, row_wgs = (row_tiles + RB * kWaves - 1) / (RB * kWaves);
+    const int blocks = (a.K + 127) / 128, sets = (a.K + 511) / 512, row_tiles = (a.R + 15) / 16, row_wgs = (row_tiles + RB * SHARE - 1) / (RB * SHARE);
     long wg = first_wg + blockIdx.x;
-    const int rt = (int)(wg % row_wgs) * (RB * kWaves) + w * RB;
+    const int rt = (int)(wg % row_wgs) * (RB * SHARE) + w / KS * RB, wk = w % KS, ws = w / KS;
     wg /= row_wgs;
     const int z = (int)(wg % a.ranges), t0 = (int)(wg / a.ranges) * TOK, from = z * range_blocks, n = min(blocks, from + range_blocks) - from;
     const uint8_t *codes[RB];
@@ -44,25 +46,29 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(const LinearArgs a, l
     for (int r = 0; r < RB; ++r) codes[r] = a.codes + ((long)min(rt + r, row_tiles - 1) * blocks + from) * 1024 + l * 16;
     const uint8_t *scales = a.scales + (long)min(rt + (l >> 4) % RB, row_tiles - 1) * sets * 256 + t16 * 16;       // RB tiles' 256 bytes, 16 lanes each
     const char *src[LOADS];
-    int first_piece;
+    int first_piece[LOADS];
     {
         constexpr int PER = 64 / PIECES;                 // tokens of a wave's load
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) src[j] = a.x.p + (long)min(t0 + (w + kWaves * j) * PER + l / PIECES, a.n_tokens - 1) * a.x.ts * (XT == X_BF16 ? 2 : 1);
-        const int t = w * PER + l / PIECES, p = l % PIECES, q = XT == X_BF16 ? p ^ (t & 15) : p ^ (t >> 1 & 7);
-        first_piece = XT == X_BF16 ? 4 * (q & 3) + (q >> 2) : XT == X_FP8 ? q : 2 * (q & 3) + (q >> 2);
+        for (int j = 0; j < LOADS; ++j) {
+            const int t = (ws + SHARE * j) * PER + l / PIECES, p = l % PIECES, q = XT == X_BF16 ? p ^ (t & 15) : p ^ (t >> 1 & 7);
+            src[j] = a.x.p + (long)min(t0 + t, a.n_tokens - 1) * a.x.ts * (XT == X_BF16 ? 2 : 1);
+            first_piece[j] = XT == X_BF16 ? 4 * (q & 3) + (q >> 2) : XT == X_FP8 ? q : 2 * (q & 3) + (q >> 2);
+        }
     }
     const int k_bytes = a.K * (XT == X_BF16 ? 2 : 1);
-    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds, mine = __builtin_amdgcn_readfirstlane(base + X + w * WAVE),
-                   piece0 = __builtin_amdgcn_readfirstlane(base + w * 1024);
+    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds, mine = __builtin_amdgcn_readfirstlane(base + KS * X + w * WAVE),
+                   piece0 = __builtin_amdgcn_readfirstlane(base + wk * X + ws * 1024);
     const auto bring = [&](int b, int slot) {
         const uint32_t to = slot * SLOT;
 #pragma unroll
         for (int r = 0; r < RB; ++r) to_lds_at(reinterpret_cast<const char *>(codes[r]) + (long)b * 1024, mine + to + r * 1024);
         to_lds_at(reinterpret_cast<const char *>(scales) + ((from + b) >> 2) * 256, mine + to + RB * 1024);
-        const int at = ((from + b) * PIECES + first_piece) * 16, off = at < k_bytes ? at : 0;        // behind the last column: weights are zero there
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) to_lds_at(src[j] + off, piece0 + to + j * (kWaves * 1024));
+        for (int j = 0; j < LOADS; ++j) {
+            const int at = ((from + b) * PIECES + first_piece[j]) * 16;
+            to_lds_at(src[j] + (at < k_bytes ? at : 0), piece0 + to + j * (SHARE * 1024));        // behind the last column: weights are zero there
+        }
     };
     if constexpr (XT != X_BF16) {                        // the tokens' scale bytes of the range, four a block
         const int all = a.K / 32;
@@ -79,13 +85,17 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(const LinearArgs a, l
 #pragma unroll
     for (int r = 0; r < RB; ++r)
 #pragma unroll
-        for (int i = 0; i < NT; ++i) acc[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int b = 0; b < min(AHEAD, n); ++b) bring(b, b);
-    for (int b = 0, slot = 0, next = AHEAD; b < n; ++b) {
-        wait_for<COUNT, AHEAD - 1>(n - 1 - b);           // this wave's pieces of block b are in LDS
-        __syncthreads();                                 // everybody's; and block b - 1, in whose place the next one comes, has been read
-        if (b + AHEAD < n) bring(b + AHEAD, next);
-        const char *x = lds + slot * SLOT, *wt = x + X + w * WAVE;
+        for (int m = 0; m < NT; ++m) acc[r][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int mine_n = (n - wk + KS - 1) / KS;           // this wave's blocks: wk, wk + KS, ...
+    for (int i = 0; i < min(AHEAD, mine_n); ++i) bring(wk + i * KS, i);
+    if constexpr (KS > 1 && XT != X_BF16) __syncthreads();
+    for (int i = 0, slot = 0, next = AHEAD; i < mine_n; ++i) {
+        const int b = wk + i * KS;
+        wait_for<COUNT, AHEAD - 1>(mine_n - 1 - i);      // this wave's pieces of block b are in LDS
+        if constexpr (KS == 1) __syncthreads();          // everybody's; and the block before, in whose place the next one comes, has been read
+        else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (i + AHEAD < mine_n) bring(b + AHEAD * KS, next);
+        const char *x = lds + slot * SLOT + wk * X, *wt = lds + slot * SLOT + KS * X + w * WAVE;
         u32x4 c[RB];
         uint32_t sc[RB];
 #pragma unroll
@@ -95,15 +105,15 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(const LinearArgs a, l
         }
         if constexpr (XT == X_FP8) {
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                const u32x4 lo = *reinterpret_cast<const u32x4 *>(x + i * 2048 + t16 * 128 + ((g ^ (t16 >> 1)) * 16));
-                const u32x4 hi = *reinterpret_cast<const u32x4 *>(x + i * 2048 + t16 * 128 + (((4 + g) ^ (t16 >> 1)) * 16));
-                const int byte = xb[b][i * 16 + t16] >> 8 * g & 255;
+            for (int m = 0; m < NT; ++m) {
+                const u32x4 lo = *reinterpret_cast<const u32x4 *>(x + m * 2048 + t16 * 128 + ((g ^ (t16 >> 1)) * 16));
+                const u32x4 hi = *reinterpret_cast<const u32x4 *>(x + m * 2048 + t16 * 128 + (((4 + g) ^ (t16 >> 1)) * 16));
+                const int byte = xb[b][m * 16 + t16] >> 8 * g & 255;
                 const i32x8 v = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
 #pragma unroll
                 for (int r = 0; r < RB; ++r) {
                     const i32x8 wv = {(int)c[r][0], (int)c[r][1], (int)c[r][2], (int)c[r][3], 0, 0, 0, 0};
-                    acc[r][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, v, acc[r][i], 4, 0, 0, (int)sc[r], 0, byte);
+                    acc[r][m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, v, acc[r][m], 4, 0, 0, (int)sc[r], 0, byte);
                 }
             }
         } else {
@@ -113,21 +123,45 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(const LinearArgs a, l
 #pragma unroll
                 for (int r = 0; r < RB; ++r) wv[r] = weights8(c[r][s], power(sc[r]));
 #pragma unroll
-                for (int i = 0; i < NT; ++i) {
+                for (int m = 0; m < NT; ++m) {
                     bf16x8 v;
                     if constexpr (XT == X_BF16) {
-                        v = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(x + i * 4096 + t16 * 256 + (((4 * s + g) ^ t16) * 16)));
+                        v = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(x + m * 4096 + t16 * 256 + (((4 * s + g) ^ t16) * 16)));
                     } else {
-                        const u32x2 o = *reinterpret_cast<const u32x2 *>(x + i * 2048 + t16 * 128 + (((4 * (s >> 1) + g) ^ (t16 >> 1)) * 16) + 8 * (s & 1));
-                        v = widened8(o[0], o[1], power(xb[b][i * 16 + t16] >> 8 * g & 255));
+                        const u32x2 o = *reinterpret_cast<const u32x2 *>(x + m * 2048 + t16 * 128 + (((4 * (s >> 1) + g) ^ (t16 >> 1)) * 16) + 8 * (s & 1));
+                        v = widened8(o[0], o[1], power(xb[b][m * 16 + t16] >> 8 * g & 255));
                     }
 #pragma unroll
-                    for (int r = 0; r < RB; ++r) acc[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[r], v, acc[r][i], 0, 0, 0);
+                    for (int r = 0; r < RB; ++r) acc[r][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[r], v, acc[r][m], 0, 0, 0);
                 }
             }
         }
         slot = slot + 1 == SLOTS ? 0 : slot + 1;
         next = next + 1 == SLOTS ? 0 : next + 1;
+    }
+    if constexpr (KS > 1) {
+        f32x4 *red = reinterpret_cast<f32x4 *>(lds);
+        __syncthreads();                                 // all blocks have been read
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+#pragma unroll
+            for (int m = 0; m < NT; ++m) red[(w * (RB * NT) + r * NT + m) * 64 + l] = acc[r][m];
+        __syncthreads();
+        for (int i = w; i < RB * NT; i += kWaves) {      // a tile's sums in the order of the waves
+            f32x4 v = red[i * 64 + l];
+#pragma unroll
+            for (int k = 1; k < KS; ++k) {
+                const f32x4 o = red[(k * (RB * NT) + i) * 64 + l];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += o[e];
+            }
+            const int t = t0 + i % NT * 16 + t16, o = (rt + i / NT) * 16 + g * 4;
+            if (t < a.n_tokens && o < a.R) {
+                if (a.ranges == 1) store4(a, t, o, v);
+                else *reinterpret_cast<f32x4 *>(a.part + ((long)z * a.n_tokens + t) * (row_tiles * 16l) + o) = v;
+            }
+        }
+        return;
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
@@ -145,20 +179,22 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(const LinearArgs a, l
 
 }  // namespace
 
-hipError_t launch_linear_some(const LinearArgs &a, int tiles, int rows, int range_blocks, hipStream_t s) {
-    const auto go = [&](auto xt, auto nt, auto rb) {
-        constexpr int XT = decltype(xt)::value, NT = decltype(nt)::value, RB = decltype(rb)::value, AHEAD = NT * RB >= 8 ? 1 : 2;
-        const long row_wgs = ((a.R + 15) / 16 + RB * kWaves - 1) / (RB * kWaves), all = row_wgs * a.ranges * ((a.n_tokens + NT * 16 - 1) / (NT * 16));
+hipError_t launch_linear_some(const LinearArgs &a, int tiles, int rows, int ks, int range_blocks, hipStream_t s) {
+    const auto go = [&](auto xt, auto nt, auto rb, auto ks) {
+        constexpr int XT = decltype(xt)::value, NT = decltype(nt)::value, RB = decltype(rb)::value, KS = decltype(ks)::value, AHEAD = NT * RB >= 8 || (KS > 1 && XT == X_BF16) ? 1 : 2;
+        constexpr int PER = RB * kWaves / KS;
+        const long row_wgs = ((a.R + 15) / 16 + PER - 1) / PER, all = row_wgs * a.ranges * ((a.n_tokens + NT * 16 - 1) / (NT * 16));
         constexpr long kMost = 1 << 23;                  // workgroups of 256 threads that a launch may have
         for (long at = 0; at < all; at += kMost)
-            linear_some<XT, NT, RB, AHEAD><<<dim3((unsigned)(all - at < kMost ? all - at : kMost)), dim3(64 * kWaves), 0, s>>>(a, at, range_blocks);
+            linear_some<XT, NT, RB, KS, AHEAD><<<dim3((unsigned)(all - at < kMost ? all - at : kMost)), dim3(64 * kWaves), 0, s>>>(a, at, range_blocks);
     };
     const auto by_size = [&](auto xt) {
         typedef std::integral_constant<int, 1> One;
         typedef std::integral_constant<int, 2> Two;
         typedef std::integral_constant<int, 4> Four;
-        if (tiles == 2) rows == 1 ? go(xt, Two{}, One{}) : go(xt, Two{}, Two{});
-        else rows == 2 ? go(xt, Four{}, Two{}) : go(xt, Four{}, Four{});
+        if (ks > 1) go(xt, Two{}, One{}, Four{});
+        else if (tiles == 2) rows == 1 ? go(xt, Two{}, One{}, One{}) : go(xt, Two{}, Two{}, One{});
+        else rows == 2 ? go(xt, Four{}, Two{}, One{}) : go(xt, Four{}, Four{}, One{});
     };
     if (a.x_type == DENSE_BF16) by_size(std::integral_constant<int, X_BF16>{});
     else if (a.out_type == DENSE_BF16) by_size(std::integral_constant<int, X_FP8>{});
