@@ -405,7 +405,7 @@ hipError_t launch_pack_gate(const void *Wg, void *WgT, int H, int E, hipStream_t
 
 hipError_t launch_route(const RouteArgs &a, hipStream_t s) {
     if (a.N <= 0) return hipSuccess;
-    if (a.scoring != nullptr && a.dtype == MOE_BF16 && (a.packed || a.E % 2 == 0)) return launch_gate_scored(a, s);
+    if (a.scoring != nullptr && a.dtype == MOE_BF16 && (a.packed || (a.E % 2 == 0 && ((uintptr_t)a.Wg & 3) == 0))) return launch_gate_scored(a, s);      // it reads pairs of experts
     if (a.dtype == MOE_BF16) {
         const int E16 = (a.E + 15) / 16 * 16, nb = E16 / 16;
         const long tot = (long)E16 * a.H;

@@ -156,12 +156,11 @@ struct Rule {
     float factor;
 };
 
-// Largest value of the wave's 64 lanes, in every lane.
+// Largest value of the wave's 64 lanes, in every lane; `least` is nobody's loss (one instruction a step, where a step's own value in its place takes two).
 template <class T>
-__device__ __forceinline__ T wave_max(T v) {
+__device__ __forceinline__ T wave_max(T v, T least) {
     const auto step = [&](auto ctrl) {
-        const int old = __builtin_bit_cast(int, v);
-        v = max(v, __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(old, old, decltype(ctrl)::value, 0xf, 0xf, false)));
+        v = max(v, __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, least), __builtin_bit_cast(int, v), decltype(ctrl)::value, 0xf, 0xf, false)));
     };
     step(std::integral_constant<int, 0x111>{});          // row_shr 1, 2, 4, 8; row_bcast 15 and 31: lane 63 holds the wave's
     step(std::integral_constant<int, 0x112>{});
@@ -253,7 +252,7 @@ __global__ __launch_bounds__(64 * (SPLIT ? NS : kTokens)) void score_topk(const 
         float m = x[0];
 #pragma unroll
         for (int c = 1; c < M; ++c) m = fmaxf(m, x[c]);
-        m = wave_max(m);
+        m = wave_max(m, -INFINITY);
         if constexpr (SPLIT) {
             if (l == 0) across[0][wv] = m;
             __syncthreads();
@@ -348,7 +347,7 @@ __global__ __launch_bounds__(64 * (SPLIT ? NS : kTokens)) void score_topk(const 
         int top = key[0].hi;
 #pragma unroll
         for (int c = 1; c < NS; ++c) top = max(top, key[c].hi);
-        top = wave_max(top);
+        top = wave_max(top, INT_MIN);
         unsigned long long at[NS];
         int n = 0;
 #pragma unroll
@@ -360,7 +359,7 @@ __global__ __launch_bounds__(64 * (SPLIT ? NS : kTokens)) void score_topk(const 
             unsigned low = 0;
 #pragma unroll
             for (int c = 0; c < NS; ++c) low = max(low, key[c].hi == top ? key[c].lo : 0u);
-            low = wave_max(low);
+            low = wave_max(low, 0u);
 #pragma unroll
             for (int c = 0; c < NS; ++c) at[c] = __ballot(key[c].hi == top && key[c].lo == low);
         }
