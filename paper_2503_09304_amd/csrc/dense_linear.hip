@@ -239,11 +239,14 @@ static Plan plan_of(int n_tokens, int R, int K, bool bf16) {
     return best;
 }
 
-int linear_ranges(int n_tokens, int R, int K, int x_type, int) { return plan_of(n_tokens, R, K, x_type == DENSE_BF16).ranges; }
+static size_t workspace_of(const Plan &p, int n_tokens, int R) { return p.ranges > 1 ? (size_t)p.ranges * n_tokens * (((size_t)R + 15) / 16 * 16) * 4 : 0; }
 
-hipError_t launch_linear(const LinearArgs &a, hipStream_t s) {
+size_t linear_workspace(int n_tokens, int R, int K, int x_type) { return workspace_of(plan_of(n_tokens, R, K, x_type == DENSE_BF16), n_tokens, R); }
+
+hipError_t launch_linear(LinearArgs a, size_t workspace_bytes, hipStream_t s) {
     const Plan p = plan_of(a.n_tokens, a.R, a.K, a.x_type == DENSE_BF16);
-    if (p.tiles == 8 || p.ranges > a.ranges) return launch_linear_many(a, s);              // or no workspace
+    if (p.tiles == 8 || workspace_bytes < workspace_of(p, a.n_tokens, a.R)) return launch_linear_many(a, s);
+    a.ranges = p.ranges;
     const int row_tiles = (a.R + 15) / 16;
     if (p.tiles > 1) {
         const hipError_t e = launch_linear_some(a, p.tiles, p.rows, p.ks, p.range_blocks, s);

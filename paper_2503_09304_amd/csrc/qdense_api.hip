@@ -117,8 +117,7 @@ size_t dense_linear_workspace_bytes(int32_t n_tokens, int32_t R, int32_t K, int3
         set_error(MOE_E_ARG, "dense_linear_workspace_bytes: bad size or type");
         return 0;
     }
-    const int ranges = qdense::linear_ranges(n_tokens, R, K, x_type, out_type);
-    return ranges > 1 ? (size_t)ranges * n_tokens * (((size_t)R + 15) / 16 * 16) * 4 : 0;
+    return qdense::linear_workspace(n_tokens, R, K, x_type);
 }
 
 int32_t dense_linear(const dense_rows *x, const dense_matrix4 *w, const dense_rows *out, int32_t n_tokens, void *workspace,
@@ -136,11 +135,8 @@ int32_t dense_linear(const dense_rows *x, const dense_matrix4 *w, const dense_ro
     if (!aligned(out->data, (size_t)element_bytes(out->type))) return set_error(MOE_E_ARG, "%s: out is not aligned to its elements", call);
     if ((rc = check_apart(out, n_tokens, 1, w->rows, call, "out"))) return rc;
     if (workspace && !aligned(workspace, 16)) return set_error(MOE_E_WORKSPACE, "%s: workspace is not 16-byte aligned", call);
-    const size_t need = workspace ? dense_linear_workspace_bytes(n_tokens, w->rows, w->cols, x->type, out->type) : 0;
-    const int ranges = need && workspace_bytes >= need ? qdense::linear_ranges(n_tokens, w->rows, w->cols, x->type, out->type) : 1;
-    const qdense::LinearArgs a{rows(x), rows(out), (const uint8_t *)w->codes, w->scales, n_tokens, w->rows, w->cols, x->type, out->type, ranges,
-                               (float *)workspace};
-    return hip_result(qdense::launch_linear(a, (hipStream_t)stream), call);
+    const qdense::LinearArgs a{rows(x), rows(out), (const uint8_t *)w->codes, w->scales, n_tokens, w->rows, w->cols, x->type, out->type, 1, (float *)workspace};
+    return hip_result(qdense::launch_linear(a, workspace ? workspace_bytes : 0, (hipStream_t)stream), call);
 }
 
 }  // extern "C"

@@ -31,12 +31,12 @@ struct LinearArgs {
     const uint8_t *codes, *scales;
     int n_tokens, R, K;
     int x_type, out_type;
-    int ranges;                   // ranges of columns in workgroups of their own; 1: no workspace
-    float *part;                  // [range][n_tokens][rows up to a multiple of 16]
+    int ranges;                   // ranges of columns in workgroups of their own (launch_linear sets it)
+    float *part;                  // workspace, [range][n_tokens][rows up to a multiple of 16]; may be nullptr
 };
-// Ranges of columns that a call is cut into: see dense_linear.hip.
-int linear_ranges(int n_tokens, int R, int K, int x_type, int out_type);
-hipError_t launch_linear(const LinearArgs &a, hipStream_t s);
+// What a call's ranges need of a workspace, 0 without any: see dense_linear.hip.
+size_t linear_workspace(int n_tokens, int R, int K, int x_type);
+hipError_t launch_linear(LinearArgs a, size_t workspace_bytes, hipStream_t s);
 // Most blocks of 128 columns of a range there (its tokens' scales are in LDS).
 constexpr int kSomeBlocks = 64;
 hipError_t launch_linear_some(const LinearArgs &a, int tiles, int rows, int ks, int range_blocks, hipStream_t s);
