@@ -217,6 +217,7 @@ static Plan plan_of(int n_tokens, int R, int K, bool bf16) {
     Plan best{8, 4, 1, 1, blocks, 0};
     float least = n_tokens > 64 ? us_of(best, n_tokens, R, K, bf16) : INFINITY;
     const auto look = [&](const Plan &p) {
+        if (p.ranges > 1 && (long)n_tokens * R * p.ranges > 1 << 26) return;          // 256 MB of sums
         const float us = us_of(p, n_tokens, R, K, bf16);
         if (us < least) {
             best = p;
@@ -224,7 +225,7 @@ static Plan plan_of(int n_tokens, int R, int K, bool bf16) {
         }
     };
     for (const int z : {1, 2, 3, 4, 6, 8, 12, 16}) {
-        if (z > 1 && (z > blocks || (long)n_tokens * R * z > 1 << 26)) break;
+        if (z > blocks) break;
         if (n_tokens <= kFewTokens) look(few_of(n_tokens, R, K, bf16, z));
         if (n_tokens <= 1024) look(some_of(K, bf16, 2, 1, 4, z));
         if (n_tokens <= 4096) {

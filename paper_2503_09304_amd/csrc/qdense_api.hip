@@ -30,6 +30,11 @@ int32_t check_rows(const dense_rows *r, int heads, const char *call, const char 
     return MOE_OK;
 }
 
+// Rows of one type that stand at the same place.
+bool same_rows(const dense_rows *a, const dense_rows *b, int n_tokens, int heads) {
+    return a->type == b->type && (n_tokens == 1 || a->token_stride == b->token_stride) && (heads == 1 || a->head_stride == b->head_stride);
+}
+
 // Rows that are written do not overlap.
 int32_t check_apart(const dense_rows *r, int n_tokens, int heads, int dim, const char *call, const char *name) {
     if ((n_tokens > 1 && r->token_stride < dim) || (heads > 1 && r->head_stride < dim)) return set_error(MOE_E_ARG, "%s: rows of %s overlap", call, name);
@@ -80,6 +85,10 @@ int32_t dense_norm(const dense_rows *x, const dense_rows *add, const dense_rows 
         (total && (rc = check_rows(total, heads, call, "total"))) || (rc = check_rows(out, heads, call, "out")) ||
         (total && (rc = check_apart(total, n_tokens, heads, dim, call, "total"))) || (rc = check_apart(out, n_tokens, heads, dim, call, "out")))
         return rc;
+    if (total && (total->data == out->data || total->data == x->data || (total->data == add->data && !same_rows(total, add, n_tokens, heads))))
+        return set_error(MOE_E_ARG, "%s: total may be add, row by row, and otherwise overlaps nothing", call);
+    if ((out->data == x->data && !same_rows(out, x, n_tokens, heads)) || (add && out->data == add->data && !same_rows(out, add, n_tokens, heads)))
+        return set_error(MOE_E_ARG, "%s: out may be x or add, row by row, and otherwise overlaps nothing", call);
     const qdense::NormArgs a{rows(x), rows(add), rows(total), rows(out), weight, (long)n_tokens * heads, heads, dim, add ? add->type : DENSE_BF16,
                              out->type, weight_type, shift, eps};
     return hip_result(qdense::launch_norm(a, (hipStream_t)stream), call);
@@ -134,6 +143,8 @@ int32_t dense_linear(const dense_rows *x, const dense_matrix4 *w, const dense_ro
     if (!out->data) return set_error(MOE_E_ARG, "%s: out is null", call);
     if (!aligned(out->data, (size_t)element_bytes(out->type))) return set_error(MOE_E_ARG, "%s: out is not aligned to its elements", call);
     if ((rc = check_apart(out, n_tokens, 1, w->rows, call, "out"))) return rc;
+    if (out->data == x->data || (workspace && (workspace == x->data || workspace == out->data)))
+        return set_error(MOE_E_ARG, "%s: out, x and the workspace overlap", call);
     if (workspace && !aligned(workspace, 16)) return set_error(MOE_E_WORKSPACE, "%s: workspace is not 16-byte aligned", call);
     const qdense::LinearArgs a{rows(x), rows(out), (const uint8_t *)w->codes, w->scales, n_tokens, w->rows, w->cols, x->type, out->type, 1, (float *)workspace};
     return hip_result(qdense::launch_linear(a, workspace ? workspace_bytes : 0, (hipStream_t)stream), call);

@@ -402,3 +402,108 @@ def test_refusals_leave_outputs_alone():
             call()
     torch.cuda.synchronize()
     assert (out == 5.0).all() and (y == 5.0).all()
+
+
+def by_c(x, scale, M, out, ws, nb):
+    """The C call itself, with a workspace of the caller's."""
+    import ctypes as C
+    from paper_2503_09304_amd import dense as d
+
+    class Rows(C.Structure):
+        _fields_ = [("data", C.c_void_p), ("scale", C.c_void_p), ("ts", C.c_int64), ("hs", C.c_int64), ("type", C.c_int32)]
+
+    kind = d._TYPES[x.dtype]
+    r = [Rows(t.data_ptr(), None if s is None else s.data_ptr(), t.stride(0), 0, d._TYPES[t.dtype]) for t, s in ((x, scale), (out, None))]
+    need = d._lib().dense_linear_workspace_bytes(len(x), M.rows, M.cols, kind, r[1].type)
+    if nb is not None:
+        rc = d._lib().dense_linear(C.addressof(r[0]), M._at, C.addressof(r[1]), len(x), ws, nb, torch.cuda.current_stream().cuda_stream)
+        assert rc == q.MOE_OK, q.moe_last_error()
+    return need
+
+
+@pytest.mark.parametrize("x_type,out_type", KINDS)
+@pytest.mark.parametrize("T,R,K", [(1, 64, 4096), (1, 128, 32768), (16, 33, 8192), (40, 100, 4096), (61, 4096, 14336), (200, 65, 6144), (300, 128, 8192)])
+def test_linear_workspaces(T, R, K, x_type, out_type):
+    """Whatever stands in a workspace, nothing behind it is touched; with less than what is asked for, or none, the product is the same within its bar."""
+    g = gen(16 + T)
+    m = matrix(g, R, K)
+    x, scale = (rows(g, (T, K)), None) if x_type is BF else eight_bit(g, T, K)
+    M = q.DenseMatrix4(*m)
+    outs = [torch.full((T, R), NAN, dtype=out_type, device=DEV) for _ in range(5)]
+    need = by_c(x, scale, M, outs[0], None, None)
+    assert (need > 0 or K <= 4096) and need % (T * (-(-R // 16) * 16) * 4) == 0
+    ws = torch.full((need + 4096,), 0xFF, dtype=torch.uint8, device=DEV)
+    for out, at, nb in zip(outs, (ws.data_ptr(), ws.data_ptr(), ws.data_ptr(), None, None), (need, need + 4096, need - 1, 0, need)):
+        by_c(x, scale, M, out, at, nb)
+        torch.cuda.synchronize()
+        assert (ws[need:] == 0xFF).all()
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[2], outs[3]) and torch.equal(outs[3], outs[4])
+    d, w = (x.double() if scale is None else decoded(x, scale)), weights(*m)
+    ref, err = d @ w.t(), ((K + 16) * 2.0 ** -24 + (2.0 ** -11 if scale is not None and out_type is BF else 0)) * (d.abs() @ w.abs().t())
+    for out in (outs[0], outs[2]):
+        assert ((out.double() - ref).abs() <= err + (HALF if out_type is BF else 2.0 ** -24) * (ref.abs() + err)).all()
+
+
+def test_two_graphs_of_one_memory_pool():
+    """Calls with workspaces, captured into graphs that take turns on the same memory."""
+    g = gen(17)
+    A, B = q.DenseMatrix4(*matrix(g, 48, 8192)), q.DenseMatrix4(*matrix(g, 8192, 512))
+    x = [torch.empty((T, 8192), dtype=BF, device=DEV) for T in (3, 40)]
+
+    def run(v):
+        y, h, z = (torch.empty((len(v), n), dtype=BF, device=DEV) for n in (48, 48, 48))
+        q.dense_linear(v, A, y)
+        q.dense_norm(y, None, h)
+        wide = torch.empty((len(v), 8192), dtype=BF, device=DEV)
+        q.dense_linear(h.repeat(1, 11)[:, :512].contiguous(), B, wide)
+        q.dense_linear(wide, A, z)
+        return z
+
+    for v in x:
+        v.copy_(torch.randn(v.shape, generator=g, device=DEV))
+        run(v)
+    torch.cuda.synchronize()
+    graphs, kept, pool = [], [], None
+    for v in x:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], pool=pool):
+            kept.append(run(v))
+        pool = graphs[0].pool()
+    for i in range(4):
+        for v, graph, out in zip(x, graphs, kept):
+            v.copy_(torch.randn(v.shape, generator=g, device=DEV))
+            graph.replay()
+            got = out.clone()
+            assert torch.equal(got, run(v))
+
+
+def test_two_threads_on_two_streams():
+    import threading
+    g = gen(18)
+    M = q.DenseMatrix4(*matrix(g, 48, 8192))
+    x, add = [rows(g, (T, 8192)) for T in (5, 90)], [rows(g, (T, 8192), F32) for T in (5, 90)]
+    bad = []
+
+    def run(i):
+        h, t, y = torch.empty_like(x[i]), torch.empty_like(add[i]), torch.empty((len(x[i]), 48), dtype=F32, device=DEV)
+        q.dense_norm(x[i], None, h, add=add[i], total=t)
+        q.dense_linear(h, M, y)
+        return y
+
+    want = [run(i) for i in range(2)]
+    torch.cuda.synchronize()
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(200):
+                y = run(i)
+                torch.cuda.current_stream().synchronize()
+                if not torch.equal(y, want[i]):
+                    bad.append(i)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad

@@ -207,3 +207,25 @@ def test_refusals():
         q.MoeScoring("tanh")
     with pytest.raises(q.MoeError):
         q.MoeScoring(choice_bias=cb.double())
+
+
+def test_two_contexts_on_two_streams():
+    want, got, all_ = [], [[], []], []
+    for i, N in enumerate((61, 700)):
+        x, Wg, lb, cb = inputs(40 + i, N, 512, 160)
+        ctx, w, keep = context(N, 512, 160, 8, Wg, torch.bfloat16)
+        rule = q.MoeScoring("softmax" if i else "sigmoid", lb, cb, 8, 3, 2, True, 1.5)
+        ctx.route_scored(x, w, rule)
+        want.append([ctx.get(n).clone() for n in ("topk_idx", "topk_w")])
+        all_.append((ctx, x, w, rule, keep))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(20):
+        for i, (ctx, x, w, rule, keep) in enumerate(all_):
+            with torch.cuda.stream(streams[i]):
+                ctx.route_scored(x, w, rule)
+                got[i].append([ctx.get(n).clone() for n in ("topk_idx", "topk_w")])
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        for c in b:
+            assert torch.equal(a[0], c[0]) and torch.equal(a[1], c[1])
