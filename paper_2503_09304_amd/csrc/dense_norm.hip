@@ -3,7 +3,9 @@
 //     r = x + add,   out = r * rsqrt(mean(r^2) + eps) * (weight + shift)
 //
 // A row stays in registers from its first read to its last write: CH pieces of 8 elements in each of TPR lanes, all requested at
-// once, so every byte moves once.
+// once, so every byte moves once.  Bound by memory (8192 rows of 4096 with a residual of bf16: 43.8 us, 6.1 TB/s; of fp32 71 us, 5.6 TB/s), one row by the way to
+// memory and back (2.4 us of one call in a graph of them, where an empty kernel takes 2).  Loads and the total's stores pass the caches by, as nothing of them is read
+// again before they would be overwritten; out goes through them: the product behind it reads it.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -78,8 +80,8 @@ constexpr int kThreads = 256;
 
 // A row has TPR lanes: some of a wave (several rows a wave), or whole waves of a workgroup.  ADD: 0 none, 1 bf16, 2 fp32.
 template <int TPR, int CH, int ADD, bool FP8>
-__global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void norm_rows(const NormArgs a, long first) {
-    constexpr int WG = TPR > kThreads ? TPR : kThreads, RPW = WG / TPR, WAVES = TPR > 64 ? TPR / 64 : 1;
+__global__ __launch_bounds__(TPR > 64 ? TPR : kThreads) void norm_rows(const NormArgs a, long first) {
+    constexpr int WG = TPR > 64 ? TPR : kThreads, RPW = WG / TPR, WAVES = TPR > 64 ? TPR / 64 : 1;
     const int lane = threadIdx.x % TPR;
     const long row = first + (long)blockIdx.x * RPW + threadIdx.x / TPR;
     if (TPR <= 64 && row >= a.rows) return;              // whole rows of lanes leave; none of them is asked by an exchange of another row
@@ -95,7 +97,7 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void norm_rows(con
             if constexpr (ADD != 0) r[c].load(a.add.p, ao + e);
         }
     }
-    // The weights are asked for before the sum where registers are there for them.
+    // The weights are asked for before the sum where registers are there for them: one way to memory less (a row of 4096 alone).
     constexpr bool EARLY = CH <= 2;
     float g[EARLY ? CH : 1][8];
     const auto weights = [&](float (&to)[8], int e) {
@@ -174,7 +176,7 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void norm_rows(con
 
 template <int TPR, int CH>
 void run(const NormArgs &a, hipStream_t s) {
-    constexpr int WG = TPR > kThreads ? TPR : kThreads, RPW = WG / TPR;
+    constexpr int WG = TPR > 64 ? TPR : kThreads, RPW = WG / TPR;
     const auto go = [&](auto add, auto fp8) {
         constexpr long most = (1l << 31) / WG * RPW;     // a launch of 2^32 threads or more would lose the excess
         for (long r = 0; r < a.rows; r += most) {
@@ -193,17 +195,21 @@ void run(const NormArgs &a, hipStream_t s) {
 
 }  // namespace
 
+// Up to 512 elements a row is within a wave: no barrier, and several rows a wave (8192 * 16 heads of 128: 24.9 us, 44 by a wave each).  Longer ones have the fewest lanes
+// that hold them a piece each: rows wait for nothing but their own loads, and their workgroups come and go side by side.  Us of rows of 1024 / 2048 / 4096 with a bf16
+// residual, 8192 of them: that many lanes 14.9 / 24.5 / 43.8, always 512 18.5 / 24.5 / 43.8, always a wave 13.5 / 24.0 / 50; 1024 of them: 3.4 / 4.7 / 7.7, 3.8 / 4.8 / 7.7,
+// 4.2 / 5.9 / 9.6.  Without a residual a lane's one load leaves much of the way unused: where rows are many, four pieces a lane (4096 rows of 4096 12.8 us instead of 15.6,
+// 4096 of 2816 9.9 instead of 13.1; 256 of 4096 4.0 instead of 3.2).
 hipError_t launch_norm(const NormArgs &a, hipStream_t s) {
     const int pieces = (a.dim + 7) / 8;
     if (pieces <= 8) run<8, 1>(a, s);
     else if (pieces <= 16) run<16, 1>(a, s);
     else if (pieces <= 32) run<32, 1>(a, s);
     else if (pieces <= 64) run<64, 1>(a, s);
-    else if (pieces <= 512 && a.rows > 1024) {
-        if (pieces <= 128) run<64, 2>(a, s);
-        else if (pieces <= 256) run<64, 4>(a, s);
-        else run<64, 8>(a, s);
-    } else if (pieces <= 512) run<512, 1>(a, s);
+    else if (pieces <= 128) run<128, 1>(a, s);
+    else if (pieces <= 256) run<256, 1>(a, s);
+    else if (pieces <= 512 && a.rows > 1024 && a.add.p == nullptr) run<128, 4>(a, s);
+    else if (pieces <= 512) run<512, 1>(a, s);
     else if (pieces <= 1024) run<512, 2>(a, s);
     else if (pieces <= 2048) run<512, 4>(a, s);
     else run<512, 8>(a, s);

@@ -33,6 +33,8 @@ __device__ __forceinline__ void to_lds(const char *from, const char *to) {
 constexpr int kMostRanges = 16, kMostWaves = 16;
 constexpr int kStage = 128;           // columns of the hidden size that stand in LDS at once
 
+// Bound by the tokens' way from memory where they are many (8192 tokens, H 4096, 160 experts: 29 us, their bytes 13), by latency where they are few (a stage's loads are
+// under way while the stage before is multiplied, and a range has few stages).
 // Products of TT * 16 tokens with all experts over a range of the hidden size: a wave has 32 experts (and, where experts are few, one of `slices` parts of the range).
 // Lane l's operands are experts 2 (l%16) and 2 (l%16) + 1 of the wave's.  Row-major weights [H][E] (E even): it takes the pairs of 8 rows and turns them over in
 // registers, so no transposed copy is written first.
@@ -209,8 +211,9 @@ __device__ __forceinline__ double largest_first(double &a, double b) {       // 
 }
 
 // A wave has a token, lane l experts l, l + 64, ..., NS in all.  SPLIT: NS waves have a token, 64 experts each up to the scores, and one of them chooses: fewer
-// instructions one after the other where tokens leave the chip idle (61 tokens on 256 experts us_split / us_one).  BEST: values that a group's worth is the sum
-// of (0: all groups count).
+// instructions one after the other where tokens leave the chip idle (61 tokens on 256 experts 6.4 us instead of 10.4).  BEST: values that a group's worth is the sum
+// of (0: all groups count).  Bound by instructions: the exponentials and divisions of 64 bits, and for each expert chosen a search over the wave whose steps wait for
+// each other (8192 tokens on 160 experts 14.5 us, 8 of 160 in 8 groups).
 template <int NS, int BEST, bool SPLIT>
 __global__ __launch_bounds__(64 * (SPLIT ? NS : kTokens)) void score_topk(const float *__restrict__ part, int planes, float *__restrict__ logits, const Rule rule,
                                                                           int32_t *__restrict__ topk_idx, float *__restrict__ topk_w, int N, int E, int k) {
@@ -386,7 +389,9 @@ __global__ __launch_bounds__(64 * (SPLIT ? NS : kTokens)) void score_topk(const 
 hipError_t launch_score(const RouteArgs &a, const float *part, int planes, hipStream_t s) {
     const moe_scoring &c = *a.scoring;
     const Rule rule{c.logit_bias, c.choice_bias, c.score == MOE_SCORE_SIGMOID, c.groups, c.top_groups, c.renormalise, c.factor};
-    const bool split = a.N <= 2048 && a.E > 64;
+    // SPLIT against not, logits included, H 2048, us: 61 tokens 11.4 / 13.1 on 128 experts, 11.7 / 15.8 on 256; 2048 tokens 15.8 / 17.3, 20.1 / 21.8; 4096 19.3 / 19.9, 25.2 / 25.8; 8192 29.1 /
+    // 27.3, 38.1 / 37.3.
+    const bool split = a.N <= 4096 && a.E > 64;
     const auto go = [&](auto ns, auto best) {
         constexpr int NS = decltype(ns)::value, BEST = decltype(best)::value;
         if (NS > 1 && split) score_topk<NS, BEST, (NS > 1)><<<dim3(a.N), dim3(64 * NS), 0, s>>>(part, planes, a.logits, rule, a.topk_idx, a.topk_w, a.N, a.E, a.k);
@@ -407,13 +412,15 @@ hipError_t launch_score(const RouteArgs &a, const float *part, int planes, hipSt
 }
 
 hipError_t launch_gate_scored(const RouteArgs &a, hipStream_t s) {
-    const int blocks = (a.E + 31) / 32, tt = a.N <= 16 ? 1 : a.N <= 32 ? 2 : 4, tiles = (a.N + tt * 16 - 1) / (tt * 16);
-    // Parts of the range a workgroup: up to 16 waves, 4 parts.  Ranges: as many as give 256 workgroups, 16 at most, each part 64 columns at least; what the scratch holds.
-    const int slices = std::max(1, std::min({4, kMostWaves / blocks, a.H / 64}));
+    // Tokens a workgroup: few while ranges can be enough workgroups all the same, as a range's products and sums are one after the other then (61 tokens on 256 experts, H 4096: 16 / 32 / 64
+    // a workgroup 11.2 / 11.3 / 12.8 us with the choice; 512 on 128 11.9 / 12.0 / 14.4); with many tokens the weights' way to the workgroups counts (8192 on 256: 87 / 56 / 52).
+    const int blocks = (a.E + 31) / 32, tt = a.N <= 512 ? 1 : a.N <= 2048 ? 2 : 4, tiles = (a.N + tt * 16 - 1) / (tt * 16);
+    // Ranges: as many as give 256 workgroups, 16 at most, what the scratch holds.  Their parts: up to 16 waves, 4 parts.  Both of a stage's columns at least.
     const long fit = (long)a.k * a.H / a.E;              // the context's room for k rows of H floats a token
-    long ranges = std::max(1l, std::min({256l / tiles, (long)kMostRanges, (long)a.H / (64 * slices), fit}));
+    long ranges = std::max(1l, std::min({256l / tiles, (long)kMostRanges, (long)a.H / kStage, fit}));
     const int range = (int)(((a.H + ranges - 1) / ranges + 63) / 64 * 64);
     ranges = (a.H + range - 1) / range;
+    const int slices = std::max(1, std::min({4, kMostWaves / blocks, (range + kStage - 1) / kStage}));
     float *part = ranges > 1 ? a.scratch : a.logits;
     const auto go = [&](auto t, auto packed) {
         constexpr int TT = decltype(t)::value;
