@@ -1,7 +1,9 @@
 // dense_linear for many tokens: a tile of 256 rows by 128 tokens a workgroup.
 //
-// Each of four waves has 64 rows and all of the tile's tokens: weights come straight into its registers, a block of 128 columns ahead, and are widened there; the tokens'
-// columns are brought to LDS while the block before is multiplied, and read by all waves.
+// Each of four waves has 64 rows and all of the tile's tokens: weights come straight into its registers, a block of 128 columns ahead, and are widened there, a step before
+// their products; the tokens' columns are brought to LDS while the block before is multiplied, and read by all waves, some products before they are needed (left to the
+// compiler, which asks for two at a time and waits for them: 8192 tokens by 4096 x 4096 in bf16 214 us, 203 so).  Bound by the matrix units and the tokens' way to LDS
+// (with the latter left out 174 us, with nothing but products 164): 200 us, 1.37 PFLOP/s; 4093 tokens by 28672 x 4096 in 8 bits 450 us, 2.1 PFLOP/s.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -11,6 +13,7 @@
 namespace qdense {
 namespace {
 
+constexpr int kXcds = 8, kGroup = 8;
 constexpr int kWaves = 4, kRowTiles = 4, NT = 8;         // a wave's tiles of 16 rows, a workgroup's of 16 tokens
 
 template <int XT>
@@ -20,28 +23,32 @@ __global__ __launch_bounds__(64 * kWaves, XT == X_WIDE ? 1 : 2) void linear_many
     static_assert(LOADS >= 1 && (TOK / LOADS) % 16 == 0, "the order of pieces goes by the token's place in 16");
     __shared__ __align__(16) char xs[2][BLOCK];
     __shared__ uint32_t xb[2][TOK];
-    const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, g = l >> 4, t16 = l & 15;
+    const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, g = l >> 4, t16 = l & 15;
     const int blocks = (a.K + 127) / 128, sets = (a.K + 511) / 512, row_tiles = (a.R + 15) / 16;
     const int row_wgs = (row_tiles + kRowTiles * kWaves - 1) / (kRowTiles * kWaves);
-    const long wg = first_wg + blockIdx.x;
-    const int rt = (int)(wg % row_wgs) * (kRowTiles * kWaves) + w * kRowTiles, t0 = (int)(wg / row_wgs) * TOK;
+    // Workgroups go to the XCDs in turn.  Each XCD has tiles that lie together, kGroup of them along the rows before the next tokens: its L2 holds what they share (tiles dealt to
+    // the XCDs in turn / kGroup 4 / 8 / 16, us: 8192 tokens by 2816 x 2048 91 / 81 / 82 / 80, 3584 by 6144 x 4096 150 / 146 / 142 / 143).
+    const long token_wgs = (a.n_tokens + TOK - 1) / TOK, all = row_wgs * token_wgs, per_xcd = (all + kXcds - 1) / kXcds;
+    const long at = first_wg + blockIdx.x, wg = at % kXcds * per_xcd + at / kXcds;
+    if (at / kXcds >= per_xcd || wg >= all) return;
+    const int group = (int)(wg / (kGroup * token_wgs)), in_group = min(kGroup, row_wgs - group * kGroup);
+    const long part = wg - group * kGroup * token_wgs;
+    const int rt = (group * kGroup + (int)(part % in_group)) * (kRowTiles * kWaves) + w * kRowTiles, t0 = (int)(part / in_group) * TOK;
     const uint8_t *codes[kRowTiles], *scales[kRowTiles];
 #pragma unroll
     for (int r = 0; r < kRowTiles; ++r) {
         const long tile = min(rt + r, row_tiles - 1);
-        codes[r] = a.codes + tile * blocks * 1024 + l * 16;
-        scales[r] = a.scales + tile * sets * 256 + l * 4;
+        codes[r] = a.codes + tile * blocks * 1024;
+        scales[r] = a.scales + tile * sets * 256;
     }
-    // The pieces that this lane brings to LDS, and in which order a token's stand there: so that the lanes of one read use all banks.
-    const char *src[LOADS];
-    int first_piece;
-    {
-        constexpr int PER = 64 / PIECES;                 // tokens of a wave's load
-#pragma unroll
-        for (int j = 0; j < LOADS; ++j) src[j] = a.x.p + (long)min(t0 + (w + kWaves * j) * PER + l / PIECES, a.n_tokens - 1) * a.x.ts * (XT == X_BF16 ? 2 : 1);
-        const int t = w * PER + l / PIECES, p = l % PIECES, q = XT == X_BF16 ? p ^ (t & 15) : p ^ (t >> 1 & 7);
-        first_piece = XT == X_BF16 ? 4 * (q & 3) + (q >> 2) : XT == X_FP8 ? q : 2 * (q & 3) + (q >> 2);
-    }
+    // The pieces that this lane brings to LDS, and in which order a token's stand there: so that the lanes of one read use all banks.  It brings `here` tokens,
+    // each STEP behind the one before, and the first again in the place of those behind the last.
+    constexpr int PER = 64 / PIECES, STEP = kWaves * PER;        // tokens of a wave's load, of the workgroup's
+    const int mine = w * PER + l / PIECES, p = l % PIECES, q = XT == X_BF16 ? p ^ (mine & 15) : p ^ (mine >> 1 & 7);
+    const int first_piece = XT == X_BF16 ? 4 * (q & 3) + (q >> 2) : XT == X_FP8 ? q : 2 * (q & 3) + (q >> 2);
+    const int here = (a.n_tokens - t0 - mine + STEP - 1) / STEP;
+    const char *const src = a.x.p + (long)min(t0 + mine, a.n_tokens - 1) * a.x.ts * (XT == X_BF16 ? 2 : 1);
+    const long step = STEP * a.x.ts * (XT == X_BF16 ? 2 : 1);
     const int k_bytes = a.K * (XT == X_BF16 ? 2 : 1);
     const uint8_t *xscale = XT == X_BF16 ? nullptr : a.x.scale + (long)min(t0 + tid % TOK, a.n_tokens - 1) * (a.K / 32);
     uint32_t next_xb[4] = {0, 0, 0, 0};
@@ -50,7 +57,7 @@ __global__ __launch_bounds__(64 * kWaves, XT == X_WIDE ? 1 : 2) void linear_many
     const auto bring = [&](int b, int buf) {
         const int at = (b * PIECES + first_piece) * 16, off = at < k_bytes ? at : 0;        // behind the last column: weights are zero there
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) to_lds(src[j] + off, &xs[buf][(w + kWaves * j) * 1024]);
+        for (int j = 0; j < LOADS; ++j) to_lds(src + off + (j < here ? j * step : 0l), &xs[buf][(w + kWaves * j) * 1024]);
         if constexpr (XT != X_BF16) {
             const int n = a.K / 32;
 #pragma unroll
@@ -58,8 +65,8 @@ __global__ __launch_bounds__(64 * kWaves, XT == X_WIDE ? 1 : 2) void linear_many
         }
 #pragma unroll
         for (int r = 0; r < kRowTiles; ++r) {
-            c[r] = *reinterpret_cast<const u32x4 *>(codes[r] + (long)b * 1024);
-            sc[r] = *reinterpret_cast<const uint32_t *>(scales[r] + (b >> 2) * 256);
+            c[r] = *reinterpret_cast<const u32x4 *>(codes[r] + (long)b * 1024 + l * 16);
+            sc[r] = *reinterpret_cast<const uint32_t *>(scales[r] + (b >> 2) * 256 + l * 4);
         }
     };
     f32x4 acc[kRowTiles][NT];
@@ -82,20 +89,50 @@ __global__ __launch_bounds__(64 * kWaves, XT == X_WIDE ? 1 : 2) void linear_many
             cs[r] = sc[r] >> 8 * (b & 3) & 255;
         }
         if (b + 1 < blocks) bring(b + 1, buf ^ 1);
+        // Operands of the tokens are asked for AHEAD pieces before their products, weights of a step widened during the step before.
         const char *x = xs[buf];
         if constexpr (XT == X_FP8) {
+            constexpr int AHEAD = 2;
             const int at = t16 * 128, sw = t16 >> 1;
+            u32x4 lo[NT], hi[NT];
+            int byte[NT];
+            const auto fetch = [&](int n) {
+                lo[n] = *reinterpret_cast<const u32x4 *>(x + n * 2048 + at + ((g ^ sw) * 16));
+                hi[n] = *reinterpret_cast<const u32x4 *>(x + n * 2048 + at + (((4 + g) ^ sw) * 16));
+                byte[n] = xb[buf][n * 16 + t16];
+            };
+#pragma unroll
+            for (int n = 0; n < AHEAD; ++n) fetch(n);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const u32x4 lo = *reinterpret_cast<const u32x4 *>(x + n * 2048 + at + ((g ^ sw) * 16));
-                const u32x4 hi = *reinterpret_cast<const u32x4 *>(x + n * 2048 + at + (((4 + g) ^ sw) * 16));
-                const int byte = xb[buf][n * 16 + t16] >> 8 * g & 255;
-                const i32x8 v = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+                if (n + AHEAD < NT) fetch(n + AHEAD);
+                const i32x8 v = {(int)lo[n][0], (int)lo[n][1], (int)lo[n][2], (int)lo[n][3], (int)hi[n][0], (int)hi[n][1], (int)hi[n][2], (int)hi[n][3]};
+                const int b8 = byte[n] >> 8 * g & 255;
 #pragma unroll
                 for (int r = 0; r < kRowTiles; ++r) {
                     const i32x8 wv = {(int)cc[r][0], (int)cc[r][1], (int)cc[r][2], (int)cc[r][3], 0, 0, 0, 0};
-                    acc[r][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, v, acc[r][n], 4, 0, 0, (int)cs[r], 0, byte);
+                    acc[r][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, v, acc[r][n], 4, 0, 0, (int)cs[r], 0, b8);
                 }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else if constexpr (XT == X_BF16) {
+            constexpr int AHEAD = 4, ALL = 4 * NT;
+            bf16x8 v[AHEAD + 1], wv[2][kRowTiles];
+            const auto fetch = [&](int i) { v[i % (AHEAD + 1)] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(x + i % NT * 4096 + t16 * 256 + (((4 * (i / NT) + g) ^ t16) * 16))); };
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) fetch(i);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int r = 0; r < kRowTiles; ++r) wv[0][r] = weights8(cc[r][0], power(cs[r]));
+#pragma unroll
+            for (int i = 0; i < ALL; ++i) {
+                const int s = i / NT, n = i % NT;
+                if (i + AHEAD < ALL) fetch(i + AHEAD);
+                if (s < 3 && n % 2 == 0) wv[(s + 1) & 1][n / 2] = weights8(cc[n / 2][s + 1], power(cs[n / 2]));
+#pragma unroll
+                for (int r = 0; r < kRowTiles; ++r) acc[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[s & 1][r], v[i % (AHEAD + 1)], acc[r][n], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
             }
         } else {
 #pragma unroll
@@ -105,13 +142,8 @@ __global__ __launch_bounds__(64 * kWaves, XT == X_WIDE ? 1 : 2) void linear_many
                 for (int r = 0; r < kRowTiles; ++r) wv[r] = weights8(cc[r][s], power(cs[r]));
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    bf16x8 v;
-                    if constexpr (XT == X_BF16) {
-                        v = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(x + n * 4096 + t16 * 256 + (((4 * s + g) ^ t16) * 16)));
-                    } else {
-                        const u32x2 o = *reinterpret_cast<const u32x2 *>(x + n * 2048 + t16 * 128 + (((4 * (s >> 1) + g) ^ (t16 >> 1)) * 16) + 8 * (s & 1));
-                        v = widened8(o[0], o[1], power(xb[buf][n * 16 + t16] >> 8 * g & 255));
-                    }
+                    const u32x2 o = *reinterpret_cast<const u32x2 *>(x + n * 2048 + t16 * 128 + (((4 * (s >> 1) + g) ^ (t16 >> 1)) * 16) + 8 * (s & 1));
+                    const bf16x8 v = widened8(o[0], o[1], power(xb[buf][n * 16 + t16] >> 8 * g & 255));
 #pragma unroll
                     for (int r = 0; r < kRowTiles; ++r) acc[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[r], v, acc[r][n], 0, 0, 0);
                 }
@@ -134,7 +166,7 @@ __global__ __launch_bounds__(64 * kWaves, XT == X_WIDE ? 1 : 2) void linear_many
 }  // namespace
 
 hipError_t launch_linear_many(const LinearArgs &a, hipStream_t s) {
-    const long row_wgs = ((a.R + 15) / 16 + kRowTiles * kWaves - 1) / (kRowTiles * kWaves), all = row_wgs * ((a.n_tokens + NT * 16 - 1) / (NT * 16));
+    const long row_wgs = ((a.R + 15) / 16 + kRowTiles * kWaves - 1) / (kRowTiles * kWaves), all = (row_wgs * ((a.n_tokens + NT * 16 - 1) / (NT * 16)) + kXcds - 1) / kXcds * kXcds;
     constexpr long kMost = 1 << 23;                      // workgroups of 256 threads that a launch may have
     for (long at = 0; at < all; at += kMost) {
         const dim3 grid((unsigned)(all - at < kMost ? all - at : kMost)), block(64 * kWaves);
