@@ -54,6 +54,72 @@ __device__ __forceinline__ void to_lds(const char *from, const char *to) {
     to_lds_at(from, __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)to));
 }
 
+// Products of a block of 128 columns: a wave's RB * 16 rows (codes c, scale bytes sc) by NT * 16 tokens, which stand in LDS (x; their scale bytes xb, four a token): pieces of 16
+// bytes, a token's in an order by its place in 16, so that the lanes of one read use all banks.  The tokens' operands are asked for AHEAD products of RB before theirs, and weights
+// are widened during the step before theirs; left to the compiler, operands come two at a time and are waited for.
+template <int XT, int RB, int NT>
+__device__ __forceinline__ void products(f32x4 (&acc)[RB][NT], const u32x4 (&c)[RB], const uint32_t (&sc)[RB], const char *x, const uint32_t *xb, int g, int t16) {
+    if constexpr (XT == X_FP8) {
+        constexpr int AHEAD = 2;
+        u32x4 lo[NT], hi[NT];
+        uint32_t byte[NT];
+        const int at = t16 * 128, sw = t16 >> 1;
+        const auto fetch = [&](int n) {
+            lo[n] = *reinterpret_cast<const u32x4 *>(x + n * 2048 + at + ((g ^ sw) * 16));
+            hi[n] = *reinterpret_cast<const u32x4 *>(x + n * 2048 + at + (((4 + g) ^ sw) * 16));
+            byte[n] = xb[n * 16 + t16];
+        };
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) fetch(n);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            if (n + AHEAD < NT) fetch(n + AHEAD);
+            const i32x8 v = {(int)lo[n][0], (int)lo[n][1], (int)lo[n][2], (int)lo[n][3], (int)hi[n][0], (int)hi[n][1], (int)hi[n][2], (int)hi[n][3]};
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                const i32x8 w = {(int)c[r][0], (int)c[r][1], (int)c[r][2], (int)c[r][3], 0, 0, 0, 0};
+                acc[r][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, v, acc[r][n], 4, 0, 0, (int)sc[r], 0, (int)(byte[n] >> 8 * g & 255));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    } else if constexpr (XT == X_BF16) {
+        constexpr int AHEAD = 4, ALL = 4 * NT;
+        bf16x8 v[AHEAD + 1], w[2][RB];
+        const auto fetch = [&](int i) { v[i % (AHEAD + 1)] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(x + i % NT * 4096 + t16 * 256 + (((4 * (i / NT) + g) ^ t16) * 16))); };
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) fetch(i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int r = 0; r < RB; ++r) w[0][r] = weights8(c[r][0], power(sc[r]));
+#pragma unroll
+        for (int i = 0; i < ALL; ++i) {
+            const int s = i / NT, n = i % NT;
+            if (i + AHEAD < ALL) fetch(i + AHEAD);
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+                if (s < 3 && r * NT / RB == n) w[(s + 1) & 1][r] = weights8(c[r][s + 1], power(sc[r]));
+#pragma unroll
+            for (int r = 0; r < RB; ++r) acc[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[s & 1][r], v[i % (AHEAD + 1)], acc[r][n], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    } else {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            bf16x8 w[RB];
+#pragma unroll
+            for (int r = 0; r < RB; ++r) w[r] = weights8(c[r][s], power(sc[r]));
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const u32x2 o = *reinterpret_cast<const u32x2 *>(x + n * 2048 + t16 * 128 + (((4 * (s >> 1) + g) ^ (t16 >> 1)) * 16) + 8 * (s & 1));
+                const bf16x8 v = widened8(o[0], o[1], power(xb[n * 16 + t16] >> 8 * g & 255));
+#pragma unroll
+                for (int r = 0; r < RB; ++r) acc[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[r], v, acc[r][n], 0, 0, 0);
+            }
+        }
+    }
+}
+
 // Four rows r .. r+3 of one token.
 __device__ __forceinline__ void store4(const LinearArgs &a, int t, int r, const f32x4 &v) {
     if (a.out_type == DENSE_F32) {

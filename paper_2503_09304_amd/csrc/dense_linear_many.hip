@@ -89,66 +89,7 @@ __global__ __launch_bounds__(64 * kWaves, XT == X_WIDE ? 1 : 2) void linear_many
             cs[r] = sc[r] >> 8 * (b & 3) & 255;
         }
         if (b + 1 < blocks) bring(b + 1, buf ^ 1);
-        // Operands of the tokens are asked for AHEAD pieces before their products, weights of a step widened during the step before.
-        const char *x = xs[buf];
-        if constexpr (XT == X_FP8) {
-            constexpr int AHEAD = 2;
-            const int at = t16 * 128, sw = t16 >> 1;
-            u32x4 lo[NT], hi[NT];
-            int byte[NT];
-            const auto fetch = [&](int n) {
-                lo[n] = *reinterpret_cast<const u32x4 *>(x + n * 2048 + at + ((g ^ sw) * 16));
-                hi[n] = *reinterpret_cast<const u32x4 *>(x + n * 2048 + at + (((4 + g) ^ sw) * 16));
-                byte[n] = xb[buf][n * 16 + t16];
-            };
-#pragma unroll
-            for (int n = 0; n < AHEAD; ++n) fetch(n);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                if (n + AHEAD < NT) fetch(n + AHEAD);
-                const i32x8 v = {(int)lo[n][0], (int)lo[n][1], (int)lo[n][2], (int)lo[n][3], (int)hi[n][0], (int)hi[n][1], (int)hi[n][2], (int)hi[n][3]};
-                const int b8 = byte[n] >> 8 * g & 255;
-#pragma unroll
-                for (int r = 0; r < kRowTiles; ++r) {
-                    const i32x8 wv = {(int)cc[r][0], (int)cc[r][1], (int)cc[r][2], (int)cc[r][3], 0, 0, 0, 0};
-                    acc[r][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, v, acc[r][n], 4, 0, 0, (int)cs[r], 0, b8);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        } else if constexpr (XT == X_BF16) {
-            constexpr int AHEAD = 4, ALL = 4 * NT;
-            bf16x8 v[AHEAD + 1], wv[2][kRowTiles];
-            const auto fetch = [&](int i) { v[i % (AHEAD + 1)] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(x + i % NT * 4096 + t16 * 256 + (((4 * (i / NT) + g) ^ t16) * 16))); };
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i) fetch(i);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int r = 0; r < kRowTiles; ++r) wv[0][r] = weights8(cc[r][0], power(cs[r]));
-#pragma unroll
-            for (int i = 0; i < ALL; ++i) {
-                const int s = i / NT, n = i % NT;
-                if (i + AHEAD < ALL) fetch(i + AHEAD);
-                if (s < 3 && n % 2 == 0) wv[(s + 1) & 1][n / 2] = weights8(cc[n / 2][s + 1], power(cs[n / 2]));
-#pragma unroll
-                for (int r = 0; r < kRowTiles; ++r) acc[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[s & 1][r], v[i % (AHEAD + 1)], acc[r][n], 0, 0, 0);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        } else {
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                bf16x8 wv[kRowTiles];
-#pragma unroll
-                for (int r = 0; r < kRowTiles; ++r) wv[r] = weights8(cc[r][s], power(cs[r]));
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const u32x2 o = *reinterpret_cast<const u32x2 *>(x + n * 2048 + t16 * 128 + (((4 * (s >> 1) + g) ^ (t16 >> 1)) * 16) + 8 * (s & 1));
-                    const bf16x8 v = widened8(o[0], o[1], power(xb[buf][n * 16 + t16] >> 8 * g & 255));
-#pragma unroll
-                    for (int r = 0; r < kRowTiles; ++r) acc[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[r], v, acc[r][n], 0, 0, 0);
-                }
-            }
-        }
+        products<XT, kRowTiles, NT>(acc, cc, cs, xs[buf], xb[buf], g, t16);
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {

@@ -103,39 +103,7 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(const LinearArgs a, l
             c[r] = *reinterpret_cast<const u32x4 *>(wt + r * 1024 + l * 16);
             sc[r] = *reinterpret_cast<const uint32_t *>(wt + RB * 1024 + r * 256 + l * 4) >> 8 * ((from + b) & 3) & 255;
         }
-        if constexpr (XT == X_FP8) {
-#pragma unroll
-            for (int m = 0; m < NT; ++m) {
-                const u32x4 lo = *reinterpret_cast<const u32x4 *>(x + m * 2048 + t16 * 128 + ((g ^ (t16 >> 1)) * 16));
-                const u32x4 hi = *reinterpret_cast<const u32x4 *>(x + m * 2048 + t16 * 128 + (((4 + g) ^ (t16 >> 1)) * 16));
-                const int byte = xb[b][m * 16 + t16] >> 8 * g & 255;
-                const i32x8 v = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-#pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    const i32x8 wv = {(int)c[r][0], (int)c[r][1], (int)c[r][2], (int)c[r][3], 0, 0, 0, 0};
-                    acc[r][m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, v, acc[r][m], 4, 0, 0, (int)sc[r], 0, byte);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                bf16x8 wv[RB];
-#pragma unroll
-                for (int r = 0; r < RB; ++r) wv[r] = weights8(c[r][s], power(sc[r]));
-#pragma unroll
-                for (int m = 0; m < NT; ++m) {
-                    bf16x8 v;
-                    if constexpr (XT == X_BF16) {
-                        v = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(x + m * 4096 + t16 * 256 + (((4 * s + g) ^ t16) * 16)));
-                    } else {
-                        const u32x2 o = *reinterpret_cast<const u32x2 *>(x + m * 2048 + t16 * 128 + (((4 * (s >> 1) + g) ^ (t16 >> 1)) * 16) + 8 * (s & 1));
-                        v = widened8(o[0], o[1], power(xb[b][m * 16 + t16] >> 8 * g & 255));
-                    }
-#pragma unroll
-                    for (int r = 0; r < RB; ++r) acc[r][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[r], v, acc[r][m], 0, 0, 0);
-                }
-            }
-        }
+        products<XT, RB, NT>(acc, c, sc, x, xb[XT == X_BF16 ? 0 : b], g, t16);
         slot = slot + 1 == SLOTS ? 0 : slot + 1;
         next = next + 1 == SLOTS ? 0 : next + 1;
     }
