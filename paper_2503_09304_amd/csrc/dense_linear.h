@@ -49,6 +49,16 @@ __device__ __forceinline__ float power(uint32_t byte) { return __uint_as_float(b
 __device__ __forceinline__ void to_lds_at(const char *from, uint32_t at) {        // at: of the wave's, in LDS
     asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(at) : "m0", "memory");
 }
+// The same from one place of the wave's, `off` bytes behind it, by the first LANES lanes (where all 64 are at work).
+template <int LANES>
+__device__ __forceinline__ void to_lds_off(const uint8_t *from, uint32_t off, uint32_t at) {
+    static_assert(LANES == 16 || LANES == 32 || LANES == 64, "whole halves of the wave, or a quarter");
+    if constexpr (LANES == 64) asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(from), "s"(at) : "m0", "memory");
+    else if constexpr (LANES == 32)
+        asm volatile("s_mov_b32 m0, %2\n\ts_mov_b32 exec_hi, 0\n\tglobal_load_lds_dwordx4 %0, %1\n\ts_mov_b32 exec_hi, -1" ::"v"(off), "s"(from), "s"(at) : "m0", "memory");
+    else
+        asm volatile("s_mov_b32 m0, %2\n\ts_mov_b64 exec, 0xffff\n\tglobal_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1" ::"v"(off), "s"(from), "s"(at) : "m0", "memory");
+}
 #pragma clang diagnostic pop
 __device__ __forceinline__ void to_lds(const char *from, const char *to) {
     to_lds_at(from, __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)to));
@@ -56,9 +66,11 @@ __device__ __forceinline__ void to_lds(const char *from, const char *to) {
 
 // Products of a block of 128 columns: a wave's RB * 16 rows (codes c, scale bytes sc) by NT * 16 tokens, which stand in LDS (x; their scale bytes xb, four a token): pieces of 16
 // bytes, a token's in an order by its place in 16, so that the lanes of one read use all banks.  The tokens' operands are asked for AHEAD products of RB before theirs, and weights
-// are widened during the step before theirs; left to the compiler, operands come two at a time and are waited for.
-template <int XT, int RB, int NT>
-__device__ __forceinline__ void products(f32x4 (&acc)[RB][NT], const u32x4 (&c)[RB], const uint32_t (&sc)[RB], const char *x, const uint32_t *xb, int g, int t16) {
+// are widened during the step before theirs; left to the compiler, operands come two at a time and are waited for.  between(i, n): called behind each of the n groups of products,
+// for loads that would keep the wave from its products if they were asked for together.
+template <int XT, int RB, int NT, class Between>
+__device__ __forceinline__ void products(f32x4 (&acc)[RB][NT], const u32x4 (&c)[RB], const uint32_t (&sc)[RB], const char *x, const uint32_t *xb, int g, int t16,
+                                         const Between &between) {
     if constexpr (XT == X_FP8) {
         constexpr int AHEAD = 2;
         u32x4 lo[NT], hi[NT];
@@ -81,10 +93,11 @@ __device__ __forceinline__ void products(f32x4 (&acc)[RB][NT], const u32x4 (&c)[
                 const i32x8 w = {(int)c[r][0], (int)c[r][1], (int)c[r][2], (int)c[r][3], 0, 0, 0, 0};
                 acc[r][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, v, acc[r][n], 4, 0, 0, (int)sc[r], 0, (int)(byte[n] >> 8 * g & 255));
             }
+            between(n, NT);
             __builtin_amdgcn_sched_barrier(0);
         }
     } else if constexpr (XT == X_BF16) {
-        constexpr int AHEAD = 4, ALL = 4 * NT;
+        constexpr int AHEAD = 3, ALL = 4 * NT;
         bf16x8 v[AHEAD + 1], w[2][RB];
         const auto fetch = [&](int i) { v[i % (AHEAD + 1)] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(x + i % NT * 4096 + t16 * 256 + (((4 * (i / NT) + g) ^ t16) * 16))); };
 #pragma unroll
@@ -101,6 +114,7 @@ __device__ __forceinline__ void products(f32x4 (&acc)[RB][NT], const u32x4 (&c)[
                 if (s < 3 && r * NT / RB == n) w[(s + 1) & 1][r] = weights8(c[r][s + 1], power(sc[r]));
 #pragma unroll
             for (int r = 0; r < RB; ++r) acc[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[s & 1][r], v[i % (AHEAD + 1)], acc[r][n], 0, 0, 0);
+            between(i, ALL);
             __builtin_amdgcn_sched_barrier(0);
         }
     } else {
@@ -115,6 +129,7 @@ __device__ __forceinline__ void products(f32x4 (&acc)[RB][NT], const u32x4 (&c)[
                 const bf16x8 v = widened8(o[0], o[1], power(xb[n * 16 + t16] >> 8 * g & 255));
 #pragma unroll
                 for (int r = 0; r < RB; ++r) acc[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[r], v, acc[r][n], 0, 0, 0);
+                between(s * NT + n, 4 * NT);
             }
         }
     }

@@ -54,19 +54,18 @@ __global__ __launch_bounds__(64 * kWaves, XT == X_WIDE ? 1 : 2) void linear_many
     uint32_t next_xb[4] = {0, 0, 0, 0};
     u32x4 c[kRowTiles];
     uint32_t sc[kRowTiles];
-    const auto bring = [&](int b, int buf) {
-        const int at = (b * PIECES + first_piece) * 16, off = at < k_bytes ? at : 0;        // behind the last column: weights are zero there
-#pragma unroll
-        for (int j = 0; j < LOADS; ++j) to_lds(src + off + (j < here ? j * step : 0l), &xs[buf][(w + kWaves * j) * 1024]);
-        if constexpr (XT != X_BF16) {
-            const int n = a.K / 32;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) next_xb[i] = xscale[min(4 * b + i, n - 1)];
-        }
-#pragma unroll
-        for (int r = 0; r < kRowTiles; ++r) {
+    constexpr int ASKS = LOADS + kRowTiles + (XT == X_BF16 ? 0 : 1);
+    const auto ask = [&](int i, int b, int buf) {        // the i-th part of what block b needs
+        if (i < LOADS) {
+            const int at = (b * PIECES + first_piece) * 16, off = at < k_bytes ? at : 0;    // behind the last column: weights are zero there
+            to_lds(src + off + (i < here ? i * step : 0l), &xs[buf][(w + kWaves * i) * 1024]);
+        } else if (i < LOADS + kRowTiles) {
+            const int r = i - LOADS;
             c[r] = *reinterpret_cast<const u32x4 *>(codes[r] + (long)b * 1024 + l * 16);
             sc[r] = *reinterpret_cast<const uint32_t *>(scales[r] + (b >> 2) * 256 + l * 4);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) next_xb[j] = xscale[min(4 * b + j, a.K / 32 - 1)];
         }
     };
     f32x4 acc[kRowTiles][NT];
@@ -74,8 +73,9 @@ __global__ __launch_bounds__(64 * kWaves, XT == X_WIDE ? 1 : 2) void linear_many
     for (int r = 0; r < kRowTiles; ++r)
 #pragma unroll
         for (int n = 0; n < NT; ++n) acc[r][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    bring(0, 0);
-    for (int b = 0; b < blocks; ++b) {
+#pragma unroll
+    for (int i = 0; i < ASKS; ++i) ask(i, 0, 0);
+    const auto block = [&](int b, auto more) {
         const int buf = b & 1;
         if constexpr (XT != X_BF16)
             if (tid < TOK) xb[buf][tid] = next_xb[0] | next_xb[1] << 8 | next_xb[2] << 16 | next_xb[3] << 24;
@@ -88,9 +88,17 @@ __global__ __launch_bounds__(64 * kWaves, XT == X_WIDE ? 1 : 2) void linear_many
             cc[r] = c[r];
             cs[r] = sc[r] >> 8 * (b & 3) & 255;
         }
-        if (b + 1 < blocks) bring(b + 1, buf ^ 1);
-        products<XT, kRowTiles, NT>(acc, cc, cs, xs[buf], xb[buf], g, t16);
-    }
+        products<XT, kRowTiles, NT>(acc, cc, cs, xs[buf], xb[buf], g, t16, [&](int i, int n) {
+            if constexpr (decltype(more)::value) {
+                constexpr int EARLY = 2;                 // in the first half: they have the second to come
+#pragma unroll
+                for (int k = 0; k < ASKS; ++k)
+                    if (k * n / EARLY / ASKS == i) ask(k, b + 1, buf ^ 1);
+            }
+        });
+    };
+    for (int b = 0; b + 1 < blocks; ++b) block(b, std::true_type{});
+    block(blocks - 1, std::false_type{});
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const int t = t0 + n * 16 + t16;

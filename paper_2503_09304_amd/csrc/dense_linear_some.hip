@@ -28,14 +28,14 @@ __device__ __forceinline__ void wait_for(int later) {    // for all but the load
 template <int XT, int NT, int RB, int KS, int AHEAD>
 __global__ __launch_bounds__(64 * kWaves) void linear_some(const LinearArgs a, long first_wg, int range_blocks) {
     constexpr int PIECES = XT == X_BF16 ? 16 : 8;        // of 16 bytes, in a token's 128 columns
-    constexpr int TOK = NT * 16, X = TOK * PIECES * 16, SHARE = kWaves / KS, LOADS = X / 1024 / SHARE, WAVE = RB * 1024 + 1024, SLOT = KS * X + kWaves * WAVE, SLOTS = AHEAD + 1;
+    constexpr int TOK = NT * 16, X = TOK * PIECES * 16, SHARE = kWaves / KS, LOADS = X / 1024 / SHARE, WAVE = RB * 1280, SLOT = KS * X + kWaves * WAVE, SLOTS = AHEAD + 1;
     constexpr int COUNT = LOADS + RB + 1;                // a wave's loads for a block
     static_assert(KS == 1 || KS == kWaves, "waves share tokens or have their own");
-    static_assert(LOADS >= 1 && (KS == 1 || SLOTS * SLOT >= kWaves * RB * NT * 1024), "room for a wave's load, and for the sums");
+    static_assert(LOADS >= 1 && SLOT % 256 == 0 && (KS == 1 || SLOTS * SLOT >= kWaves * RB * NT * 1024), "room for a wave's load, and for the sums");
     static_assert(COUNT * AHEAD < 64, "the counter of loads under way has six bits");
     __shared__ __align__(16) char lds[SLOTS * SLOT];
     __shared__ uint32_t xb[XT == X_BF16 ? 1 : kSomeBlocks][XT == X_BF16 ? 1 : TOK];
-    const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, g = l >> 4, t16 = l & 15;
+    const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, g = l >> 4, t16 = l & 15;
     const int blocks = (a.K + 127) / 128, sets = (a.K + 511) / 512, row_tiles = (a.R + 15) / 16, row_wgs = (row_tiles + RB * SHARE - 1) / (RB * SHARE);
     long wg = first_wg + blockIdx.x;
     const int rt = (int)(wg % row_wgs) * (RB * SHARE) + w / KS * RB, wk = w % KS, ws = w / KS;
@@ -43,30 +43,33 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(const LinearArgs a, l
     const int z = (int)(wg % a.ranges), t0 = (int)(wg / a.ranges) * TOK, from = z * range_blocks, n = min(blocks, from + range_blocks) - from;
     const uint8_t *codes[RB];
 #pragma unroll
-    for (int r = 0; r < RB; ++r) codes[r] = a.codes + ((long)min(rt + r, row_tiles - 1) * blocks + from) * 1024 + l * 16;
-    const uint8_t *scales = a.scales + (long)min(rt + (l >> 4) % RB, row_tiles - 1) * sets * 256 + t16 * 16;       // RB tiles' 256 bytes, 16 lanes each
+    for (int r = 0; r < RB; ++r) codes[r] = a.codes + ((long)min(rt + r, row_tiles - 1) * blocks + from) * 1024;
+    const uint8_t *const scales = a.scales + (long)min(rt, row_tiles - 1) * sets * 256;
+    const uint32_t scale_at = (uint32_t)(min(rt + (l >> 4) % RB, row_tiles - 1) - min(rt, row_tiles - 1)) * (sets * 256) + t16 * 16;         // RB tiles' 256 bytes, 16 lanes each
+    constexpr int ORDERS = KS == 1 ? 1 : LOADS;          // tokens whose places in 16 are the same have their pieces in the same order
     const char *src[LOADS];
-    int first_piece[LOADS];
+    int first_piece[ORDERS];
     {
         constexpr int PER = 64 / PIECES;                 // tokens of a wave's load
+        static_assert(KS > 1 || SHARE * PER % 16 == 0, "one order");
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
             const int t = (ws + SHARE * j) * PER + l / PIECES, p = l % PIECES, q = XT == X_BF16 ? p ^ (t & 15) : p ^ (t >> 1 & 7);
             src[j] = a.x.p + (long)min(t0 + t, a.n_tokens - 1) * a.x.ts * (XT == X_BF16 ? 2 : 1);
-            first_piece[j] = XT == X_BF16 ? 4 * (q & 3) + (q >> 2) : XT == X_FP8 ? q : 2 * (q & 3) + (q >> 2);
+            if (j < ORDERS) first_piece[j] = XT == X_BF16 ? 4 * (q & 3) + (q >> 2) : XT == X_FP8 ? q : 2 * (q & 3) + (q >> 2);
         }
     }
     const int k_bytes = a.K * (XT == X_BF16 ? 2 : 1);
     const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds, mine = __builtin_amdgcn_readfirstlane(base + KS * X + w * WAVE),
                    piece0 = __builtin_amdgcn_readfirstlane(base + wk * X + ws * 1024);
-    const auto bring = [&](int b, int slot) {
+    const auto ask = [&](int i, int b, int slot) {       // the i-th part of what block b needs
         const uint32_t to = slot * SLOT;
-#pragma unroll
-        for (int r = 0; r < RB; ++r) to_lds_at(reinterpret_cast<const char *>(codes[r]) + (long)b * 1024, mine + to + r * 1024);
-        to_lds_at(reinterpret_cast<const char *>(scales) + ((from + b) >> 2) * 256, mine + to + RB * 1024);
-#pragma unroll
-        for (int j = 0; j < LOADS; ++j) {
-            const int at = ((from + b) * PIECES + first_piece[j]) * 16;
+        if (i < RB) {
+            to_lds_off<64>(codes[i] + (long)b * 1024, l * 16, mine + to + i * 1024);
+        } else if (i == RB) {
+            to_lds_off<16 * RB>(scales + ((from + b) >> 2) * 256, scale_at, mine + to + RB * 1024);
+        } else {
+            const int j = i - RB - 1, at = ((from + b) * PIECES + first_piece[j % ORDERS]) * 16;
             to_lds_at(src[j] + (at < k_bytes ? at : 0), piece0 + to + j * (SHARE * 1024));        // behind the last column: weights are zero there
         }
     };
@@ -87,14 +90,22 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(const LinearArgs a, l
 #pragma unroll
         for (int m = 0; m < NT; ++m) acc[r][m] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int mine_n = (n - wk + KS - 1) / KS;           // this wave's blocks: wk, wk + KS, ...
-    for (int i = 0; i < min(AHEAD, mine_n); ++i) bring(wk + i * KS, i);
+    for (int i = 0; i < min(AHEAD, mine_n); ++i)
+#pragma unroll
+        for (int k = 0; k < COUNT; ++k) ask(k, wk + i * KS, i);
     if constexpr (KS > 1 && XT != X_BF16) __syncthreads();
-    for (int i = 0, slot = 0, next = AHEAD; i < mine_n; ++i) {
+    int slot = 0, next = AHEAD;
+    const auto block = [&](int i, auto more) {
         const int b = wk + i * KS;
         wait_for<COUNT, AHEAD - 1>(mine_n - 1 - i);      // this wave's pieces of block b are in LDS
         if constexpr (KS == 1) __syncthreads();          // everybody's; and the block before, in whose place the next one comes, has been read
         else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (i + AHEAD < mine_n) bring(b + AHEAD * KS, next);
+        if constexpr (AHEAD == 1) {
+            if (i + 1 < mine_n) {
+#pragma unroll
+                for (int k = 0; k < COUNT; ++k) ask(k, b + KS, next);
+            }
+        }
         const char *x = lds + slot * SLOT + wk * X, *wt = lds + slot * SLOT + KS * X + w * WAVE;
         u32x4 c[RB];
         uint32_t sc[RB];
@@ -103,9 +114,21 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(const LinearArgs a, l
             c[r] = *reinterpret_cast<const u32x4 *>(wt + r * 1024 + l * 16);
             sc[r] = *reinterpret_cast<const uint32_t *>(wt + RB * 1024 + r * 256 + l * 4) >> 8 * ((from + b) & 3) & 255;
         }
-        products<XT, RB, NT>(acc, c, sc, x, xb[XT == X_BF16 ? 0 : b], g, t16);
+        products<XT, RB, NT>(acc, c, sc, x, xb[XT == X_BF16 ? 0 : b], g, t16, [&](int at, int n) {
+            if constexpr (AHEAD > 1 && decltype(more)::value) {      // beside the first half of the products: all at once they would keep the wave from them
+#pragma unroll
+                for (int k = 0; k < COUNT; ++k)
+                    if (k * n / 2 / COUNT == at) ask(k, b + AHEAD * KS, next);
+            }
+        });
         slot = slot + 1 == SLOTS ? 0 : slot + 1;
         next = next + 1 == SLOTS ? 0 : next + 1;
+    };
+    if constexpr (AHEAD == 1) {
+        for (int i = 0; i < mine_n; ++i) block(i, std::false_type{});
+    } else {
+        for (int i = 0; i < mine_n - AHEAD; ++i) block(i, std::true_type{});
+        for (int i = max(0, mine_n - AHEAD); i < mine_n; ++i) block(i, std::false_type{});
     }
     if constexpr (KS > 1) {
         f32x4 *red = reinterpret_cast<f32x4 *>(lds);
@@ -149,12 +172,16 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(const LinearArgs a, l
 
 hipError_t launch_linear_some(const LinearArgs &a, int tiles, int rows, int ks, int range_blocks, hipStream_t s) {
     const auto go = [&](auto xt, auto nt, auto rb, auto ks) {
-        constexpr int XT = decltype(xt)::value, NT = decltype(nt)::value, RB = decltype(rb)::value, KS = decltype(ks)::value, AHEAD = NT * RB >= 8 || (KS > 1 && XT == X_BF16) ? 1 : 2;
+        constexpr int XT = decltype(xt)::value, NT = decltype(nt)::value, RB = decltype(rb)::value, KS = decltype(ks)::value;
         constexpr int PER = RB * kWaves / KS;
         const long row_wgs = ((a.R + 15) / 16 + PER - 1) / PER, all = row_wgs * a.ranges * ((a.n_tokens + NT * 16 - 1) / (NT * 16));
         constexpr long kMost = 1 << 23;                  // workgroups of 256 threads that a launch may have
-        for (long at = 0; at < all; at += kMost)
-            linear_some<XT, NT, RB, KS, AHEAD><<<dim3((unsigned)(all - at < kMost ? all - at : kMost)), dim3(64 * kWaves), 0, s>>>(a, at, range_blocks);
+        const auto run = [&](auto ahead) {
+            for (long at = 0; at < all; at += kMost)
+                linear_some<XT, NT, RB, KS, decltype(ahead)::value><<<dim3((unsigned)(all - at < kMost ? all - at : kMost)), dim3(64 * kWaves), 0, s>>>(a, at, range_blocks);
+        };
+        if constexpr (NT * RB == 16) all <= 256 ? run(std::integral_constant<int, 2>{}) : run(std::integral_constant<int, 1>{});
+        else run(std::integral_constant<int, (KS > 1 && XT == X_BF16) ? 1 : 2>{});
     };
     const auto by_size = [&](auto xt) {
         typedef std::integral_constant<int, 1> One;
