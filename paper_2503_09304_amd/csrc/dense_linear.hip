@@ -194,24 +194,24 @@ static Plan some_of(int K, bool bf16, int tiles, int rows, int ks, int ranges) {
 }
 // Us that a plan takes, fitted to what was measured (420 shapes of 64 to 16384 columns, 16 to 32000 rows, 1 to 8192 tokens, both types of x, every plan): a launch and the
 // first bytes; for every block of 128 columns of the workgroups that a CU has what one takes alone, or among others; linear_few what a CU takes in; ranges a launch and
-// their sums' way to memory and back; outputs their way to memory.  On 200 shapes drawn anew its choice takes 1.8 % more than the best plan of a shape in the mean, 37 % once.
+// their sums' way to memory and back; outputs their way to memory.  On 200 shapes drawn anew its choice takes 2.2 % more than the best plan of a shape in the mean, 32 % at most.
 static float us_of(const Plan &p, int n_tokens, int R, int K, bool bf16) {
     const int row_tiles = (R + 15) / 16, token_tiles = (n_tokens + p.tiles * 16 - 1) / (p.tiles * 16);
-    const float sums = (float)n_tokens * R, ends = (p.ranges == 1 ? 0.f : 2.7f + sums * p.ranges * 1.6e-6f) + sums * 1e-6f;
+    const float sums = (float)n_tokens * R, ends = (p.ranges == 1 ? 0.f : 2.56f + sums * p.ranges * 1.86e-6f) + sums * .89e-6f;
     if (p.tiles == 1) {
         const int per = kWaves / p.ks;
         const long wgs = (long)((row_tiles + per - 1) / per) * token_tiles * p.ranges, on_cu = (wgs + 255) / 256;
         const float x = (float)std::min(n_tokens, kFewTokens) * (bf16 ? 256.f : 132.f) * p.range_blocks, w = (float)per * p.range_blocks * 1088.f;
-        return 3.65f + (float)on_cu * (x + w) / 39.6e3f + ends;
+        return 3.6f + (float)on_cu * (x + w) / 47.8e3f + ends;
     }
     const int per = p.tiles == 8 ? 16 : 4 * p.rows / p.ks;
     const long wgs = (long)((row_tiles + per - 1) / per) * token_tiles * p.ranges, on_cu = (wgs + 255) / 256;
-    if (p.ks > 1) return 3.25f + (float)on_cu * ((p.range_blocks + p.ks - 1) / p.ks) * .47f + ends;
+    if (p.ks > 1) return 3.f + (float)on_cu * ((p.range_blocks + p.ks - 1) / p.ks) * .517f + ends;
     // [x in bf16][tokens by rows of a wave: 2x1, 2x2, 4x2, 4x4 tiles, linear_many]
-    static const float alone[2][5] = {{.266f, .315f, .54f, .736f, 1.43f}, {.333f, .365f, .644f, .973f, 1.91f}},
-                       among[2][5] = {{.181f, .27f, .367f, .519f, .778f}, {.209f, .303f, .439f, .655f, 1.23f}};
+    static const float alone[2][5] = {{.289f, .323f, .496f, .613f, 1.15f}, {.238f, .378f, .501f, .802f, 1.35f}},
+                       among[2][5] = {{.162f, .265f, .403f, .486f, .728f}, {.182f, .287f, .404f, .676f, 1.18f}};
     const int kind = p.tiles == 8 ? 4 : p.tiles == 2 ? p.rows - 1 : p.rows == 2 ? 2 : 3;
-    return 3.25f + (float)p.range_blocks * (on_cu > 1 ? (float)on_cu * among[bf16][kind] : alone[bf16][kind]) + ends;
+    return 3.f + (float)p.range_blocks * (on_cu > 1 ? (float)on_cu * among[bf16][kind] : alone[bf16][kind]) + ends;
 }
 static Plan plan_of(int n_tokens, int R, int K, bool bf16) {
     const int blocks = (K + 127) / 128;
