@@ -17,7 +17,6 @@ namespace {
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // ---- gate GEMM ----
 
@@ -31,19 +30,19 @@ __device__ __forceinline__ void to_lds(const char *from, const char *to) {
 #pragma clang diagnostic pop
 
 constexpr int kMostRanges = 16, kMostWaves = 16;
+constexpr int EB = 2;                 // experts a lane (4, in half as many waves: nothing won)
 constexpr int kStage = 128;           // columns of the hidden size that stand in LDS at once
 
-// Bound by the tokens' way from memory where they are many (8192 tokens, H 4096, 160 experts: 29 us, their bytes 13), by latency where they are few (a stage's loads are
-// under way while the stage before is multiplied, and a range has few stages).
-// Products of TT * 16 tokens with all experts over a range of the hidden size: a wave has 32 experts (and, where experts are few, one of `slices` parts of the range).
-// Lane l's operands are experts 2 (l%16) and 2 (l%16) + 1 of the wave's.  Row-major weights [H][E] (E even): it takes the pairs of 8 rows and turns them over in
-// registers, so no transposed copy is written first.
+// Products of TT * 16 tokens with all experts over a range of the hidden size: a wave has 16 * EB = 32 experts (and, where experts are few, one of `slices` parts of the range),
+// lane l's operands are those from EB * (l%16) on.  Row-major weights [H][E] (E a multiple of EB): it takes EB elements of each of 8 rows and turns them over in
+// registers, so no transposed copy is written first.  Tokens stand in LDS, a stage ahead; the next stage's weights of a step are asked for as soon as this
+// stage's have become operands, between the products.
 template <int TT, bool PACKED>
-__global__ __launch_bounds__(64 * kMostWaves) void gate_ranges(const uint16_t *__restrict__ x, const uint16_t *__restrict__ Wg, float *__restrict__ part, int N, int H, int E,
-                                                   int blocks, int slices, int range) {
+__global__ __launch_bounds__(64 * kMostWaves) void gate_ranges(const uint16_t *x, const uint16_t *Wg, float *part, int N, int H, int E,
+                                                                   int blocks, int slices, int range) {
     extern __shared__ __align__(16) char lds[];
-    constexpr int STEPS = kStage / 32, PIECES = kStage / 8, STAGE_BYTES = TT * 16 * kStage * 2;
-    const int w = threadIdx.x >> 6, l = threadIdx.x & 63, t16 = l & 15, g = l >> 4;
+    constexpr int STEPS = kStage / 32, PIECES = kStage / 8, STAGE_BYTES = TT * 16 * kStage * 2, ASKS = PACKED ? EB : 8;      // a step's loads
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, t16 = l & 15, g = l >> 4;
     const int pb = w % blocks, sl = w / blocks;
     const int t0 = blockIdx.x * (TT * 16), from = blockIdx.y * range, to = min(H, from + range);
     const int per = ((to - from + slices - 1) / slices + 31) / 32 * 32, k0 = min(to, from + sl * per), k1 = min(to, k0 + per);
@@ -55,63 +54,64 @@ __global__ __launch_bounds__(64 * kMostWaves) void gate_ranges(const uint16_t *_
             to_lds((const char *)(x + (long)min(t0 + t, N - 1) * H + (at < H ? at : 0)), mine + buf * STAGE_BYTES + j * 1024);
         }
     };
-    const int e0 = pb * 32 + 2 * t16;
-    u32x4 wv[STEPS][2];
-    uint32_t raw[STEPS][8];
-    const auto ask = [&](int k) {
+    typedef unsigned int words __attribute__((ext_vector_type(EB / 2)));
+    const int e0 = pb * (16 * EB) + EB * t16;
+    u32x4 packed[STEPS][EB];
+    words raw[STEPS][8];
+    const auto ask = [&](int s, int k) {
+        const int row = min(k + 32 * s + 8 * g, H - 8);  // behind the range: not multiplied
+        if constexpr (PACKED) {
+#pragma unroll
+            for (int h = 0; h < EB; ++h) packed[s][h] = *reinterpret_cast<const u32x4 *>(Wg + (long)min(e0 + h, E - 1) * H + row);
+        } else {
+            const uint16_t *p = Wg + (long)row * E + min(e0, E - EB);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) raw[s][i] = *reinterpret_cast<const words *>(p + (long)i * E);
+        }
+    };
+    f32x4 acc[TT][EB];
+#pragma unroll
+    for (int n = 0; n < TT; ++n)
+#pragma unroll
+        for (int h = 0; h < EB; ++h) acc[n][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int rounds = (per + kStage - 1) / kStage;      // of all slices alike: they share the barriers
+    bring(min(k0, H - 1) & ~31, 0);
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) ask(s, k0);
+    const auto stage = [&](int i, auto more) {
+        const int k = k0 + i * kStage;
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(STEPS * ASKS) : "memory");      // this wave's pieces are in LDS: the weights were asked for behind them
+        __syncthreads();
+        if constexpr (decltype(more)::value) bring(k + kStage, (i + 1) & 1);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-            if (k + 32 * s >= k1) break;
-            const int row = k + 32 * s + 8 * g;
-            if constexpr (PACKED) {
-                wv[s][0] = *reinterpret_cast<const u32x4 *>(Wg + (long)min(e0, E - 1) * H + row);
-                wv[s][1] = *reinterpret_cast<const u32x4 *>(Wg + (long)min(e0 + 1, E - 1) * H + row);
-            } else {
-                const uint16_t *p = Wg + (long)row * E + min(e0, E - 2);
+            bf16x8 now[EB], a[TT];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) raw[s][i] = *reinterpret_cast<const uint32_t *>(p + (long)i * E);
+            for (int n = 0; n < TT; ++n)
+                a[n] = *reinterpret_cast<const bf16x8 *>(mine + (i & 1) * STAGE_BYTES + (n * 16 + t16) * (PIECES * 16) + ((4 * s + g) ^ t16) * 16);
+#pragma unroll
+            for (int h = 0; h < EB; ++h) {
+                if constexpr (PACKED) {
+                    now[h] = __builtin_bit_cast(bf16x8, packed[s][h]);
+                } else {
+                    u32x4 v;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)          // rows 2r and 2r + 1
+                        v[r] = __builtin_amdgcn_perm(raw[s][2 * r + 1][h / 2], raw[s][2 * r][h / 2], h % 2 ? 0x07060302u : 0x05040100u);
+                    now[h] = __builtin_bit_cast(bf16x8, v);
+                }
+            }
+            if constexpr (decltype(more)::value) ask(s, k + kStage);
+            if (k + 32 * s >= k1) continue;
+#pragma unroll
+            for (int n = 0; n < TT; ++n) {
+#pragma unroll
+                for (int h = 0; h < EB; ++h) acc[n][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[n], now[h], acc[n][h], 0, 0, 0);
             }
         }
     };
-    f32x4 acc[TT][2];
-#pragma unroll
-    for (int n = 0; n < TT; ++n) acc[n][0] = acc[n][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int rounds = (per + kStage - 1) / kStage;      // of all slices alike: they share the barriers
-    bring(min(k0, H - 1) & ~31, 0);
-    ask(k0);
-    for (int i = 0; i < rounds; ++i) {
-        const int k = k0 + i * kStage;
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); // this wave's pieces are in LDS
-        __syncthreads();
-        u32x4 now[STEPS][2];
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            if constexpr (PACKED) {
-                now[s][0] = wv[s][0];
-                now[s][1] = wv[s][1];
-            } else {
-#pragma unroll
-                for (int h = 0; h < 4; ++h) {            // rows 2h and 2h + 1
-                    now[s][0][h] = __builtin_amdgcn_perm(raw[s][2 * h + 1], raw[s][2 * h], 0x05040100u);
-                    now[s][1][h] = __builtin_amdgcn_perm(raw[s][2 * h + 1], raw[s][2 * h], 0x07060302u);
-                }
-            }
-        }
-        if (i + 1 < rounds && k + kStage < k1) {
-            bring(k + kStage, (i + 1) & 1);
-            ask(k + kStage);
-        }
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            if (k + 32 * s >= k1) break;
-#pragma unroll
-            for (int n = 0; n < TT; ++n) {
-                const bf16x8 a = *reinterpret_cast<const bf16x8 *>(mine + (i & 1) * STAGE_BYTES + (n * 16 + t16) * (PIECES * 16) + ((4 * s + g) ^ t16) * 16);
-                acc[n][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, now[s][0]), acc[n][0], 0, 0, 0);
-                acc[n][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, now[s][1]), acc[n][1], 0, 0, 0);
-            }
-        }
-    }
+    for (int i = 0; i + 1 < rounds; ++i) stage(i, std::true_type{});
+    stage(rounds - 1, std::false_type{});
     if (slices > 1) {
         f32x4 *red = reinterpret_cast<f32x4 *>(lds);
         __syncthreads();                                 // the tokens have been read
@@ -119,19 +119,20 @@ __global__ __launch_bounds__(64 * kMostWaves) void gate_ranges(const uint16_t *_
 #pragma unroll
             for (int n = 0; n < TT; ++n)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) red[((w - blocks) * (2 * TT) + 2 * n + h) * 64 + l] = acc[n][h];
+                for (int h = 0; h < EB; ++h) red[((w - blocks) * (EB * TT) + EB * n + h) * 64 + l] = acc[n][h];
         __syncthreads();
         if (sl > 0) return;
         for (int i = 1; i < slices; ++i)
 #pragma unroll
             for (int n = 0; n < TT; ++n)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const f32x4 o = red[((w + (i - 1) * blocks) * (2 * TT) + 2 * n + h) * 64 + l];
+                for (int h = 0; h < EB; ++h) {
+                    const f32x4 o = red[((w + (i - 1) * blocks) * (EB * TT) + EB * n + h) * 64 + l];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[n][h][e] += o[e];
                 }
     }
+    typedef float floats __attribute__((ext_vector_type(EB)));
 #pragma unroll
     for (int n = 0; n < TT; ++n)
 #pragma unroll
@@ -139,11 +140,15 @@ __global__ __launch_bounds__(64 * kMostWaves) void gate_ranges(const uint16_t *_
             const int t = t0 + n * 16 + 4 * g + i;
             float *o = part + ((long)blockIdx.y * N + t) * E + e0;
             if (t >= N || e0 >= E) continue;
-            if (E % 2 == 0) {
-                *reinterpret_cast<f32x2 *>(o) = f32x2{acc[n][0][i], acc[n][1][i]};
+            if (E % EB == 0) {
+                floats v;
+#pragma unroll
+                for (int h = 0; h < EB; ++h) v[h] = acc[n][h][i];
+                *reinterpret_cast<floats *>(o) = v;
             } else {
-                o[0] = acc[n][0][i];
-                if (e0 + 1 < E) o[1] = acc[n][1][i];
+#pragma unroll
+                for (int h = 0; h < EB; ++h)
+                    if (e0 + h < E) o[h] = acc[n][h][i];
             }
         }
 }
@@ -412,9 +417,10 @@ hipError_t launch_score(const RouteArgs &a, const float *part, int planes, hipSt
 }
 
 hipError_t launch_gate_scored(const RouteArgs &a, hipStream_t s) {
+    const int tt = a.N <= 512 ? 1 : a.N <= 2048 ? 2 : 4, tiles = (a.N + tt * 16 - 1) / (tt * 16);
+    const int blocks = (a.E + 16 * EB - 1) / (16 * EB);
     // Tokens a workgroup: few while ranges can be enough workgroups all the same, as a range's products and sums are one after the other then (61 tokens on 256 experts, H 4096: 16 / 32 / 64
     // a workgroup 11.2 / 11.3 / 12.8 us with the choice; 512 on 128 11.9 / 12.0 / 14.4); with many tokens the weights' way to the workgroups counts (8192 on 256: 87 / 56 / 52).
-    const int blocks = (a.E + 31) / 32, tt = a.N <= 512 ? 1 : a.N <= 2048 ? 2 : 4, tiles = (a.N + tt * 16 - 1) / (tt * 16);
     // Ranges: as many as give 256 workgroups, 16 at most, what the scratch holds.  Their parts: up to 16 waves, 4 parts.  Both of a stage's columns at least.
     const long fit = (long)a.k * a.H / a.E;              // the context's room for k rows of H floats a token
     long ranges = std::max(1l, std::min({256l / tiles, (long)kMostRanges, (long)a.H / kStage, fit}));
@@ -424,9 +430,9 @@ hipError_t launch_gate_scored(const RouteArgs &a, hipStream_t s) {
     float *part = ranges > 1 ? a.scratch : a.logits;
     const auto go = [&](auto t, auto packed) {
         constexpr int TT = decltype(t)::value;
-        const size_t lds = std::max<size_t>((size_t)slices * 2 * TT * 16 * kStage * 2, (size_t)(slices - 1) * blocks * 2 * TT * 1024);
-        gate_ranges<TT, decltype(packed)::value><<<dim3(tiles, (unsigned)ranges), dim3(64 * blocks * slices), lds, s>>>((const uint16_t *)a.x, (const uint16_t *)a.Wg, part, a.N, a.H, a.E, blocks,
-                                                                                                                    slices, range);
+        const size_t lds = std::max<size_t>((size_t)slices * 2 * TT * 16 * kStage * 2, (size_t)(slices - 1) * blocks * EB * TT * 1024);
+        gate_ranges<TT, decltype(packed)::value><<<dim3(tiles, (unsigned)ranges), dim3(64 * blocks * slices), lds, s>>>((const uint16_t *)a.x, (const uint16_t *)a.Wg, part, a.N, a.H, a.E,
+                                                                                                                        blocks, slices, range);
     };
     const auto by_layout = [&](auto t) { a.packed ? go(t, std::true_type{}) : go(t, std::false_type{}); };
     if (tt == 1) by_layout(std::integral_constant<int, 1>{});
