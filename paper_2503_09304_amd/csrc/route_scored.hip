@@ -37,6 +37,8 @@ constexpr int kStage = 128;           // columns of the hidden size that stand i
 // lane l's operands are those from EB * (l%16) on.  Row-major weights [H][E] (E a multiple of EB): it takes EB elements of each of 8 rows and turns them over in
 // registers, so no transposed copy is written first.  Tokens stand in LDS, a stage ahead; the next stage's weights of a step are asked for as soon as this
 // stage's have become operands, between the products.
+// Bound by latency where tokens are few (a range has few stages, each a way to memory), else by that and the tokens' bytes together: 8192 tokens, H 4096: on 64 experts 28 us
+// with the choice, on 160 41 to 44, where the bytes alone take 13.  Tried: weights through LDS (27 to 29 us for this kernel alone instead of 30; 61 tokens 8.9 instead of 6.6).
 template <int TT, bool PACKED>
 __global__ __launch_bounds__(64 * kMostWaves) void gate_ranges(const uint16_t *x, const uint16_t *Wg, float *part, int N, int H, int E,
                                                                    int blocks, int slices, int range) {
