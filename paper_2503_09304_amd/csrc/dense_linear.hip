@@ -18,7 +18,8 @@
 namespace qdense {
 namespace {
 
-// Up to 16 tokens: bound by the matrix.  A wave has 16 rows and a slice of the columns, and streams its part of the matrix, AHEAD tiles ahead of their use; KS waves of a
+// Up to 16 tokens: bound by the matrix, and, as it is small, by the launch and the first bytes (one token by 6144 x 4096 5.3 us, 2.5 TB/s, of which 3.6 are there for any size;
+// 8 by 32000 x 2048 10.0 us, 3.6 TB/s).  A wave has 16 rows and a slice of the columns, and streams its part of the matrix, AHEAD tiles ahead of their use; KS waves of a
 // workgroup share rows and add their sums in LDS.  The tokens' columns of the workgroup's range are in LDS from the start.
 constexpr int kWaves = 8, kFewTokens = 16;
 constexpr size_t kMostLds = 128 * 1024;
@@ -119,7 +120,7 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few(const LinearArgs a, lo
     else *reinterpret_cast<f32x4 *>(a.part + ((long)z * a.n_tokens + t) * (row_tiles * 16l) + o) = acc;
 }
 
-// The ranges' sums, added in their order.
+// The ranges' sums, added in their order: a launch, and a way to memory and back (61 tokens, 4096 rows, 8 ranges 4.7 us).
 __global__ __launch_bounds__(256) void join_ranges(const LinearArgs a) {
     const int quads = (a.R + 15) / 16 * 4;
     const long i = (long)blockIdx.x * 256 + threadIdx.x;
@@ -192,6 +193,9 @@ static Plan some_of(int K, bool bf16, int tiles, int rows, int ks, int ranges) {
     cut(p, blocks, bf16 ? ranges : std::max(ranges, (blocks + kSomeBlocks - 1) / kSomeBlocks));
     return p;
 }
+// Each variant where it is best, us, x in bf16, with its best number of ranges: 1 token by 6144 x 4096 linear_few 5.9, linear_some with waves that share rows 12, with tiles
+// of 2x1 (16 tokens by 16 rows of a wave) 8.9; 64 by 1024 x 1024 shared rows 4.4, 2x1 5.2, 2x2 6.2; 64 by 6144 x 4096 2x1 12.8, 2x2 13.6, 4x2 14.3, 4x4 17.5, linear_many 42; 256
+// 23.6, 21.2, 20.0, 24.2, 45; 1024 80, 62, 53, 56, 56; 4096 323, 240, 184, 168, 149.  Ranges: 61 by 4096 x 14336 in tiles of 4x2 with 8 of them 16.5, with 2 33.
 // Us that a plan takes, fitted to what was measured (420 shapes of 64 to 16384 columns, 16 to 32000 rows, 1 to 8192 tokens, both types of x, every plan): a launch and the
 // first bytes; for every block of 128 columns of the workgroups that a CU has what one takes alone, or among others; linear_few what a CU takes in; ranges a launch and
 // their sums' way to memory and back; outputs their way to memory.  On 200 shapes drawn anew its choice takes 2.2 % more than the best plan of a shape in the mean, 32 % at most.

@@ -3,7 +3,8 @@
 // Each of four waves has 64 rows and all of the tile's tokens: weights come straight into its registers, a block of 128 columns ahead, and are widened there, a step before
 // their products; the tokens' columns are brought to LDS while the block before is multiplied, and read by all waves, some products before they are needed (left to the
 // compiler, which asks for two at a time and waits for them: 8192 tokens by 4096 x 4096 in bf16 214 us, 203 so).  Bound by the matrix units and the tokens' way to LDS
-// (with the latter left out 174 us, with nothing but products 164): 200 us, 1.37 PFLOP/s; 4093 tokens by 28672 x 4096 in 8 bits 450 us, 2.1 PFLOP/s.
+// (with the latter left out 174 us, with nothing but products 164), at a clock that power holds at 2.0 to 2.1 GHz: 198 us, 1.39 PFLOP/s; 4093 tokens by 28672 x 4096 in 8 bits 455 us,
+// 2.1 PFLOP/s.  (Tokens and weights both through LDS, one workgroup a CU, two blocks ahead: 241 and 516.)
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
