@@ -50,7 +50,8 @@ typedef struct {
  * x: bf16.  add: bf16 or fp32, or NULL.  total: rows of add's type, or NULL; needs add.  out: bf16 or fp8.  weight [device]
  * [dim], 16-byte aligned, of weight_type bf16 or fp32; NULL: 1 (and shift is not looked at).  shift: 1 for weights that are kept
  * as differences from 1, else 0.  eps > 0.  dim: a multiple of 8 (32 for an fp8 out), at most 32768; n_tokens * heads: at most 2^30.
- * total may be add, and out may be x or add where types and strides are the same; otherwise outputs overlap neither inputs nor each other.
+ * total may be add, and out may be x or add, where types and strides are the same; otherwise outputs overlap neither inputs nor each other (rows that
+ * begin at the same address are refused, other overlaps are the caller's to avoid).
  * fp8: the scale of 32 elements is the smallest power of two, 2^-126 at least, for which none is over 448 (one that would round
  * to 2^128 to 1.875 * 2^127); each element is rounded once.  32 elements of which one is not finite have the scale byte 255 (NaN).
  * Rows whose sum of squares is over the largest fp32 give zeros (elements of 2^63 and more). */
@@ -82,10 +83,10 @@ int32_t dense_pack4(const uint8_t *codes, const uint8_t *scales, const dense_mat
  * by the matrix unit's scaled products, which drop, of the few neighbouring products that they add first, what is below 2^-14 of
  * the largest (measured: of normally distributed rows 2^-18 of a result, 2^-14 with large outliers); with an fp32 out they are
  * widened to bf16, exactly, and multiplied as such.
- * n_tokens: at most 2^24.  out overlaps no input.
+ * n_tokens: at most 2^24.  out overlaps no input, the workspace neither.
  * workspace ([device], 16-byte aligned, may be NULL; its contents before and after the call are of no account): where rows are so few that
  * they leave CUs idle, the sums are cut into ranges of columns that run side by side, and a second launch adds them in order.
- * dense_linear_workspace_bytes(...) is what that takes, 0 where nothing is cut; with less than that nothing is cut either. */
+ * dense_linear_workspace_bytes(...) is what that takes, at most 256 MB, 0 where nothing is cut; with less than that nothing is cut either. */
 size_t dense_linear_workspace_bytes(int32_t n_tokens, int32_t rows, int32_t cols, int32_t x_type, int32_t out_type);
 int32_t dense_linear(const dense_rows *x, const dense_matrix4 *w, const dense_rows *out, int32_t n_tokens, void *workspace,
                      size_t workspace_bytes, void *stream);
