@@ -217,12 +217,13 @@ static float us_of(const Plan &p, int n_tokens, int R, int K, bool bf16) {
     const int kind = p.tiles == 8 ? 4 : p.tiles == 2 ? p.rows - 1 : p.rows == 2 ? 2 : 3;
     return 3.f + (float)p.range_blocks * (on_cu > 1 ? (float)on_cu * among[bf16][kind] : alone[bf16][kind]) + ends;
 }
+static size_t workspace_of(const Plan &p, int n_tokens, int R) { return p.ranges > 1 ? (size_t)p.ranges * n_tokens * (((size_t)R + 15) / 16 * 16) * 4 : 0; }
 static Plan plan_of(int n_tokens, int R, int K, bool bf16) {
     const int blocks = (K + 127) / 128;
     Plan best{8, 4, 1, 1, blocks, 0};
     float least = n_tokens > 64 ? us_of(best, n_tokens, R, K, bf16) : INFINITY;
     const auto look = [&](const Plan &p) {
-        if (p.ranges > 1 && (long)n_tokens * R * p.ranges > 1 << 26) return;          // 256 MB of sums
+        if (p.ranges > 1 && workspace_of(p, n_tokens, R) > (size_t)1 << 28) return;
         const float us = us_of(p, n_tokens, R, K, bf16);
         if (us < least) {
             best = p;
@@ -244,8 +245,6 @@ static Plan plan_of(int n_tokens, int R, int K, bool bf16) {
     }
     return best;
 }
-
-static size_t workspace_of(const Plan &p, int n_tokens, int R) { return p.ranges > 1 ? (size_t)p.ranges * n_tokens * (((size_t)R + 15) / 16 * 16) * 4 : 0; }
 
 size_t linear_workspace(int n_tokens, int R, int K, int x_type) { return workspace_of(plan_of(n_tokens, R, K, x_type == DENSE_BF16), n_tokens, R); }
 

@@ -138,7 +138,7 @@ def test_workspaces_hold_whole_ranges_and_stay_small():
         for x in (BF, F8):
             nb = L.dense_linear_workspace_bytes(n, R, 32 * K, x, BF)
             one = n * (-(-R // 16) * 16) * 4
-            assert nb % one == 0 and nb // one != 1 and nb // one <= -(-32 * K // 128) and nb <= (1 << 28) * -(-R // 16) * 16 / R
+            assert nb % one == 0 and nb // one != 1 and nb // one <= -(-32 * K // 128) and nb <= 1 << 28
             assert nb == L.dense_linear_workspace_bytes(n, R, 32 * K, x, F32)
             some += nb > 0
     assert some > 1000
@@ -250,3 +250,13 @@ def test_matrices_of_odd_sources_are_refused():
         with pytest.raises(q.MoeError) as e:
             q.DenseMatrix4(codes, scales)
         assert e.value.code == q.MOE_E_ARG
+
+
+def test_two_workgroups_of_many_tokens_share_a_cu(tmp_path):
+    """256 threads are a wave on each SIMD of 512 registers: two workgroups need at most 256 registers and 80 KB of LDS."""
+    from test_kernel_resources import usage
+    many = {n: u for n, u in usage("dense_linear_many.hip", tmp_path).items() if "linear_manyILi0E" in n or "linear_manyILi1E" in n}
+    some = {n: u for n, u in usage("dense_linear_some.hip", tmp_path).items() if not n.split("linear_some")[1].startswith(tuple(f"ILi{x}ELi4ELi4ELi1ELi2E" for x in range(3)))}
+    assert len(many) == 2 and len(some) == 15
+    for name, (regs, lds) in {**many, **some}.items():
+        assert regs <= 256 and lds <= 80 * 1024, (name, regs, lds)

@@ -229,3 +229,24 @@ def test_two_contexts_on_two_streams():
     for a, b in zip(want, got):
         for c in b:
             assert torch.equal(a[0], c[0]) and torch.equal(a[1], c[1])
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("N,E,groups,take,best", [(20, 256, 8, 4, 2), (20, 48, 1, 1, 1), (5000, 160, 8, 3, 4)])
+def test_rows_that_are_not_finite(score, N, E, groups, take, best):
+    """Their experts are k different ones all the same, and other rows have what they have without them."""
+    x, Wg, lb, cb = inputs(50, N, 256, E)
+    ctx, w, keep = context(N, 256, E, 8, Wg, torch.bfloat16)
+    rule = q.MoeScoring(score, lb, cb, groups, take, best, True, 1.0)
+    ctx.route_scored(x, w, rule)
+    idx, wt = ctx.get("topk_idx").clone(), ctx.get("topk_w").clone()
+    for row, value in ((3, math.nan), (7, math.inf), (N - 1, -math.inf)):
+        x[row, 5] = value
+    ctx.route_scored(x, w, rule)
+    got = ctx.get("topk_idx")
+    assert ((got >= 0) & (got < E)).all() and (got.sort(1)[0].diff(dim=1) > 0).all()
+    rest = torch.ones(N, dtype=torch.bool, device=DEV)
+    rest[[3, 7, N - 1]] = False
+    assert torch.equal(got[rest], idx[rest]) and torch.equal(ctx.get("topk_w")[rest], wt[rest])
+    cursor = ctx.permute(torch.zeros(N, dtype=torch.uint8, device=DEV))
+    assert cursor.n_units > 0 and int(ctx.get("counts").sum()) == 8 * N
