@@ -195,25 +195,26 @@ static Plan some_of(int K, bool bf16, int tiles, int rows, int ks, int ranges) {
 }
 // Each variant where it is best, us, x in bf16, with its best number of ranges: 1 token by 6144 x 4096 linear_few 5.9, linear_some with waves that share rows 12, with tiles
 // of 2x1 (16 tokens by 16 rows of a wave) 8.9; 64 by 1024 x 1024 shared rows 4.4, 2x1 5.2, 2x2 6.2; 64 by 6144 x 4096 2x1 12.8, 2x2 13.6, 4x2 14.3, 4x4 17.5, linear_many 42; 256
-// 23.6, 21.2, 20.0, 24.2, 45; 1024 80, 62, 53, 56, 56; 4096 323, 240, 184, 168, 149.  Ranges: 61 by 4096 x 14336 in tiles of 4x2 with 8 of them 16.5, with 2 33.
+// 23.6, 21.2, 20.0 (18.1 by twice the waves), 24.2, 45; 1024 80, 62, 53, 56, 56; 4096 323, 240, 184, 168, 149.  Ranges: 61 by 4096 x 14336 in tiles of 4x2 with 8 of them 16.5, with 2 33.
 // Us that a plan takes, fitted to what was measured (420 shapes of 64 to 16384 columns, 16 to 32000 rows, 1 to 8192 tokens, both types of x, every plan): a launch and the
 // first bytes; for every block of 128 columns of the workgroups that a CU has what one takes alone, or among others; linear_few what a CU takes in; ranges a launch and
-// their sums' way to memory and back; outputs their way to memory.  On 200 shapes drawn anew its choice takes 2.2 % more than the best plan of a shape in the mean, 32 % at most.
+// their sums' way to memory and back; outputs their way to memory.  On 200 shapes drawn anew its choice takes 2.6 % more than the best plan of a shape in the mean, 44 % once.
 static float us_of(const Plan &p, int n_tokens, int R, int K, bool bf16) {
     const int row_tiles = (R + 15) / 16, token_tiles = (n_tokens + p.tiles * 16 - 1) / (p.tiles * 16);
-    const float sums = (float)n_tokens * R, ends = (p.ranges == 1 ? 0.f : 2.56f + sums * p.ranges * 1.86e-6f) + sums * .89e-6f;
+    const float sums = (float)n_tokens * R, ends = (p.ranges == 1 ? 0.f : 2.57f + sums * p.ranges * 1.93e-6f) + sums * 1.07e-6f;
     if (p.tiles == 1) {
         const int per = kWaves / p.ks;
         const long wgs = (long)((row_tiles + per - 1) / per) * token_tiles * p.ranges, on_cu = (wgs + 255) / 256;
         const float x = (float)std::min(n_tokens, kFewTokens) * (bf16 ? 256.f : 132.f) * p.range_blocks, w = (float)per * p.range_blocks * 1088.f;
         return 3.6f + (float)on_cu * (x + w) / 47.8e3f + ends;
     }
-    const int per = p.tiles == 8 ? 16 : 4 * p.rows / p.ks;
+    const int per = p.tiles == 8 ? 16 : p.ks == 4 ? p.rows : 4 * p.rows;
     const long wgs = (long)((row_tiles + per - 1) / per) * token_tiles * p.ranges, on_cu = (wgs + 255) / 256;
-    if (p.ks > 1) return 3.f + (float)on_cu * ((p.range_blocks + p.ks - 1) / p.ks) * .517f + ends;
+    if (p.ks == 4) return 3.f + (float)on_cu * ((p.range_blocks + 3) / 4) * .519f + ends;
+    if (p.ks == 2) return 3.f + (float)on_cu * ((p.range_blocks + 1) / 2) * (bf16 ? .971f : .877f) + ends;
     // [x in bf16][tokens by rows of a wave: 2x1, 2x2, 4x2, 4x4 tiles, linear_many]
-    static const float alone[2][5] = {{.289f, .323f, .496f, .613f, 1.15f}, {.238f, .378f, .501f, .802f, 1.35f}},
-                       among[2][5] = {{.162f, .265f, .403f, .486f, .728f}, {.182f, .287f, .404f, .676f, 1.18f}};
+    static const float alone[2][5] = {{.287f, .289f, .585f, .653f, 1.13f}, {.237f, .377f, .516f, .801f, 1.24f}},
+                       among[2][5] = {{.150f, .236f, .327f, .438f, .656f}, {.164f, .279f, .413f, .691f, 1.16f}};
     const int kind = p.tiles == 8 ? 4 : p.tiles == 2 ? p.rows - 1 : p.rows == 2 ? 2 : 3;
     return 3.f + (float)p.range_blocks * (on_cu > 1 ? (float)on_cu * among[bf16][kind] : alone[bf16][kind]) + ends;
 }
@@ -240,6 +241,7 @@ static Plan plan_of(int n_tokens, int R, int K, bool bf16) {
         }
         if (n_tokens > 32) {
             look(some_of(K, bf16, 4, 2, 1, z));
+            look(some_of(K, bf16, 4, 2, 2, z));
             look(some_of(K, bf16, 4, 4, 1, z));
         }
     }

@@ -13,7 +13,7 @@
 namespace qdense {
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int waves_of(int ks) { return ks == 2 ? 8 : 4; }
 
 template <int N>
 __device__ __forceinline__ void wait_but() {             // for all loads but the last N of this wave
@@ -27,15 +27,18 @@ __device__ __forceinline__ void wait_for(int later) {    // for all but the load
 }
 
 // KS 4: the workgroup has 16 * RB rows, and each wave every fourth block of the range, with tokens of its own and no barrier between blocks; the waves' sums meet in LDS.
+// KS 2: two times four waves, with every second block each: a wave alone on its SIMD issues an instruction every four or five clocks at best (256 tokens by 6144 x 4096 20.5 us, 18.1 so).
 template <int XT, int NT, int RB, int KS, int AHEAD>
-__global__ __launch_bounds__(64 * kWaves) void linear_some(const LinearArgs a, long first_wg, int range_blocks) {
+__global__ __launch_bounds__(64 * waves_of(KS)) void linear_some(const LinearArgs a, long first_wg, int range_blocks) {
+    constexpr int kWaves = waves_of(KS);
     constexpr int PIECES = XT == X_BF16 ? 16 : 8;        // of 16 bytes, in a token's 128 columns
     constexpr int TOK = NT * 16, X = TOK * PIECES * 16, SHARE = kWaves / KS, LOADS = X / 1024 / SHARE, WAVE = RB * 1280, SLOT = KS * X + kWaves * WAVE, SLOTS = AHEAD + 1;
     constexpr int COUNT = LOADS + RB + 1;                // a wave's loads for a block
-    static_assert(KS == 1 || KS == kWaves, "waves share tokens or have their own");
-    static_assert(LOADS >= 1 && SLOT % 256 == 0 && (KS == 1 || SLOTS * SLOT >= kWaves * RB * NT * 1024), "room for a wave's load, and for the sums");
+    constexpr bool TOGETHER = SHARE > 1;                 // waves that share tokens
+    static_assert(LOADS >= 1 && SLOT % 256 == 0, "whole loads");
+    constexpr int SUMS = KS == 1 ? 0 : kWaves * RB * NT * 1024;
     static_assert(COUNT * AHEAD < 64, "the counter of loads under way has six bits");
-    __shared__ __align__(16) char lds[SLOTS * SLOT];
+    __shared__ __align__(16) char lds[SLOTS * SLOT > SUMS ? SLOTS * SLOT : SUMS];
     __shared__ uint32_t xb[XT == X_BF16 ? 1 : kSomeBlocks][XT == X_BF16 ? 1 : TOK];
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, g = l >> 4, t16 = l & 15;
     const int blocks = (a.K + 127) / 128, sets = (a.K + 511) / 512, row_tiles = (a.R + 15) / 16, row_wgs = (row_tiles + RB * SHARE - 1) / (RB * SHARE);
@@ -48,12 +51,12 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(const LinearArgs a, l
     for (int r = 0; r < RB; ++r) codes[r] = a.codes + ((long)min(rt + r, row_tiles - 1) * blocks + from) * 1024;
     const uint8_t *const scales = a.scales + (long)min(rt, row_tiles - 1) * sets * 256;
     const uint32_t scale_at = (uint32_t)(min(rt + (l >> 4) % RB, row_tiles - 1) - min(rt, row_tiles - 1)) * (sets * 256) + t16 * 16;         // RB tiles' 256 bytes, 16 lanes each
-    constexpr int ORDERS = KS == 1 ? 1 : LOADS;          // tokens whose places in 16 are the same have their pieces in the same order
+    constexpr int ORDERS = TOGETHER ? 1 : LOADS;          // tokens whose places in 16 are the same have their pieces in the same order
     const char *src[LOADS];
     int first_piece[ORDERS];
     {
         constexpr int PER = 64 / PIECES;                 // tokens of a wave's load
-        static_assert(KS > 1 || SHARE * PER % 16 == 0, "one order");
+        static_assert(!TOGETHER || SHARE * PER % 16 == 0, "one order");
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
             const int t = (ws + SHARE * j) * PER + l / PIECES, p = l % PIECES, q = XT == X_BF16 ? p ^ (t & 15) : p ^ (t >> 1 & 7);
@@ -91,16 +94,16 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(const LinearArgs a, l
     for (int r = 0; r < RB; ++r)
 #pragma unroll
         for (int m = 0; m < NT; ++m) acc[r][m] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int mine_n = (n - wk + KS - 1) / KS;           // this wave's blocks: wk, wk + KS, ...
+    const int mine_n = (n - wk + KS - 1) / KS, rounds = TOGETHER ? (n + KS - 1) / KS : mine_n;        // this wave's blocks: wk, wk + KS, ...; waves that share tokens go on together
     for (int i = 0; i < min(AHEAD, mine_n); ++i)
 #pragma unroll
         for (int k = 0; k < COUNT; ++k) ask(k, wk + i * KS, i);
-    if constexpr (KS > 1 && XT != X_BF16) __syncthreads();
+    if constexpr (!TOGETHER && XT != X_BF16) __syncthreads();
     int slot = 0, next = AHEAD;
     const auto block = [&](int i, auto more) {
         const int b = wk + i * KS;
         wait_for<COUNT, AHEAD - 1>(mine_n - 1 - i);      // this wave's pieces of block b are in LDS
-        if constexpr (KS == 1) __syncthreads();          // everybody's; and the block before, in whose place the next one comes, has been read
+        if constexpr (TOGETHER) __syncthreads();         // everybody's; and the block before, in whose place the next one comes, has been read
         else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if constexpr (AHEAD == 1) {
             if (i + 1 < mine_n) {
@@ -108,6 +111,7 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(const LinearArgs a, l
                 for (int k = 0; k < COUNT; ++k) ask(k, b + KS, next);
             }
         }
+        if (KS == 2 && i >= mine_n) return;              // the last round of an odd number of blocks
         const char *x = lds + slot * SLOT + wk * X, *wt = lds + slot * SLOT + KS * X + w * WAVE;
         u32x4 c[RB];
         uint32_t sc[RB];
@@ -127,10 +131,10 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(const LinearArgs a, l
         next = next + 1 == SLOTS ? 0 : next + 1;
     };
     if constexpr (AHEAD == 1) {
-        for (int i = 0; i < mine_n; ++i) block(i, std::false_type{});
+        for (int i = 0; i < rounds; ++i) block(i, std::false_type{});
     } else {
         for (int i = 0; i < mine_n - AHEAD; ++i) block(i, std::true_type{});
-        for (int i = max(0, mine_n - AHEAD); i < mine_n; ++i) block(i, std::false_type{});
+        for (int i = max(0, mine_n - AHEAD); i < rounds; ++i) block(i, std::false_type{});
     }
     if constexpr (KS > 1) {
         f32x4 *red = reinterpret_cast<f32x4 *>(lds);
@@ -140,11 +144,11 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(const LinearArgs a, l
 #pragma unroll
             for (int m = 0; m < NT; ++m) red[(w * (RB * NT) + r * NT + m) * 64 + l] = acc[r][m];
         __syncthreads();
-        for (int i = w; i < RB * NT; i += kWaves) {      // a tile's sums in the order of the waves
-            f32x4 v = red[i * 64 + l];
+        for (int i = wk; i < RB * NT; i += KS) {         // a tile's sums in the order of the waves
+            f32x4 v = red[(ws * KS * (RB * NT) + i) * 64 + l];
 #pragma unroll
             for (int k = 1; k < KS; ++k) {
-                const f32x4 o = red[(k * (RB * NT) + i) * 64 + l];
+                const f32x4 o = red[((ws * KS + k) * (RB * NT) + i) * 64 + l];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] += o[e];
             }
@@ -175,22 +179,23 @@ __global__ __launch_bounds__(64 * kWaves) void linear_some(const LinearArgs a, l
 hipError_t launch_linear_some(const LinearArgs &a, int tiles, int rows, int ks, int range_blocks, hipStream_t s) {
     const auto go = [&](auto xt, auto nt, auto rb, auto ks) {
         constexpr int XT = decltype(xt)::value, NT = decltype(nt)::value, RB = decltype(rb)::value, KS = decltype(ks)::value;
-        constexpr int PER = RB * kWaves / KS;
+        constexpr int kWaves = waves_of(KS), PER = RB * kWaves / KS;
         const long row_wgs = ((a.R + 15) / 16 + PER - 1) / PER, all = row_wgs * a.ranges * ((a.n_tokens + NT * 16 - 1) / (NT * 16));
-        constexpr long kMost = 1 << 23;                  // workgroups of 256 threads that a launch may have
+        constexpr long kMost = 1 << 22;                  // workgroups of 512 threads that a launch may have
         const auto run = [&](auto ahead) {
             for (long at = 0; at < all; at += kMost)
                 linear_some<XT, NT, RB, KS, decltype(ahead)::value><<<dim3((unsigned)(all - at < kMost ? all - at : kMost)), dim3(64 * kWaves), 0, s>>>(a, at, range_blocks);
         };
         // Where a CU has one workgroup, LDS has room for two blocks ahead (512 tokens by 6144 x 4096 33.5 us, 30.9 so; for two workgroups one block ahead is better: 8192 by 4096 x 4096 222).
         if constexpr (NT * RB == 16) all <= 256 ? run(std::integral_constant<int, 2>{}) : run(std::integral_constant<int, 1>{});
-        else run(std::integral_constant<int, (KS > 1 && XT == X_BF16) ? 1 : 2>{});
+        else run(std::integral_constant<int, (KS == 4 && XT == X_BF16) ? 1 : 2>{});
     };
     const auto by_size = [&](auto xt) {
         typedef std::integral_constant<int, 1> One;
         typedef std::integral_constant<int, 2> Two;
         typedef std::integral_constant<int, 4> Four;
-        if (ks > 1) go(xt, Two{}, One{}, Four{});
+        if (ks == 2) go(xt, Four{}, Two{}, Two{});
+        else if (ks > 1) go(xt, Two{}, One{}, Four{});
         else if (tiles == 2) rows == 1 ? go(xt, Two{}, One{}, One{}) : go(xt, Two{}, Two{}, One{});
         else rows == 2 ? go(xt, Four{}, Two{}, One{}) : go(xt, Four{}, Four{}, One{});
     };
