@@ -13,7 +13,6 @@
 namespace qdense {
 namespace {
 
-constexpr int waves_of(int ks) { return ks == 2 ? 8 : 4; }
 
 template <int N>
 __device__ __forceinline__ void wait_but() {             // for all loads but the last N of this wave
@@ -26,13 +25,14 @@ __device__ __forceinline__ void wait_for(int later) {    // for all but the load
     else wait_for<C, R - 1>(later);
 }
 
-// KS 4: the workgroup has 16 * RB rows, and each wave every fourth block of the range, with tokens of its own and no barrier between blocks; the waves' sums meet in LDS.
-// KS 2: two times four waves, with every second block each: a wave alone on its SIMD issues an instruction every four or five clocks at best (256 tokens by 6144 x 4096 20.5 us, 18.1 so).
-template <int XT, int NT, int RB, int KS, int AHEAD>
-__global__ __launch_bounds__(64 * waves_of(KS)) void linear_some(const LinearArgs a, long first_wg, int range_blocks) {
-    constexpr int kWaves = waves_of(KS);
+// SHARE waves have rows of their own and the tokens in common; KS times as many share the rows, each with every KS-th block of the range, and their sums meet in LDS.  SHARE 4, KS 2: a wave
+// alone on its SIMD issues an instruction every four or five clocks at best (64 tokens by 6144 x 4096 in tiles of 2x1 12.9 us with KS 1, 10.0 with 2, 9.6 with 4; 256 in tiles of 4x2
+// 20.5 and 18.1).  SHARE 1, KS 4: small matrices; each wave has tokens of its own, and no barrier stands between blocks.
+template <int XT, int NT, int RB, int KS, int SHARE, int AHEAD>
+__global__ __launch_bounds__(64 * KS * SHARE) void linear_some(const LinearArgs a, long first_wg, int range_blocks) {
+    constexpr int kWaves = KS * SHARE;
     constexpr int PIECES = XT == X_BF16 ? 16 : 8;        // of 16 bytes, in a token's 128 columns
-    constexpr int TOK = NT * 16, X = TOK * PIECES * 16, SHARE = kWaves / KS, LOADS = X / 1024 / SHARE, WAVE = RB * 1280, SLOT = KS * X + kWaves * WAVE, SLOTS = AHEAD + 1;
+    constexpr int TOK = NT * 16, X = TOK * PIECES * 16, LOADS = X / 1024 / SHARE, WAVE = RB * 1280, SLOT = KS * X + kWaves * WAVE, SLOTS = AHEAD + 1;
     constexpr int COUNT = LOADS + RB + 1;                // a wave's loads for a block
     constexpr bool TOGETHER = SHARE > 1;                 // waves that share tokens
     static_assert(LOADS >= 1 && SLOT % 256 == 0, "whole loads");
@@ -111,7 +111,7 @@ __global__ __launch_bounds__(64 * waves_of(KS)) void linear_some(const LinearArg
                 for (int k = 0; k < COUNT; ++k) ask(k, b + KS, next);
             }
         }
-        if (KS == 2 && i >= mine_n) return;              // the last round of an odd number of blocks
+        if (KS > 1 && TOGETHER && i >= mine_n) return;              // the last round of an odd number of blocks
         const char *x = lds + slot * SLOT + wk * X, *wt = lds + slot * SLOT + KS * X + w * WAVE;
         u32x4 c[RB];
         uint32_t sc[RB];
@@ -176,28 +176,29 @@ __global__ __launch_bounds__(64 * waves_of(KS)) void linear_some(const LinearArg
 
 }  // namespace
 
-hipError_t launch_linear_some(const LinearArgs &a, int tiles, int rows, int ks, int range_blocks, hipStream_t s) {
-    const auto go = [&](auto xt, auto nt, auto rb, auto ks) {
-        constexpr int XT = decltype(xt)::value, NT = decltype(nt)::value, RB = decltype(rb)::value, KS = decltype(ks)::value;
-        constexpr int kWaves = waves_of(KS), PER = RB * kWaves / KS;
+hipError_t launch_linear_some(const LinearArgs &a, int tiles, int rows, int ks, int share, int range_blocks, hipStream_t s) {
+    const auto go = [&](auto xt, auto nt, auto rb, auto ks, auto share) {
+        constexpr int XT = decltype(xt)::value, NT = decltype(nt)::value, RB = decltype(rb)::value, KS = decltype(ks)::value, SHARE = decltype(share)::value;
+        constexpr int kWaves = KS * SHARE, PER = RB * SHARE;
         const long row_wgs = ((a.R + 15) / 16 + PER - 1) / PER, all = row_wgs * a.ranges * ((a.n_tokens + NT * 16 - 1) / (NT * 16));
         constexpr long kMost = 1 << 22;                  // workgroups of 512 threads that a launch may have
         const auto run = [&](auto ahead) {
             for (long at = 0; at < all; at += kMost)
-                linear_some<XT, NT, RB, KS, decltype(ahead)::value><<<dim3((unsigned)(all - at < kMost ? all - at : kMost)), dim3(64 * kWaves), 0, s>>>(a, at, range_blocks);
+                linear_some<XT, NT, RB, KS, SHARE, decltype(ahead)::value><<<dim3((unsigned)(all - at < kMost ? all - at : kMost)), dim3(64 * kWaves), 0, s>>>(a, at, range_blocks);
         };
         // Where a CU has one workgroup, LDS has room for two blocks ahead (512 tokens by 6144 x 4096 33.5 us, 30.9 so; for two workgroups one block ahead is better: 8192 by 4096 x 4096 222).
         if constexpr (NT * RB == 16) all <= 256 ? run(std::integral_constant<int, 2>{}) : run(std::integral_constant<int, 1>{});
-        else run(std::integral_constant<int, (KS == 4 && XT == X_BF16) ? 1 : 2>{});
+        else run(std::integral_constant<int, SHARE == 1 && XT == X_BF16 ? 1 : 2>{});
     };
     const auto by_size = [&](auto xt) {
         typedef std::integral_constant<int, 1> One;
         typedef std::integral_constant<int, 2> Two;
         typedef std::integral_constant<int, 4> Four;
-        if (ks == 2) go(xt, Four{}, Two{}, Two{});
-        else if (ks > 1) go(xt, Two{}, One{}, Four{});
-        else if (tiles == 2) rows == 1 ? go(xt, Two{}, One{}, One{}) : go(xt, Two{}, Two{}, One{});
-        else rows == 2 ? go(xt, Four{}, Two{}, One{}) : go(xt, Four{}, Four{}, One{});
+        if (share == 1) go(xt, Two{}, One{}, Four{}, One{});
+        else if (tiles == 2 && rows == 1) ks == 1 ? go(xt, Two{}, One{}, One{}, Four{}) : go(xt, Two{}, One{}, Two{}, Four{});
+        else if (tiles == 2) go(xt, Two{}, Two{}, Two{}, Four{});
+        else if (rows == 2) ks == 1 ? go(xt, Four{}, Two{}, One{}, Four{}) : go(xt, Four{}, Two{}, Two{}, Four{});
+        else go(xt, Four{}, Four{}, One{}, Four{});
     };
     if (a.x_type == DENSE_BF16) by_size(std::integral_constant<int, X_BF16>{});
     else if (a.out_type == DENSE_BF16) by_size(std::integral_constant<int, X_FP8>{});
