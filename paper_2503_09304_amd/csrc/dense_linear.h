@@ -72,7 +72,7 @@ template <int XT, int RB, int NT, class Between>
 __device__ __forceinline__ void products(f32x4 (&acc)[RB][NT], const u32x4 (&c)[RB], const uint32_t (&sc)[RB], const char *x, const uint32_t *xb, int g, int t16,
                                          const Between &between) {
     if constexpr (XT == X_FP8) {
-        constexpr int AHEAD = 2;
+        constexpr int AHEAD = NT < 2 ? NT : 2;
         u32x4 lo[NT], hi[NT];
         uint32_t byte[NT];
         const int at = t16 * 128, sw = t16 >> 1;

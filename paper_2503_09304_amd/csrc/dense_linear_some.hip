@@ -1,9 +1,9 @@
-// dense_linear for some tens of tokens: bound by the matrix, with more tokens than a wave's registers or LDS hold at once.
+// dense_linear for some tokens to some thousand: bound by the matrix, then by a wave's instructions and its products.
 //
-// A workgroup has 64 * RB rows, NT * 16 tokens and a range of columns; it goes through them in blocks of 128.  Weights, their scales and the tokens of a block all
+// A workgroup has 16 * SHARE * RB rows, NT * 16 tokens and a range of columns; it goes through them in blocks of 128.  Weights, their scales and the tokens of a block all
 // come to LDS past the registers, AHEAD blocks before their use: what is under way hides the latency of memory, which registers could not hold (64 tokens by 6144 x 4096
 // 18.9 us with weights straight into registers, 13.6 so; more than two blocks ahead change nothing).  They are asked for between a block's products: all at once they keep a wave
-// from its first product (256 by 6144 x 4096 24.5 us, 20.5 so).  61 tokens by 4096 x 14336 11.8 us and its ranges' sums; 256 by 6144 x 4096 20 us, 0.65 PFLOP/s.
+// from its first product (256 by 6144 x 4096 24.5 us, 20.5 so).  61 tokens by 4096 x 14336 11.3 us and its ranges' sums; 256 by 6144 x 4096 17 us, 0.75 PFLOP/s.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -32,10 +32,10 @@ template <int XT, int NT, int RB, int KS, int SHARE, int AHEAD>
 __global__ __launch_bounds__(64 * KS * SHARE) void linear_some(const LinearArgs a, long first_wg, int range_blocks) {
     constexpr int kWaves = KS * SHARE;
     constexpr int PIECES = XT == X_BF16 ? 16 : 8;        // of 16 bytes, in a token's 128 columns
-    constexpr int TOK = NT * 16, X = TOK * PIECES * 16, LOADS = X / 1024 / SHARE, WAVE = RB * 1280, SLOT = KS * X + kWaves * WAVE, SLOTS = AHEAD + 1;
-    constexpr int COUNT = LOADS + RB + 1;                // a wave's loads for a block
+    constexpr int TOK = NT * 16, X = TOK * PIECES * 16, PLACES = X / 1024, LOADS = PLACES < SHARE ? 1 : PLACES / SHARE, WAVE = RB * 1280, SLOT = KS * X + kWaves * WAVE, SLOTS = AHEAD + 1;
+    constexpr int COUNT = LOADS + RB + 1;                // a wave's loads for a block (16 tokens in 8 bits: two waves bring the same)
     constexpr bool TOGETHER = SHARE > 1;                 // waves that share tokens
-    static_assert(LOADS >= 1 && SLOT % 256 == 0, "whole loads");
+    static_assert(PLACES % SHARE % 2 == 0 && SLOT % 256 == 0, "whole loads");
     constexpr int SUMS = KS == 1 ? 0 : kWaves * RB * NT * 1024;
     static_assert(COUNT * AHEAD < 64, "the counter of loads under way has six bits");
     __shared__ __align__(16) char lds[SLOTS * SLOT > SUMS ? SLOTS * SLOT : SUMS];
@@ -59,14 +59,14 @@ __global__ __launch_bounds__(64 * KS * SHARE) void linear_some(const LinearArgs 
         static_assert(!TOGETHER || SHARE * PER % 16 == 0, "one order");
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
-            const int t = (ws + SHARE * j) * PER + l / PIECES, p = l % PIECES, q = XT == X_BF16 ? p ^ (t & 15) : p ^ (t >> 1 & 7);
+            const int t = (ws + SHARE * j) % PLACES * PER + l / PIECES, p = l % PIECES, q = XT == X_BF16 ? p ^ (t & 15) : p ^ (t >> 1 & 7);
             src[j] = a.x.p + (long)min(t0 + t, a.n_tokens - 1) * a.x.ts * (XT == X_BF16 ? 2 : 1);
             if (j < ORDERS) first_piece[j] = XT == X_BF16 ? 4 * (q & 3) + (q >> 2) : XT == X_FP8 ? q : 2 * (q & 3) + (q >> 2);
         }
     }
     const int k_bytes = a.K * (XT == X_BF16 ? 2 : 1);
     const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds, mine = __builtin_amdgcn_readfirstlane(base + KS * X + w * WAVE),
-                   piece0 = __builtin_amdgcn_readfirstlane(base + wk * X + ws * 1024);
+                   piece0 = __builtin_amdgcn_readfirstlane(base + wk * X + ws % PLACES * 1024);
     const auto ask = [&](int i, int b, int slot) {       // the i-th part of what block b needs
         const uint32_t to = slot * SLOT;
         if (i < RB) {
@@ -181,7 +181,7 @@ hipError_t launch_linear_some(const LinearArgs &a, int tiles, int rows, int ks, 
         constexpr int XT = decltype(xt)::value, NT = decltype(nt)::value, RB = decltype(rb)::value, KS = decltype(ks)::value, SHARE = decltype(share)::value;
         constexpr int kWaves = KS * SHARE, PER = RB * SHARE;
         const long row_wgs = ((a.R + 15) / 16 + PER - 1) / PER, all = row_wgs * a.ranges * ((a.n_tokens + NT * 16 - 1) / (NT * 16));
-        constexpr long kMost = 1 << 22;                  // workgroups of 512 threads that a launch may have
+        constexpr long kMost = 1 << 21;                  // workgroups of 1024 threads that a launch may have
         const auto run = [&](auto ahead) {
             for (long at = 0; at < all; at += kMost)
                 linear_some<XT, NT, RB, KS, SHARE, decltype(ahead)::value><<<dim3((unsigned)(all - at < kMost ? all - at : kMost)), dim3(64 * kWaves), 0, s>>>(a, at, range_blocks);
@@ -195,6 +195,7 @@ hipError_t launch_linear_some(const LinearArgs &a, int tiles, int rows, int ks, 
         typedef std::integral_constant<int, 2> Two;
         typedef std::integral_constant<int, 4> Four;
         if (share == 1) go(xt, Two{}, One{}, Four{}, One{});
+        else if (tiles == 1) ks == 2 ? go(xt, One{}, One{}, Two{}, Four{}) : go(xt, One{}, One{}, Four{}, Four{});
         else if (tiles == 2 && rows == 1) ks == 1 ? go(xt, Two{}, One{}, One{}, Four{}) : go(xt, Two{}, One{}, Two{}, Four{});
         else if (tiles == 2) go(xt, Two{}, Two{}, Two{}, Four{});
         else if (rows == 2) ks == 1 ? go(xt, Four{}, Two{}, One{}, Four{}) : go(xt, Four{}, Two{}, Two{}, Four{});
