@@ -122,9 +122,8 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few(const LinearArgs a, lo
 
 // The ranges' sums, added in their order: a launch, and a way to memory and back (61 tokens, 4096 rows, 8 ranges 4.7 us).
 __global__ __launch_bounds__(256) void join_ranges(const LinearArgs a) {
-    const int quads = (a.R + 15) / 16 * 4;
-    const long i = (long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= (long)a.n_tokens * quads) return;
+    const unsigned quads = (unsigned)(a.R + 15) / 16 * 4, i = blockIdx.x * 256 + threadIdx.x;       // 2^23 at most, as the workspace has 256 MB
+    if (i >= a.n_tokens * quads) return;
     const int t = (int)(i / quads), r = (int)(i % quads) * 4;
     if (r >= a.R) return;
     const long plane = (long)a.n_tokens * quads * 4;
