@@ -3,6 +3,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include "lds_loads.h"
 #include "qdense_internal.h"
 
 namespace qdense {
@@ -41,28 +42,6 @@ __device__ __forceinline__ bf16x8 widened8(uint32_t lo, uint32_t hi, float scale
     return __builtin_bit_cast(bf16x8, r);
 }
 __device__ __forceinline__ float power(uint32_t byte) { return __uint_as_float(byte << 23); }
-
-// 16 bytes a lane from memory to LDS, lane l's at `to` + 16 l.  In assembly: the compiler would wait for it in front of every read of LDS that it cannot tell
-// apart.  Nothing is returned; the caller waits (vmcnt) before the barrier behind which the bytes are read.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"          // that m0 is reserved: nothing else here uses it
-__device__ __forceinline__ void to_lds_at(const char *from, uint32_t at) {        // at: of the wave's, in LDS
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(at) : "m0", "memory");
-}
-// The same from one place of the wave's, `off` bytes behind it, by the first LANES lanes (where all 64 are at work).
-template <int LANES>
-__device__ __forceinline__ void to_lds_off(const uint8_t *from, uint32_t off, uint32_t at) {
-    static_assert(LANES == 16 || LANES == 32 || LANES == 64, "whole halves of the wave, or a quarter");
-    if constexpr (LANES == 64) asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(from), "s"(at) : "m0", "memory");
-    else if constexpr (LANES == 32)
-        asm volatile("s_mov_b32 m0, %2\n\ts_mov_b32 exec_hi, 0\n\tglobal_load_lds_dwordx4 %0, %1\n\ts_mov_b32 exec_hi, -1" ::"v"(off), "s"(from), "s"(at) : "m0", "memory");
-    else
-        asm volatile("s_mov_b32 m0, %2\n\ts_mov_b64 exec, 0xffff\n\tglobal_load_lds_dwordx4 %0, %1\n\ts_mov_b64 exec, -1" ::"v"(off), "s"(from), "s"(at) : "m0", "memory");
-}
-#pragma clang diagnostic pop
-__device__ __forceinline__ void to_lds(const char *from, const char *to) {
-    to_lds_at(from, __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)to));
-}
 
 // Products of a block of 128 columns: a wave's RB * 16 rows (codes c, scale bytes sc) by NT * 16 tokens, which stand in LDS (x; their scale bytes xb, four a token): pieces of 16
 // bytes, a token's in an order by its place in 16, so that the lanes of one read use all banks.  The tokens' operands are asked for AHEAD products of RB before theirs, and weights

@@ -9,6 +9,7 @@
 #include <climits>
 #include <type_traits>
 
+#include "lds_loads.h"
 #include "qmoe_internal.h"
 
 namespace qmoe {
@@ -19,15 +20,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // ---- gate GEMM ----
-
-// 16 bytes a lane from memory to LDS, lane l's at `to` + 16 l; the caller waits (vmcnt) before the barrier behind which they are read.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"          // that m0 is reserved: nothing else here uses it
-__device__ __forceinline__ void to_lds(const char *from, const char *to) {
-    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)to);
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(at) : "m0", "memory");
-}
-#pragma clang diagnostic pop
 
 constexpr int kMostRanges = 16, kMostWaves = 16;
 constexpr int EB = 2;                 // experts a lane (4, in half as many waves: nothing won)
