@@ -212,9 +212,10 @@ __device__ __forceinline__ double largest_first(double &a, double b) {       // 
 // A wave has a token, lane l experts l, l + 64, ..., NS in all.  SPLIT: NS waves have a token, 64 experts each up to the scores, and one of them chooses: fewer
 // instructions one after the other where tokens leave the chip idle (61 tokens on 256 experts 6.4 us instead of 10.4).  BEST: values that a group's worth is the sum
 // of (0: all groups count).  Bound by instructions: the exponentials and divisions of 64 bits, and for each expert chosen a search over the wave whose steps wait for
-// each other (8192 tokens on 160 experts 14.5 us, 8 of 160 in 8 groups).
+// each other (8192 tokens on 160 experts 14.5 us, 8 of 160 in 8 groups).  A single plane of sums is the logits' own array, read and written in place: a wave reads what it
+// writes itself and nothing else, lanes behind the last expert its first (another wave may be writing the last one).
 template <int NS, int BEST, bool SPLIT>
-__global__ __launch_bounds__(64 * (SPLIT ? NS : kTokens)) void score_topk(const float *__restrict__ part, int planes, float *__restrict__ logits, const Rule rule,
+__global__ __launch_bounds__(64 * (SPLIT ? NS : kTokens)) void score_topk(const float *part, int planes, float *logits, const Rule rule,
                                                                           int32_t *__restrict__ topk_idx, float *__restrict__ topk_w, int N, int E, int k) {
     constexpr int ROWS = SPLIT ? 1 : kTokens, M = SPLIT ? 1 : NS;        // M: slots of this wave
     __shared__ double value[BEST || SPLIT ? ROWS : 1][BEST || SPLIT ? NS * 64 : 1], score[ROWS][NS * 64];
@@ -233,7 +234,7 @@ __global__ __launch_bounds__(64 * (SPLIT ? NS : kTokens)) void score_topk(const 
         for (int z = 0; z < kMostRanges; ++z)
             if (z < planes)
 #pragma unroll
-                for (int c = 0; c < M; ++c) q[c][z] = p[(long)z * N * E + min(l + 64 * (c + c0), E - 1)];
+                for (int c = 0; c < M; ++c) q[c][z] = p[(long)z * N * E + (l + 64 * (c + c0) < E ? l + 64 * (c + c0) : 64 * (c + c0))];
 #pragma unroll
         for (int c = 0; c < M; ++c) {
             const int e = l + 64 * (c + c0);
