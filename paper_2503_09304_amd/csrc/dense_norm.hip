@@ -120,10 +120,15 @@ __global__ __launch_bounds__(TPR > 64 ? TPR : kThreads) void norm_rows(const Nor
         for (int c = 0; c < CH; ++c)
             if ((c * TPR + lane) * 8 < a.dim) weights(g[c], (c * TPR + lane) * 8);
     }
-    float sum = 0.f;
+    // <128, 4> and <512, 1> have rows of the same sizes, by how many there are: a row has the same sums in both, added in the same order, of each piece's lanes by waves.
+    constexpr int SUMS = TPR == 128 && CH == 4 ? CH : 1;
+    float sums[SUMS];
+#pragma unroll
+    for (int c = 0; c < SUMS; ++c) sums[c] = 0.f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int e = (c * TPR + lane) * 8;
+        float &sum = sums[c % SUMS];
         if (e < a.dim) {
             if constexpr (ADD != 0) {
                 float v[8];
@@ -139,14 +144,19 @@ __global__ __launch_bounds__(TPR > 64 ? TPR : kThreads) void norm_rows(const Nor
         }
     }
 #pragma unroll
-    for (int d = 1; d < (TPR < 64 ? TPR : 64); d <<= 1) sum += __shfl_xor(sum, d, 64);
+    for (int d = 1; d < (TPR < 64 ? TPR : 64); d <<= 1)
+#pragma unroll
+        for (int c = 0; c < SUMS; ++c) sums[c] += __shfl_xor(sums[c], d, 64);
+    float sum = sums[0];
     if constexpr (WAVES > 1) {
-        __shared__ float part[WAVES];
-        if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = sum;
+        __shared__ float part[SUMS * WAVES];
+        if (threadIdx.x % 64 == 0)
+#pragma unroll
+            for (int c = 0; c < SUMS; ++c) part[c * WAVES + threadIdx.x / 64] = sums[c];
         __syncthreads();
         sum = part[0];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) sum += part[w];
+        for (int w = 1; w < SUMS * WAVES; ++w) sum += part[w];
     }
     const float inv = rsqrtf(sum / (float)a.dim + a.eps);
 #pragma unroll
@@ -198,8 +208,9 @@ void run(const NormArgs &a, hipStream_t s) {
 // Up to 512 elements a row is within a wave: no barrier, and several rows a wave (8192 * 16 heads of 128: 24.9 us, 44 by a wave each).  Longer ones have the fewest lanes
 // that hold them a piece each: rows wait for nothing but their own loads, and their workgroups come and go side by side.  Us of rows of 1024 / 2048 / 4096 with a bf16
 // residual, 8192 of them: that many lanes 14.9 / 24.5 / 43.8, always 512 18.5 / 24.5 / 43.8, always a wave 13.5 / 24.0 / 50; 1024 of them: 3.4 / 4.7 / 7.7, 3.8 / 4.8 / 7.7,
-// 4.2 / 5.9 / 9.6.  Without a residual a lane's one load leaves much of the way unused: where rows are many, four pieces a lane (4096 rows of 4096 12.8 us instead of 15.6,
-// 4096 of 2816 9.9 instead of 13.1; 256 of 4096 4.0 instead of 3.2).
+// 4.2 / 5.9 / 9.6.  Without a residual a lane's one load leaves much of the way unused: where rows are many, four pieces a lane (4096 rows of 4096 12.7 us instead of 15.6,
+// 4096 of 2816 10.3 instead of 13.1; 256 of 4096 4.0 instead of 3.2), each piece's squares summed by themselves as <512, 1> has them, so that a row's bits do not go by
+// the number of rows (with one sum a lane 12.7 and 10.0).
 hipError_t launch_norm(const NormArgs &a, hipStream_t s) {
     const int pieces = (a.dim + 7) / 8;
     if (pieces <= 8) run<8, 1>(a, s);
