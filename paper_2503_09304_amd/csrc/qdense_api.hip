@@ -35,10 +35,18 @@ bool same_rows(const dense_rows *a, const dense_rows *b, int n_tokens, int heads
     return a->type == b->type && (n_tokens == 1 || a->token_stride == b->token_stride) && (heads == 1 || a->head_stride == b->head_stride);
 }
 
-// Rows that are written do not overlap.
+// Rows that are written do not overlap: neither those of one token or one head, nor, where heads of a token reach past the next token and the other way round,
+// head h of a token with the two tokens between whose rows it begins.
 int32_t check_apart(const dense_rows *r, int n_tokens, int heads, int dim, const char *call, const char *name) {
-    if ((n_tokens > 1 && r->token_stride < dim) || (heads > 1 && r->head_stride < dim)) return set_error(MOE_E_ARG, "%s: rows of %s overlap", call, name);
-    return MOE_OK;
+    typedef __int128 wide;
+    const wide ts = r->token_stride, hs = r->head_stride;
+    bool apart = (n_tokens == 1 || ts >= dim) && (heads == 1 || hs >= dim);
+    if (apart && n_tokens > 1 && heads > 1 && ts < (heads - 1) * hs + dim && hs < (n_tokens - 1) * ts + dim)
+        for (int h = 1; h < heads && apart; ++h) {
+            const wide t = h * hs / ts, past = h * hs % ts;
+            apart = (t >= n_tokens || past >= dim) && (t + 1 >= n_tokens || ts - past >= dim);
+        }
+    return apart ? MOE_OK : set_error(MOE_E_ARG, "%s: rows of %s overlap", call, name);
 }
 
 qdense::Rows rows(const dense_rows *r) {
