@@ -5,6 +5,7 @@ handle); nothing is computed here."""
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from typing import Optional
 
@@ -361,7 +362,10 @@ class Context:
             of, shape = i32, (nb.value // 16, 4)
         else:
             raise KeyError(what)
-        off = ((p.value or 0) - self._ws_at) // of.element_size()
+        size = of.element_size()
+        if math.prod(shape) * size != nb.value:
+            raise MoeError(MOE_E_STATE, f"{what} has {nb.value} bytes, not those of {list(shape)}: the layer-batch was not routed by this object")
+        off = (p.value - self._ws_at) // size
         return of.as_strided(shape, (shape[1], 1) if len(shape) == 2 else (1,), off)
 
 
