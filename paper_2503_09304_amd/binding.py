@@ -261,11 +261,18 @@ class Context:
         return rc
 
     def route_scored(self, x, w: MoeWeights, scoring: MoeScoring, n_tokens=None):
-        """The router by scores, a bias for the choice alone, and groups of experts."""
+        """The router by scores, a bias for the choice alone, and groups of experts, for the first n_tokens rows of x (None: all), a dense tensor [.., H] of the context's type on its GPU."""
+        import torch
+        cfg, device = self.cfg, self.ws.get_device()
         for b in (scoring.logit_bias, scoring.choice_bias):
-            if b is not None and (b.shape[0] != self.cfg.E or b.get_device() != self.ws.get_device()):
-                raise MoeError(MOE_E_ARG, f"logit_bias and choice_bias must have {self.cfg.E} elements on {self.ws.device}")
-        n = x.shape[0] if n_tokens is None else n_tokens
+            if b is not None and (b.shape[0] != cfg.E or b.get_device() != device):
+                raise MoeError(MOE_E_ARG, f"logit_bias and choice_bias must have {cfg.E} elements on {self.ws.device}")
+        shape, dtype = x.shape, torch.bfloat16 if cfg.dtype == MOE_BF16 else torch.float32
+        if x.dtype is not dtype or x.get_device() != device or len(shape) == 0 or shape[-1] != cfg.H or not x.is_contiguous():
+            raise MoeError(MOE_E_ARG, f"x must be a dense {dtype} tensor [tokens, {cfg.H}] on {self.ws.device}, not {x.dtype} {list(shape)} on {x.device}")
+        n = shape[0] if n_tokens is None else n_tokens
+        if n < 0 or n * cfg.H > x.numel():
+            raise MoeError(MOE_E_ARG, f"n_tokens is {n}, x has {x.numel() // cfg.H} rows")
         rc = _check(lib().moe_route_scored(self.h, _ptr(x), n, C.byref(w), C.byref(scoring._c), self._stream()))
         self.N, self._w = n, w
         return rc
