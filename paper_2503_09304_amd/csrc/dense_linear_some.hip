@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "dense_linear.h"
+#include "dense_plan.h"
 
 namespace qdense {
 namespace {

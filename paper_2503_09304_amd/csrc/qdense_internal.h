@@ -37,8 +37,6 @@ struct LinearArgs {
 // What a call's ranges need of a workspace, 0 without any: see dense_linear.hip.
 size_t linear_workspace(int n_tokens, int R, int K, int x_type);
 hipError_t launch_linear(LinearArgs a, size_t workspace_bytes, hipStream_t s);
-// Most blocks of 128 columns of a range there (its tokens' scales are in LDS).
-constexpr int kSomeBlocks = 64;
 hipError_t launch_linear_some(const LinearArgs &a, int tiles, int rows, int ks, int share, int range_blocks, hipStream_t s);
 hipError_t launch_linear_many(const LinearArgs &a, hipStream_t s);
 hipError_t launch_pack4(const uint8_t *codes, const uint8_t *scales, int R, int K, uint8_t *dst_codes, uint8_t *dst_scales, hipStream_t s);

@@ -1,0 +1,68 @@
+"""The rule that picks dense_linear's kernel, tiles and ranges of columns, run on the CPU."""
+import ctypes as C
+import os
+import random
+import subprocess
+from collections import namedtuple
+
+import pytest
+
+from test_dense_cpu import BF, CSRC, F8, STUB, d
+
+Plan = namedtuple("Plan", "tiles rows ks share ranges range_blocks us bytes")
+MANY = 8                                                           # tiles of the kernel for many tokens
+ALL = 1 << 40
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    so = str(tmp_path_factory.mktemp("plan") / "plan.so")
+    r = subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-shared", "-fPIC", "-I", CSRC, os.path.join(STUB, "plan_lib.cpp"), "-o", so], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-4000:]
+    L = C.CDLL(so)
+    L.plan.argtypes = [C.c_int] * 4 + [C.c_long, C.c_void_p, C.POINTER(C.c_float), C.POINTER(C.c_long)]
+
+    def call(T, R, K, bf16=True, nb=ALL):
+        out, us, need = (C.c_int * 6)(), C.c_float(), C.c_long()
+        L.plan(T, R, K, int(bf16), nb, out, C.byref(us), C.byref(need))
+        return Plan(*out, us.value, need.value)
+
+    return call
+
+
+def shapes(n, seed=1):
+    rng = random.Random(seed)
+    for i in range(n):
+        T, R, K = (int(2 ** rng.uniform(0, top)) for top in ((13, 15, 9), (6, 15, 9), (11, 13, 9))[i % 3])
+        yield T, R, 32 * K
+
+
+def test_the_workspace_asked_for_is_the_plan_s(plan):
+    for T, R, K in shapes(2000):
+        for bf16 in (True, False):
+            p = plan(T, R, K, bf16)
+            assert p.bytes == d._lib().dense_linear_workspace_bytes(T, R, K, BF if bf16 else F8, BF)
+            assert plan(T, R, K, bf16, p.bytes) == p                  # more than that changes nothing
+
+
+def test_with_less_the_best_plan_without_ranges(plan):
+    """Not the kernel for many tokens, whatever their number: only where it is the best, or where nothing else takes the shape (8-bit rows too long to go uncut)."""
+    cut = 0
+    for T, R, K in shapes(3000):
+        for bf16 in (True, False):
+            full = plan(T, R, K, bf16)
+            if full.bytes == 0:
+                continue
+            cut += 1
+            none = plan(T, R, K, bf16, 0)
+            assert none.ranges == 1 and none.bytes == 0 and plan(T, R, K, bf16, full.bytes - 1) == none
+            if none.tiles == MANY:
+                assert (not bf16 and K > 8192) or T > 64
+            else:
+                assert full.us <= none.us
+    assert cut > 500
+
+
+def test_a_down_projection_of_61_tokens(plan):
+    full, none = plan(61, 4096, 14336), plan(61, 4096, 14336, True, 0)
+    assert full.ranges > 2 and full.us < 17 and none.ranges == 1 and none.us < 18 and none.tiles != MANY
