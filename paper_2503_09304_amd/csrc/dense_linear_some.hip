@@ -36,6 +36,7 @@ __global__ __launch_bounds__(64 * KS * SHARE) void linear_some(const LinearArgs 
     constexpr int TOK = NT * 16, X = TOK * PIECES * 16, PLACES = X / 1024, LOADS = PLACES < SHARE ? 1 : PLACES / SHARE, WAVE = RB * 1280, SLOT = KS * X + kWaves * WAVE, SLOTS = AHEAD + 1;
     constexpr int COUNT = LOADS + RB + 1;                // a wave's loads for a block (16 tokens in 8 bits: two waves bring the same)
     constexpr bool TOGETHER = SHARE > 1;                 // waves that share tokens
+    static_assert(kSomeBlocks % KS == 0, "all of a round's blocks have their scales in place");
     static_assert(PLACES % SHARE % 2 == 0 && SLOT % 256 == 0, "whole loads");
     constexpr int SUMS = KS == 1 ? 0 : kWaves * RB * NT * 1024;
     static_assert(COUNT * AHEAD < 64, "the counter of loads under way has six bits");
@@ -79,17 +80,19 @@ __global__ __launch_bounds__(64 * KS * SHARE) void linear_some(const LinearArgs 
             to_lds_at(src[j] + (at < k_bytes ? at : 0), piece0 + to + j * (SHARE * 1024));        // behind the last column: weights are zero there
         }
     };
-    if constexpr (XT != X_BF16) {                        // the tokens' scale bytes of the range, four a block
+    // The tokens' scale bytes, four a block, of the kSomeBlocks blocks from block b0 of the range on.
+    const auto bring_scales = [&](int b0) {
         const int all = a.K / 32;
-        for (int i = tid; i < n * TOK; i += 64 * kWaves) {
+        for (int i = tid; i < min(n - b0, kSomeBlocks) * TOK; i += 64 * kWaves) {
             const int b = i / TOK, t = i % TOK;
             const uint8_t *s = a.x.scale + (long)min(t0 + t, a.n_tokens - 1) * all;
             uint32_t v = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v |= (uint32_t)s[min(4 * (from + b) + e, all - 1)] << 8 * e;
+            for (int e = 0; e < 4; ++e) v |= (uint32_t)s[min(4 * (from + b0 + b) + e, all - 1)] << 8 * e;
             xb[b][t] = v;
         }
-    }
+    };
+    if constexpr (XT != X_BF16) bring_scales(0);
     f32x4 acc[RB][NT];
 #pragma unroll
     for (int r = 0; r < RB; ++r)
@@ -106,6 +109,11 @@ __global__ __launch_bounds__(64 * KS * SHARE) void linear_some(const LinearArgs 
         wait_for<COUNT, AHEAD - 1>(mine_n - 1 - i);      // this wave's pieces of block b are in LDS
         if constexpr (TOGETHER) __syncthreads();         // everybody's; and the block before, in whose place the next one comes, has been read
         else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if constexpr (XT != X_BF16 && TOGETHER)
+            if (i > 0 && i * KS % kSomeBlocks == 0) {    // a range that is longer than the scales' place, as all waves see (KS divides it)
+                bring_scales(i * KS);
+                __syncthreads();
+            }
         if constexpr (AHEAD == 1) {
             if (i + 1 < mine_n) {
 #pragma unroll
@@ -121,7 +129,7 @@ __global__ __launch_bounds__(64 * KS * SHARE) void linear_some(const LinearArgs 
             c[r] = *reinterpret_cast<const u32x4 *>(wt + r * 1024 + l * 16);
             sc[r] = *reinterpret_cast<const uint32_t *>(wt + RB * 1024 + r * 256 + l * 4) >> 8 * ((from + b) & 3) & 255;
         }
-        products<XT, RB, NT>(acc, c, sc, x, xb[XT == X_BF16 ? 0 : b], g, t16, [&](int at, int n) {
+        products<XT, RB, NT>(acc, c, sc, x, xb[XT == X_BF16 ? 0 : b % kSomeBlocks], g, t16, [&](int at, int n) {
             if constexpr (AHEAD > 1 && decltype(more)::value) {      // beside the first half of the products: all at once they would keep the wave from them
 #pragma unroll
                 for (int k = 0; k < COUNT; ++k)

@@ -10,7 +10,8 @@ namespace qdense {
 constexpr int kFewWaves = 8, kFewTokens = 16;              // of a workgroup of linear_few
 constexpr size_t kMostLds = 128 * 1024;
 constexpr size_t kMostWorkspace = (size_t)1 << 28;
-// Most blocks of 128 columns of a range in linear_some (its tokens' scales are in LDS).
+// Blocks of 128 columns whose tokens' scales linear_some has in LDS at once.  Ranges are no longer where they can be more (and nowhere where waves have tokens of their own:
+// they do not wait for each other); one that is stops for the next scales (61 tokens in 8 bits by 4096 x 14336 without a workspace 19 us, by linear_many 105).
 constexpr int kSomeBlocks = 64;
 
 // How a call is cut into workgroups.
@@ -36,10 +37,9 @@ inline Plan few_of(int n_tokens, int R, int K, bool bf16, int ranges) {
     p.lds = std::max<size_t>((size_t)p.range_blocks * per_block + 1024, (size_t)(p.ks > 1 ? kFewWaves * 1024 : 0));
     return p;
 }
-inline Plan some_of(int K, bool bf16, int tiles, int rows, int ks, int ranges, int share = 4) {
+inline Plan some_of(int K, int tiles, int rows, int ks, int ranges, int share = 4) {
     Plan p{tiles, rows, ks, share, 1, 1, 0};
-    const int blocks = (K + 127) / 128;
-    cut(p, blocks, bf16 ? ranges : std::max(ranges, (blocks + kSomeBlocks - 1) / kSomeBlocks));
+    cut(p, (K + 127) / 128, ranges);
     return p;
 }
 // Each variant where it is best, us, x in bf16, with its best number of ranges: 1 token by 6144 x 4096 linear_few 5.9, linear_some with tiles of 1x1 (16
@@ -82,27 +82,29 @@ inline Plan plan_of(int n_tokens, int R, int K, bool bf16, size_t most) {
             least = us;
         }
     };
+    const int whole = bf16 ? 1 : (blocks + kSomeBlocks - 1) / kSomeBlocks;       // ranges whose scales are in LDS at once
     int in_vain = 0;
     for (const int z : {1, 2, 3, 4, 6, 8, 12, 16}) {
         if (z > blocks || in_vain == 2) break;           // two more ranges without a gain: the host's time counts too
         const float before = least;
+        const int cuts = std::max(z, most == 0 ? 1 : whole);
         if (n_tokens <= kFewTokens) look(few_of(n_tokens, R, K, bf16, z));
         if (n_tokens <= 64) {
-            look(some_of(K, bf16, 1, 1, 2, z));
-            look(some_of(K, bf16, 1, 1, 4, z));
+            look(some_of(K, 1, 1, 2, cuts));
+            look(some_of(K, 1, 1, 4, cuts));
         }
-        if (n_tokens <= 1024) look(some_of(K, bf16, 2, 1, 4, z, 1));
+        if (n_tokens <= 1024) look(some_of(K, 2, 1, 4, std::max(z, whole), 1));
         if (n_tokens <= 4096) {
-            look(some_of(K, bf16, 2, 1, 1, z));
-            look(some_of(K, bf16, 4, 2, 2, z));
+            look(some_of(K, 2, 1, 1, cuts));
+            look(some_of(K, 4, 2, 2, cuts));
         }
         if (n_tokens <= 2048) {
-            look(some_of(K, bf16, 2, 1, 2, z));
-            look(some_of(K, bf16, 2, 2, 2, z));
+            look(some_of(K, 2, 1, 2, cuts));
+            look(some_of(K, 2, 2, 2, cuts));
         }
         if (n_tokens > 32) {
-            look(some_of(K, bf16, 4, 2, 1, z));
-            look(some_of(K, bf16, 4, 4, 1, z));
+            look(some_of(K, 4, 2, 1, cuts));
+            look(some_of(K, 4, 4, 1, cuts));
         }
         in_vain = least < before ? 0 : in_vain + 1;
     }

@@ -46,7 +46,7 @@ def test_the_workspace_asked_for_is_the_plan_s(plan):
 
 
 def test_with_less_the_best_plan_without_ranges(plan):
-    """Not the kernel for many tokens, whatever their number: only where it is the best, or where nothing else takes the shape (8-bit rows too long to go uncut)."""
+    """Not the kernel for many tokens, whatever their number: only where it is the best."""
     cut = 0
     for T, R, K in shapes(3000):
         for bf16 in (True, False):
@@ -56,13 +56,29 @@ def test_with_less_the_best_plan_without_ranges(plan):
             cut += 1
             none = plan(T, R, K, bf16, 0)
             assert none.ranges == 1 and none.bytes == 0 and plan(T, R, K, bf16, full.bytes - 1) == none
-            if none.tiles == MANY:
-                assert (not bf16 and K > 8192) or T > 64
-            else:
-                assert full.us <= none.us
+            assert none.tiles != MANY or T > 64
+            assert full.us <= none.us or not bf16 and K > 8192
     assert cut > 500
 
 
 def test_a_down_projection_of_61_tokens(plan):
-    full, none = plan(61, 4096, 14336), plan(61, 4096, 14336, True, 0)
-    assert full.ranges > 2 and full.us < 17 and none.ranges == 1 and none.us < 18 and none.tiles != MANY
+    for bf16 in (True, False):
+        full, none = plan(61, 4096, 14336, bf16), plan(61, 4096, 14336, bf16, 0)
+        assert full.ranges >= 2 and full.us < 17 and none.ranges == 1 and none.us < 20 and none.tiles != MANY
+
+
+def test_ranges_whose_scales_are_in_lds_at_once(plan):
+    """8-bit rows: 64 blocks of 128 columns, where there is a workspace; in the kernel whose waves do not wait for each other always."""
+    for T, R, K in shapes(3000, 2):
+        for nb in (ALL, 0):
+            p = plan(T, R, K, False, nb)
+            if p.tiles != MANY and p.share > 0 and (nb or p.share == 1):
+                assert p.range_blocks <= 64
+
+
+def test_long_rows_in_8_bits_reach_every_kernel_that_takes_them(plan):
+    """The shapes of test_gpu_dense_plans.py: each variant whose range is longer than its scales' place, whole rounds of blocks and odd ones behind it."""
+    from test_gpu_dense_plans import LONG
+    met = {p[:4] for p in (plan(*s, False, 0) for s in LONG) if p.range_blocks > 64 and p.tiles != MANY and p.share}
+    wanted = {p[:4] for p in (plan(T, R, K + 8192, False, 0) for T, R, K in shapes(6000, 3)) if p.tiles != MANY and p.share}
+    assert met == wanted, (met ^ wanted)
