@@ -82,3 +82,28 @@ def test_long_rows_in_8_bits_reach_every_kernel_that_takes_them(plan):
     met = {p[:4] for p in (plan(*s, False, 0) for s in LONG) if p.range_blocks > 64 and p.tiles != MANY and p.share}
     wanted = {p[:4] for p in (plan(T, R, K + 8192, False, 0) for T, R, K in shapes(6000, 3)) if p.tiles != MANY and p.share}
     assert met == wanted, (met ^ wanted)
+
+
+def variant(p, T, R):
+    """What tells one plan's code from another's: kernel, tiles, waves, sums by ranges or whole, and with the largest tiles how many blocks are asked for ahead."""
+    if p.tiles == MANY:
+        return MANY
+    groups = -(-(-(-R // 16)) // (4 * p.rows)) * -(-T // (16 * p.tiles)) * p.ranges
+    return p[:4] + (p.ranges > 1,) + ((groups <= 256,) if (p.tiles, p.rows) == (4, 4) else ())
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+def test_every_plan_is_compared_on_the_gpu(plan, bf16):
+    """Whatever the rule gives on shapes of the whole range stands among those of test_gpu_dense_plans.py: a change of its constants that leaves a variant without one fails here."""
+    from test_gpu_dense_plans import BF, F8, SHAPES
+    mine = SHAPES[BF if bf16 else F8]
+    met = {variant(plan(*s, bf16), s[0], s[1]) for s in mine}
+    rng, wanted = random.Random(4), set()
+    for _ in range(40000):
+        T, R, K = int(2 ** rng.uniform(0, 13)), int(2 ** rng.uniform(0, 15.1)), 32 * int(2 ** rng.uniform(0, 9))
+        wanted.add(variant(plan(T, R, K, bf16), T, R))
+    assert len(wanted) > 20 and wanted <= met, wanted - met
+    many = [s for s in mine if plan(*s, bf16).tiles == MANY]
+    assert any(s[1] > 8 * 256 * 3 for s in many) and any(s[0] > 1024 for s in many) and all(s[0] % 16 and s[1] % 16 and s[2] % 128 for s in many)
+    # groups of eight tiles of rows, the last one whole or not
+    assert len({-(-s[1] // 256) % 8 for s in many}) > 2

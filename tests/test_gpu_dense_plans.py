@@ -36,3 +36,21 @@ LONG = [(1, 5000, 8224), (9, 17199, 8448), (15, 22902, 9280), (16, 40, 8224), (1
 @pytest.mark.parametrize("T,R,K", LONG)
 def test_long_rows_in_8_bits_without_a_workspace(T, R, K, x_type, out_type):
     check(T, R, K, x_type, out_type, workspace=False)
+
+
+# Shapes of every plan that the rule gives: kernel, tiles, waves, one range or some, blocks ahead; rows, tokens and columns that fill no tile.  The last five are the kernel
+# for many tokens: few and many groups of rows, tokens that end inside a tile.
+SHAPES = {BF: [(1, 32753, 13472), (2, 21667, 13120), (1, 32007, 16192), (5, 8185, 13600), (7, 26237, 3264), (7, 6817, 12576), (2, 16059, 16224), (5, 4089, 14400), (19, 7209, 4384),
+               (15, 3799, 8032), (3, 7987, 15264), (12, 1355, 15840), (2924, 247, 832), (3097, 23, 8416), (722, 577, 1440), (314, 279, 6848), (147, 769, 5312), (123, 79, 15520),
+               (57, 15665, 672), (932, 87, 7392), (4620, 131, 992), (4719, 41, 3104), (3354, 263, 672), (2223, 67, 4512), (143, 33063, 800), (5725, 267, 672), (2763, 131, 10976),
+               (4405, 131, 3232), (547, 10941, 672), (1449, 4315, 672), (207, 26063, 672), (7096, 773, 704), (1900, 7169, 608)],
+          F8: [(1, 32753, 13472), (7, 17587, 4896), (7, 26237, 3264), (8, 8587, 8736), (6, 34285, 2912), (11, 3751, 14496), (3, 14375, 13920), (11, 4093, 15968), (19, 7209, 4384),
+               (13, 3941, 11616), (7, 6817, 12576), (12, 1879, 16352), (1402, 393, 1088), (3097, 23, 8416), (722, 577, 1440), (314, 279, 6848), (147, 769, 5312), (91, 497, 13280),
+               (57, 15665, 672), (932, 87, 7392), (4620, 131, 992), (4719, 41, 3104), (35, 24319, 704), (2223, 67, 4512), (69, 34721, 864), (5725, 267, 672), (2763, 131, 10976),
+               (34, 3113, 11456), (549, 14641, 672), (1099, 7517, 672), (209, 32971, 832), (5011, 1591, 672), (1900, 7169, 608)]}
+
+
+@pytest.mark.parametrize("x_type,out_type", KINDS)
+@pytest.mark.parametrize("i", range(33))
+def test_every_plan(i, x_type, out_type):
+    check(*SHAPES[x_type][i], x_type, out_type)
