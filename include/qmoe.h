@@ -104,7 +104,7 @@ enum { MOE_W_ROWMAJOR = 0, MOE_W_PACKED = 1, MOE_W_MXFP4_ROWMAJOR = 2, MOE_W_MXF
  * activations, Sec. 4 "Models and Dataset", without naming a format; this library takes the open
  * microscaling FP4 format): an element is a 4-bit float e2m1 (sign, 2 exponent bits, 1 mantissa bit:
  * +-{0, 0.5, 1, 1.5, 2, 3, 4, 6}), every 32 consecutive elements along K share one scale byte e8m0
- * (2^(byte-127)); value = element * scale, always exactly a bf16.  cfg.dtype stays MOE_BF16 (x, y and
+ * (2^(byte-127)); value = element * scale, exactly a bf16 where it is below 2^128.  cfg.dtype stays MOE_BF16 (x, y and
  * the activation are bf16, Wg is bf16 [H,E]); only W1, W3, W2 are 4-bit.
  * MOE_W_MXFP4_ROWMAJOR (input of moe_pack_weights only): W1/W3 [E,F,H/2] and W2 [E,H,F/2] bytes, the
  * element with even k in the low nibble; S1/S3 [E,F,H/32], S2 [E,H,F/32] scale bytes.

@@ -23,7 +23,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 // How rows of x are multiplied: bf16; fp8 by the scaled instruction; fp8 widened to bf16 (fp32 outputs).
 enum { X_BF16 = 0, X_FP8 = 1, X_WIDE = 2 };
 
-// 8 weights (a word of codes) as bf16: exact for every scale byte (0 is 2^-127, 255 NaN), in hardware.
+// 8 weights (a word of codes) as bf16, in hardware: exact for every scale byte (0 is 2^-127, 255 NaN), but infinite from 2^128 on (bytes 253 and 254), which bf16 does not have.
 __device__ __forceinline__ bf16x8 weights8(uint32_t w, float scale) {
     u32x4 r;
     r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
@@ -32,7 +32,7 @@ __device__ __forceinline__ bf16x8 weights8(uint32_t w, float scale) {
     r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
     return __builtin_bit_cast(bf16x8, r);
 }
-// 8 e4m3 elements as bf16: exact.
+// 8 e4m3 elements as bf16: exact from 2^-133 to below 2^128; parts below that (scale bytes 0 to 2) are rounded, larger ones (bytes from 247 on) are infinite.
 __device__ __forceinline__ bf16x8 widened8(uint32_t lo, uint32_t hi, float scale) {
     u32x4 r;
     r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false));
