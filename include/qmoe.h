@@ -196,7 +196,9 @@ int32_t moe_route(moe_ctx *ctx, const void *x, int32_t n_tokens, const moe_weigh
  * -inf bars an expert) less than any other: such experts are chosen where nothing else is left.  Where all chosen scores are 0 and
  * renormalise is set, w[n,j] = factor / k.
  * groups: 1..64, a divisor of E; top_groups 1..groups; group_best 1..4, at most E / groups; k at most top_groups * E / groups (each refused with MOE_E_ARG);
- * factor finite.  logit_bias, choice_bias [device] float[E] or NULL.  Everything else as moe_route; moe_permute and what follows are the same. */
+ * factor finite.  logit_bias, choice_bias [device] float[E] or NULL.  Everything else as moe_route, but for the logits' last bits: the same call gives the same ones, and a token's do not
+ * go by the other tokens' values, but by their number (n_tokens, and the context's configuration and the weights' layout): the order of the sums over H is fitted to it.  So a token whose values are nearer than that may get
+ * other experts as part of a longer batch, where moe_route's logits are the same bits in any.  moe_permute and what follows are the same. */
 enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 };
 typedef struct {
     int32_t score;            /* MOE_SCORE_x */
