@@ -211,8 +211,8 @@ __device__ __forceinline__ double largest_first(double &a, double b) {       // 
 
 // A wave has a token, lane l experts l, l + 64, ..., NS in all.  SPLIT: NS waves have a token, 64 experts each up to the scores, and one of them chooses: fewer
 // instructions one after the other where tokens leave the chip idle (61 tokens on 256 experts 6.4 us instead of 10.4).  BEST: values that a group's worth is the sum
-// of (0: all groups count).  Bound by instructions: the exponentials and divisions of 64 bits, and for each expert chosen a search over the wave whose steps wait for
-// each other (8192 tokens on 160 experts 14.5 us, 8 of 160 in 8 groups).  A single plane of sums is the logits' own array, read and written in place: a wave reads what it
+// of (0: all groups count).  Bound by latency: for each expert chosen a search over the wave whose steps wait for
+// each other, and the exponentials and divisions of 64 bits; half of the issue is free (8192 tokens on 160 experts 14.5 us, 6 of 160 in 8 groups).  A single plane of sums is the logits' own array, read and written in place: a wave reads what it
 // writes itself and nothing else, lanes behind the last expert its first (another wave may be writing the last one).
 template <int NS, int BEST, bool SPLIT>
 __global__ __launch_bounds__(64 * (SPLIT ? NS : kTokens)) void score_topk(const float *part, int planes, float *logits, const Rule rule,
