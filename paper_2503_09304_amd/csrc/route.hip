@@ -405,6 +405,20 @@ hipError_t launch_pack_gate(const void *Wg, void *WgT, int H, int E, hipStream_t
 
 hipError_t launch_route(const RouteArgs &a, hipStream_t s) {
     if (a.N <= 0) return hipSuccess;
+    constexpr int kMost = 1 << 25;                       // tokens of a launch: up to 64 threads each, and one of 2^32 threads or more would lose the excess
+    if (a.N > kMost) {
+        for (long at = 0; at < a.N; at += kMost) {
+            RouteArgs part = a;
+            part.N = (int)(a.N - at < kMost ? a.N - at : kMost);
+            part.x = (const char *)a.x + at * a.H * (a.dtype == MOE_BF16 ? 2 : 4);
+            part.logits = a.logits + at * a.E;
+            part.topk_idx = a.topk_idx + at * a.k;
+            part.topk_w = a.topk_w + at * a.k;
+            const hipError_t e = launch_route(part, s);
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    }
     if (a.scoring != nullptr && a.dtype == MOE_BF16 && (a.packed || (a.E % 2 == 0 && ((uintptr_t)a.Wg & 3) == 0))) return launch_gate_scored(a, s);      // it reads pairs of experts
     if (a.dtype == MOE_BF16) {
         const int E16 = (a.E + 15) / 16 * 16, nb = E16 / 16;
